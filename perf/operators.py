@@ -1,0 +1,628 @@
+"""The 4-bit pool and the block-sparse prompt attention: their calls, their plain forms and their results in 64 bits.
+
+pack     louiskv.pack_pool_q4, then louiskv.gather_rows_q4 of every row: prompt keys and values quantised into the
+         4-bit pool in cluster order, and read back as the values they stand for.
+store    louiskv.segment_output_q4 at a step that evicts: the window's oldest segment becomes a unit (mean key) and
+         its rows enter the 4-bit pool; louiskv.gather_rows_q4 reads them back.
+attn     louiskv.sparse_decode_attn_rows_q4: one decode step's attention over listed rows of a 4-bit pool and the
+         local window.
+select   louiskv.retrieve_blocks: for every tile of prompt queries the key blocks it attends to.
+prompt   louiskv.sparse_prefill_attn: causal attention of the prompt's queries over their selected blocks.
+
+The 4-bit format: 32 consecutive channels of a row share the scale 2^E, the smallest power of two with max|x| <= 7 * 2^E
+(E >= -125), stored as the byte E + 127; an element is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the scale with
+its sign (ties to the even code), two to a byte, the lower channel in the lower nibble.  A block with an infinity or
+NaN has the byte 255 and stands for NaN.  A pool row is 64 key bytes and 64 value bytes (`codes`), and four key scales
+and four value scales (`scales`).
+"""
+import math
+
+import torch
+
+own = False
+
+D = 128
+SCALE = 1.0 / math.sqrt(D)
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+# ------------------------------------------------------------------- cases
+
+def _pack(name, slices, prompt, dtype="bf16"):
+    return {"name": name, "kind": "pack", "slices": slices, "prompt": prompt, "dtype": dtype}
+
+
+def _store(name, slices, window=128, seg=32, evicted=3, clusters=64, dtype="bf16"):
+    return {"name": name, "kind": "store", "slices": slices, "window": window, "seg": seg, "evicted": evicted,
+            "clusters": clusters, "dtype": dtype}
+
+
+def _attn(name, groups, kv_heads, q_heads, rows, budget, window=128, local=100, start=37, dtype="bf16"):
+    return {"name": name, "kind": "attn", "groups": groups, "kv_heads": kv_heads, "q_heads": q_heads, "rows": rows,
+            "budget": budget, "window": window, "local": local, "start": start, "dtype": dtype}
+
+
+def _blocks(kind, name, groups, kv_heads, q_heads, queries, keys, block, tile, first, recent, top, dtype="bf16"):
+    return {"name": name, "kind": kind, "groups": groups, "kv_heads": kv_heads, "q_heads": q_heads,
+            "queries": queries, "keys": keys, "block": block, "tile": tile, "first": first, "recent": recent,
+            "top": top, "dtype": dtype}
+
+
+def listed():
+    return [
+        # one layer of a short ragged float32 prompt: the smallest write
+        _pack("pack-layer-777-f32", 8, 777, dtype="f32"),
+        # eight layers of a 32K prompt at once
+        _pack("pack-8-layers-32k", 64, 32768),
+        # one layer's step that evicts a segment: latency
+        _store("store-layer", 8),
+        # every layer of four sequences, late in a generation
+        _store("store-all-b4", 1024, evicted=200, clusters=512),
+        # a layer at a time over a 32K context: the serving loop at batch 1
+        _attn("attn-layer", 1, 8, 32, 32768, 2048),
+        # every layer of a 32K context in one call
+        _attn("attn-all", 32, 8, 32, 32768, 2048),
+        # float32 queries and window, an odd budget, eight heads to a KV head
+        _attn("attn-f32-g8", 2, 4, 32, 5003, 1237, window=64, local=63, start=5, dtype="f32"),
+        # the prompt of one layer, 64 queries to a tile
+        _blocks("select", "select-layer-32k", 1, 8, 32, 32768, 32768, 64, 64, 1, 4, 24),
+        # a ragged second chunk of a prompt, small tiles and pages
+        _blocks("select", "select-chunk-1003", 1, 8, 32, 1003, 20011, 32, 16, 2, 2, 40),
+        # one token over a 32K context
+        _blocks("prompt", "prompt-token", 1, 8, 32, 1, 32768, 64, 1, 1, 4, 27),
+        # a ragged second chunk of a prompt
+        _blocks("prompt", "prompt-chunk-1003", 1, 8, 32, 1003, 20011, 32, 16, 2, 2, 40),
+        # the whole prompt of one layer
+        _blocks("prompt", "prompt-layer-32k", 1, 8, 32, 32768, 32768, 64, 64, 1, 4, 24),
+    ]
+
+
+def _unnamed(case):
+    return {k: v for k, v in case.items() if k != "name"}
+
+
+def _log_int(rng, lo, hi):
+    return int(round(lo * (hi / lo) ** rng.random()))
+
+
+def draw(rng):
+    kind = rng.choice(["pack", "store", "attn", "attn", "select", "prompt", "prompt"])
+    dtype = "f32" if rng.random() < 0.25 else "bf16"
+    if kind == "pack":
+        prompt = _log_int(rng, 1, 40000)
+        most = (1 << 21) if dtype == "bf16" else (1 << 20)      # rows of all slices
+        return _unnamed(_pack("", _log_int(rng, 1, max(1, min(256, most // prompt))), prompt, dtype))
+    if kind == "store":
+        seg = rng.choice([1, 5, 8, 16, 32, 32, 64])
+        return _unnamed(_store("", _log_int(rng, 1, 1024), seg * rng.randint(1, 4), seg, rng.randint(0, 300),
+                               rng.randint(1, 512), dtype))
+    kv = rng.choice([1, 2, 4, 8, 8, 8])
+    g = rng.choice([1, 2, 4, 4, 4, 8])
+    if kind == "attn":
+        rows = _log_int(rng, 100, 40000)
+        budget = min(_log_int(rng, 1, 8192), rows)
+        most = 256 * 2048 if dtype == "bf16" else 64 * 2048     # attended rows of all slices
+        groups = _log_int(rng, 1, max(1, min(64, most // (kv * (budget + 256)))))
+        window = rng.choice([1, 32, 64, 128, 128, 256])
+        return _unnamed(_attn("", groups, kv, kv * g, rows, budget, window, rng.randint(0, window),
+                              rng.randrange(window), dtype))
+    block = rng.choice([16, 32, 64, 64, 128])
+    tile = rng.choice([1, 7, 16, 32, 64, 64, 100, 128])
+    keys = _log_int(rng, 1, 32768)
+    queries = keys if rng.random() < 0.4 else min(keys, _log_int(rng, 1, 4096))
+    if kind == "select":
+        queries = min(queries, 4096 * tile)
+    else:
+        # (queries * heads * keys attended) within the largest listed prompt, a quarter of that in float32
+        most = 32768 * 32 * 1856 // (4 if dtype == "f32" else 1)
+        queries = min(queries, 2048 * tile, max(1, most // (kv * g * 4096)))
+    first, recent = rng.randint(0, 2), rng.randint(0, 4)
+    top = _log_int(rng, 1, max(1, 2048 // block))
+    return _unnamed(_blocks(kind, "", 1, kv, kv * g, queries, keys, block, tile, first, recent, top, dtype))
+
+
+# ------------------------------------------------------------------- inputs
+
+def _gen(seed, tag):
+    return torch.Generator(device="cuda").manual_seed((int(seed) * 1000003 + tag) & ((1 << 62) - 1))
+
+
+def _randn(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+def _rand(g, *shape):
+    return torch.rand(*shape, generator=g, device="cuda")
+
+
+def _some(slices, n):
+    """Slices taken at a time so that their float32 rows stay within a quarter of a GiB."""
+    step = max(1, (1 << 19) // max(1, n))
+    return [(i, min(slices, i + step)) for i in range(0, slices, step)]
+
+
+def _keys(g, slices, n, dtype):
+    """Keys that drift as a text does, four channels eight times the others'."""
+    out = torch.empty(slices, n, D, dtype=dtype, device="cuda")
+    topics = max(1, n // 48)
+    pos = torch.arange(n, device="cuda")
+    for a, b in _some(slices, n):
+        c = _randn(g, b - a, topics, D)
+        z = torch.randint(0, topics, (b - a, n), generator=g, device="cuda")
+        stay = _rand(g, b - a, n) < 0.9
+        stay[:, 0] = False
+        last = torch.where(stay, torch.zeros_like(z), pos.expand_as(z)).cummax(1).values
+        k = 0.3 * _randn(g, b - a, n, D)
+        k += torch.gather(c, 1, z.gather(1, last).unsqueeze(-1).expand(-1, -1, D))
+        k[..., :4] *= 8.0
+        out[a:b] = k
+    return out
+
+
+def _values(g, slices, n, dtype):
+    out = torch.empty(slices, n, D, dtype=dtype, device="cuda")
+    for a, b in _some(slices, n):
+        out[a:b] = _randn(g, b - a, n, D)
+    return out
+
+
+def _prepare_pack(case, seed):
+    s, n, dt = case["slices"], case["prompt"], DTYPES[case["dtype"]]
+    g = _gen(seed, 1)
+    perm = torch.stack([_rand(g, n).argsort() for _ in range(s)]).to(torch.int32)
+    return {"keys": _keys(g, s, n, dt), "values": _values(g, s, n, dt), "perm": perm,
+            "codes": torch.zeros(s, n, 128, dtype=torch.uint8, device="cuda"),
+            "scales": torch.zeros(s, n, 8, dtype=torch.uint8, device="cuda"),
+            "k_back": torch.zeros(s, n, D, dtype=dt, device="cuda"),
+            "v_back": torch.zeros(s, n, D, dtype=dt, device="cuda")}
+
+
+def _prepare_store(case, seed):
+    s, w, seg, e, c, dt = (case[k] for k in ("slices", "window", "seg", "evicted", "clusters", "dtype"))
+    dt = DTYPES[dt]
+    g = _gen(seed, 2)
+    cap, rows, prompt = c + e + 1, 100 + (e + 1) * seg, 100
+    first = prompt + e * seg
+    lst = torch.arange(first, first + seg, dtype=torch.int32, device="cuda").expand(s, seg).contiguous()
+    return {"k_new": _keys(g, s, 1, dt)[:, 0].contiguous(), "v_new": _values(g, s, 1, dt)[:, 0].contiguous(),
+            "k_local": _keys(g, s, w, dt), "v_local": _values(g, s, w, dt), "step": w + e * seg, "prompt": prompt,
+            "clusters": c,
+            "reps": torch.zeros(s, cap, D, device="cuda"),
+            "unit_start": torch.zeros(s, cap, dtype=torch.int32, device="cuda"),
+            "unit_size": torch.zeros(s, cap, dtype=torch.int32, device="cuda"),
+            "codes": torch.zeros(s, rows, 128, dtype=torch.uint8, device="cuda"),
+            "scales": torch.zeros(s, rows, 8, dtype=torch.uint8, device="cuda"),
+            "list": lst, "n_list": torch.full((s,), seg, dtype=torch.int32, device="cuda"),
+            "k_back": torch.zeros(s, seg, D, dtype=dt, device="cuda"),
+            "v_back": torch.zeros(s, seg, D, dtype=dt, device="cuda")}
+
+
+def _prepare_attn(case, seed):
+    s, n, b, w, dt = case["groups"] * case["kv_heads"], case["rows"], case["budget"], case["window"], DTYPES[case["dtype"]]
+    g = _gen(seed, 3)
+    codes = torch.empty(s, n, 128, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(s, n, 8, dtype=torch.uint8, device="cuda")
+    sel = torch.zeros(s, b, dtype=torch.int32, device="cuda")
+    for i, j in _some(s, n):
+        for at, x in ((0, _keys(g, j - i, n, dt)), (64, _values(g, j - i, n, dt))):
+            code, e = _to_codes(x)
+            codes[i:j, :, at:at + 64] = code
+            scales[i:j, :, at // 16:at // 16 + 4] = e
+        # units of 32 rows on average, in a ranking's order, rows ascending inside a unit
+        unit = (_rand(g, j - i, n) < 1.0 / 32).cumsum(1)
+        rank = _rand(g, j - i, n + 1).argsort(1).gather(1, unit)
+        sel[i:j] = rank.sort(dim=1, stable=True).indices[:, :b].to(torch.int32)
+    # a prefix stop leaves less than a unit of the budget
+    n_sel = (b - torch.randint(0, 32, (s,), generator=g, device="cuda")).clamp(min=0).to(torch.int32)
+    dims = (case["groups"], case["q_heads"], D)
+    return {"q": _randn(g, *dims).to(dt), "codes": codes, "scales": scales, "sel": sel, "n_sel": n_sel,
+            "k_local": _keys(g, s, w, dt), "v_local": _values(g, s, w, dt), "kv_heads": case["kv_heads"],
+            "start": case["start"], "local": case["local"], "out": torch.zeros(*dims, dtype=dt, device="cuda"),
+            "lse": torch.zeros(dims[:2], device="cuda")}
+
+
+def _geometry(case):
+    """Positions of the queries, tiles, key blocks and the room for a tile's list."""
+    n_q, n_k, block, tile = case["queries"], case["keys"], case["block"], case["tile"]
+    tiles = -(-n_q // tile)
+    blocks = -(-n_k // block)
+    diag = (tile + block - 2) // block + 1
+    return n_k - n_q, tiles, blocks, min(blocks, case["first"] + case["recent"] + diag + case["top"])
+
+
+def _prepare_blocks(case, seed):
+    s, n_k, dt, block = case["groups"] * case["kv_heads"], case["keys"], DTYPES[case["dtype"]], case["block"]
+    start, tiles, blocks, cap = _geometry(case)
+    g = _gen(seed, 4)
+    keys = _keys(g, s, n_k, dt)
+    pad = torch.zeros(s, blocks * block, D, device="cuda")
+    pad[:, :n_k] = keys.float()
+    size = (n_k - block * torch.arange(blocks, device="cuda")).clamp(max=block)
+    dims = (case["groups"], case["q_heads"], case["queries"], D)
+    # queries that look for a topic of the text: a key of an earlier position and noise
+    q = torch.empty(dims, dtype=dt, device="cuda")
+    per = case["q_heads"] // case["kv_heads"]
+    flat = q.view(s, per, case["queries"], D)
+    pos = start + torch.arange(case["queries"], device="cuda")
+    for i in range(s):
+        for j in range(per):
+            hop = (pos // 256 * 256 * (0.5 + 0.5 * math.sin(1.0 + i + 0.1 * j))).long().clamp(max=n_k - 1)
+            flat[i, j] = 0.4 * keys[i, hop].float() + _randn(g, case["queries"], D)
+    state = {"case": case, "q": q, "keys": keys, "kv_heads": case["kv_heads"], "start": start,
+             "reps": pad.view(s, blocks, block, D).double().sum(2).div(size[:, None]).float(),
+             "sel": torch.zeros(s, tiles, cap, dtype=torch.int32, device="cuda"),
+             "n_sel": torch.zeros(s, tiles, dtype=torch.int32, device="cuda")}
+    if case["kind"] == "prompt":
+        state["values"] = _values(g, s, n_k, dt)
+        state["out"] = torch.zeros(dims, dtype=dt, device="cuda")
+        state["lse"] = torch.zeros(dims[:3], device="cuda")
+        _lists(state, g, case, tiles, blocks, cap)
+    return state
+
+
+def _lists(state, g, case, tiles, blocks, cap):
+    """Lists as the selection makes them (ascending, the first blocks, the tile's own and those before it, and others
+    at random), without running it."""
+    score = _rand(g, *state["sel"].shape[:2], blocks)
+    forced, seen = _forced(case, tiles, blocks)
+    score = score.masked_fill(forced, 2.0).masked_fill(~seen, -1.0)
+    most = min(cap, blocks)
+    best = score.sort(dim=-1, descending=True, stable=True)
+    room = (forced.sum(-1, keepdim=True) + case["top"]).minimum(seen.sum(-1, keepdim=True))
+    rank = torch.arange(most, device="cuda")
+    idx = best.indices[..., :most].masked_fill(rank >= room, blocks).sort(-1).values
+    state["sel"][:] = idx.masked_fill(idx == blocks, 0).to(torch.int32)
+    state["n_sel"][:] = room[:, 0].to(torch.int32)
+
+
+def _forced(case, tiles, blocks):
+    """[tiles][blocks]: blocks that a tile always takes, and blocks that its last query sees the start of."""
+    start = case["keys"] - case["queries"]
+    t = torch.arange(tiles, device="cuda")[:, None]
+    b = torch.arange(blocks, device="cuda")
+    lo = (start + t * case["tile"]) // case["block"]
+    hi = (start + (t * case["tile"] + case["tile"] - 1).clamp(max=case["queries"] - 1)) // case["block"]
+    seen = b <= hi
+    return seen & ((b < case["first"]) | (b >= lo - case["recent"])), seen
+
+
+def prepare(case, seed):
+    return {"kind": case["kind"], **{"pack": _prepare_pack, "store": _prepare_store, "attn": _prepare_attn,
+                                     "select": _prepare_blocks, "prompt": _prepare_blocks}[case["kind"]](case, seed)}
+
+
+# ------------------------------------------------------------------- plain forms
+
+def _to_codes(x):
+    """Code bytes [..., 64] and scale bytes [..., 4] of rows x [..., 128]."""
+    b = x.float().reshape(*x.shape[:-1], 4, 32)
+    top = b.abs().amax(-1, keepdim=True)
+    m, e = torch.frexp(top)
+    e = torch.where(m <= 0.875, e - 3, e - 2).masked_fill(top == 0, -125).clamp(min=-125)
+    good = torch.isfinite(top)
+    y = torch.where(good, torch.ldexp(b, torch.where(good, -e, 0)), torch.zeros_like(b))
+    t = y.abs()
+    step = torch.where(t < 2, 0.5, torch.where(t < 4, 1.0, 2.0))
+    t = ((t / step).round() * step).clamp(max=6.0)
+    # 0, .5, 1, 1.5, 2, 3, 4, 6 are the codes 0..7
+    code = torch.where(t < 2, 2 * t, torch.where(t < 4, t + 2, t / 2 + 4)).to(torch.uint8)
+    code = code + 8 * torch.signbit(y).to(torch.uint8)
+    code = code.reshape(*x.shape[:-1], 64, 2)
+    return code[..., 0] + 16 * code[..., 1], torch.where(good, e + 127, 255).to(torch.uint8).squeeze(-1)
+
+
+def _from_codes(code, scale):
+    """The float32 values [..., 128] of code bytes [..., 64] and scale bytes [..., 4]."""
+    n = torch.stack((code & 15, code >> 4), -1).reshape(*code.shape[:-1], 4, 32)
+    mag = (n & 7).float()
+    mag = torch.where(mag < 4, mag / 2, torch.where(mag < 6, mag - 2, 2 * mag - 8))
+    v = torch.where(n >= 8, -mag, mag)
+    s = torch.ldexp(torch.ones_like(scale, dtype=torch.float32), scale.to(torch.int32) - 127)
+    s = s.masked_fill(scale == 255, float("nan"))
+    return (v * s.unsqueeze(-1)).reshape(*code.shape[:-1], 128)
+
+
+def _plain_pack(st):
+    at = st["perm"].long()
+    for i in range(at.shape[0]):      # a slice at a time: the float32 copies of all would not fit beside each other
+        for half, src in ((0, st["keys"]), (1, st["values"])):
+            q, e = _to_codes(src[i][at[i]])
+            st["codes"][i, :, 64 * half:64 * half + 64] = q
+            st["scales"][i, :, 4 * half:4 * half + 4] = e
+        st["k_back"][i] = _from_codes(st["codes"][i, :, :64], st["scales"][i, :, :4]).to(st["k_back"].dtype)
+        st["v_back"][i] = _from_codes(st["codes"][i, :, 64:], st["scales"][i, :, 4:]).to(st["v_back"].dtype)
+
+
+def _plain_store(st):
+    w, seg, step = st["k_local"].shape[1], st["list"].shape[1], st["step"]
+    at = (torch.arange(seg, device="cuda") + (step - w)) % w
+    k, v = st["k_local"][:, at], st["v_local"][:, at]
+    rows = st["list"][0].long()
+    unit = st["reps"].shape[1] - 1
+    for half, x, back in ((0, k, "k_back"), (1, v, "v_back")):
+        q, e = _to_codes(x)
+        st["codes"][:, rows, 64 * half:64 * half + 64] = q
+        st["scales"][:, rows, 4 * half:4 * half + 4] = e
+        st[back][:] = _from_codes(q, e).to(x.dtype)
+    st["reps"][:, unit] = (k.double().sum(1) / seg).float()
+    st["unit_start"][:, unit] = rows[0].to(torch.int32)
+    st["unit_size"][:, unit] = seg
+    st["k_local"][:, step % w] = st["k_new"]
+    st["v_local"][:, step % w] = st["v_new"]
+
+
+def _softmax_rows(logits, values):
+    """softmax(logits) @ values and the log of its denominator, masked logits being -inf; a row without any: 0, -inf."""
+    top = logits.amax(-1, keepdim=True)
+    top = torch.where(top == -math.inf, torch.zeros_like(top), top)
+    e = torch.exp(logits - top)
+    total = e.sum(-1, keepdim=True)
+    o = torch.matmul(e, values) / torch.where(total > 0, total, torch.ones_like(total))
+    return o, (top + torch.log(total)).squeeze(-1)
+
+
+def _plain_attn(st):
+    s, b = st["sel"].shape
+    w, h = st["k_local"].shape[1], st["kv_heads"]
+    g = st["q"].shape[1] // h
+    q = st["q"].reshape(s, g, D).float()
+    at = (st["start"] + torch.arange(st["local"], device="cuda")) % w
+    out, lse = [], []
+    step = max(1, (1 << 18) // (b + w))
+    for i in range(0, s, step):       # some slices at a time: float32 rows of all would not fit three times over
+        j = slice(i, i + step)
+        rows = st["sel"][j].long()
+        code = torch.gather(st["codes"][j], 1, rows.unsqueeze(-1).expand(-1, -1, 128))
+        scale = torch.gather(st["scales"][j], 1, rows.unsqueeze(-1).expand(-1, -1, 8))
+        k = torch.cat((_from_codes(code[..., :64], scale[..., :4]), st["k_local"][j][:, at].float()), 1)
+        v = torch.cat((_from_codes(code[..., 64:], scale[..., 4:]), st["v_local"][j][:, at].float()), 1)
+        dead = torch.arange(b + len(at), device="cuda")
+        dead = (dead >= st["n_sel"][j][:, None]) & (dead < b)
+        x = torch.matmul(q[j], k.transpose(1, 2)) * SCALE
+        o, e = _softmax_rows(x.masked_fill(dead[:, None], -math.inf), v)
+        out.append(o)
+        lse.append(e)
+    return torch.cat(out).reshape(st["q"].shape).to(st["q"].dtype), torch.cat(lse).reshape(st["q"].shape[:2])
+
+
+def _plain_select(st):
+    case = st["case"]
+    s, tiles, cap = st["sel"].shape
+    blocks, tile = st["reps"].shape[1], case["tile"]
+    per = case["q_heads"] // case["kv_heads"]
+    q = torch.zeros(s, per, tiles * tile, D, device="cuda", dtype=torch.float64)
+    q[:, :, :case["queries"]] = st["q"].reshape(s, per, -1, D).double()
+    q = q.reshape(s, per, tiles, tile, D).sum((1, 3))
+    forced, seen = _forced(case, tiles, blocks)
+    score = torch.matmul(q, st["reps"].double().transpose(1, 2))     # the sums decide: 64 bits
+    score = score.masked_fill(forced, math.inf).masked_fill(~seen, -math.inf)
+    order = score.sort(dim=-1, descending=True, stable=True).indices
+    room = (forced.sum(-1) + case["top"]).minimum(seen.sum(-1))
+    most = min(cap, blocks)
+    idx = order[..., :most].masked_fill(torch.arange(most, device="cuda") >= room[:, None], blocks).sort(-1).values
+    st["sel"][..., :most] = torch.where(idx < blocks, idx.to(torch.int32), st["sel"][..., :most])
+    st["n_sel"][:] = room.to(torch.int32)
+
+
+def _plain_prompt(st):
+    case = st["case"]
+    s, tiles, cap = st["sel"].shape
+    n_q, n_k, block, tile = case["queries"], case["keys"], case["block"], case["tile"]
+    per = case["q_heads"] // case["kv_heads"]
+    q = torch.zeros(s, per, tiles * tile, D, device="cuda")
+    q[:, :, :n_q] = st["q"].reshape(s, per, n_q, D).float()
+    q = q.reshape(s, per, tiles, tile, D).transpose(1, 2)
+    out = torch.empty(s, tiles, per, tile, D, device="cuda")
+    lse = torch.empty(s, tiles, per, tile, device="cuda")
+    inside = torch.arange(block, device="cuda")
+    slices = torch.arange(s, device="cuda")[:, None, None]
+    step = max(1, (1 << 19) // (s * cap * block))
+    for t in range(0, tiles, step):   # some tiles at a time: their gathered keys and values are many times the prompt
+        j = slice(t, t + step)
+        n = st["sel"][:, j].shape[1]
+        key = (st["sel"][:, j].long().unsqueeze(-1) * block + inside).reshape(s, n, cap * block)
+        live = (torch.arange(cap, device="cuda") < st["n_sel"][:, j].unsqueeze(-1)).repeat_interleave(block, -1)
+        live = live & (key < n_k)
+        pos = st["start"] + (t + torch.arange(n, device="cuda"))[:, None] * tile + torch.arange(tile, device="cuda")
+        ok = live[:, :, None, None] & (key[:, :, None, None] <= pos[:, None, :, None])
+        key = key.clamp(max=n_k - 1)
+        k, v = st["keys"][slices, key].float(), st["values"][slices, key].float()
+        x = torch.matmul(q[:, j].reshape(s, n, per * tile, D), k.transpose(2, 3).contiguous()) * SCALE
+        x = x.reshape(s, n, per, tile, -1).masked_fill(~ok, -math.inf).reshape(s, n, per * tile, -1)
+        o, e = _softmax_rows(x, v)
+        out[:, j] = o.reshape(s, n, per, tile, D)
+        lse[:, j] = e.reshape(s, n, per, tile)
+    out = out.transpose(1, 2).reshape(s, per, tiles * tile, D)[:, :, :n_q]
+    lse = lse.transpose(1, 2).reshape(s, per, tiles * tile)[:, :, :n_q]
+    return out.reshape(st["q"].shape).to(st["q"].dtype), lse.reshape(st["q"].shape[:3])
+
+
+# ------------------------------------------------------------------- one pass
+
+def run(state):
+    st = state
+    if own:
+        from paper_2510_11292_amd import louiskv as L
+    if st["kind"] == "pack":
+        if own:
+            L.pack_pool_q4(st["keys"], st["values"], st["perm"], st["codes"], st["scales"])
+            L.gather_rows_q4(st["codes"], st["scales"], None, None, st["k_back"], st["v_back"])
+        else:
+            _plain_pack(st)
+        return {"keys": st["k_back"], "values": st["v_back"]}
+    if st["kind"] == "store":
+        if own:
+            L.segment_output_q4(st["k_new"], st["v_new"], st["k_local"], st["v_local"], st["step"],
+                                st["list"].shape[1], st["reps"], st["unit_start"], st["unit_size"], st["clusters"],
+                                st["codes"], st["scales"], prompt_len=st["prompt"])
+            L.gather_rows_q4(st["codes"], st["scales"], st["list"], st["n_list"], st["k_back"], st["v_back"])
+        else:
+            _plain_store(st)
+        return {k: st[k] for k in ("k_back", "v_back", "reps", "unit_start", "unit_size", "k_local", "v_local")}
+    if st["kind"] == "attn":
+        if own:
+            L.sparse_decode_attn_rows_q4(st["q"], st["kv_heads"], st["codes"], st["scales"], st["sel"], st["n_sel"],
+                                         st["k_local"], st["v_local"], st["start"], st["local"], st["out"], st["lse"])
+            return {"out": st["out"], "lse": st["lse"]}
+        out, lse = _plain_attn(st)
+        return {"out": out, "lse": lse}
+    case = st["case"]
+    if st["kind"] == "select":
+        if own:
+            L.retrieve_blocks(st["q"], st["kv_heads"], st["reps"], case["keys"], st["start"], case["tile"],
+                              case["block"], case["first"], case["recent"], case["top"], st["sel"], st["n_sel"])
+        else:
+            _plain_select(st)
+        return {"blocks": st["sel"], "n": st["n_sel"]}
+    if own:
+        L.sparse_prefill_attn(st["q"], st["kv_heads"], st["keys"], st["values"], case["keys"], st["start"],
+                              case["tile"], case["block"], st["sel"], st["n_sel"], st["out"], st["lse"])
+        return {"out": st["out"], "lse": st["lse"]}
+    out, lse = _plain_prompt(st)
+    return {"out": out, "lse": lse}
+
+
+def _attended(case):
+    """(keys that all tiles' lists hold, query-key pairs of one head that the causal mask leaves) of one slice."""
+    start, tiles, blocks, _ = _geometry(case)
+    block, tile = case["block"], case["tile"]
+    rows = pairs = 0
+    for t in range(tiles):
+        p0 = start + t * tile
+        p1 = start + min((t + 1) * tile, case["queries"]) - 1
+        hi, lo = p1 // block, max(0, p0 // block - case["recent"])
+        whole = min(lo, case["first"])                       # forced blocks before the recent ones
+        whole += min(case["top"], lo - whole)                # and ranked ones: every query sees them whole
+        whole = whole * block + (p0 // block - lo) * block
+        edge = p0 // block * block
+        rows += whole + min((hi + 1) * block, case["keys"]) - edge
+        pairs += (p1 - p0 + 1) * (whole - edge) + (p0 + p1 + 2) * (p1 - p0 + 1) // 2
+    return rows, pairs
+
+
+def work(case):
+    size = 2 if case["dtype"] == "bf16" else 4
+    row = 2 * D * size                       # a key and its value
+    held = 128 + 8                           # the same in the 4-bit pool
+    if case["kind"] == "pack":
+        n = case["slices"] * case["prompt"]
+        return {"bytes": n * (row + 4 + held + held + row), "flops": 0}
+    if case["kind"] == "store":
+        n = case["slices"] * case["seg"]
+        return {"bytes": n * (row + held + 4 + held + row) + case["slices"] * (2 * row + 4 * D + 8), "flops": 0}
+    if case["kind"] == "attn":
+        s, g = case["groups"] * case["kv_heads"], case["q_heads"] // case["kv_heads"]
+        n = max(0, case["budget"] - 16)      # the lists end up to 31 rows short of the budget
+        return {"bytes": s * (n * (held + 4) + case["local"] * row + g * (2 * D * size + 4)),
+                "flops": 4 * D * g * s * (n + case["local"])}
+    s, g = case["groups"] * case["kv_heads"], case["q_heads"] // case["kv_heads"]
+    _, tiles, blocks, cap = _geometry(case)
+    if case["kind"] == "select":
+        return {"bytes": s * (g * case["queries"] * D * size + blocks * D * 4 + tiles * (cap + 1) * 4),
+                "flops": s * (g * case["queries"] * D + 2 * tiles * blocks * D)}
+    rows, pairs = _attended(case)
+    seen = min(case["keys"], rows)           # keys and values come from memory once
+    return {"bytes": s * (seen * row + g * case["queries"] * (2 * D * size + 4) + tiles * (cap + 1) * 4),
+            "flops": 4 * D * g * s * pairs}
+
+
+# ------------------------------------------------------------------- 64 bits
+
+_LEVELS = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def _held(x):
+    """The values, in 64 bits, that rows x stand for once held in four bits: the nearest level of each element."""
+    b = x.double().reshape(-1, 32)
+    top = b.abs().amax(-1)
+    lg = torch.full_like(top, -125.0)
+    for e in range(-125, 127):
+        lg = torch.where(top > 7.0 * 2.0 ** e, torch.full_like(lg, e + 1.0), lg)
+    unit = torch.exp2(lg).unsqueeze(-1)
+    t = (b / unit).abs()
+    v = torch.zeros_like(t)
+    for i in range(1, 8):
+        mid = (_LEVELS[i - 1] + _LEVELS[i]) / 2
+        v = torch.where((t > mid) | ((t == mid) & (i % 2 == 0)), torch.full_like(v, _LEVELS[i]), v)
+    v = torch.where(torch.isfinite(top).unsqueeze(-1), v * unit * torch.sign(b), torch.full_like(v, math.nan))
+    return v.reshape(x.shape)
+
+
+def _value_of_byte():
+    lv = torch.tensor(_LEVELS + tuple(-x for x in _LEVELS), dtype=torch.float64, device="cuda")
+    b = torch.arange(256, device="cuda")
+    return torch.stack((lv[b & 15], lv[b >> 4]), -1)
+
+
+def _exact_attention(q, k, v, ok):
+    x = torch.matmul(q, k.transpose(-1, -2)) / math.sqrt(D)
+    x = torch.where(ok, x, torch.full_like(x, -math.inf))
+    lse = torch.logsumexp(x, -1)
+    p = torch.exp(x - torch.where(torch.isinf(lse), torch.zeros_like(lse), lse).unsqueeze(-1))
+    return torch.matmul(p, v), lse
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "pack":
+        out = {"keys": [], "values": []}
+        for i in range(case["slices"]):
+            for n in out:
+                # float32 holds every level exactly; 64-bit copies of a large pool would not fit three times
+                out[n].append(_held(st[n][i].index_select(0, st["perm"][i])).float())
+        return {n: torch.stack(v) for n, v in out.items()}
+    if kind == "store":
+        w, seg, step = case["window"], case["seg"], st["step"]
+        slot = [(step + r) % w for r in range(seg)]
+        reps, start, size = st["reps"].double(), st["unit_start"], st["unit_size"]
+        k, v = st["k_local"].double(), st["v_local"].double()
+        unit = case["clusters"] + case["evicted"]
+        reps[:, unit] = k[:, slot].mean(1)
+        start[:, unit] = st["prompt"] + case["evicted"] * seg
+        size[:, unit] = seg
+        back = [_held(x[:, slot]) for x in (st["k_local"], st["v_local"])]
+        k[:, step % w] = st["k_new"].double()
+        v[:, step % w] = st["v_new"].double()
+        return {"k_back": back[0], "v_back": back[1], "reps": reps, "unit_start": start, "unit_size": size,
+                "k_local": k, "v_local": v}
+    if kind == "attn":
+        s, h = st["sel"].shape[0], case["kv_heads"]
+        q = st["q"].double().reshape(s, -1, D)
+        table = _value_of_byte()
+        out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], dtype=torch.float64, device="cuda")
+        ring = [(case["start"] + i) % case["window"] for i in range(case["local"])]
+        for i in range(s):
+            rows = st["sel"][i, :int(st["n_sel"][i])].long()
+            x = table[st["codes"][i, rows].long()].reshape(len(rows), 8, 32)
+            x = x * torch.exp2(st["scales"][i, rows].double() - 127).unsqueeze(-1)
+            x = x.reshape(len(rows), 256)
+            k = torch.cat((x[:, :128], st["k_local"][i, ring].double()))
+            v = torch.cat((x[:, 128:], st["v_local"][i, ring].double()))
+            if len(k):
+                out[i], lse[i] = _exact_attention(q[i], k, v, torch.ones(1, len(k), dtype=torch.bool, device="cuda"))
+            else:
+                lse[i] = -math.inf
+        return {"out": out.reshape(st["q"].shape), "lse": lse.reshape(st["q"].shape[:2])}
+    if kind == "select":
+        return None                          # lists of whole numbers: the same on both sides
+    per = case["q_heads"] // case["kv_heads"]
+    s, tiles, _ = st["sel"].shape
+    q = st["q"].reshape(s, per, case["queries"], D)
+    out = torch.empty(q.shape, dtype=torch.float64, device="cuda")
+    lse = torch.empty(q.shape[:3], dtype=torch.float64, device="cuda")
+    block, tile = case["block"], case["tile"]
+    if s * tiles > 20000:
+        return None                          # a product at a time: over 20 seconds
+    inside = torch.arange(block, device="cuda")
+    n_sel = st["n_sel"].tolist()
+    for i in range(s):
+        for t in range(tiles):
+            a, b = t * tile, min((t + 1) * tile, case["queries"])
+            key = (st["sel"][i, t, :n_sel[i][t]].long()[:, None] * block + inside).reshape(-1)
+            key = key[key < case["keys"]]
+            ok = key[None] <= st["start"] + torch.arange(a, b, device="cuda")[:, None]
+            o, e = _exact_attention(q[i, :, a:b].double(), st["keys"][i, key].double()[None],
+                                    st["values"][i, key].double()[None], ok[None])
+            out[i, :, a:b], lse[i, :, a:b] = o, e
+    return {"out": out.reshape(st["q"].shape), "lse": lse.reshape(st["q"].shape[:3])}
