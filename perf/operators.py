@@ -10,8 +10,8 @@ select   louiskv.retrieve_blocks: for every tile of prompt queries the key block
 prompt   louiskv.sparse_prefill_attn: causal attention of the prompt's queries over their selected blocks.
 
 The 4-bit format: 32 consecutive channels of a row share the scale 2^E, the smallest power of two with max|x| <= 7 * 2^E
-(E >= -125), stored as the byte E + 127; an element is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the scale with
-its sign (ties to the even code), two to a byte, the lower channel in the lower nibble.  A block with an infinity or
+(-125 <= E <= 125), stored as the byte E + 127; an element is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the
+scale with its sign (ties to the even code), two to a byte, the lower channel in the lower nibble.  A block with an infinity or
 NaN has the byte 255 and stands for NaN.  A pool row is 64 key bytes and 64 value bytes (`codes`), and four key scales
 and four value scales (`scales`).
 """
@@ -298,7 +298,7 @@ def _to_codes(x):
     b = x.float().reshape(*x.shape[:-1], 4, 32)
     top = b.abs().amax(-1, keepdim=True)
     m, e = torch.frexp(top)
-    e = torch.where(m <= 0.875, e - 3, e - 2).masked_fill(top == 0, -125).clamp(min=-125)
+    e = torch.where(m <= 0.875, e - 3, e - 2).masked_fill(top == 0, -125).clamp(min=-125, max=125)
     good = torch.isfinite(top)
     y = torch.where(good, torch.ldexp(b, torch.where(good, -e, 0)), torch.zeros_like(b))
     t = y.abs()
@@ -536,7 +536,7 @@ def _held(x):
     b = x.double().reshape(-1, 32)
     top = b.abs().amax(-1)
     lg = torch.full_like(top, -125.0)
-    for e in range(-125, 127):
+    for e in range(-125, 125):
         lg = torch.where(top > 7.0 * 2.0 ** e, torch.full_like(lg, e + 1.0), lg)
     unit = torch.exp2(lg).unsqueeze(-1)
     t = (b / unit).abs()
