@@ -878,6 +878,206 @@ int louiskv_sparse_decode_attn_rows_per_head(const void* q, int32_t dtype, int64
                                              void* out, int32_t out_dtype, float* lse_out,
                                              void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* The pool in 4 bits                                                        */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * A KV pool in device memory that holds every row in 4-bit floating point: 136
+ * bytes for a key and its value, where bfloat16 takes 512.
+ *
+ * Format      The d = 128 channels of a row are four blocks of 32.  A block has
+ *             the scale 2^E with the smallest E in [-125, 125] for which
+ *             max|x| <= 7 * 2^E (125 if there is none), and an element is the nearest of 0, 0.5, 1, 1.5,
+ *             2, 3, 4, 6 times the scale, with its sign (ties to the even code;
+ *             more than 6 scales become 6): below 7 * 2^125 no element is
+ *             off by more than one scale, half the widest step.  A block with an infinity or NaN
+ *             reads as 32 NaN.
+ * codes       [n_slices][pool_rows][128] uint8, 16-byte aligned: bytes 0..63 of
+ *             a row its key, 64..127 its value.  A byte holds channel 2i in its
+ *             low and 2i+1 in its high four bits, each a sign and the 3-bit index
+ *             of the level above.
+ * scales      [n_slices][pool_rows][8] uint8, 8-byte aligned: E + 127 of the
+ *             four key blocks, then of the four value blocks; 255 for a block
+ *             that is not finite.  Finite blocks have bytes 2 to 252; others mean
+ *             nothing.
+ * Limit       pool_rows <= LOUISKV_Q4_MAX_POOL_ROWS (LOUISKV_ERR_SHAPE).
+ */
+#define LOUISKV_Q4_MAX_POOL_ROWS (1 << 24)
+
+/*
+ * louiskv_pack_pool into a 4-bit pool: row r of each slice holds the key and
+ * value of token perm[r], quantised; rows behind n_tokens stay as they were.
+ *
+ * keys, values [n_slices][n_tokens][d] dtype, both required.
+ * perm        [n_slices][n_tokens] int32 as written by louiskv_cluster_prefill
+ *             (entries are clamped into [0, n_tokens)), or NULL: token order, the
+ *             pool of louiskv_page_prefill.
+ */
+int louiskv_pack_pool_q4(const void* keys, const void* values, int32_t dtype,
+                         int64_t n_slices, int32_t n_tokens, int32_t d,
+                         const int32_t* perm, uint8_t* codes, uint8_t* scales,
+                         int64_t pool_rows, void* stream);
+
+/*
+ * Rows of a 4-bit pool as the values they stand for, in a dense buffer (the
+ * KV_critical that louiskv_sparse_decode_attn reads): row i of slice s is pool
+ * row sel_rows[s][i], i < n_sel[s]; rows behind n_sel stay as they were.  Every
+ * value is exact in bfloat16 and float32.
+ *
+ * sel_rows    [n_slices][buf_rows] int32, clamped into [0, pool_rows), or NULL:
+ *             rows 0, 1, ... of the pool (buf_rows <= pool_rows).
+ * n_sel       [n_slices] int32 (clamped into [0, buf_rows]), or NULL: buf_rows.
+ * k_buf, v_buf out [n_slices][buf_rows][d] dtype.
+ */
+int louiskv_gather_rows_q4(const uint8_t* codes, const uint8_t* scales, int64_t n_slices,
+                           int64_t pool_rows, int32_t d, const int32_t* sel_rows,
+                           const int32_t* n_sel, int32_t buf_rows, void* k_buf, void* v_buf,
+                           int32_t dtype, void* stream);
+
+/*
+ * louiskv_segment_output with the evicted segment's rows quantised into a
+ * 4-bit pool.  The window and the segment's mean key stay in full precision
+ * (the mean is of the window's keys, not of what the pool holds of them).
+ * codes, scales NULL (both): no pool is written.  Other arguments as there.
+ */
+int louiskv_segment_output_q4(const void* k_new, const void* v_new, int32_t dtype,
+                              int64_t n_slices, int32_t d,
+                              void* k_local, void* v_local, int32_t window,
+                              int32_t step, int32_t seg_len,
+                              float* reps, int32_t* unit_start, int32_t* unit_size,
+                              int32_t units_cap, int32_t n_clusters,
+                              uint8_t* codes, uint8_t* scales, int64_t pool_rows,
+                              int32_t prompt_len, void* stream);
+
+/*
+ * louiskv_segment_output_boundary with the evicted segment's rows quantised
+ * into a 4-bit pool; arguments as there, codes and scales as above.
+ */
+int louiskv_segment_output_boundary_q4(const void* k_new, const void* v_new, int32_t dtype,
+                                       int64_t n_slices, int32_t n_kv_heads, int32_t d,
+                                       void* k_local, void* v_local, int32_t window,
+                                       int32_t step, int32_t seg_max, const uint8_t* fire,
+                                       int32_t* seg_state, float* reps, int32_t* unit_start,
+                                       int32_t* unit_size, int32_t units_cap,
+                                       int32_t n_clusters, uint8_t* codes, uint8_t* scales,
+                                       int64_t pool_rows, int32_t prompt_len, void* stream);
+
+size_t louiskv_sparse_decode_attn_rows_q4_workspace_size(int64_t n_slices, int32_t group_size,
+                                                         int32_t d, int32_t budget,
+                                                         int32_t window);
+
+/*
+ * louiskv_sparse_decode_attn_rows over a 4-bit pool: the listed rows are read
+ * from codes and scales, the window's rows in dtype.  Arguments, outputs and
+ * the empty slice as there.  Keys and values enter the arithmetic as the exact
+ * values they stand for; scores, softmax and sums are float32, and for
+ * LOUISKV_BF16 the softmax weights are rounded to bfloat16 once, for the matrix
+ * cores (their sum and lse_out use the unrounded ones).
+ * workspace  louiskv_sparse_decode_attn_rows_q4_workspace_size() bytes, 0 where
+ *            one block takes a slice.
+ */
+int louiskv_sparse_decode_attn_rows_q4(const void* q, int32_t dtype, int64_t n_slices,
+                                       int32_t n_kv_heads, int32_t group_size, int32_t d,
+                                       float scale, const uint8_t* codes,
+                                       const uint8_t* scales, int64_t pool_rows,
+                                       const int32_t* sel_rows, const int32_t* n_sel,
+                                       int32_t budget, const void* k_local,
+                                       const void* v_local, int32_t window,
+                                       int32_t local_start, int32_t n_local, void* out,
+                                       int32_t out_dtype, float* lse_out, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/* The same with each slice's own window (louiskv_sparse_decode_attn_rows_seg). */
+int louiskv_sparse_decode_attn_rows_q4_seg(const void* q, int32_t dtype, int64_t n_slices,
+                                           int32_t n_kv_heads, int32_t group_size, int32_t d,
+                                           float scale, const uint8_t* codes,
+                                           const uint8_t* scales, int64_t pool_rows,
+                                           const int32_t* sel_rows, const int32_t* n_sel,
+                                           int32_t budget, const void* k_local,
+                                           const void* v_local, int32_t window,
+                                           const int32_t* seg_state, int32_t n_tokens,
+                                           void* out, int32_t out_dtype, float* lse_out,
+                                           void* workspace, size_t workspace_bytes,
+                                           void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* The prompt's attention over selected blocks of its keys                   */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The prompt's keys 0..n_keys-1 are cut into blocks of block_len (the last one
+ * holds the remainder; louiskv_page_prefill with page_len = block_len makes
+ * their mean keys), its queries into tiles of q_block consecutive tokens.  The
+ * queries are tokens q_start .. q_start + n_q - 1 of the sequence (a whole
+ * prompt, a chunk of it, or one token); a query sees the keys up to its own.
+ * All query heads of a KV head share a tile's selection, as in the decode
+ * stage (Appendix B).
+ *
+ * A tile whose queries are tokens p0..p1 attends to
+ *   blocks 0..n_first-1,
+ *   blocks p0/block_len - n_recent .. p1/block_len (its own and those before),
+ *   the n_top others before them with the largest scores
+ *     s_b = sum over the tile's queries and the group's heads of q . reps_b
+ *   in float64, equal scores to the lower block, a NaN below every number;
+ * or to all blocks 0..p1/block_len where there are no more than that.
+ */
+
+/* Entries a tile's list can need: min(ceil(n_keys / block_len), n_first +
+ * n_recent + n_top + blocks that q_block tokens can touch); 0 for sizes that
+ * louiskv_retrieve_blocks refuses. */
+size_t louiskv_retrieve_blocks_cap(int32_t n_keys, int32_t q_block, int32_t block_len,
+                                   int32_t n_first, int32_t n_recent, int32_t n_top);
+
+/*
+ * The selection.
+ * q           [n_groups][n_kv_heads*group_size][n_q][d] dtype.
+ * reps        [n_slices][units_cap][d] float32, row b the index vector of block b.
+ * sel_blocks  out [n_slices][n_tiles][sel_cap] int32, n_tiles = ceil(n_q / q_block):
+ *             the tile's blocks, ascending; entries behind them stay as they were.
+ * n_sel_blocks out [n_slices][n_tiles] int32.
+ * Requires 1 <= group_size <= 8, 1 <= q_block <= 128, block_len 16, 32, 64, 128
+ * or 256, q_start >= 0, q_start + n_q <= n_keys, at most 8192 blocks,
+ * blocks <= units_cap and sel_cap >= louiskv_retrieve_blocks_cap().
+ */
+int louiskv_retrieve_blocks(const void* q, int32_t dtype, int64_t n_slices,
+                            int32_t n_kv_heads, int32_t group_size, int32_t n_q, int32_t d,
+                            const float* reps, int32_t units_cap, int32_t n_keys,
+                            int32_t q_start, int32_t q_block, int32_t block_len,
+                            int32_t n_first, int32_t n_recent, int32_t n_top,
+                            int32_t* sel_blocks, int32_t sel_cap, int32_t* n_sel_blocks,
+                            void* stream);
+
+size_t louiskv_sparse_prefill_attn_workspace_size(int64_t n_slices, int32_t group_size,
+                                                  int32_t n_q, int32_t d, int32_t q_block,
+                                                  int32_t block_len, int32_t sel_cap);
+
+/*
+ * The attention: o = softmax(q K^T * scale) V for every query and head over the
+ * keys of its tile's blocks that are not behind the query's own.
+ * keys, values [n_slices][key_rows][d] dtype, rows 0..n_keys-1 (key_rows >= n_keys:
+ *             a buffer that later chunks are appended to).
+ * sel_blocks, n_sel_blocks  as louiskv_retrieve_blocks writes them, in any order
+ *             (counts are clamped into [0, sel_cap], entries into the blocks there
+ *             are; a block listed twice counts twice).
+ * out         [n_groups][n_kv_heads*group_size][n_q][d] in out_dtype.
+ * lse_out     [n_groups][n_kv_heads*group_size][n_q] float32 or NULL, as
+ *             louiskv_sparse_decode_attn; -inf and o = 0 where a query sees no key.
+ * workspace   louiskv_sparse_prefill_attn_workspace_size() bytes (partials where
+ *             few tiles have their lists split over several blocks), may be 0.
+ * Arithmetic as louiskv_sparse_decode_attn_rows_q4; group_size 1, 2, 4 or 8,
+ * other sizes as louiskv_retrieve_blocks, sel_cap >= 1.
+ */
+int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t n_slices,
+                                int32_t n_kv_heads, int32_t group_size, int32_t n_q,
+                                int32_t d, float scale, const void* keys,
+                                const void* values, int64_t key_rows, int32_t n_keys,
+                                int32_t q_start, int32_t q_block, int32_t block_len,
+                                const int32_t* sel_blocks, int32_t sel_cap,
+                                const int32_t* n_sel_blocks, void* out, int32_t out_dtype,
+                                float* lse_out, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
 #ifdef __cplusplus
 }
 #endif

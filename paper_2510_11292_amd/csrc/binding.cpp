@@ -194,6 +194,17 @@ PyMethodDef methods[] = {
     LKV_ENTRY(page_prefill, 1),
     LKV_ENTRY(retrieve_rows_per_head, 1),
     LKV_ENTRY(sparse_decode_attn_rows_per_head, 1),
+    LKV_ENTRY(pack_pool_q4, 1),
+    LKV_ENTRY(gather_rows_q4, 1),
+    LKV_ENTRY(segment_output_q4, 1),
+    LKV_ENTRY(segment_output_boundary_q4, 1),
+    LKV_ENTRY(sparse_decode_attn_rows_q4_workspace_size, 0),
+    LKV_ENTRY(sparse_decode_attn_rows_q4, 1),
+    LKV_ENTRY(sparse_decode_attn_rows_q4_seg, 1),
+    LKV_ENTRY(retrieve_blocks_cap, 0),
+    LKV_ENTRY(retrieve_blocks, 1),
+    LKV_ENTRY(sparse_prefill_attn_workspace_size, 0),
+    LKV_ENTRY(sparse_prefill_attn, 1),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -131,6 +131,31 @@ _SIGS = {
         _P, _P, _P, _I32, _I32, _P, _I32,
         _P, _P, _I64, _I32, _I32, _I32, _I32, _P,
         _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "louiskv_pack_pool_q4": (ctypes.c_int, [_P, _P, _I32, _I64, _I32, _I32, _P, _P, _P, _I64, _P]),
+    "louiskv_gather_rows_q4": (ctypes.c_int, [_P, _P, _I64, _I64, _I32, _P, _P, _I32, _P, _P, _I32, _P]),
+    "louiskv_segment_output_q4": (ctypes.c_int, [
+        _P, _P, _I32, _I64, _I32, _P, _P, _I32, _I32, _I32,
+        _P, _P, _P, _I32, _I32, _P, _P, _I64, _I32, _P]),
+    "louiskv_segment_output_boundary_q4": (ctypes.c_int, [
+        _P, _P, _I32, _I64, _I32, _I32, _P, _P, _I32, _I32, _I32, _P, _P,
+        _P, _P, _P, _I32, _I32, _P, _P, _I64, _I32, _P]),
+    "louiskv_sparse_decode_attn_rows_q4_workspace_size": (_SZ, [_I64, _I32, _I32, _I32, _I32]),
+    "louiskv_sparse_decode_attn_rows_q4": (ctypes.c_int, [
+        _P, _I32, _I64, _I32, _I32, _I32, _F,
+        _P, _P, _I64, _P, _P, _I32, _P, _P, _I32, _I32, _I32,
+        _P, _I32, _P, _P, _SZ, _P]),
+    "louiskv_sparse_decode_attn_rows_q4_seg": (ctypes.c_int, [
+        _P, _I32, _I64, _I32, _I32, _I32, _F,
+        _P, _P, _I64, _P, _P, _I32, _P, _P, _I32, _P, _I32,
+        _P, _I32, _P, _P, _SZ, _P]),
+    "louiskv_retrieve_blocks_cap": (_SZ, [_I32, _I32, _I32, _I32, _I32, _I32]),
+    "louiskv_retrieve_blocks": (ctypes.c_int, [
+        _P, _I32, _I64, _I32, _I32, _I32, _I32, _P, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _I32,
+        _P, _I32, _P, _P]),
+    "louiskv_sparse_prefill_attn_workspace_size": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I32, _I32]),
+    "louiskv_sparse_prefill_attn": (ctypes.c_int, [
+        _P, _I32, _I64, _I32, _I32, _I32, _I32, _F, _P, _P, _I64, _I32, _I32, _I32, _I32,
+        _P, _I32, _P, _P, _I32, _P, _P, _SZ, _P]),
 }
 
 EXPORTED = sorted(_SIGS)
@@ -664,3 +689,140 @@ def pack_pool(keys, values, perm, k_pool, v_pool=None, pool_on_host: bool = Fals
     _check(_native().pack_pool(
         keys, values, _dtype_code(keys), s, n, d, perm, k_pool, v_pool,
         k_pool.shape[1], int(pool_on_host), stream))
+
+
+# ---------------------------------------------------------------- the pool in 4 bits
+
+Q4_MAX_POOL_ROWS = 1 << 24
+
+
+def _pool_q4(codes, scales, n_slices: int) -> int:
+    """Rows per slice of a 4-bit pool (codes [S][rows][128], scales [S][rows][8], uint8)."""
+    rows = codes.shape[1] if codes.dim() == 3 else -1
+    if (codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or tuple(codes.shape) != (n_slices, rows, 128)
+            or tuple(scales.shape) != (n_slices, rows, 8)):
+        raise ValueError(f"a 4-bit pool of {n_slices} slices is codes [{n_slices}][rows][128] and scales "
+                         f"[{n_slices}][rows][8], uint8: got {tuple(codes.shape)} {codes.dtype}, "
+                         f"{tuple(scales.shape)} {scales.dtype}")
+    return rows
+
+
+def pack_pool_q4(keys, values, perm, codes, scales, stream=None):
+    """Prompt K/V rows quantised into a 4-bit pool in perm order (perm None: token order)."""
+    s, n, d = keys.shape
+    rows = _pool_q4(codes, scales, s)
+    _check(_native().pack_pool_q4(keys, values, _dtype_code(keys), s, n, d, perm, codes, scales, rows, stream))
+
+
+def gather_rows_q4(codes, scales, sel_rows, n_sel, k_buf, v_buf, stream=None):
+    """Rows of a 4-bit pool as the values they stand for: sel_rows [S][n] (None: rows 0, 1, ...), n_sel [S] of
+    them (None: all), into k_buf and v_buf [S][n][d]."""
+    s, n, d = k_buf.shape
+    rows = _pool_q4(codes, scales, s)
+    _check(_native().gather_rows_q4(codes, scales, s, rows, d, sel_rows, n_sel, n, k_buf, v_buf,
+                                    _dtype_code(k_buf), stream))
+
+
+def segment_output_q4(k_new, v_new, k_local, v_local, step: int, seg_len: int, reps, unit_start, unit_size,
+                      n_clusters: int, codes=None, scales=None, prompt_len: int = 0, stream=None):
+    """segment_output with the evicted rows quantised into a 4-bit pool."""
+    s, d = k_new.shape
+    rows = _pool_q4(codes, scales, s) if codes is not None else 0
+    _check(_native().segment_output_q4(
+        k_new, v_new, _dtype_code(k_new), s, d, k_local, v_local, k_local.shape[1],
+        step, seg_len, reps, unit_start, unit_size, reps.shape[1], n_clusters,
+        codes, scales, rows, prompt_len, stream))
+
+
+def segment_output_boundary_q4(k_new, v_new, k_local, v_local, step: int, seg_max: int, fire, seg_state, reps,
+                               unit_start, unit_size, n_clusters: int, n_kv_heads: int, codes=None, scales=None,
+                               prompt_len: int = 0, stream=None):
+    """segment_output_boundary with the evicted rows quantised into a 4-bit pool."""
+    s, d = k_new.shape
+    rows = _pool_q4(codes, scales, s) if codes is not None else 0
+    _check(_native().segment_output_boundary_q4(
+        k_new, v_new, _dtype_code(k_new), s, n_kv_heads, d, k_local, v_local,
+        k_local.shape[1], step, seg_max, fire, seg_state, reps, unit_start,
+        unit_size, reps.shape[1], n_clusters, codes, scales, rows, prompt_len, stream))
+
+
+def sparse_decode_attn_rows_q4_workspace_size(n_slices, group_size, budget, window, d=128) -> int:
+    return _native().sparse_decode_attn_rows_q4_workspace_size(n_slices, group_size, d, budget, window)
+
+
+def sparse_decode_attn_rows_q4(q, n_kv_heads: int, codes, scales, sel_rows, n_sel, k_local, v_local,
+                               local_start: int, n_local: int, out, lse_out=None, scale: Optional[float] = None,
+                               workspace=None, stream=None):
+    """sparse_decode_attn_rows over a 4-bit pool."""
+    g, hq, d = q.shape
+    s = n_sel.shape[0]
+    gs = hq // n_kv_heads
+    budget = sel_rows.shape[1]
+    window = k_local.shape[1]
+    rows = _pool_q4(codes, scales, s)
+    ws, wsb = _ws(workspace, q.device, sparse_decode_attn_rows_q4_workspace_size, s, gs, budget, window, d)
+    sc = (1.0 / d ** 0.5) if scale is None else scale
+    _check(_native().sparse_decode_attn_rows_q4(
+        q, _dtype_code(q), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel, budget,
+        k_local, v_local, window, local_start, n_local, out, _dtype_code(out), lse_out, ws, wsb, stream))
+
+
+def sparse_decode_attn_rows_q4_seg(q, n_kv_heads: int, codes, scales, sel_rows, n_sel, k_local, v_local, seg_state,
+                                   n_tokens: int, out, lse_out=None, scale: Optional[float] = None, workspace=None,
+                                   stream=None):
+    """sparse_decode_attn_rows_seg over a 4-bit pool."""
+    g, hq, d = q.shape
+    s = n_sel.shape[0]
+    gs = hq // n_kv_heads
+    budget = sel_rows.shape[1]
+    window = k_local.shape[1]
+    rows = _pool_q4(codes, scales, s)
+    ws, wsb = _ws(workspace, q.device, sparse_decode_attn_rows_q4_workspace_size, s, gs, budget, window, d)
+    sc = (1.0 / d ** 0.5) if scale is None else scale
+    _check(_native().sparse_decode_attn_rows_q4_seg(
+        q, _dtype_code(q), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel, budget,
+        k_local, v_local, window, seg_state, n_tokens, out, _dtype_code(out), lse_out, ws, wsb, stream))
+
+
+# ---------------------------------------------------------------- the prompt's attention over selected blocks
+
+def retrieve_blocks_cap(n_keys: int, q_block: int, block_len: int, n_first: int, n_recent: int, n_top: int) -> int:
+    """Entries a tile's list can need (0 for sizes that retrieve_blocks refuses)."""
+    return _native().retrieve_blocks_cap(n_keys, q_block, block_len, n_first, n_recent, n_top)
+
+
+def retrieve_blocks(q, n_kv_heads: int, reps, n_keys: int, q_start: int, q_block: int, block_len: int, n_first: int,
+                    n_recent: int, n_top: int, sel_blocks, n_sel_blocks, stream=None):
+    """The key blocks that every tile of q_block queries attends to: q [G][Hq][n_q][d], reps [S][blocks..][d] (the
+    mean keys, as page_prefill makes them), sel_blocks [S][tiles][cap], n_sel_blocks [S][tiles]."""
+    g, hq, n_q, d = q.shape
+    s = g * n_kv_heads
+    if tuple(sel_blocks.shape[:2]) != (s, -(-n_q // max(q_block, 1))) or n_sel_blocks.shape != sel_blocks.shape[:2]:
+        raise ValueError(f"sel_blocks {tuple(sel_blocks.shape)} and n_sel_blocks {tuple(n_sel_blocks.shape)} do not "
+                         f"hold a list for each of {s} slices' {-(-n_q // max(q_block, 1))} tiles")
+    _check(_native().retrieve_blocks(
+        q, _dtype_code(q), s, n_kv_heads, hq // n_kv_heads, n_q, d, reps, reps.shape[1], n_keys, q_start, q_block,
+        block_len, n_first, n_recent, n_top, sel_blocks, sel_blocks.shape[2], n_sel_blocks, stream))
+
+
+def sparse_prefill_attn_workspace_size(n_slices, group_size, n_q, q_block, block_len, sel_cap, d=128) -> int:
+    return _native().sparse_prefill_attn_workspace_size(n_slices, group_size, n_q, d, q_block, block_len, sel_cap)
+
+
+def sparse_prefill_attn(q, n_kv_heads: int, keys, values, n_keys: int, q_start: int, q_block: int, block_len: int,
+                        sel_blocks, n_sel_blocks, out, lse_out=None, scale: Optional[float] = None, workspace=None,
+                        stream=None):
+    """Causal attention of queries q_start.. over their tiles' key blocks: q and out [G][Hq][n_q][d], keys and
+    values [S][rows >= n_keys][d], the lists as retrieve_blocks writes them."""
+    g, hq, n_q, d = q.shape
+    s = g * n_kv_heads
+    gs = hq // n_kv_heads
+    if tuple(sel_blocks.shape[:2]) != (s, -(-n_q // max(q_block, 1))) or n_sel_blocks.shape != sel_blocks.shape[:2]:
+        raise ValueError(f"sel_blocks {tuple(sel_blocks.shape)} and n_sel_blocks {tuple(n_sel_blocks.shape)} do not "
+                         f"hold a list for each of {s} slices' {-(-n_q // max(q_block, 1))} tiles")
+    cap = sel_blocks.shape[2]
+    ws, wsb = _ws(workspace, q.device, sparse_prefill_attn_workspace_size, s, gs, n_q, q_block, block_len, cap, d)
+    sc = (1.0 / d ** 0.5) if scale is None else scale
+    _check(_native().sparse_prefill_attn(
+        q, _dtype_code(q), s, n_kv_heads, gs, n_q, d, float(sc), keys, values, keys.shape[1], n_keys, q_start,
+        q_block, block_len, sel_blocks, cap, n_sel_blocks, out, _dtype_code(out), lse_out, ws, wsb, stream))

@@ -1,0 +1,189 @@
+"""The 4-bit pool and the prompt's block calls without a GPU: the oracle's format
+against facts that do not retype it, and the refusals of every entry point,
+which return before any launch."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import blocks as ob
+from oracle import pool4 as o4
+
+P = ctypes.c_void_p
+OK, NULL, SHAPE, DTYPE, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3, 4, 5
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2510_11292_amd import louiskv
+    if not os.path.exists(louiskv.LIB_PATH):
+        pytest.fail("liblouiskv.so is not built")
+    return louiskv.load_library()
+
+
+def test_levels_and_nibbles_round_trip():
+    rng = np.random.default_rng(0)
+    codes = rng.integers(0, 256, (5, 128), dtype=np.uint8)
+    scales = rng.integers(100, 150, (5, 8), dtype=np.uint8)
+    k, v = o4.values(codes, scales)
+    assert k[0, 0] == (-1.0 if codes[0, 0] & 8 else 1.0) * o4.LEVELS[codes[0, 0] & 7] * 2.0 ** (int(scales[0, 0]) - 127)
+    assert v[4, 127] == ((-1.0 if codes[4, 127] & 128 else 1.0) * o4.LEVELS[(codes[4, 127] >> 4) & 7]
+                         * 2.0 ** (int(scales[4, 7]) - 127))
+    # what the values quantise to stands for the same values: a fixed point
+    for x in (k, v):
+        c, s = o4.quantise(x)
+        b, sc = o4.pack_bytes(c, s, c, s)
+        np.testing.assert_array_equal(o4.values(b, sc)[0], x)
+
+
+def test_quantisation_is_nearest_and_within_a_scale():
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((40, 128)) * 2.0 ** rng.integers(-30, 30, (40, 1))
+    c, s = o4.quantise(x)
+    held = o4.values(*o4.pack_bytes(c, s, c, s))[0]
+    unit = np.repeat(2.0 ** (s.astype(float) - 127), 32, axis=1)
+    assert np.all(np.abs(held - x) <= unit)
+    grid = np.concatenate([-o4.LEVELS, o4.LEVELS])
+    best = np.abs(x[..., None] - grid * unit[..., None]).min(-1)
+    np.testing.assert_array_equal(np.abs(held - x), best)
+    top = np.abs(x).reshape(40, 4, 32).max(-1)
+    assert np.all(top <= 7 * 2.0 ** (s.astype(float) - 127)) and np.all(top > 3.5 * 2.0 ** (s.astype(float) - 127))
+
+
+def test_ties_extremes_and_blocks_that_are_not_finite():
+    x = np.zeros((4, 128))
+    x[0, :16] = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, -0.25, -5.0, 6.5, 4.999, -7.0, 0.0, 1.0, 6.0]
+    x[1, 3], x[1, 40] = np.inf, np.nan
+    x[2, :3] = [2.0 ** -133, 2.0 ** -126, 2.0 ** -125]
+    x[3, 0] = 3.3e38
+    c, s = o4.quantise(x)
+    held = o4.values(*o4.pack_bytes(c, s, c, s))[0]
+    np.testing.assert_array_equal(held[0, :16], [0, 1, 1, 2, 2, 4, 4, 6, 0, -4, 6, 4, -6, 0, 1, 6])
+    assert np.isnan(held[1, :64]).all() and (held[1, 64:] == 0).all()
+    assert s[2, 0] == 2 and list(held[2, :3]) == [0.0, 2.0 ** -126, 2.0 ** -125]
+    assert s[3, 0] == 252 and held[3, 0] == 6 * 2.0 ** 125
+
+
+def test_oracle_selection_and_attention():
+    rng = np.random.default_rng(2)
+    reps = rng.standard_normal((20, 8))
+    q = rng.standard_normal((6, 8))
+    got = ob.tile_blocks(q, reps, 16 * 18 + 3, 16 * 19 + 2, 16, 1, 2, 3)
+    assert got[0] == 0 and got[-4:] == [16, 17, 18, 19] and len(got) == 8
+    score = q.sum(0) @ reps.T
+    assert set(got[1:4]) == set(1 + np.argsort(-score[1:16])[:3])
+    assert ob.tile_blocks(q, reps, 0, 5, 16, 1, 2, 3) == [0]
+    assert ob.tile_blocks(q, np.ones((9, 8)), 16 * 8, 16 * 8, 16, 0, 0, 2) == [0, 1, 8]   # equal scores: the lower block
+    k, v, qq = rng.standard_normal((9, 8)), rng.standard_normal((9, 8)), rng.standard_normal((3, 8))
+    see = rng.random((3, 9)) < 0.5
+    see[1] = False
+    see[0, 0] = see[2, 1] = True
+    out, lse, _, _ = ob.masked_attention(qq, k, v, see, 0.3)
+    t = torch.nn.functional.scaled_dot_product_attention(*(torch.from_numpy(x)[None] for x in (qq, k, v)),
+                                                         attn_mask=torch.from_numpy(see)[None], scale=0.3)[0].numpy()
+    np.testing.assert_allclose(out[[0, 2]], t[[0, 2]], rtol=1e-12)
+    assert np.isneginf(lse[1]) and (out[1] == 0).all()
+
+
+# ------------------------------------------------------------------- refusals
+
+def _statuses(fn, base, table):
+    for change, want in table:
+        args = list(base)
+        for i, v in change.items():
+            args[i] = v
+        got = fn(*args)
+        assert got == want, f"{change}: {got}, expected {want}"
+
+
+D16 = P(4096)
+
+
+def test_pack_and_gather_refuse(lib):
+    base = [D16, D16, 1, 2, 64, 128, None, D16, D16, 64, None]
+    _statuses(lib.louiskv_pack_pool_q4, base, [
+        ({0: None}, NULL), ({1: None}, NULL), ({7: None}, NULL), ({8: None}, NULL), ({2: 2}, DTYPE),
+        ({5: 64}, UNSUPPORTED), ({3: 0}, SHAPE), ({4: 0}, SHAPE), ({9: 63}, SHAPE), ({9: (1 << 24) + 1}, SHAPE),
+        ({7: P(4104)}, UNSUPPORTED), ({8: P(4100)}, UNSUPPORTED)])
+    base = [D16, D16, 2, 64, 128, None, None, 64, D16, D16, 1, None]
+    _statuses(lib.louiskv_gather_rows_q4, base, [
+        ({0: None}, NULL), ({9: None}, NULL), ({10: 5}, DTYPE), ({4: 96}, UNSUPPORTED), ({2: 0}, SHAPE),
+        ({7: 0}, SHAPE), ({7: 65}, SHAPE), ({3: 0}, SHAPE), ({0: P(4100)}, UNSUPPORTED)])
+
+
+def test_segment_stores_refuse(lib):
+    #       k_new v_new dt S  d    kl   vl  win step seg reps st  size cap nc codes scales rows prompt
+    base = [D16, D16, 1, 8, 128, D16, D16, 64, 64, 32, D16, D16, D16, 10, 9, D16, D16, 132, 100, None]
+    _statuses(lib.louiskv_segment_output_q4, base, [
+        ({0: None}, NULL), ({6: None}, NULL), ({10: None}, NULL), ({15: None}, NULL), ({16: None}, NULL),
+        ({2: 9}, DTYPE), ({4: 64}, UNSUPPORTED), ({3: 0}, SHAPE), ({7: 60}, SHAPE), ({8: -1}, SHAPE),
+        ({13: 9}, SHAPE), ({14: -1}, SHAPE), ({17: 131}, SHAPE), ({18: -1}, SHAPE), ({15: P(4097)}, UNSUPPORTED)])
+    #       k_new v_new dt S kv d    kl   vl  win step max fire state reps st size cap nc codes scales rows prompt
+    base = [D16, D16, 1, 8, 8, 128, D16, D16, 64, 0, 16, None, D16, D16, D16, D16, 20, 10, D16, D16, 200, 100, None]
+    _statuses(lib.louiskv_segment_output_boundary_q4, base, [
+        ({0: None}, NULL), ({12: None}, NULL), ({13: None}, NULL), ({18: None}, NULL), ({2: -1}, DTYPE),
+        ({5: 64}, UNSUPPORTED), ({4: 3}, SHAPE), ({8: 1}, SHAPE), ({10: 64}, SHAPE), ({9: -2}, SHAPE), ({17: 0}, SHAPE),
+        ({17: 21}, SHAPE), ({20: 99}, SHAPE), ({21: -1}, SHAPE), ({20: 0}, SHAPE)])
+
+
+def test_attention_refuses(lib):
+    ws = lib.louiskv_sparse_decode_attn_rows_q4_workspace_size(8, 4, 128, 2048, 128)
+    assert ws > 0 and lib.louiskv_sparse_decode_attn_rows_q4_workspace_size(4096, 4, 128, 2048, 128) == 0
+    assert lib.louiskv_sparse_decode_attn_rows_q4_workspace_size(0, 4, 128, 2048, 128) == 0
+    #       q  dt S kv g  d   scale codes scales rows sel n_sel budget kl vl win start n out odt lse ws bytes
+    base = [D16, 1, 8, 8, 4, 128, 0.1, D16, D16, 4096, D16, D16, 2048, D16, D16, 128, 0, 128, D16, 1, None, D16, ws, None]
+    table = [
+        ({0: None}, NULL), ({7: None}, NULL), ({8: None}, NULL), ({10: None}, NULL), ({11: None}, NULL),
+        ({13: None}, NULL), ({18: None}, NULL), ({1: 3}, DTYPE), ({19: 2}, DTYPE), ({5: 64}, UNSUPPORTED),
+        ({4: 3}, UNSUPPORTED), ({4: 16}, UNSUPPORTED), ({3: 3}, SHAPE), ({9: 0}, SHAPE), ({9: 1 << 25}, SHAPE),
+        ({12: -1}, SHAPE), ({17: 129}, SHAPE), ({16: 128}, SHAPE), ({21: None}, WORKSPACE), ({22: ws - 1}, WORKSPACE)]
+    _statuses(lib.louiskv_sparse_decode_attn_rows_q4, base, table)
+    seg = base[:16] + [D16, 5] + base[18:]
+    _statuses(lib.louiskv_sparse_decode_attn_rows_q4_seg, seg, [
+        ({16: None}, NULL), ({13: None}, NULL), ({14: None}, NULL), ({15: 1}, SHAPE), ({17: 0}, SHAPE),
+        ({22: ws - 1}, WORKSPACE)])
+
+
+def test_block_calls_refuse(lib):
+    cap = lib.louiskv_retrieve_blocks_cap
+    assert cap(32768, 64, 64, 1, 4, 24) == 1 + 4 + 24 + 2
+    assert cap(100, 64, 64, 1, 4, 24) == 2 and cap(4096, 1, 16, 0, 0, 0) == 1
+    assert cap(0, 64, 64, 1, 4, 24) == cap(100, 129, 64, 1, 4, 24) == cap(100, 64, 48, 1, 4, 24) == 0
+    assert cap(100, 64, 64, -1, 4, 24) == cap(100, 0, 64, 1, 4, 24) == 0
+    big = (1 << 31) - 1
+    assert cap(big, 128, 16, big, big, big) == -(-big // 16)
+    #       q  dt S kv g nq  d  reps cap keys start tile block first recent top sel cap n_sel
+    base = [D16, 1, 8, 8, 4, 500, 128, D16, 32, 2000, 1500, 64, 64, 1, 2, 4, D16, 9, D16, None]
+    _statuses(lib.louiskv_retrieve_blocks, base, [
+        ({0: None}, NULL), ({7: None}, NULL), ({16: None}, NULL), ({18: None}, NULL), ({1: 2}, DTYPE),
+        ({6: 64}, UNSUPPORTED), ({4: 9}, UNSUPPORTED), ({4: 0}, UNSUPPORTED), ({11: 0}, UNSUPPORTED),
+        ({11: 129}, UNSUPPORTED), ({12: 48}, UNSUPPORTED), ({3: 5}, SHAPE), ({5: 0}, SHAPE), ({9: 0}, SHAPE),
+        ({10: -1}, SHAPE), ({10: 1501}, SHAPE), ({8: 31}, SHAPE), ({17: 8}, SHAPE), ({13: -1}, SHAPE), ({14: -1}, SHAPE),
+        ({15: -1}, SHAPE), ({9: 200000, 12: 16, 8: 20000, 17: 100}, SHAPE)])
+    #       q  dt S kv g nq  d  scale k v rows keys start tile block sel cap n_sel out odt lse ws bytes
+    base = [D16, 1, 8, 8, 4, 500, 128, 0.1, D16, D16, 2000, 2000, 1500, 64, 64, D16, 9, D16, D16, 1, None, None, 0, None]
+    _statuses(lib.louiskv_sparse_prefill_attn, base, [
+        ({0: None}, NULL), ({8: None}, NULL), ({9: None}, NULL), ({15: None}, NULL), ({17: None}, NULL),
+        ({18: None}, NULL), ({1: 2}, DTYPE), ({19: 2}, DTYPE), ({6: 64}, UNSUPPORTED), ({4: 3}, UNSUPPORTED),
+        ({13: 0}, UNSUPPORTED), ({14: 512}, UNSUPPORTED), ({3: 5}, SHAPE), ({10: 1999}, SHAPE), ({16: 0}, SHAPE),
+        ({12: 1501}, SHAPE)])
+
+
+def test_python_calls_check_shapes():
+    from paper_2510_11292_amd import louiskv as L
+    k = torch.zeros(2, 10, 128)
+    with pytest.raises(ValueError, match="4-bit pool"):
+        L.pack_pool_q4(k, k, None, torch.zeros(2, 10, 64, dtype=torch.uint8), torch.zeros(2, 10, 8, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="4-bit pool"):
+        L.gather_rows_q4(torch.zeros(2, 10, 128, dtype=torch.uint8), torch.zeros(2, 9, 8, dtype=torch.uint8), None, None, k, k)
+    q = torch.zeros(1, 4, 100, 128)
+    sel, n = torch.zeros(2, 3, 4, dtype=torch.int32), torch.zeros(2, 3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="lists|list for each"):
+        L.retrieve_blocks(q, 2, torch.zeros(2, 8, 128), 100, 0, 64, 16, 0, 0, 1, sel, n)
+    with pytest.raises(ValueError, match="lists|list for each"):
+        L.sparse_prefill_attn(q, 2, k, k, 100, 0, 64, 16, sel, n, q)
+    with pytest.raises(ValueError, match="contiguous"):
+        c = torch.zeros(2, 10, 256, dtype=torch.uint8)[..., :128]
+        L.pack_pool_q4(k, k, None, c, torch.zeros(2, 10, 8, dtype=torch.uint8))
