@@ -175,6 +175,372 @@ struct PrefillArgs {
   float* lse_out;
 };
 
+// ---- bf16: matrix cores
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// Waits for every copy and LDS access of the wave, then for the block's waves.
+__device__ __forceinline__ void sync_stage() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// 64 lanes copy 16 bytes each from base + off (per lane) to LDS lds + 16 * lane.
+__device__ __forceinline__ void copy_to_lds(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+
+typedef __attribute__((address_space(3))) char* lds_ptr;
+__device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(lds_ptr)p; }
+
+// Rows of 256 bytes lie in LDS with their sixteen 16-byte pieces permuted, piece c
+// of row r at c ^ swizzle(r): sixteen consecutive rows put a piece in sixteen
+// different places (the key reads, a lane a row), and four consecutive rows put
+// a run of four pieces in four different ones (the transposing value reads).
+__device__ __forceinline__ int swizzle(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
+
+constexpr float kGrow = 8.0f;   // base-2 logits may pass the base by this much before the sums are rescaled
+
+// Block (slice, tile, row group, split): rows r of the tile are (token r / g, head
+// r % g), 32 NT of them a wave, WR waves of rows by WK waves that share the keys.
+// Keys and values of 64 list positions at a time are copied to LDS (two stages,
+// one in flight).  A wave computes S^T = K Q^T for 32 keys, so that a lane holds 16 scores
+// of one query row; their exponentials are, unmoved, the B operand of
+// O^T += V^T P^T, whose A operand comes from LDS through transposing reads.  The
+// running base, sum and the rescale are then a lane's own.
+constexpr int kStageKeys = 64;
+constexpr int kStageBytes = kStageKeys * kHeadDim * 2;   // of the keys, and of the values
+
+template <int NT, int WR, int WK>
+__global__ __launch_bounds__(WR * WK * 64, NT == 1 ? 2 : 1)
+void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) {
+  constexpr int NW = WR * WK;
+  constexpr int kGroups = kStageKeys / 16 / NW;   // 16-row groups that a wave copies
+  static_assert(kStageKeys % (16 * NW) == 0 && 2 % WK == 0, "waves share a stage evenly");
+  __shared__ __align__(256) char s_stage0[2 * kStageBytes], s_stage1[2 * kStageBytes];
+  __shared__ int s_bad;
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, n = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wr = w % WR, wk = w / WR;
+  // Neighbouring tiles of a slice, which share blocks, go to one XCD (blocks are
+  // dealt to the eight in turn).
+  int64_t id = blockIdx.x;
+  if (n_blocks >= 64) {
+    const int64_t per = n_blocks >> 3, rest = n_blocks & 7, x = id & 7;
+    id = x * per + min<int64_t>(x, rest) + (id >> 3);
+  }
+  const int split = (int)(id % a.n_split);
+  id /= a.n_split;
+  const int rgrp = (int)(id % row_groups);
+  id /= row_groups;
+  const int64_t s = id / a.n_tiles;
+  const int t = (int)(id - s * a.n_tiles);
+  const int lg = 31 - __builtin_clz(a.group_size);
+  const int i0 = t * a.q_block, n_tok = min(a.q_block, a.n_q - i0), n_rows = n_tok << lg;
+  const int row0 = (rgrp * WR + wr) * 32 * NT;    // of this wave, in the tile
+  if (rgrp * WR * 32 * NT >= n_rows) return;      // the tile is shorter than the others (block-uniform)
+
+  // this lane's rows
+  bf16x8 q[NT][8];
+  int qpos[NT];
+  const float qs = a.scale * kLog2E;
+  const uint32_t flip = qs < 0.f ? 0x80008000u : 0u;     // |scale| multiplies the scores of -q
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+    const int r = min(row0 + 32 * x + n, n_rows - 1);
+    const int tok = r >> lg;
+    qpos[x] = a.q_start + i0 + tok;
+    const uint4* src = reinterpret_cast<const uint4*>(
+        static_cast<const uint16_t*>(a.q) + (((size_t)s * a.group_size + (r & (a.group_size - 1))) * a.n_q + i0 + tok) * kHeadDim);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      uint4 v = src[2 * c + h];
+      v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
+      q[x][c] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the queries are in before the copies start
+#pragma unroll
+  for (int x = 0; x < NT; ++x)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) asm volatile("" : "+v"(q[x][c]));
+  const float mult = fabsf(qs);
+  const int first_pos = a.q_start + i0 + (min(row0, n_rows - 1) >> lg);
+  const int last_pos = a.q_start + i0 + (min(row0 + 32 * NT - 1, n_rows - 1) >> lg);
+  const int block_first = a.q_start + i0 + ((rgrp * WR * 32 * NT) >> lg);   // first token of the block
+
+  const int64_t list = s * a.n_tiles + t;
+  const int32_t* sel = a.sel + (size_t)list * a.sel_cap;
+  const int n_list = max(0, min(a.n_sel[list], a.sel_cap));
+  const int e0 = (int)((int64_t)n_list * split / a.n_split), e1 = (int)((int64_t)n_list * (split + 1) / a.n_split);
+  const int last_block = (a.n_keys - 1) >> a.log_block;
+  const int n_groups = (e1 - e0) << (a.log_block - 4);           // of 16 keys
+  const int n_stages = (n_groups + kStageKeys / 16 - 1) / (kStageKeys / 16);
+  // Entries e0 + 64 c + lane of the list, and the next 64.
+  int cur = 0, nxt = 0, cur_base = 0;
+  auto entries = [&](int at) { return min(max(sel[min(e0 + at + lane, max(e1 - 1, 0))], 0), last_block); };
+  if (n_list > 0 && e1 > e0) {
+    cur = entries(0);
+    nxt = entries(64);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" : "+v"(cur), "+v"(nxt));
+  // token of the first key of 16-key group gi (which is below n_groups)
+  auto group_pos = [&](int gi) -> int {
+    const int e = gi >> (a.log_block - 4);
+    const int v = e - cur_base < 64 ? __builtin_amdgcn_readlane(cur, (e - cur_base) & 63)
+                                    : __builtin_amdgcn_readlane(nxt, (e - cur_base) & 63);
+    return (v << a.log_block) + ((gi & ((1 << (a.log_block - 4)) - 1)) << 4);
+  };
+  const char* kb = static_cast<const char*>(a.keys) + (size_t)s * a.key_rows * kHeadDim * 2;
+  const char* vb = static_cast<const char*>(a.values) + (size_t)s * a.key_rows * kHeadDim * 2;
+  // groups w, w + NW, .. of stage st to LDS; a group past the list repeats its last
+  auto copy_stage = [&](int st, char* buf) {
+#pragma unroll
+    for (int x = 0; x < kGroups; ++x) {
+      const int g16 = w + NW * x;
+      const int pos = group_pos(min(st * (kStageKeys / 16) + g16, n_groups - 1));
+      const int from = min(pos, a.n_keys - 1);                          // rows behind the last key repeat it
+      const char* kg = kb + (size_t)from * (kHeadDim * 2);
+      const char* vg = vb + (size_t)from * (kHeadDim * 2);
+      const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(buf) + g16 * 16 * kHeadDim * 2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = min(4 * i + (lane >> 4), a.n_keys - 1 - from);
+        const uint32_t off = r * (kHeadDim * 2) + (((lane & 15) ^ swizzle(4 * i + (lane >> 4))) << 4);
+        copy_to_lds(kg, off, dst + i * 1024);
+        copy_to_lds(vg, off, dst + kStageBytes + i * 1024);
+      }
+    }
+  };
+
+  f32x16 o[NT][4];
+  float base[NT], grow_at[NT], sum[NT];
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+    base[x] = 0.f;
+    grow_at[x] = -__builtin_inff();
+    sum[x] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[x][dt][i] = 0.f;
+  }
+  // byte offsets of this lane's reads in a 32-key half of a stage
+  const uint32_t k_off = n * 256 + ((h ^ swizzle(n & 15)) << 4);                      // piece 2c + h: ^ (c << 5)
+  const int j4 = (lane & 15) >> 2, xp = (((lane >> 4) & 1) << 1) | ((lane & 3) >> 1);
+  const uint32_t v_off = (4 * h + j4) * 256 + (((j4 << 2) | (xp ^ h)) << 4) + ((lane & 1) << 3);   // ^ (dt << 6)
+
+  auto subtile = [&](const char* buf, int st, int sub) {
+    const int gi = st * (kStageKeys / 16) + 2 * sub;
+    if (gi >= n_groups) return;
+    const int p0 = group_pos(gi);
+    const int p1 = gi + 1 < n_groups ? group_pos(gi + 1) : INT32_MAX - 16;   // no key there
+    if (min(p0, p1) > last_pos) return;
+    const char* kt = buf + sub * 32 * 256;
+    const char* vt = buf + kStageBytes + sub * 32 * 256;
+    f32x16 sc[NT];
+#pragma unroll
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[x][i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + (k_off ^ (c << 5)));
+#pragma unroll
+      for (int x = 0; x < NT; ++x) sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[x][c], sc[x], 0, 0, 0);
+    }
+    const bool masked = max(p0, p1) + 15 > first_pos;
+    bf16x8 pb[NT][2];
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+      float m = mult;
+      if (masked) {
+        m = 1.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = (i < 8 ? p0 : p1) + (i & 3) + 8 * ((i >> 2) & 1) + 4 * h;
+          sc[x][i] = key <= qpos[x] ? sc[x][i] * mult : -__builtin_inff();
+        }
+      }
+      float top = sc[x][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[x][i]);
+      top *= m;
+      if (__builtin_amdgcn_ballot_w64(top > grow_at[x])) {
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        if (top > grow_at[x]) {
+          // before the first finite score the sums are 0 (or NaN): any factor does
+          const float f = grow_at[x] == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(base[x] - top);
+          base[x] = top;
+          grow_at[x] = top + kGrow;
+          sum[x] *= f;
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt) o[x][dt] *= f;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(sc[x][8 * k + j], m, -base[x]));
+          sum[x] += p;
+          pb[x][k][j] = (__bf16)p;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        // rows 16 k + 4 h + 0..3, then those + 8 (the same swizzle but for bit 1)
+        const char* vp = vt + 16 * 256 * k;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(vp + (v_off ^ (dt << 6))));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(vp + 8 * 256 + (v_off ^ (dt << 6) ^ 32)));
+        const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
+          o[x][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pb[x][k], o[x][dt], 0, 0, 0);
+      }
+  };
+
+  // Values that a query may not see must not reach it: 0 * inf is NaN.  In a stage
+  // that holds keys behind the block's first query, values that are not finite
+  // become 0 and are added to the queries that do see them.
+  auto clear_not_finite = [&](char* buf, int st) {
+    const int gi = st * (kStageKeys / 16);
+    int top = 0;
+#pragma unroll
+    for (int x = 0; x < kStageKeys / 16; ++x) top = max(top, gi + x < n_groups ? group_pos(gi + x) : INT32_MAX - 16);
+    if (top + 15 <= block_first) return;       // block-uniform
+    uint4* v = reinterpret_cast<uint4*>(buf + kStageBytes);
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kStageBytes / 16 / (NW * 64); ++i) {
+      uint4 u = v[tid + i * NW * 64];
+      uint32_t* e = &u.x;
+      bool bad = false;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const bool b0 = (e[c] & 0x7f80u) == 0x7f80u, b1 = (e[c] & 0x7f800000u) == 0x7f800000u;
+        e[c] &= (b0 ? 0xffff0000u : ~0u) & (b1 ? 0x0000ffffu : ~0u);
+        bad |= b0 | b1;
+      }
+      if (bad) v[tid + i * NW * 64] = u;
+      any |= bad;
+    }
+    if (any) s_bad = st + 1;
+    __syncthreads();
+    if (s_bad != st + 1) return;
+    for (int x = 0; x < kStageKeys; ++x) {
+      if (x / 32 % WK != wk || gi + x / 16 >= n_groups) continue;
+      const int pos = group_pos(gi + x / 16) + (x & 15);
+      if (pos > last_pos) continue;
+      const uint16_t* row = reinterpret_cast<const uint16_t*>(vb) + (size_t)pos * kHeadDim;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float f = bf16_to_f32(row[32 * dt + (i & 3) + 8 * (i >> 2) + 4 * h]);
+          if (__builtin_isfinite(f)) continue;
+#pragma unroll
+          for (int y = 0; y < NT; ++y) o[y][dt][i] += pos <= qpos[y] ? f : 0.f;
+        }
+    }
+  };
+
+  auto stage = [&](char* buf, char* other, int st) {
+    sync_stage();                               // stage st is in LDS; `other` is free
+    if (((st * (kStageKeys / 16)) >> (a.log_block - 4)) - cur_base >= 64) {   // the list's next 64 entries
+      cur = nxt;
+      cur_base += 64;
+      nxt = entries(cur_base + 64);
+      asm volatile("s_waitcnt vmcnt(0)" : "+v"(nxt));   // now, not at a use that copies are in flight at
+    }
+    if (st + 1 < n_stages) copy_stage(st + 1, other);
+    clear_not_finite(buf, st);
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+      if (sub % WK == wk || WK == 1) subtile(buf, st, sub);
+  };
+  if (tid == 0) s_bad = 0;
+  if (n_stages > 0) copy_stage(0, s_stage0);
+  for (int st = 0; st < n_stages; st += 2) {
+    stage(s_stage0, s_stage1, st);
+    if (st + 1 < n_stages) stage(s_stage1, s_stage0, st + 1);
+  }
+  sync_stage();
+
+  // the waves that shared the keys: wk = 1 leaves its sums in LDS, wk = 0 adds them
+  float m[NT];
+#pragma unroll
+  for (int x = 0; x < NT; ++x) m[x] = grow_at[x] == -__builtin_inff() ? -__builtin_inff() : base[x];
+  if constexpr (WK > 1) {
+    static_assert(NT == 1 && WK == 2 && WR * 34 * 256 <= 2 * kStageBytes, "half of a wave's sums fit a stage");
+    float* s0 = reinterpret_cast<float*>(s_stage0) + wr * 34 * 64 + lane;
+    float* s1 = reinterpret_cast<float*>(s_stage1) + wr * 34 * 64 + lane;
+    if (wk == 1) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        s0[i * 64] = o[0][i >> 4][i & 15];
+        s1[i * 64] = o[0][2 + (i >> 4)][i & 15];
+      }
+      s0[32 * 64] = m[0];
+      s1[32 * 64] = sum[0];
+    }
+    __syncthreads();
+    if (wk == 1) return;
+    const float m1 = s0[32 * 64], mm = fmaxf(m[0], m1);
+    const float f0 = __builtin_amdgcn_exp2f(m[0] - max_base(mm)), f1 = __builtin_amdgcn_exp2f(m1 - max_base(mm));
+    m[0] = mm;
+    sum[0] = sum[0] * f0 + s1[32 * 64] * f1;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      o[0][i >> 4][i & 15] = o[0][i >> 4][i & 15] * f0 + s0[i * 64] * f1;
+      o[0][2 + (i >> 4)][i & 15] = o[0][2 + (i >> 4)][i & 15] * f0 + s1[i * 64] * f1;
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+    const int r = row0 + 32 * x + n;
+    const float total = sum[x] + __shfl_xor(sum[x], 32, kWave);
+    if (r >= n_rows) continue;
+    const size_t row = ((size_t)s * a.group_size + (r & (a.group_size - 1))) * a.n_q + i0 + (r >> lg);
+    if (a.n_split > 1) {
+      float* p = a.part + (row * a.n_split + split) * kPartFloats;
+      if (h == 0) *reinterpret_cast<float2*>(p) = make_float2(m[x], total);
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2)
+          *reinterpret_cast<float2*>(p + 2 + 32 * dt + (i & 3) + 8 * (i >> 2) + 4 * h) =
+              make_float2(o[x][dt][i], o[x][dt][i + 1]);
+      continue;
+    }
+    const float inv = inv_sum(total);
+    if (a.lse_out && h == 0) a.lse_out[row] = lse_of(m[x], total);
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const size_t at = row * kHeadDim + 32 * dt + 2 * i + 4 * h;
+        const float y0 = o[x][dt][i] * inv, y1 = o[x][dt][i + 1] * inv, y2 = o[x][dt][i + 2] * inv, y3 = o[x][dt][i + 3] * inv;
+        if (a.out_bf16) {
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) =
+              make_uint2(f32_to_bf16(y0) | (uint32_t)f32_to_bf16(y1) << 16, f32_to_bf16(y2) | (uint32_t)f32_to_bf16(y3) << 16);
+        } else {
+          *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(y0, y1, y2, y3);
+        }
+      }
+  }
+}
+
+template <int NT, int WR, int WK>
+void launch_prefill_mfma(const PrefillArgs& a, int row_groups, int64_t n_blocks, hipStream_t s) {
+  prefill_mfma_kernel<NT, WR, WK><<<(unsigned)n_blocks, WR * WK * 64, 0, s>>>(a, row_groups, n_blocks);
+}
+
+// ---- float32: vector ALUs
+
 template <class T>
 __device__ __forceinline__ void row8(const T* p, float (&x)[8]) {
 #pragma unroll
@@ -236,6 +602,21 @@ void prefill_attn_kernel(const PrefillArgs a, int64_t n_rows) {
 int check_dtype(int dtype) {
   if (dtype != LOUISKV_F32 && dtype != LOUISKV_BF16) return fail(LOUISKV_ERR_DTYPE, "unknown dtype %d", dtype);
   return LOUISKV_OK;
+}
+
+// Rows (tokens by heads) that a block of the matrix-core kernel takes, for tiles of
+// `rows`.
+int block_rows(int rows) { return rows > 128 ? 256 : rows > 64 ? 128 : rows > 32 ? 64 : 32; }
+
+// Parts that a tile's list is split into: one where there are tiles for the chip;
+// otherwise enough blocks for it, with 128 keys or more in each.
+constexpr int kFullGrid = 256, kSplitGrid = 512, kSplitKeys = 128;
+int prefill_splits(int64_t n_slices, int group_size, int n_q, int q_block, int block_len, int sel_cap) {
+  const int rows = std::min(q_block, n_q) * group_size, per = block_rows(rows);
+  const int64_t blocks = n_slices * (((int64_t)n_q + q_block - 1) / q_block) * ((rows + per - 1) / per);
+  if (blocks >= kFullGrid) return 1;
+  const int64_t by_keys = std::max<int64_t>(1, (int64_t)sel_cap * block_len / kSplitKeys);
+  return (int)std::min<int64_t>(by_keys, kSplitGrid / blocks);
 }
 
 int log2_block(int block_len) {
@@ -318,8 +699,11 @@ extern "C" int louiskv_retrieve_blocks(const void* q, int32_t dtype, int64_t n_s
 extern "C" size_t louiskv_sparse_prefill_attn_workspace_size(int64_t n_slices, int32_t group_size, int32_t n_q,
                                                              int32_t d, int32_t q_block, int32_t block_len,
                                                              int32_t sel_cap) {
-  (void)n_slices; (void)group_size; (void)n_q; (void)d; (void)q_block; (void)block_len; (void)sel_cap;
-  return 0;
+  (void)d;
+  if (n_slices < 1 || group_size < 1 || n_q < 1 || q_block < 1 || q_block > kMaxTile || log2_block(block_len) < 0 ||
+      sel_cap < 1)
+    return 0;
+  return part_bytes(n_slices * group_size * n_q, prefill_splits(n_slices, group_size, n_q, q_block, block_len, sel_cap));
 }
 
 extern "C" int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads,
@@ -328,7 +712,6 @@ extern "C" int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t
                                            int32_t q_block, int32_t block_len, const int32_t* sel_blocks,
                                            int32_t sel_cap, const int32_t* n_sel_blocks, void* out, int32_t out_dtype,
                                            float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
-  (void)workspace; (void)workspace_bytes;
   if (!q || !keys || !values || !sel_blocks || !n_sel_blocks || !out)
     return fail(LOUISKV_ERR_NULL, "q, keys, values, sel_blocks, n_sel_blocks and out are required");
   int st = check_dtype(dtype);
@@ -345,9 +728,28 @@ extern "C" int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t
   a.part = nullptr; a.out = out; a.out_bf16 = out_dtype == LOUISKV_BF16; a.lse_out = lse_out;
   const int64_t n_rows = n_slices * group_size * n_q;
   if ((n_rows + 15) / 16 > INT32_MAX) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
-  const unsigned grid = (unsigned)((n_rows + 15) / 16);
-  if (dtype == LOUISKV_BF16) prefill_attn_kernel<uint16_t><<<grid, 256, 0, as_stream(stream)>>>(a, n_rows);
-  else prefill_attn_kernel<float><<<grid, 256, 0, as_stream(stream)>>>(a, n_rows);
+  const int rows = std::min(q_block, n_q) * group_size, per = block_rows(rows), row_groups = (rows + per - 1) / per;
+  const int n_split = prefill_splits(n_slices, group_size, n_q, q_block, block_len, sel_cap);
+  const size_t need = part_bytes(n_rows, n_split);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, workspace_bytes);
+  hipStream_t hs = as_stream(stream);
+  if (dtype == LOUISKV_F32) {
+    prefill_attn_kernel<float><<<(unsigned)((n_rows + 15) / 16), 256, 0, hs>>>(a, n_rows);
+    LKV_CHECK_LAUNCH();
+    return LOUISKV_OK;
+  }
+  a.n_split = n_split;
+  a.part = static_cast<float*>(workspace);
+  const int64_t n_blocks = n_slices * a.n_tiles * row_groups * n_split;
+  if (n_blocks > INT32_MAX) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
+  switch (per) {
+    case 256: launch_prefill_mfma<2, 4, 1>(a, row_groups, n_blocks, hs); break;
+    case 128: launch_prefill_mfma<1, 4, 1>(a, row_groups, n_blocks, hs); break;
+    case 64: launch_prefill_mfma<1, 2, 2>(a, row_groups, n_blocks, hs); break;
+    default: launch_prefill_mfma<1, 1, 2>(a, row_groups, n_blocks, hs); break;
+  }
   LKV_CHECK_LAUNCH();
-  return LOUISKV_OK;
+  if (n_split == 1) return LOUISKV_OK;
+  return merge_parts(a.part, n_split, n_rows, out, out_dtype, lse_out, hs);
 }
