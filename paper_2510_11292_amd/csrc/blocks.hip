@@ -1,5 +1,7 @@
 // The prompt's attention over selected blocks of its keys: the selection of each
 // query tile's blocks by their index vectors, and the causal attention over them.
+#include <type_traits>
+
 #include "common.h"
 #include "merge.h"
 
@@ -202,22 +204,23 @@ __device__ __forceinline__ int swizzle(int r) { return ((r & 3) << 2) | ((r >> 2
 constexpr float kGrow = 8.0f;   // base-2 logits may pass the base by this much before the sums are rescaled
 
 // Block (slice, tile, row group, split): rows r of the tile are (token r / g, head
-// r % g), 32 NT of them a wave, WR waves of rows by WK waves that share the keys.
+// r % g), 32 of them a wave, WR waves of rows by WK waves that share the keys.
 // Keys and values of 64 list positions at a time are copied to LDS (two stages,
-// one in flight).  A wave computes S^T = K Q^T for 32 keys, so that a lane holds 16 scores
-// of one query row; their exponentials are, unmoved, the B operand of
+// one in flight; two in flight were no faster, 1.14 against 1.12 ms for a layer of
+// 32K tokens).  A wave computes S^T = K Q^T for 32 keys, so that a lane holds
+// 16 scores of one query row; their exponentials are, unmoved, the B operand of
 // O^T += V^T P^T, whose A operand comes from LDS through transposing reads.  The
 // running base, sum and the rescale are then a lane's own.
 constexpr int kStageKeys = 64;
 constexpr int kStageBytes = kStageKeys * kHeadDim * 2;   // of the keys, and of the values
 
-template <int NT, int WR, int WK>
-__global__ __launch_bounds__(WR * WK * 64, NT == 1 ? 2 : 1)
+template <int WR, int WK>
+__global__ __launch_bounds__(WR * WK * 64, 2)
 void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) {
   constexpr int NW = WR * WK;
-  constexpr int kGroups = kStageKeys / 16 / NW;   // 16-row groups that a wave copies
-  static_assert(kStageKeys % (16 * NW) == 0 && 2 % WK == 0, "waves share a stage evenly");
-  __shared__ __align__(256) char s_stage0[2 * kStageBytes], s_stage1[2 * kStageBytes];
+  constexpr int kCopies = kStageKeys / 4 / NW;    // four-row copies of a wave, of keys and of values
+  static_assert(kStageKeys % (4 * NW) == 0 && 2 % WK == 0, "waves share a stage evenly");
+  __shared__ __align__(256) char s_ring[2][2 * kStageBytes];
   __shared__ int s_bad;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, n = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wr = w % WR, wk = w / WR;
@@ -236,37 +239,29 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
   const int t = (int)(id - s * a.n_tiles);
   const int lg = 31 - __builtin_clz(a.group_size);
   const int i0 = t * a.q_block, n_tok = min(a.q_block, a.n_q - i0), n_rows = n_tok << lg;
-  const int row0 = (rgrp * WR + wr) * 32 * NT;    // of this wave, in the tile
-  if (rgrp * WR * 32 * NT >= n_rows) return;      // the tile is shorter than the others (block-uniform)
+  const int row0 = (rgrp * WR + wr) * 32;    // of this wave, in the tile
+  if (rgrp * WR * 32 >= n_rows) return;      // the tile is shorter than the others (block-uniform)
 
   // this lane's rows
-  bf16x8 q[NT][8];
-  int qpos[NT];
+  bf16x8 q[8];
   const float qs = a.scale * kLog2E;
   const uint32_t flip = qs < 0.f ? 0x80008000u : 0u;     // |scale| multiplies the scores of -q
+  const int r = min(row0 + n, n_rows - 1), qpos = a.q_start + i0 + (r >> lg);
+  const size_t row = ((size_t)s * a.group_size + (r & (a.group_size - 1))) * a.n_q + i0 + (r >> lg);
+  const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + row * kHeadDim);
 #pragma unroll
-  for (int x = 0; x < NT; ++x) {
-    const int r = min(row0 + 32 * x + n, n_rows - 1);
-    const int tok = r >> lg;
-    qpos[x] = a.q_start + i0 + tok;
-    const uint4* src = reinterpret_cast<const uint4*>(
-        static_cast<const uint16_t*>(a.q) + (((size_t)s * a.group_size + (r & (a.group_size - 1))) * a.n_q + i0 + tok) * kHeadDim);
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      uint4 v = src[2 * c + h];
-      v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
-      q[x][c] = __builtin_bit_cast(bf16x8, v);
-    }
+  for (int c = 0; c < 8; ++c) {
+    uint4 v = src[2 * c + h];
+    v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
+    q[c] = __builtin_bit_cast(bf16x8, v);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the queries are in before the copies start
 #pragma unroll
-  for (int x = 0; x < NT; ++x)
-#pragma unroll
-    for (int c = 0; c < 8; ++c) asm volatile("" : "+v"(q[x][c]));
+  for (int c = 0; c < 8; ++c) asm volatile("" : "+v"(q[c]));
   const float mult = fabsf(qs);
   const int first_pos = a.q_start + i0 + (min(row0, n_rows - 1) >> lg);
-  const int last_pos = a.q_start + i0 + (min(row0 + 32 * NT - 1, n_rows - 1) >> lg);
-  const int block_first = a.q_start + i0 + ((rgrp * WR * 32 * NT) >> lg);   // first token of the block
+  const int last_pos = a.q_start + i0 + (min(row0 + 31, n_rows - 1) >> lg);
+  const int block_first = a.q_start + i0 + ((rgrp * WR * 32) >> lg);   // first token of the block
 
   const int64_t list = s * a.n_tiles + t;
   const int32_t* sel = a.sel + (size_t)list * a.sel_cap;
@@ -283,140 +278,165 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
     nxt = entries(64);
   }
   asm volatile("s_waitcnt vmcnt(0)" : "+v"(cur), "+v"(nxt));
-  // token of the first key of 16-key group gi (which is below n_groups)
+  // token of the first key of 16-key group gi (below n_groups)
   auto group_pos = [&](int gi) -> int {
-    const int e = gi >> (a.log_block - 4);
-    const int v = e - cur_base < 64 ? __builtin_amdgcn_readlane(cur, (e - cur_base) & 63)
-                                    : __builtin_amdgcn_readlane(nxt, (e - cur_base) & 63);
+    const int e = (gi >> (a.log_block - 4)) - cur_base;
+    const int v = __builtin_amdgcn_readlane(e < 64 ? cur : nxt, e & 63);
     return (v << a.log_block) + ((gi & ((1 << (a.log_block - 4)) - 1)) << 4);
+  };
+  struct StagePos { int at[kStageKeys / 16]; };   // of a stage's groups; no token where the list has ended
+  constexpr int kNoToken = INT32_MAX - 16;
+  auto stage_pos = [&](int st) {
+    StagePos p;
+#pragma unroll
+    for (int x = 0; x < kStageKeys / 16; ++x) {
+      const int gi = st * (kStageKeys / 16) + x;
+      p.at[x] = gi < n_groups ? group_pos(gi) : kNoToken;
+    }
+    return p;
   };
   const char* kb = static_cast<const char*>(a.keys) + (size_t)s * a.key_rows * kHeadDim * 2;
   const char* vb = static_cast<const char*>(a.values) + (size_t)s * a.key_rows * kHeadDim * 2;
-  // groups w, w + NW, .. of stage st to LDS; a group past the list repeats its last
+  // a wave's share of stage st to LDS, four rows a copy; a group past the list repeats its last
   auto copy_stage = [&](int st, char* buf) {
+    constexpr int kPer = kCopies < 4 ? kCopies : 4;    // copies of one 16-row group
 #pragma unroll
-    for (int x = 0; x < kGroups; ++x) {
-      const int g16 = w + NW * x;
+    for (int x = 0; x < kCopies / kPer; ++x) {
+      const int c0 = w * kCopies + x * kPer, g16 = c0 >> 2;
       const int pos = group_pos(min(st * (kStageKeys / 16) + g16, n_groups - 1));
       const int from = min(pos, a.n_keys - 1);                          // rows behind the last key repeat it
       const char* kg = kb + (size_t)from * (kHeadDim * 2);
       const char* vg = vb + (size_t)from * (kHeadDim * 2);
-      const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(buf) + g16 * 16 * kHeadDim * 2);
+      const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(buf) + c0 * 1024);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = min(4 * i + (lane >> 4), a.n_keys - 1 - from);
-        const uint32_t off = r * (kHeadDim * 2) + (((lane & 15) ^ swizzle(4 * i + (lane >> 4))) << 4);
+      for (int i = 0; i < kPer; ++i) {
+        const int r16 = ((c0 & 3) + i) * 4 + (lane >> 4);               // row of the group
+        const int r = min(r16, a.n_keys - 1 - from);
+        const uint32_t off = r * (kHeadDim * 2) + (((lane & 15) ^ swizzle(r16)) << 4);
         copy_to_lds(kg, off, dst + i * 1024);
         copy_to_lds(vg, off, dst + kStageBytes + i * 1024);
       }
     }
   };
 
-  f32x16 o[NT][4];
-  float base[NT], grow_at[NT], sum[NT];
+  f32x16 o[4];
+  float base = 0.f, grow_at = -__builtin_inff(), sum = 0.f;
 #pragma unroll
-  for (int x = 0; x < NT; ++x) {
-    base[x] = 0.f;
-    grow_at[x] = -__builtin_inff();
-    sum[x] = 0.f;
+  for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  // LDS addresses of this lane's reads in a 32-key half of a stage: pieces 2 c + h of
+  // key n, and of the values rows 4 h + 0..3 and, in the second, those + 8 (the
+  // same swizzle but for bit 1) of channels 32 dt + 0..31
+  uint32_t k_at[8], v_at[4][2];
+  {
+    const uint32_t k0 = lds_addr(s_ring) + n * 256, kp = (h ^ swizzle(n & 15)) << 4;
+    const int j4 = (lane & 15) >> 2, xp = (((lane >> 4) & 1) << 1) | ((lane & 3) >> 1);
+    const uint32_t v0 = lds_addr(s_ring) + kStageBytes + (4 * h + j4) * 256 + ((lane & 1) << 3);
+    const uint32_t vp = ((j4 << 2) | (xp ^ h)) << 4;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[x][dt][i] = 0.f;
+    for (int c = 0; c < 8; ++c) k_at[c] = k0 + (kp ^ (c << 5));
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) {
+      v_at[dt][0] = v0 + (vp ^ (dt << 6));
+      v_at[dt][1] = v0 + 8 * 256 + (vp ^ (dt << 6) ^ 32);
+    }
   }
-  // byte offsets of this lane's reads in a 32-key half of a stage
-  const uint32_t k_off = n * 256 + ((h ^ swizzle(n & 15)) << 4);                      // piece 2c + h: ^ (c << 5)
-  const int j4 = (lane & 15) >> 2, xp = (((lane >> 4) & 1) << 1) | ((lane & 3) >> 1);
-  const uint32_t v_off = (4 * h + j4) * 256 + (((j4 << 2) | (xp ^ h)) << 4) + ((lane & 1) << 3);   // ^ (dt << 6)
-
-  auto subtile = [&](const char* buf, int st, int sub) {
-    const int gi = st * (kStageKeys / 16) + 2 * sub;
-    if (gi >= n_groups) return;
-    const int p0 = group_pos(gi);
-    const int p1 = gi + 1 < n_groups ? group_pos(gi + 1) : INT32_MAX - 16;   // no key there
-    if (min(p0, p1) > last_pos) return;
-    const char* kt = buf + sub * 32 * 256;
-    const char* vt = buf + kStageBytes + sub * 32 * 256;
-    f32x16 sc[NT];
+  typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8;
+  typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+  // Keys 32 sub .. + 31 of the stage `off` bytes into the ring, and their values.
+  auto load_keys = [&](uint32_t off, int sub, bf16x8 (&kf)[8]) {
 #pragma unroll
-    for (int x = 0; x < NT; ++x)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[x][i] = 0.f;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + (k_off ^ (c << 5)));
-#pragma unroll
-      for (int x = 0; x < NT; ++x) sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[x][c], sc[x], 0, 0, 0);
-    }
-    const bool masked = max(p0, p1) + 15 > first_pos;
-    bf16x8 pb[NT][2];
-#pragma unroll
-    for (int x = 0; x < NT; ++x) {
-      float m = mult;
-      if (masked) {
-        m = 1.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = (i < 8 ? p0 : p1) + (i & 3) + 8 * ((i >> 2) & 1) + 4 * h;
-          sc[x][i] = key <= qpos[x] ? sc[x][i] * mult : -__builtin_inff();
-        }
-      }
-      float top = sc[x][0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[x][i]);
-      top *= m;
-      if (__builtin_amdgcn_ballot_w64(top > grow_at[x])) {
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        if (top > grow_at[x]) {
-          // before the first finite score the sums are 0 (or NaN): any factor does
-          const float f = grow_at[x] == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(base[x] - top);
-          base[x] = top;
-          grow_at[x] = top + kGrow;
-          sum[x] *= f;
-#pragma unroll
-          for (int dt = 0; dt < 4; ++dt) o[x][dt] *= f;
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(sc[x][8 * k + j], m, -base[x]));
-          sum[x] += p;
-          pb[x][k][j] = (__bf16)p;
-        }
-    }
+    for (int c = 0; c < 8; ++c) kf[c] = *(lds_bf16x8)(uintptr_t)(k_at[c] + off + sub * 32 * 256);
+  };
+  auto load_values = [&](uint32_t off, int sub, s16x8 (&vf)[2][4]) {
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt) {
-        // rows 16 k + 4 h + 0..3, then those + 8 (the same swizzle but for bit 1)
-        const char* vp = vt + 16 * 256 * k;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(vp + (v_off ^ (dt << 6))));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(vp + 8 * 256 + (v_off ^ (dt << 6) ^ 32)));
-        const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-        for (int x = 0; x < NT; ++x)
-          o[x][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pb[x][k], o[x][dt], 0, 0, 0);
+        const uint32_t at = off + (sub * 32 + 16 * k) * 256;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(v_at[dt][0] + at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(v_at[dt][1] + at));
+        vf[k][dt] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
+  };
+  auto scores = [&](const bf16x8 (&kf)[8]) {
+    f32x16 sc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], q[c], sc, 0, 0, 0);
+    return sc;
+  };
+  // Masks scores of keys from tokens p0 and p1 on (16 each).
+  auto mask = [&](f32x16& sc, int p0, int p1) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int key = (i < 8 ? p0 : p1) + (i & 3) + 8 * ((i >> 2) & 1) + 4 * h;
+      sc[i] = key <= qpos ? sc[i] * mult : -__builtin_inff();
+    }
+  };
+  auto largest = [&](const f32x16& sc) {
+    float top = sc[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
+    return top;
+  };
+  // Raises the base where a lane's scores pass it.
+  auto rebase = [&](float top) {
+    if (!__builtin_amdgcn_ballot_w64(top > grow_at)) return;
+    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    const bool grows = top > grow_at;
+    // before the first finite score the sums are 0 (or NaN): any factor does
+    const float f = grows && grow_at != -__builtin_inff() ? __builtin_amdgcn_exp2f(base - top) : 1.f;
+    base = grows ? top : base;
+    grow_at = grows ? top + kGrow : grow_at;
+    sum *= f;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) o[dt] *= f;
+  };
+  auto weights = [&](const f32x16& sc, float m, bf16x8 (&pb)[2]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(sc[8 * k + j], m, -base));
+        sum += p;
+        pb[k][j] = (__bf16)p;
+      }
+  };
+  auto add_values = [&](const s16x8 (&vf)[2][4], const bf16x8 (&pb)[2]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k][dt]), pb[k], o[dt], 0, 0, 0);
+  };
+  auto soften = [&](f32x16& sc, int p0, int p1, bf16x8 (&pb)[2]) {
+    float m = mult;
+    if (max(p0, p1) + 15 > first_pos) {
+      mask(sc, p0, p1);
+      m = 1.f;
+    }
+    rebase(largest(sc) * m);
+    weights(sc, m, pb);
   };
 
   // Values that a query may not see must not reach it: 0 * inf is NaN.  In a stage
   // that holds keys behind the block's first query, values that are not finite
-  // become 0 and are added to the queries that do see them.
-  auto clear_not_finite = [&](char* buf, int st) {
-    const int gi = st * (kStageKeys / 16);
+  // become 0; after the loop they are added to the queries that do see them.
+  auto holds_later_keys = [&](const StagePos& p) {   // block-uniform
     int top = 0;
 #pragma unroll
-    for (int x = 0; x < kStageKeys / 16; ++x) top = max(top, gi + x < n_groups ? group_pos(gi + x) : INT32_MAX - 16);
-    if (top + 15 <= block_first) return;       // block-uniform
-    uint4* v = reinterpret_cast<uint4*>(buf + kStageBytes);
-    bool any = false;
+    for (int x = 0; x < kStageKeys / 16; ++x) top = max(top, p.at[x]);
+    return top + 15 > block_first;
+  };
+  // Of the rows that this wave copied.
+  auto clear_not_finite = [&](char* buf) {
 #pragma unroll
-    for (int i = 0; i < kStageBytes / 16 / (NW * 64); ++i) {
-      uint4 u = v[tid + i * NW * 64];
+    for (int i = 0; i < kCopies; ++i) {
+      uint4* v = reinterpret_cast<uint4*>(buf + kStageBytes + (w * kCopies + i) * 1024) + lane;
+      uint4 u = *v;
       uint32_t* e = &u.x;
       bool bad = false;
 #pragma unroll
@@ -425,118 +445,157 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
         e[c] &= (b0 ? 0xffff0000u : ~0u) & (b1 ? 0x0000ffffu : ~0u);
         bad |= b0 | b1;
       }
-      if (bad) v[tid + i * NW * 64] = u;
-      any |= bad;
+      if (bad) {
+        *v = u;
+        s_bad = 1;
+      }
     }
-    if (any) s_bad = st + 1;
-    __syncthreads();
-    if (s_bad != st + 1) return;
-    for (int x = 0; x < kStageKeys; ++x) {
-      if (x / 32 % WK != wk || gi + x / 16 >= n_groups) continue;
-      const int pos = group_pos(gi + x / 16) + (x & 15);
-      if (pos > last_pos) continue;
-      const uint16_t* row = reinterpret_cast<const uint16_t*>(vb) + (size_t)pos * kHeadDim;
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float f = bf16_to_f32(row[32 * dt + (i & 3) + 8 * (i >> 2) + 4 * h]);
-          if (__builtin_isfinite(f)) continue;
-#pragma unroll
-          for (int y = 0; y < NT; ++y) o[y][dt][i] += pos <= qpos[y] ? f : 0.f;
-        }
-    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+  // the list's next 64 entries, once stage st begins among them
+  auto refill = [&](int st) {
+    if (((st * (kStageKeys / 16)) >> (a.log_block - 4)) - cur_base < 64) return;
+    cur = nxt;
+    cur_base += 64;
+    nxt = entries(cur_base + 64);
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(nxt));   // now, not at a use that copies are in flight at
   };
 
-  auto stage = [&](char* buf, char* other, int st) {
-    sync_stage();                               // stage st is in LDS; `other` is free
-    if (((st * (kStageKeys / 16)) >> (a.log_block - 4)) - cur_base >= 64) {   // the list's next 64 entries
-      cur = nxt;
-      cur_base += 64;
-      nxt = entries(cur_base + 64);
-      asm volatile("s_waitcnt vmcnt(0)" : "+v"(nxt));   // now, not at a use that copies are in flight at
-    }
-    if (st + 1 < n_stages) copy_stage(st + 1, other);
-    clear_not_finite(buf, st);
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub)
-      if (sub % WK == wk || WK == 1) subtile(buf, st, sub);
-  };
   if (tid == 0) s_bad = 0;
-  if (n_stages > 0) copy_stage(0, s_stage0);
+  __syncthreads();
+  StagePos pos{};
+  // Stage st, which lies at place `at` of the ring (a constant where it is inlined).
+  auto stage = [&](int st, int at) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const StagePos p = pos;
+    if (holds_later_keys(p)) clear_not_finite(s_ring[at]);
+    sync_stage();                               // stage st is in LDS; the other place is free
+    if (st + 1 < n_stages) {
+      refill(st + 1);
+      copy_stage(st + 1, s_ring[at ^ 1]);
+      pos = stage_pos(st + 1);
+    }
+    const uint32_t off = at * 2 * kStageBytes;
+    bf16x8 kf[8], pb[2];
+    s16x8 vf[2][4];
+    auto half = [&](int sub, int p0, int p1, bool more) {
+      f32x16 sc = scores(kf);
+      load_values(off, sub, vf);
+      if (more) load_keys(off, 1, kf);
+      __builtin_amdgcn_sched_barrier(0);
+      soften(sc, p0, p1, pb);
+      add_values(vf, pb);
+    };
+    if constexpr (WK == 1) {
+      const bool see0 = min(p.at[0], p.at[1]) <= last_pos, see1 = min(p.at[2], p.at[3]) <= last_pos;
+      load_keys(off, see0 ? 0 : 1, kf);
+      if (see0) half(0, p.at[0], p.at[1], true);
+      if (see1) half(1, p.at[2], p.at[3], false);
+    } else {
+      const int p0 = wk ? p.at[2] : p.at[0], p1 = wk ? p.at[3] : p.at[1];
+      if (min(p0, p1) > last_pos) return;
+      load_keys(off, wk, kf);
+      half(wk, p0, p1, false);
+    }
+  };
+  if (n_stages > 0) {
+    copy_stage(0, s_ring[0]);
+    pos = stage_pos(0);
+  }
   for (int st = 0; st < n_stages; st += 2) {
-    stage(s_stage0, s_stage1, st);
-    if (st + 1 < n_stages) stage(s_stage1, s_stage0, st + 1);
+    stage(st, 0);
+    if (st + 1 < n_stages) stage(st + 1, 1);
   }
   sync_stage();
+  if (s_bad) {                                  // block-uniform, rare
+    if (n_list > 0 && e1 > e0) {
+      cur_base = 0;
+      cur = entries(0);
+      nxt = entries(64);
+    }
+#pragma unroll 1
+    for (int gi = 0; gi < n_groups; ++gi) {
+      if ((gi >> (a.log_block - 4)) - cur_base >= 64) {
+        cur = nxt;
+        cur_base += 64;
+        nxt = entries(cur_base + 64);
+      }
+      if (gi / 2 % WK != wk || !holds_later_keys(stage_pos(gi / (kStageKeys / 16)))) continue;
+      const int p0 = group_pos(gi);
+#pragma unroll 1
+      for (int pos = p0; pos < min(p0 + 16, last_pos + 1); ++pos) {
+        const uint16_t* v = reinterpret_cast<const uint16_t*>(vb) + (size_t)pos * kHeadDim;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float f = bf16_to_f32(v[32 * dt + (i & 3) + 8 * (i >> 2) + 4 * h]);
+            o[dt][i] += pos <= qpos && !__builtin_isfinite(f) ? f : 0.f;
+          }
+      }
+    }
+  }
 
   // the waves that shared the keys: wk = 1 leaves its sums in LDS, wk = 0 adds them
-  float m[NT];
-#pragma unroll
-  for (int x = 0; x < NT; ++x) m[x] = grow_at[x] == -__builtin_inff() ? -__builtin_inff() : base[x];
+  float m = grow_at == -__builtin_inff() ? -__builtin_inff() : base;
   if constexpr (WK > 1) {
-    static_assert(NT == 1 && WK == 2 && WR * 34 * 256 <= 2 * kStageBytes, "half of a wave's sums fit a stage");
-    float* s0 = reinterpret_cast<float*>(s_stage0) + wr * 34 * 64 + lane;
-    float* s1 = reinterpret_cast<float*>(s_stage1) + wr * 34 * 64 + lane;
+    static_assert(WK == 2 && WR * 34 * 256 <= 2 * kStageBytes, "half of a wave's sums fit a stage");
+    float* s0 = reinterpret_cast<float*>(s_ring[0]) + wr * 34 * 64 + lane;
+    float* s1 = reinterpret_cast<float*>(s_ring[1]) + wr * 34 * 64 + lane;
     if (wk == 1) {
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
-        s0[i * 64] = o[0][i >> 4][i & 15];
-        s1[i * 64] = o[0][2 + (i >> 4)][i & 15];
+        s0[i * 64] = o[i >> 4][i & 15];
+        s1[i * 64] = o[2 + (i >> 4)][i & 15];
       }
-      s0[32 * 64] = m[0];
-      s1[32 * 64] = sum[0];
+      s0[32 * 64] = m;
+      s1[32 * 64] = sum;
     }
     __syncthreads();
     if (wk == 1) return;
-    const float m1 = s0[32 * 64], mm = fmaxf(m[0], m1);
-    const float f0 = __builtin_amdgcn_exp2f(m[0] - max_base(mm)), f1 = __builtin_amdgcn_exp2f(m1 - max_base(mm));
-    m[0] = mm;
-    sum[0] = sum[0] * f0 + s1[32 * 64] * f1;
+    const float m1 = s0[32 * 64], mm = fmaxf(m, m1);
+    const float f0 = __builtin_amdgcn_exp2f(m - max_base(mm)), f1 = __builtin_amdgcn_exp2f(m1 - max_base(mm));
+    m = mm;
+    sum = sum * f0 + s1[32 * 64] * f1;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-      o[0][i >> 4][i & 15] = o[0][i >> 4][i & 15] * f0 + s0[i * 64] * f1;
-      o[0][2 + (i >> 4)][i & 15] = o[0][2 + (i >> 4)][i & 15] * f0 + s1[i * 64] * f1;
+      o[i >> 4][i & 15] = o[i >> 4][i & 15] * f0 + s0[i * 64] * f1;
+      o[2 + (i >> 4)][i & 15] = o[2 + (i >> 4)][i & 15] * f0 + s1[i * 64] * f1;
     }
   }
-#pragma unroll
-  for (int x = 0; x < NT; ++x) {
-    const int r = row0 + 32 * x + n;
-    const float total = sum[x] + __shfl_xor(sum[x], 32, kWave);
-    if (r >= n_rows) continue;
-    const size_t row = ((size_t)s * a.group_size + (r & (a.group_size - 1))) * a.n_q + i0 + (r >> lg);
-    if (a.n_split > 1) {
-      float* p = a.part + (row * a.n_split + split) * kPartFloats;
-      if (h == 0) *reinterpret_cast<float2*>(p) = make_float2(m[x], total);
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2)
-          *reinterpret_cast<float2*>(p + 2 + 32 * dt + (i & 3) + 8 * (i >> 2) + 4 * h) =
-              make_float2(o[x][dt][i], o[x][dt][i + 1]);
-      continue;
-    }
-    const float inv = inv_sum(total);
-    if (a.lse_out && h == 0) a.lse_out[row] = lse_of(m[x], total);
+  const float total = sum + __shfl_xor(sum, 32, kWave);
+  if (row0 + n >= n_rows) return;
+  if (a.n_split > 1) {
+    float* p = a.part + (row * a.n_split + split) * kPartFloats;
+    if (h == 0) *reinterpret_cast<float2*>(p) = make_float2(m, total);
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const size_t at = row * kHeadDim + 32 * dt + 2 * i + 4 * h;
-        const float y0 = o[x][dt][i] * inv, y1 = o[x][dt][i + 1] * inv, y2 = o[x][dt][i + 2] * inv, y3 = o[x][dt][i + 3] * inv;
-        if (a.out_bf16) {
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) =
-              make_uint2(f32_to_bf16(y0) | (uint32_t)f32_to_bf16(y1) << 16, f32_to_bf16(y2) | (uint32_t)f32_to_bf16(y3) << 16);
-        } else {
-          *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(y0, y1, y2, y3);
-        }
-      }
+      for (int i = 0; i < 16; i += 2)
+        *reinterpret_cast<float2*>(p + 2 + 32 * dt + (i & 3) + 8 * (i >> 2) + 4 * h) =
+            make_float2(o[dt][i], o[dt][i + 1]);
+    return;
   }
+  const float inv = inv_sum(total);
+  if (a.lse_out && h == 0) a.lse_out[row] = lse_of(m, total);
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const size_t at = row * kHeadDim + 32 * dt + 2 * i + 4 * h;
+      const float y0 = o[dt][i] * inv, y1 = o[dt][i + 1] * inv, y2 = o[dt][i + 2] * inv, y3 = o[dt][i + 3] * inv;
+      if (a.out_bf16) {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) =
+            make_uint2(f32_to_bf16(y0) | (uint32_t)f32_to_bf16(y1) << 16, f32_to_bf16(y2) | (uint32_t)f32_to_bf16(y3) << 16);
+      } else {
+        *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(y0, y1, y2, y3);
+      }
+    }
 }
 
-template <int NT, int WR, int WK>
+template <int WR, int WK>
 void launch_prefill_mfma(const PrefillArgs& a, int row_groups, int64_t n_blocks, hipStream_t s) {
-  prefill_mfma_kernel<NT, WR, WK><<<(unsigned)n_blocks, WR * WK * 64, 0, s>>>(a, row_groups, n_blocks);
+  prefill_mfma_kernel<WR, WK><<<(unsigned)n_blocks, WR * WK * 64, 0, s>>>(a, row_groups, n_blocks);
 }
 
 // ---- float32: vector ALUs
@@ -744,10 +803,10 @@ extern "C" int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t
   const int64_t n_blocks = n_slices * a.n_tiles * row_groups * n_split;
   if (n_blocks > INT32_MAX) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   switch (per) {
-    case 256: launch_prefill_mfma<2, 4, 1>(a, row_groups, n_blocks, hs); break;
-    case 128: launch_prefill_mfma<1, 4, 1>(a, row_groups, n_blocks, hs); break;
-    case 64: launch_prefill_mfma<1, 2, 2>(a, row_groups, n_blocks, hs); break;
-    default: launch_prefill_mfma<1, 1, 2>(a, row_groups, n_blocks, hs); break;
+    case 256: launch_prefill_mfma<8, 1>(a, row_groups, n_blocks, hs); break;
+    case 128: launch_prefill_mfma<4, 1>(a, row_groups, n_blocks, hs); break;
+    case 64: launch_prefill_mfma<2, 2>(a, row_groups, n_blocks, hs); break;
+    default: launch_prefill_mfma<1, 2>(a, row_groups, n_blocks, hs); break;
   }
   LKV_CHECK_LAUNCH();
   if (n_split == 1) return LOUISKV_OK;
