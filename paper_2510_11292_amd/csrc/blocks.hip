@@ -32,128 +32,185 @@ __device__ __forceinline__ uint64_t ordered(double x) {
   return (u >> 63) ? ~u : u | (1ull << 63);
 }
 
-__device__ __forceinline__ double elem(const uint16_t* p) { return (double)bf16_to_f32(*p); }
-__device__ __forceinline__ double elem(const float* p) { return (double)*p; }
+// Eight channels of a query as they are stored.
+template <class T> struct Eight;
+template <> struct Eight<uint16_t> {
+  uint4 v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ float at(int e) const {
+    const uint32_t w = (&v.x)[e >> 1];
+    return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+  }
+};
+template <> struct Eight<float> {
+  float4 v[2];
+  __device__ __forceinline__ void load(const float* p) {
+    v[0] = reinterpret_cast<const float4*>(p)[0];
+    v[1] = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ float at(int e) const { return (&v[e >> 2].x)[e & 3]; }
+};
 
 constexpr int kSelThreads = 256;
+constexpr int kSelWaves = kSelThreads / 64;
 
-// Block (slice, tile): the sum of the tile's queries in float64, the score of
-// every ranked block, then the n_top-th largest key by radix selection (8 bits a
-// pass, only the keys that share the digits found so far are counted) and the
-// list in block order.
+// Block (slice, tile): the sum of the tile's queries in float64 (16 lanes a row, the
+// waves share the rows), the scores of the ranked blocks (four lanes a block, each
+// with 32 of the sum's channels in registers), then the first wave finds the
+// n_top-th largest key by radix selection (8 bits a pass, only the keys that share
+// the digits found so far are counted) and writes the list in block order.  Bound
+// by the read of the queries where there are many tiles (a layer of 32K tokens:
+// 68 us, 4.0 TB/s; four tiles to a block, whose index vectors pass through LDS once
+// for all of them, 123 us: the phases of fewer waves overlap less) and by trips
+// to memory where there are few.
 template <class T>
 __global__ __launch_bounds__(kSelThreads)
 void select_blocks_kernel(const SelectArgs a) {
-  extern __shared__ uint64_t s_key[];   // one per ranked block
-  __shared__ double s_q[kHeadDim], s_half[kHeadDim];
+  extern __shared__ uint64_t s_key[];            // one per ranked block
+  __shared__ double s_q[kSelWaves][kHeadDim];
   __shared__ int s_hist[256];
-  __shared__ int s_wave[kSelThreads / 64][2];
-  __shared__ int s_digit, s_above, s_equal;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int64_t s = blockIdx.x / a.n_tiles;
-  const int t = (int)(blockIdx.x - s * a.n_tiles), tid = threadIdx.x;
-  const int i0 = t * a.q_block, i1 = min(i0 + a.q_block, a.n_q);
-  const int p0 = a.q_start + i0, p1 = a.q_start + i1 - 1;
-  const int hi = p1 >> a.log_block, lo = max(0, (p0 >> a.log_block) - a.n_recent);
-  const int first = min(a.n_first, lo), ranked = lo - first;
+  const int t = (int)(blockIdx.x - s * a.n_tiles);
+  const int i0 = t * a.q_block, n_tok = min(a.q_block, a.n_q - i0);
+  // blocks [first, lo) are ranked; those before and lo..hi are taken
+  const int hi = (a.q_start + i0 + n_tok - 1) >> a.log_block;
+  const int lo = max(0, ((a.q_start + i0) >> a.log_block) - a.n_recent), first = min(a.n_first, lo);
+  const int ranked = lo - first, n_pick = min(a.n_top, ranked);
+  if (n_pick > 0 && n_pick < ranked) {           // block-uniform
+    {
+      const int sub = lane & 15, n_rows = n_tok * a.group_size;
+      const T* q = static_cast<const T*>(a.q) + ((size_t)s * a.group_size * a.n_q + i0) * kHeadDim + 8 * sub;
+      constexpr int kFlight = sizeof(T) == 2 ? 16 : 8, kGroups = 4 * kSelWaves;   // rows in flight of a 16-lane group
+      double sum[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] = 0.0;
+      const int r0 = w * 4 + (lane >> 4);
+      int head = 0, tok = r0;                    // of row r: r = head * n_tok + tok
+      for (int r = r0; r < n_rows; r += kGroups * kFlight) {
+        Eight<T> v[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+          if (r + kGroups * i < n_rows) {
+            while (tok >= n_tok) {
+              tok -= n_tok;
+              ++head;
+            }
+            v[i].load(q + ((size_t)head * a.n_q + tok) * kHeadDim);
+          }
+          tok += kGroups;
+        }
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i)
+          if (r + kGroups * i < n_rows) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += (double)v[i].at(e);
+          }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        double y = sum[e] + __shfl_xor(sum[e], 16, kWave);
+        y += __shfl_xor(y, 32, kWave);
+        if (lane < 16) s_q[w][8 * sub + e] = y;
+      }
+    }
+    __syncthreads();
+    // lane j of a quad: channels 16 k + 4 j + 0..3
+    double sum[8][4];
+    const int j = lane & 3;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        double y = 0.0;
+#pragma unroll
+        for (int p = 0; p < kSelWaves; ++p) y += s_q[p][16 * k + 4 * j + c];
+        sum[k][c] = y;
+      }
+    const float* reps = a.reps + (size_t)s * a.units_cap * kHeadDim + 4 * j;
+#pragma unroll 2
+    for (int b = first + (tid >> 2); b < lo; b += kSelThreads / 4) {
+      float4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const float4*>(reps + (size_t)b * kHeadDim + 16 * k);
+      double acc = 0.0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        acc = fma(sum[k][0], (double)v[k].x, acc);
+        acc = fma(sum[k][1], (double)v[k].y, acc);
+        acc = fma(sum[k][2], (double)v[k].z, acc);
+        acc = fma(sum[k][3], (double)v[k].w, acc);
+      }
+      acc += __shfl_xor(acc, 1, kWave);
+      acc += __shfl_xor(acc, 2, kWave);
+      if (j == 0) s_key[b - first] = ordered(acc);
+    }
+    __syncthreads();
+  }
+  if (w > 0) return;
   int32_t* sel = a.sel + ((size_t)s * a.n_tiles + t) * a.sel_cap;
-  const int n_pick = min(a.n_top, ranked);
-  const int n_total = first + n_pick + hi - lo + 1;
-  if (tid == 0) a.n_sel[(size_t)s * a.n_tiles + t] = n_total;
-  for (int b = tid; b < first; b += kSelThreads) sel[b] = b;
-  for (int b = lo + tid; b <= hi; b += kSelThreads) sel[first + n_pick + b - lo] = b;
+  if (lane == 0) a.n_sel[(size_t)s * a.n_tiles + t] = first + n_pick + hi - lo + 1;
+  for (int b = lane; b < first; b += kWave) sel[b] = b;
+  for (int b = lo + lane; b <= hi; b += kWave) sel[first + n_pick + b - lo] = b;
   if (n_pick == 0) return;
   if (n_pick == ranked) {
-    for (int b = tid; b < ranked; b += kSelThreads) sel[first + b] = first + b;
+    for (int b = lane; b < ranked; b += kWave) sel[first + b] = first + b;
     return;
-  }
-  {
-    const int c = tid & 127, part = tid >> 7;
-    double x = 0.0;
-    for (int j = 0; j < a.group_size; ++j) {
-      const T* q = static_cast<const T*>(a.q) + (((size_t)s * a.group_size + j) * a.n_q) * kHeadDim + c;
-      for (int i = i0 + part; i < i1; i += 2) x += elem(q + (size_t)i * kHeadDim);
-    }
-    if (part) s_half[c] = x;
-    __syncthreads();
-    if (!part) s_q[c] = x + s_half[c];
-    __syncthreads();
-  }
-  for (int b = tid; b < ranked; b += kSelThreads) {
-    const float4* rep = reinterpret_cast<const float4*>(a.reps + ((size_t)s * a.units_cap + first + b) * kHeadDim);
-    double x = 0.0;
-    for (int k = 0; k < kHeadDim / 4; ++k) {
-      const float4 f = rep[k];
-      x += s_q[4 * k] * (double)f.x;
-      x += s_q[4 * k + 1] * (double)f.y;
-      x += s_q[4 * k + 2] * (double)f.z;
-      x += s_q[4 * k + 3] * (double)f.w;
-    }
-    s_key[b] = ordered(x);
   }
   uint64_t prefix = 0, mask = 0;
   int need = n_pick;              // still to take among the keys that match the prefix
   for (int shift = 56; shift >= 0; shift -= 8) {
-    s_hist[tid] = 0;
-    __syncthreads();
-    for (int b = tid; b < ranked; b += kSelThreads) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s_hist[lane + 64 * e] = 0;
+    __builtin_amdgcn_wave_barrier();
+    for (int b = lane; b < ranked; b += kWave) {
       const uint64_t k = s_key[b];
       if ((k & mask) == prefix) atomicAdd(&s_hist[(int)((k >> shift) & 255)], 1);
     }
-    __syncthreads();
-    if (tid < 64) {               // the digit at which the count from the top reaches `need`
-      int c[4], sum = 0;
+    __builtin_amdgcn_wave_barrier();
+    // the digit at which the count from the top reaches `need`
+    int c[4], mine = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        c[e] = s_hist[255 - (4 * tid + e)];
-        sum += c[e];
-      }
-      int before = sum;
-      for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(before, o, kWave);
-        if (tid >= o) before += y;
-      }
-      before -= sum;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (before < need && before + c[e] >= need) {
-          s_digit = 255 - (4 * tid + e);
-          s_above = before;
-          s_equal = c[e];
-        }
-        before += c[e];
-      }
+    for (int e = 0; e < 4; ++e) {
+      c[e] = s_hist[255 - (4 * lane + e)];
+      mine += c[e];
     }
-    __syncthreads();
-    prefix |= (uint64_t)s_digit << shift;
+    int before = mine;
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int y = __shfl_up(before, o, kWave);
+      if (lane >= o) before += y;
+    }
+    before -= mine;
+    int digit = 0, above = 0, equal = 0;
+    bool here = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (before < need && before + c[e] >= need) {
+        digit = 255 - (4 * lane + e);
+        above = before;
+        equal = c[e];
+        here = true;
+      }
+      before += c[e];
+    }
+    const int src = __ffsll((unsigned long long)__ballot(here)) - 1;   // exactly one lane: need <= keys counted
+    digit = __shfl(digit, src, kWave);
+    need -= __shfl(above, src, kWave);
+    prefix |= (uint64_t)digit << shift;
     mask |= 255ull << shift;
-    need -= s_above;
-    const bool all = s_equal == need;
-    __syncthreads();
-    if (all) break;               // every key with this prefix is taken
+    if (__shfl(equal, src, kWave) == need) break;      // every key with this prefix is taken
   }
   // taken: keys above the prefix, and the first `need` that match it
   int taken = 0, equal = 0;
-  for (int b0 = 0; b0 < ranked; b0 += kSelThreads) {
-    const int b = b0 + tid, w = tid >> 6, lane = tid & 63;
+  for (int b0 = 0; b0 < ranked; b0 += kWave) {
+    const int b = b0 + lane;
     const uint64_t k = b < ranked ? s_key[b] & mask : 0;
     const bool above = b < ranked && k > prefix, eq = b < ranked && k == prefix;
-    const uint64_t eqs = __ballot(eq), abv = __ballot(above), below = (1ull << lane) - 1;
-    if (lane == 0) {
-      s_wave[w][0] = __popcll(abv);
-      s_wave[w][1] = __popcll(eqs);
-    }
-    __syncthreads();
-    int my_above = taken + __popcll(abv & below), my_eq = equal + __popcll(eqs & below);
-    for (int x = 0; x < kSelThreads / 64; ++x) {
-      if (x < w) {
-        my_above += s_wave[x][0];
-        my_eq += s_wave[x][1];
-      }
-      taken += s_wave[x][0];
-      equal += s_wave[x][1];
-    }
+    const uint64_t abv = __ballot(above), eqs = __ballot(eq), below = (1ull << lane) - 1;
+    const int my_above = taken + __popcll(abv & below), my_eq = equal + __popcll(eqs & below);
     if (above || (eq && my_eq < need)) sel[first + my_above + min(my_eq, need)] = first + b;
-    __syncthreads();
+    taken += __popcll(abv);
+    equal += __popcll(eqs);
   }
 }
 
