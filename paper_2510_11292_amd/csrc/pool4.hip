@@ -314,13 +314,49 @@ __device__ __forceinline__ void window_of(const AttnQ4& a, int64_t s, int& start
   start = first >= 0 ? first % a.window : 0;
 }
 
+// The waves' maxima, sums and weighted sums of a block to its output rows, or to
+// its partials where a slice has several blocks.
+template <int G, int NW>
+__device__ __forceinline__ void merge_waves(const AttnQ4& a, const float (*s_m)[G], const float (*s_l)[G],
+                                            const float (*s_acc)[G][kHeadDim], int64_t s, int chunk, int tid) {
+  for (int i = tid; i < G * kHeadDim; i += NW * 64) {
+    const int j = i / kHeadDim, k = i % kHeadDim;
+    float mm = -__builtin_inff();
+#pragma unroll
+    for (int x = 0; x < NW; ++x) mm = fmaxf(mm, s_m[x][j]);
+    const float base = max_base(mm);
+    float ll = 0.f, o = 0.f;
+#pragma unroll
+    for (int x = 0; x < NW; ++x) {
+      const float c = __builtin_amdgcn_exp2f(s_m[x][j] - base);
+      ll += s_l[x][j] * c;
+      o += s_acc[x][j][k] * c;
+    }
+    const size_t row = (size_t)s * G + j;
+    if (a.n_chunks > 1) {
+      float* p = a.part + (row * a.n_chunks + chunk) * kPartFloats;
+      p[2 + k] = o;
+      if (k == 0) {
+        p[0] = mm;
+        p[1] = ll;
+      }
+      continue;
+    }
+    o *= inv_sum(ll);
+    if (a.out_bf16) static_cast<uint16_t*>(a.out)[row * kHeadDim + k] = f32_to_bf16(o);
+    else static_cast<float*>(a.out)[row * kHeadDim + k] = o;
+    if (a.lse_out && k == 0) a.lse_out[row] = lse_of(mm, ll);
+  }
+}
+
+// ---- float32: vector ALUs
+
 // Block (slice, chunk): softmax over the chunk's share of the slice's rows, one
-// pass, 16 lanes a row (lane sub owns channels 8 sub..+7), float32 on the vector
-// ALUs.  Every 16-lane group keeps its own running maximum, sum and weighted
+// pass, 16 lanes a row (lane sub owns channels 8 sub..+7).  Every 16-lane group keeps its own running maximum, sum and weighted
 // sum; they are joined at the end.
 constexpr int kAttnWaves = 8;
 
-template <class T, int G>
+template <int G>
 __global__ __launch_bounds__(kAttnWaves * 64)
 void attn_q4_kernel(const AttnQ4 a) {
   constexpr int kGroups = kAttnWaves * 4;
@@ -338,7 +374,7 @@ void attn_q4_kernel(const AttnQ4 a) {
   float q[G][8];
 #pragma unroll
   for (int j = 0; j < G; ++j) {
-    load8(static_cast<const T*>(a.q) + ((size_t)s * G + j) * kHeadDim + 8 * sub, q[j]);
+    load8(static_cast<const float*>(a.q) + ((size_t)s * G + j) * kHeadDim + 8 * sub, q[j]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) q[j][e] *= qs;
   }
@@ -350,23 +386,7 @@ void attn_q4_kernel(const AttnQ4 a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[j][e] = 0.f;
   }
-  for (int r = r0 + grp; r < r1; r += kGroups) {
-    float k[8], v[8];
-    if (r < nsel) {
-      const int64_t src = min<int64_t>(max(a.rows[(size_t)s * a.budget + r], 0), a.pool_rows - 1);
-      const size_t row = (size_t)s * a.pool_rows + src;
-      const uint32_t kc = *reinterpret_cast<const uint32_t*>(a.codes + row * kCodeBytes + 4 * sub);
-      const uint32_t vc = *reinterpret_cast<const uint32_t*>(a.codes + row * kCodeBytes + 64 + 4 * sub);
-      const uint32_t kb = a.scales[row * kScaleBytes + (sub >> 2)], vb = a.scales[row * kScaleBytes + 4 + (sub >> 2)];
-      expand8(kc, scale_of(kb), k);
-      expand8(vc, scale_of(vb), v);
-    } else {
-      int slot = local_start + (r - nsel);
-      slot -= slot >= a.window ? a.window : 0;
-      const size_t o = ((size_t)s * a.window + slot) * kHeadDim + 8 * sub;
-      load8(static_cast<const T*>(a.k_local) + o, k);
-      load8(static_cast<const T*>(a.v_local) + o, v);
-    }
+  auto attend = [&](const float (&k)[8], const float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < G; ++j) {
       float d = 0.f;
@@ -380,6 +400,41 @@ void attn_q4_kernel(const AttnQ4 a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[j][e] = fmaf(acc[j][e], c, p * v[e]);
     }
+  };
+  // kRows of a group's rows on their way together: their list entries, then their codes
+  constexpr int kRows = 4;
+  const int p1 = min(r1, nsel);
+  for (int r = r0 + grp; r < p1; r += kRows * kGroups) {
+    size_t row[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u)
+      row[u] = (size_t)s * a.pool_rows +
+               min<int64_t>(max(a.rows[(size_t)s * a.budget + min(r + u * kGroups, p1 - 1)], 0), a.pool_rows - 1);
+    uint32_t kc[kRows], vc[kRows], ks[kRows], vs[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      kc[u] = *reinterpret_cast<const uint32_t*>(a.codes + row[u] * kCodeBytes + 4 * sub);
+      vc[u] = *reinterpret_cast<const uint32_t*>(a.codes + row[u] * kCodeBytes + 64 + 4 * sub);
+      ks[u] = a.scales[row[u] * kScaleBytes + (sub >> 2)];
+      vs[u] = a.scales[row[u] * kScaleBytes + 4 + (sub >> 2)];
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      if (r + u * kGroups >= p1) break;
+      float k[8], v[8];
+      expand8(kc[u], scale_of(ks[u]), k);
+      expand8(vc[u], scale_of(vs[u]), v);
+      attend(k, v);
+    }
+  }
+  for (int r = max(r0, nsel) + grp; r < r1; r += kGroups) {
+    int slot = local_start + (r - nsel);
+    slot -= slot >= a.window ? a.window : 0;
+    const size_t o = ((size_t)s * a.window + slot) * kHeadDim + 8 * sub;
+    float k[8], v[8];
+    load8(static_cast<const float*>(a.k_local) + o, k);
+    load8(static_cast<const float*>(a.v_local) + o, v);
+    attend(k, v);
   }
   // the wave's four groups, then its totals into LDS
 #pragma unroll
@@ -403,52 +458,276 @@ void attn_q4_kernel(const AttnQ4 a) {
     }
   }
   __syncthreads();
-  for (int i = tid; i < G * kHeadDim; i += kAttnWaves * 64) {
-    const int j = i / kHeadDim, k = i % kHeadDim;
-    float mm = -__builtin_inff();
-#pragma unroll
-    for (int x = 0; x < kAttnWaves; ++x) mm = fmaxf(mm, s_m[x][j]);
-    const float base = max_base(mm);
-    float ll = 0.f, o = 0.f;
-#pragma unroll
-    for (int x = 0; x < kAttnWaves; ++x) {
-      const float c = __builtin_amdgcn_exp2f(s_m[x][j] - base);
-      ll += s_l[x][j] * c;
-      o += s_acc[x][j][k] * c;
-    }
-    const size_t row = (size_t)s * G + j;
-    if (a.n_chunks > 1) {
-      float* p = a.part + (row * a.n_chunks + chunk) * kPartFloats;
-      p[2 + k] = o;
-      if (k == 0) {
-        p[0] = mm;
-        p[1] = ll;
-      }
-      continue;
-    }
-    o *= inv_sum(ll);
-    if (a.out_bf16) static_cast<uint16_t*>(a.out)[row * kHeadDim + k] = f32_to_bf16(o);
-    else static_cast<float*>(a.out)[row * kHeadDim + k] = o;
-    if (a.lse_out && k == 0) a.lse_out[row] = lse_of(mm, ll);
-  }
+  merge_waves<G, kAttnWaves>(a, s_m, s_l, s_acc, s, chunk, tid);
 }
 
-// Chunks of a slice's rows: enough blocks for the chip, none below kMinRows rows.
-constexpr int kTargetBlocks = 512, kMinRows = 128;
+// ---- bf16: matrix cores
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// The eight channels of a code word as four bfloat16 pairs.
+__device__ __forceinline__ uint4 expand8_bf16(uint32_t c, float scale) {
+  uint4 v;
+  v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
+  v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
+  v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
+  v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
+  return v;
+}
+
+constexpr float kGrow = 8.0f;   // base-2 logits may pass the base by this much before the sums are rescaled
+
+// Block (slice, chunk), eight waves, each with tiles of 32 rows.  Lane (c = l % 16,
+// h = l / 16).
+//   scores  S^T = K Q^T, 16 rows at a time: the lane holds 32 channels (a block of
+//           the format, one scale) of key row c as the A operand, and as the B
+//           operand the same channels of head c % G, so that it receives the
+//           scores of head c for rows 4 h + 0..3 and 16 + 4 h + 0..3.
+//   values  O = P V: those eight weights, unmoved, are the lane's part of the A
+//           operand (k index = its eight rows), and its part of the B operand is
+//           one channel of the same eight rows.  It has word c (eight channels, in
+//           one block of the format) of each of them; the i-th channel of all of
+//           them, paired by byte permutes, is the operand of the i-th product, whose
+//           columns are channels 8 c + i.
+// Rows are loaded 16 bytes a lane, five loads a tile; the values' words and the
+// scales change lanes through LDS.  (Loaded where they are used, in twenty loads of
+// 1 and 4 bytes, rows came at 4.9 TB/s however many were in flight.)
+template <int G>
+__global__ __launch_bounds__(kAttnWaves * 64)
+void attn_q4_mfma_kernel(const AttnQ4 a) {
+  constexpr int NW = kAttnWaves;
+  __shared__ float s_m[NW][G], s_l[NW][G];
+  __shared__ float s_acc[NW][G][kHeadDim];
+  __shared__ __align__(16) uint32_t s_v[NW][32 * 16 + 7 * 16], s_sc[NW][64];
+  // word of a tile's row in s_v: 16 more after every four rows, so that a read of
+  // rows 4 h + j by the four groups of lanes falls into different banks
+  auto value_word = [](int r) { return r * 16 + (r >> 2) * 16; };
+  const int64_t s = blockIdx.x / a.n_chunks;
+  const int chunk = (int)(blockIdx.x - s * a.n_chunks);
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, h = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int local_start, n_local;
+  window_of(a, s, local_start, n_local);
+  const int nsel = max(0, min(a.n_sel[s], a.budget));
+  const int total = nsel + n_local;
+  const int r0 = (int)((int64_t)total * chunk / a.n_chunks), r1 = (int)((int64_t)total * (chunk + 1) / a.n_chunks);
+  const int p1 = min(r1, nsel), n_pool = max(p1 - r0, 0);               // pool rows r0..p1-1 of the chunk
+  const int w0 = max(r0, nsel) - nsel, n_win = max(r1 - max(r0, nsel), 0);   // window rows w0.. of it
+  const int n_pool_tiles = (n_pool + 31) / 32, n_win_tiles = (n_win + 31) / 32;
+
+  bf16x8 q[4];
+  const float qs = a.scale * kLog2E, mult = fabsf(qs);
+  const uint32_t flip = qs < 0.f ? 0x80008000u : 0u;                    // |scale| multiplies the scores of -q
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + ((size_t)s * G + c % G) * kHeadDim +
+                                              32 * h + 8 * k);
+    v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
+    q[k] = __builtin_bit_cast(bf16x8, v);
+  }
+  float base = 0.f, grow_at = -__builtin_inff(), sum = 0.f;
+  f32x4 o[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const uint8_t* codes = a.codes + (size_t)s * a.pool_rows * kCodeBytes;
+  const uint8_t* scales = a.scales + (size_t)s * a.pool_rows * kScaleBytes;
+  // A tile as it is loaded: 32 channels of rows c and 16 + c, and the four scales of
+  // the keys (lanes 0..31) or values of row l % 32.
+  struct Raw {
+    uint4 k[2], v[2];
+    uint32_t scale;
+  };
+  const uint8_t* kc = codes + 16 * h;
+  const uint8_t* sc4 = scales + 4 * (lane >> 5);
+  static_assert(kCodeBytes == 16 * kScaleBytes, "a row's scales are at a sixteenth of its codes' offset");
+  // byte offsets of the codes of rows c, 16 + c and l % 32 of tile t; a row behind
+  // the chunk's last is that one
+  struct Rows { uint32_t at[2], own; };
+  const int32_t* list = a.rows + (size_t)s * a.budget + r0;
+  auto find = [&](int t, Rows& x) {
+    auto row = [&](int r) {
+      return (uint32_t)min(max(list[min(32 * t + r, n_pool - 1)], 0), (int)a.pool_rows - 1) * (uint32_t)kCodeBytes;
+    };
+    x.at[0] = row(c);
+    x.at[1] = row(16 + c);
+    x.own = row(lane & 31);
+  };
+  auto fetch = [&](const Rows& r, Raw& x) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      x.k[i] = *reinterpret_cast<const uint4*>(kc + r.at[i]);
+      x.v[i] = *reinterpret_cast<const uint4*>(kc + r.at[i] + 64);
+    }
+    x.scale = *reinterpret_cast<const uint32_t*>(sc4 + (r.own >> 4));
+  };
+  // scores of 32 rows, of which n are there, and their values' pairs
+  auto attend = [&](f32x4 (&sc)[2], const uint4 (&v)[8], int n) {
+    float m = mult;
+    if (n < 32) {                                                        // wave-uniform
+      m = 1.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        sc[j >> 2][j & 3] = 16 * (j >> 2) + 4 * h + (j & 3) < n ? sc[j >> 2][j & 3] * mult : -__builtin_inff();
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[j >> 2][j & 3]);
+    top *= m;
+    if (__builtin_amdgcn_ballot_w64(top > grow_at)) {
+      top = fmaxf(top, __shfl_xor(top, 16, kWave));
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      const bool grows = top > grow_at;
+      // before the first finite score the sums are 0 (or NaN): any factor does
+      const float f = grows && grow_at != -__builtin_inff() ? __builtin_amdgcn_exp2f(base - top) : 1.f;
+      base = grows ? top : base;
+      grow_at = grows ? top + kGrow : grow_at;
+      sum *= f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float fe = __shfl(f, 4 * h + e, kWave);                   // the factor of head 4 h + e
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i][e] *= fe;
+      }
+    }
+    bf16x8 p;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float y = __builtin_amdgcn_exp2f(fmaf(sc[j >> 2][j & 3], m, -base));
+      sum += y;
+      p[j] = (__bf16)y;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint4 b;
+      constexpr uint32_t kLow = 0x05040100, kHigh = 0x07060302;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        (&b.x)[t] = __builtin_amdgcn_perm((&v[2 * t + 1].x)[i >> 1], (&v[2 * t].x)[i >> 1], i & 1 ? kHigh : kLow);
+      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, __builtin_bit_cast(bf16x8, b), o[i], 0, 0, 0);
+    }
+  };
+  auto score = [&](const uint4 (&k)[4]) {
+    f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[i]), q[i], sc, 0, 0, 0);
+    return sc;
+  };
+
+  auto tile = [&](int t, const Raw& x) {
+    // through the wave's LDS: values to the lanes of their columns, scales to their rows'
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4*>(&s_v[w][value_word(16 * i + c) + 4 * h]) = x.v[i];
+    s_sc[w][lane] = x.scale;
+    __builtin_amdgcn_wave_barrier();
+    const uint8_t* sb = reinterpret_cast<const uint8_t*>(s_sc[w]);
+    f32x4 sc[2];
+    uint4 v[8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float f = scale_of(sb[4 * (16 * i + c) + h]);
+      uint4 k[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[e] = expand8_bf16((&x.k[i].x)[e], f);
+      sc[i] = score(k);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int r = 16 * (j >> 2) + 4 * h + (j & 3);
+      v[j] = expand8_bf16(s_v[w][value_word(r) + c], scale_of(sb[128 + 4 * r + (c >> 2)]));
+    }
+    attend(sc, v, n_pool - 32 * t);
+  };
+  // a tile's rows are on their way while the one before is at hand, its list
+  // entries while the one two before is
+  Rows ra, rb;
+  Raw xa, xb;
+  if (w < n_pool_tiles) {
+    find(w, ra);
+    find(w + NW, rb);
+    fetch(ra, xa);
+  }
+  const uint16_t* kl = static_cast<const uint16_t*>(a.k_local) + (size_t)s * a.window * kHeadDim;
+  const uint16_t* vl = static_cast<const uint16_t*>(a.v_local) + (size_t)s * a.window * kHeadDim;
+  // waves from the last on take the window's tiles, so that the shares even out
+  for (int t = NW - 1 - w; t < n_win_tiles; t += NW) {
+    auto slot = [&](int r) {
+      const int y = local_start + w0 + min(32 * t + r, n_win - 1);
+      return y >= a.window ? y - a.window : y;
+    };
+    uint4 v[8];
+    f32x4 sc[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint4* src = reinterpret_cast<const uint4*>(kl + (size_t)slot(16 * i + c) * kHeadDim + 32 * h);
+      uint4 k[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[e] = src[e];
+      sc[i] = score(k);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      v[j] = *reinterpret_cast<const uint4*>(vl + (size_t)slot(16 * (j >> 2) + 4 * h + (j & 3)) * kHeadDim + 8 * c);
+    attend(sc, v, n_win - 32 * t);
+  }
+  for (int t = w; t < n_pool_tiles; t += 2 * NW) {
+    if (t + NW < n_pool_tiles) fetch(rb, xb);
+    if (t + 2 * NW < n_pool_tiles) find(t + 2 * NW, ra);
+    __builtin_amdgcn_sched_barrier(0);
+    tile(t, xa);
+    if (t + NW >= n_pool_tiles) break;
+    if (t + 2 * NW < n_pool_tiles) fetch(ra, xa);
+    if (t + 3 * NW < n_pool_tiles) find(t + 3 * NW, rb);
+    __builtin_amdgcn_sched_barrier(0);
+    tile(t + NW, xb);
+  }
+  // the wave's sums: head c of lanes c < G, and heads 4 h + e of the channels 8 c + i
+  sum += __shfl_xor(sum, 16, kWave);
+  sum += __shfl_xor(sum, 32, kWave);
+  if (lane < G) {
+    s_m[w][lane] = grow_at == -__builtin_inff() ? -__builtin_inff() : base;
+    s_l[w][lane] = sum;
+  }
+  if (4 * h < G) {
+#pragma unroll
+    for (int e = 0; e < (G < 4 ? G : 4); ++e) {
+      float* dst = &s_acc[w][4 * h + e][8 * c];
+      reinterpret_cast<float4*>(dst)[0] = make_float4(o[0][e], o[1][e], o[2][e], o[3][e]);
+      reinterpret_cast<float4*>(dst)[1] = make_float4(o[4][e], o[5][e], o[6][e], o[7][e]);
+    }
+  }
+  __syncthreads();
+  merge_waves<G, NW>(a, s_m, s_l, s_acc, s, chunk, tid);
+}
+
+// Chunks of a slice's rows: blocks for the chip, with the rows that a block has in
+// flight at once, a half tile a wave (8 slices of 2148 rows, attention alone: 128
+// rows a block 5.8 us, 256 rows 7.0; 256 slices: one chunk 20 us, two and their
+// merge 25).
+constexpr int kTargetBlocks = 256, kMinRows = 128;
 int attn_q4_chunks(int64_t S, int budget, int window) {
   const int64_t cap = (int64_t)budget + window;
-  const int64_t by_rows = std::max<int64_t>(1, cap / kMinRows);
+  const int64_t by_rows = std::max<int64_t>(1, (cap + kMinRows - 1) / kMinRows);
   const int64_t by_grid = std::max<int64_t>(1, kTargetBlocks / S);
   return (int)std::min(by_rows, by_grid);
 }
 
-template <class T>
-void launch_attn_q4(const AttnQ4& a, int group_size, unsigned grid, hipStream_t s) {
+void launch_attn_q4(const AttnQ4& a, int dtype, int group_size, unsigned grid, hipStream_t s) {
+  if (dtype == LOUISKV_BF16) {
+    switch (group_size) {
+      case 1: attn_q4_mfma_kernel<1><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
+      case 2: attn_q4_mfma_kernel<2><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
+      case 4: attn_q4_mfma_kernel<4><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
+      default: attn_q4_mfma_kernel<8><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
+    }
+    return;
+  }
   switch (group_size) {
-    case 1: attn_q4_kernel<T, 1><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
-    case 2: attn_q4_kernel<T, 2><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
-    case 4: attn_q4_kernel<T, 4><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
-    default: attn_q4_kernel<T, 8><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
+    case 1: attn_q4_kernel<1><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
+    case 2: attn_q4_kernel<2><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
+    case 4: attn_q4_kernel<4><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
+    default: attn_q4_kernel<8><<<grid, kAttnWaves * 64, 0, s>>>(a); break;
   }
 }
 
@@ -529,8 +808,7 @@ int attn_q4(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads, 
   a.out = out; a.out_bf16 = out_dtype == LOUISKV_BF16; a.lse_out = lse_out;
   const unsigned grid = (unsigned)(n_slices * n_chunks);
   hipStream_t s = as_stream(stream);
-  if (dtype == LOUISKV_BF16) launch_attn_q4<uint16_t>(a, group_size, grid, s);
-  else launch_attn_q4<float>(a, group_size, grid, s);
+  launch_attn_q4(a, dtype, group_size, grid, s);
   LKV_CHECK_LAUNCH();
   if (n_chunks == 1) return LOUISKV_OK;
   return merge_parts(a.part, n_chunks, n_slices * group_size, out, out_dtype, lse_out, s);

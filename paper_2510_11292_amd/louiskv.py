@@ -698,12 +698,11 @@ Q4_MAX_POOL_ROWS = 1 << 24
 
 def _pool_q4(codes, scales, n_slices: int) -> int:
     """Rows per slice of a 4-bit pool (codes [S][rows][128], scales [S][rows][8], uint8)."""
-    rows = codes.shape[1] if codes.dim() == 3 else -1
-    if (codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or tuple(codes.shape) != (n_slices, rows, 128)
-            or tuple(scales.shape) != (n_slices, rows, 8)):
+    a, b = codes.shape, scales.shape
+    rows = a[1] if len(a) == 3 else -1
+    if a != (n_slices, rows, 128) or b != (n_slices, rows, 8) or not (codes.dtype is scales.dtype is torch.uint8):
         raise ValueError(f"a 4-bit pool of {n_slices} slices is codes [{n_slices}][rows][128] and scales "
-                         f"[{n_slices}][rows][8], uint8: got {tuple(codes.shape)} {codes.dtype}, "
-                         f"{tuple(scales.shape)} {scales.dtype}")
+                         f"[{n_slices}][rows][8], uint8: got {tuple(a)} {codes.dtype}, {tuple(b)} {scales.dtype}")
     return rows
 
 
