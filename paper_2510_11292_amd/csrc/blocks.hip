@@ -234,11 +234,12 @@ struct PrefillArgs {
   float* lse_out;
 };
 
-// ---- bf16: matrix cores
+// The waves' products are on the matrix cores.
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // Waits for every copy and LDS access of the wave, then for the block's waves.
@@ -252,11 +253,17 @@ __device__ __forceinline__ void copy_to_lds(const void* base, uint32_t off, uint
 typedef __attribute__((address_space(3))) char* lds_ptr;
 __device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(lds_ptr)p; }
 
-// Rows of 256 bytes lie in LDS with their sixteen 16-byte pieces permuted, piece c
-// of row r at c ^ swizzle(r): sixteen consecutive rows put a piece in sixteen
-// different places (the key reads, a lane a row), and four consecutive rows put
-// a run of four pieces in four different ones (the transposing value reads).
-__device__ __forceinline__ int swizzle(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
+// Rows lie in LDS with their 16-byte pieces permuted, piece c of row r at
+// c ^ swizzle(r).  Sixteen consecutive rows put a piece in sixteen different places
+// (the key reads, a lane a row).  bfloat16, 16 pieces: four consecutive rows put a
+// run of four pieces in four different ones (the transposing value reads).
+// float32, 32 pieces: rows four apart put a run of eight in different halves of the
+// banks (the value reads of the two halves of a wave).
+template <class T>
+__device__ __forceinline__ int swizzle(int r) {
+  if constexpr (sizeof(T) == 2) return ((r & 3) << 2) | ((r >> 2) & 3);
+  else return (r & 3) | ((r >> 3) & 1) << 2 | ((r >> 2) & 1) << 3;
+}
 
 constexpr float kGrow = 8.0f;   // base-2 logits may pass the base by this much before the sums are rescaled
 
@@ -268,15 +275,20 @@ constexpr float kGrow = 8.0f;   // base-2 logits may pass the base by this much 
 // 16 scores of one query row; their exponentials are, unmoved, the B operand of
 // O^T += V^T P^T, whose A operand comes from LDS through transposing reads.  The
 // running base, sum and the rescale are then a lane's own.
-constexpr int kStageKeys = 64;
-constexpr int kStageBytes = kStageKeys * kHeadDim * 2;   // of the keys, and of the values
+// float32: the same with 32 positions a stage and products of two channels or keys
+// at a time, k index = half of the wave; the scores need no rounding.
+constexpr int kStageBytes = 16384;   // of the keys, and of the values
 
-template <int WR, int WK>
+template <class T, int WR, int WK>
 __global__ __launch_bounds__(WR * WK * 64, 2)
-void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) {
+void prefill_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) {
   constexpr int NW = WR * WK;
-  constexpr int kCopies = kStageKeys / 4 / NW;    // four-row copies of a wave, of keys and of values
-  static_assert(kStageKeys % (4 * NW) == 0 && 2 % WK == 0, "waves share a stage evenly");
+  constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int kRowBytes = kHeadDim * sizeof(T), kPieces = kRowBytes / 16;
+  constexpr int kStageKeys = kStageBytes / kRowBytes, kHalves = kStageKeys / 32;
+  constexpr int kCopyRows = 1024 / kRowBytes;             // rows of one copy of 64 x 16 bytes
+  constexpr int kCopies = kStageBytes / 1024 / NW;        // copies of a wave, of keys and of values
+  static_assert(kStageBytes % (1024 * NW) == 0 && kHalves % WK == 0, "waves share a stage evenly");
   __shared__ __align__(256) char s_ring[2][2 * kStageBytes];
   __shared__ int s_bad;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, n = lane & 31;
@@ -299,22 +311,23 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
   const int row0 = (rgrp * WR + wr) * 32;    // of this wave, in the tile
   if (rgrp * WR * 32 >= n_rows) return;      // the tile is shorter than the others (block-uniform)
 
-  // this lane's rows
-  bf16x8 q[8];
+  // this lane's row: 16-byte pieces 2 c + h (bfloat16) or 16 h + c (float32)
+  constexpr int kQ = kPieces / 2;
+  typename std::conditional<kBf16, bf16x8, f32x4>::type q[kQ];
   const float qs = a.scale * kLog2E;
-  const uint32_t flip = qs < 0.f ? 0x80008000u : 0u;     // |scale| multiplies the scores of -q
+  const uint32_t flip = qs < 0.f ? (kBf16 ? 0x80008000u : 0x80000000u) : 0u;     // |scale| multiplies the scores of -q
   const int r = min(row0 + n, n_rows - 1), qpos = a.q_start + i0 + (r >> lg);
   const size_t row = ((size_t)s * a.group_size + (r & (a.group_size - 1))) * a.n_q + i0 + (r >> lg);
-  const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + row * kHeadDim);
+  const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + row * kHeadDim);
 #pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    uint4 v = src[2 * c + h];
+  for (int c = 0; c < kQ; ++c) {
+    uint4 v = src[kBf16 ? 2 * c + h : 16 * h + c];
     v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
-    q[c] = __builtin_bit_cast(bf16x8, v);
+    q[c] = __builtin_bit_cast(typename std::remove_reference<decltype(q[c])>::type, v);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the queries are in before the copies start
 #pragma unroll
-  for (int c = 0; c < 8; ++c) asm volatile("" : "+v"(q[c]));
+  for (int c = 0; c < kQ; ++c) asm volatile("" : "+v"(q[c]));
   const float mult = fabsf(qs);
   const int first_pos = a.q_start + i0 + (min(row0, n_rows - 1) >> lg);
   const int last_pos = a.q_start + i0 + (min(row0 + 31, n_rows - 1) >> lg);
@@ -352,24 +365,24 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
     }
     return p;
   };
-  const char* kb = static_cast<const char*>(a.keys) + (size_t)s * a.key_rows * kHeadDim * 2;
-  const char* vb = static_cast<const char*>(a.values) + (size_t)s * a.key_rows * kHeadDim * 2;
-  // a wave's share of stage st to LDS, four rows a copy; a group past the list repeats its last
+  const char* kb = static_cast<const char*>(a.keys) + (size_t)s * a.key_rows * kRowBytes;
+  const char* vb = static_cast<const char*>(a.values) + (size_t)s * a.key_rows * kRowBytes;
+  // a wave's share of stage st to LDS; a group past the list repeats its last
   auto copy_stage = [&](int st, char* buf) {
-    constexpr int kPer = kCopies < 4 ? kCopies : 4;    // copies of one 16-row group
+    constexpr int kOfGroup = 16 / kCopyRows, kPer = kCopies < kOfGroup ? kCopies : kOfGroup;   // copies of a 16-row group
 #pragma unroll
     for (int x = 0; x < kCopies / kPer; ++x) {
-      const int c0 = w * kCopies + x * kPer, g16 = c0 >> 2;
+      const int c0 = w * kCopies + x * kPer, g16 = c0 / kOfGroup;
       const int pos = group_pos(min(st * (kStageKeys / 16) + g16, n_groups - 1));
       const int from = min(pos, a.n_keys - 1);                          // rows behind the last key repeat it
-      const char* kg = kb + (size_t)from * (kHeadDim * 2);
-      const char* vg = vb + (size_t)from * (kHeadDim * 2);
+      const char* kg = kb + (size_t)from * kRowBytes;
+      const char* vg = vb + (size_t)from * kRowBytes;
       const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(buf) + c0 * 1024);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int r16 = ((c0 & 3) + i) * 4 + (lane >> 4);               // row of the group
+        const int r16 = (c0 % kOfGroup + i) * kCopyRows + lane / kPieces;   // row of the group
         const int r = min(r16, a.n_keys - 1 - from);
-        const uint32_t off = r * (kHeadDim * 2) + (((lane & 15) ^ swizzle(r16)) << 4);
+        const uint32_t off = r * kRowBytes + (((lane % kPieces) ^ swizzle<T>(r16)) << 4);
         copy_to_lds(kg, off, dst + i * 1024);
         copy_to_lds(vg, off, dst + kStageBytes + i * 1024);
       }
@@ -382,47 +395,76 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-  // LDS addresses of this lane's reads in a 32-key half of a stage: pieces 2 c + h of
-  // key n, and of the values rows 4 h + 0..3 and, in the second, those + 8 (the
-  // same swizzle but for bit 1) of channels 32 dt + 0..31
+  // LDS addresses of this lane's reads in 32 keys of a stage.  bfloat16: pieces
+  // 2 c + h of key n, and of the values rows 4 h + 0..3 and, in the second, those + 8
+  // (the same swizzle but for bit 1) of channels 32 dt + 0..31.  float32: pieces
+  // 16 h + c of key n, and channel n % 4 of piece n / 4 (+ 8 dt) of rows 4 h + i.
   uint32_t k_at[8], v_at[4][2];
   {
-    const uint32_t k0 = lds_addr(s_ring) + n * 256, kp = (h ^ swizzle(n & 15)) << 4;
-    const int j4 = (lane & 15) >> 2, xp = (((lane >> 4) & 1) << 1) | ((lane & 3) >> 1);
-    const uint32_t v0 = lds_addr(s_ring) + kStageBytes + (4 * h + j4) * 256 + ((lane & 1) << 3);
-    const uint32_t vp = ((j4 << 2) | (xp ^ h)) << 4;
+    const uint32_t k0 = lds_addr(s_ring) + n * kRowBytes, v0 = lds_addr(s_ring) + kStageBytes;
+    if constexpr (kBf16) {
+      const uint32_t kp = (h ^ swizzle<T>(n & 15)) << 4;
+      const int j4 = (lane & 15) >> 2, xp = (((lane >> 4) & 1) << 1) | ((lane & 3) >> 1);
+      const uint32_t v1 = v0 + (4 * h + j4) * kRowBytes + ((lane & 1) << 3), vp = ((j4 << 2) | (xp ^ h)) << 4;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) k_at[c] = k0 + (kp ^ (c << 5));
+      for (int c = 0; c < 8; ++c) k_at[c] = k0 + (kp ^ (c << 5));
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt) {
-      v_at[dt][0] = v0 + (vp ^ (dt << 6));
-      v_at[dt][1] = v0 + 8 * 256 + (vp ^ (dt << 6) ^ 32);
+      for (int dt = 0; dt < 4; ++dt) {
+        v_at[dt][0] = v1 + (vp ^ (dt << 6));
+        v_at[dt][1] = v1 + 8 * kRowBytes + (vp ^ (dt << 6) ^ 32);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) k_at[c] = k0 + h * 256 + ((c ^ swizzle<T>(n & 15)) << 4);    // and ^ 128 for c + 8
+      // row (i & 3) + 8 (i >> 2) + 4 h: its swizzle is (i & 3) | (i >> 2 & 1) << 2 | h << 3
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+        v_at[dt][0] = v0 + 4 * h * kRowBytes + (((8 * dt + (n >> 2)) ^ (h << 3)) << 4) + ((n & 3) << 2);
     }
   }
   typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8;
+  typedef const __attribute__((address_space(3))) f32x4* lds_f32x4;
+  typedef const __attribute__((address_space(3))) float* lds_f32;
   typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-  // Keys 32 sub .. + 31 of the stage `off` bytes into the ring, and their values.
-  auto load_keys = [&](uint32_t off, int sub, bf16x8 (&kf)[8]) {
+  // Keys 32 sub .. + 31 of the stage `off` bytes into the ring, and their values
+  // (float32: read where they are used).
+  typedef typename std::conditional<kBf16, bf16x8[8], int>::type Keys;
+  typedef typename std::conditional<kBf16, s16x8[2][4], int>::type Values;
+  typedef typename std::conditional<kBf16, bf16x8[2], f32x16>::type Weights;
+  auto load_keys = [&](uint32_t off, int sub, Keys& kf) {
+    if constexpr (kBf16) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) kf[c] = *(lds_bf16x8)(uintptr_t)(k_at[c] + off + sub * 32 * 256);
+      for (int c = 0; c < 8; ++c) kf[c] = *(lds_bf16x8)(uintptr_t)(k_at[c] + off + sub * 32 * kRowBytes);
+    }
   };
-  auto load_values = [&](uint32_t off, int sub, s16x8 (&vf)[2][4]) {
+  auto load_values = [&](uint32_t off, int sub, Values& vf) {
+    if constexpr (kBf16) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt) {
-        const uint32_t at = off + (sub * 32 + 16 * k) * 256;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(v_at[dt][0] + at));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(v_at[dt][1] + at));
-        vf[k][dt] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
+        for (int dt = 0; dt < 4; ++dt) {
+          const uint32_t at = off + (sub * 32 + 16 * k) * kRowBytes;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(v_at[dt][0] + at));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(v_at[dt][1] + at));
+          vf[k][dt] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
   };
-  auto scores = [&](const bf16x8 (&kf)[8]) {
+  auto scores = [&](uint32_t off, const Keys& kf) {
     f32x16 sc;
 #pragma unroll
     for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+    if constexpr (kBf16) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], q[c], sc, 0, 0, 0);
+      for (int c = 0; c < 8; ++c) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], q[c], sc, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {
+        const f32x4 k = *(lds_f32x4)(uintptr_t)((k_at[c & 7] ^ (c >> 3 << 7)) + off);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[c][e], sc, 0, 0, 0);
+      }
+    }
     return sc;
   };
   // Masks scores of keys from tokens p0 and p1 on (16 each).
@@ -452,24 +494,34 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) o[dt] *= f;
   };
-  auto weights = [&](const f32x16& sc, float m, bf16x8 (&pb)[2]) {
+  auto weights = [&](const f32x16& sc, float m, Weights& pb) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(sc[8 * k + j], m, -base));
-        sum += p;
-        pb[k][j] = (__bf16)p;
-      }
+    for (int i = 0; i < 16; ++i) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], m, -base));
+      sum += p;
+      if constexpr (kBf16) pb[i >> 3][i & 7] = (__bf16)p;
+      else pb[i] = p;
+    }
   };
-  auto add_values = [&](const s16x8 (&vf)[2][4], const bf16x8 (&pb)[2]) {
+  auto add_values = [&](uint32_t off, const Values& vf, const Weights& pb) {
+    if constexpr (kBf16) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k][dt]), pb[k], o[dt], 0, 0, 0);
+        for (int dt = 0; dt < 4; ++dt)
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k][dt]), pb[k], o[dt], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+          const uint32_t at = v_at[dt][0] + ((i & 3) + 8 * (i >> 2)) * kRowBytes;
+          const float v = *(lds_f32)(uintptr_t)((at ^ (((i & 3) | ((i >> 2) & 1) << 2) << 4)) + off);
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, pb[i], o[dt], 0, 0, 0);
+        }
+    }
   };
-  auto soften = [&](f32x16& sc, int p0, int p1, bf16x8 (&pb)[2]) {
+  auto soften = [&](f32x16& sc, int p0, int p1, Weights& pb) {
     float m = mult;
     if (max(p0, p1) + 15 > first_pos) {
       mask(sc, p0, p1);
@@ -498,8 +550,8 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
       bool bad = false;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const bool b0 = (e[c] & 0x7f80u) == 0x7f80u, b1 = (e[c] & 0x7f800000u) == 0x7f800000u;
-        e[c] &= (b0 ? 0xffff0000u : ~0u) & (b1 ? 0x0000ffffu : ~0u);
+        const bool b0 = kBf16 && (e[c] & 0x7f80u) == 0x7f80u, b1 = (e[c] & 0x7f800000u) == 0x7f800000u;
+        e[c] &= (b0 ? 0xffff0000u : ~0u) & (b1 ? (kBf16 ? 0x0000ffffu : 0u) : ~0u);
         bad |= b0 | b1;
       }
       if (bad) {
@@ -533,17 +585,20 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
       pos = stage_pos(st + 1);
     }
     const uint32_t off = at * 2 * kStageBytes;
-    bf16x8 kf[8], pb[2];
-    s16x8 vf[2][4];
+    Keys kf;
+    Values vf;
+    Weights pb;
     auto half = [&](int sub, int p0, int p1, bool more) {
-      f32x16 sc = scores(kf);
+      f32x16 sc = scores(off, kf);
       load_values(off, sub, vf);
       if (more) load_keys(off, 1, kf);
       __builtin_amdgcn_sched_barrier(0);
       soften(sc, p0, p1, pb);
-      add_values(vf, pb);
+      add_values(off, vf, pb);
     };
-    if constexpr (WK == 1) {
+    if constexpr (kHalves == 1) {
+      if (min(p.at[0], p.at[1]) <= last_pos) half(0, p.at[0], p.at[1], false);
+    } else if constexpr (WK == 1) {
       const bool see0 = min(p.at[0], p.at[1]) <= last_pos, see1 = min(p.at[2], p.at[3]) <= last_pos;
       load_keys(off, see0 ? 0 : 1, kf);
       if (see0) half(0, p.at[0], p.at[1], true);
@@ -581,12 +636,12 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
       const int p0 = group_pos(gi);
 #pragma unroll 1
       for (int pos = p0; pos < min(p0 + 16, last_pos + 1); ++pos) {
-        const uint16_t* v = reinterpret_cast<const uint16_t*>(vb) + (size_t)pos * kHeadDim;
+        const T* v = reinterpret_cast<const T*>(vb) + (size_t)pos * kHeadDim;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const float f = bf16_to_f32(v[32 * dt + (i & 3) + 8 * (i >> 2) + 4 * h]);
+            const float f = load_as_f32(v, 32 * dt + (i & 3) + 8 * (i >> 2) + 4 * h);
             o[dt][i] += pos <= qpos && !__builtin_isfinite(f) ? f : 0.f;
           }
       }
@@ -650,69 +705,9 @@ void prefill_mfma_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) 
     }
 }
 
-template <int WR, int WK>
-void launch_prefill_mfma(const PrefillArgs& a, int row_groups, int64_t n_blocks, hipStream_t s) {
-  prefill_mfma_kernel<WR, WK><<<(unsigned)n_blocks, WR * WK * 64, 0, s>>>(a, row_groups, n_blocks);
-}
-
-// ---- float32: vector ALUs
-
-template <class T>
-__device__ __forceinline__ void row8(const T* p, float (&x)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = load_as_f32(p, e);
-}
-
-// Sixteen lanes per (query, head), lane sub with channels 8 sub..+7: one pass over
-// the keys of the tile's blocks.
-template <class T>
-__global__ __launch_bounds__(256)
-void prefill_attn_kernel(const PrefillArgs a, int64_t n_rows) {
-  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  if (row >= n_rows) return;
-  const int sub = threadIdx.x & 15;
-  const int64_t sh = row / a.n_q, s = sh / a.group_size;
-  const int i = (int)(row - sh * a.n_q), pos = a.q_start + i;
-  const int64_t list = s * a.n_tiles + i / a.q_block;
-  const int n = max(0, min(a.n_sel[list], a.sel_cap));
-  float q[8], acc[8];
-  row8(static_cast<const T*>(a.q) + (size_t)row * kHeadDim + 8 * sub, q);
-  const float qs = a.scale * kLog2E;
-  float m = -__builtin_inff(), l = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    q[e] *= qs;
-    acc[e] = 0.f;
-  }
-  const int last = min(a.n_keys - 1, pos);
-  for (int x = 0; x < n; ++x) {
-    const int b = min(max(a.sel[list * a.sel_cap + x], 0), (a.n_keys - 1) >> a.log_block);
-    const int k0 = b << a.log_block, k1 = min(k0 + (1 << a.log_block) - 1, last);
-    for (int k = k0; k <= k1; ++k) {
-      const size_t o = ((size_t)s * a.key_rows + k) * kHeadDim + 8 * sub;
-      float kv[8], vv[8];
-      row8(static_cast<const T*>(a.keys) + o, kv);
-      row8(static_cast<const T*>(a.values) + o, vv);
-      float d = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) d = fmaf(q[e], kv[e], d);
-      d = row16_add(d);
-      const float mn = fmaxf(m, d), base = max_base(mn);
-      const float c = __builtin_amdgcn_exp2f(m - base), p = __builtin_amdgcn_exp2f(d - base);
-      m = mn;
-      l = l * c + p;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = fmaf(acc[e], c, p * vv[e]);
-    }
-  }
-  const float inv = inv_sum(l);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const size_t o = (size_t)row * kHeadDim + 8 * sub + e;
-    if (a.out_bf16) static_cast<uint16_t*>(a.out)[o] = f32_to_bf16(acc[e] * inv);
-    else static_cast<float*>(a.out)[o] = acc[e] * inv;
-  }
-  if (a.lse_out && sub == 0) a.lse_out[row] = lse_of(m, l);
+template <class T, int WR, int WK>
+void launch_prefill(const PrefillArgs& a, int row_groups, int64_t n_blocks, hipStream_t s) {
+  prefill_kernel<T, WR, WK><<<(unsigned)n_blocks, WR * WK * 64, 0, s>>>(a, row_groups, n_blocks);
 }
 
 int check_dtype(int dtype) {
@@ -850,20 +845,24 @@ extern "C" int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, workspace_bytes);
   hipStream_t hs = as_stream(stream);
-  if (dtype == LOUISKV_F32) {
-    prefill_attn_kernel<float><<<(unsigned)((n_rows + 15) / 16), 256, 0, hs>>>(a, n_rows);
-    LKV_CHECK_LAUNCH();
-    return LOUISKV_OK;
-  }
   a.n_split = n_split;
   a.part = static_cast<float*>(workspace);
   const int64_t n_blocks = n_slices * a.n_tiles * row_groups * n_split;
   if (n_blocks > INT32_MAX) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
-  switch (per) {
-    case 256: launch_prefill_mfma<8, 1>(a, row_groups, n_blocks, hs); break;
-    case 128: launch_prefill_mfma<4, 1>(a, row_groups, n_blocks, hs); break;
-    case 64: launch_prefill_mfma<2, 2>(a, row_groups, n_blocks, hs); break;
-    default: launch_prefill_mfma<1, 2>(a, row_groups, n_blocks, hs); break;
+  if (dtype == LOUISKV_BF16) {
+    switch (per) {
+      case 256: launch_prefill<uint16_t, 8, 1>(a, row_groups, n_blocks, hs); break;
+      case 128: launch_prefill<uint16_t, 4, 1>(a, row_groups, n_blocks, hs); break;
+      case 64: launch_prefill<uint16_t, 2, 2>(a, row_groups, n_blocks, hs); break;
+      default: launch_prefill<uint16_t, 1, 2>(a, row_groups, n_blocks, hs); break;
+    }
+  } else {
+    switch (per) {
+      case 256: launch_prefill<float, 8, 1>(a, row_groups, n_blocks, hs); break;
+      case 128: launch_prefill<float, 4, 1>(a, row_groups, n_blocks, hs); break;
+      case 64: launch_prefill<float, 2, 1>(a, row_groups, n_blocks, hs); break;
+      default: launch_prefill<float, 1, 1>(a, row_groups, n_blocks, hs); break;
+    }
   }
   LKV_CHECK_LAUNCH();
   if (n_split == 1) return LOUISKV_OK;
