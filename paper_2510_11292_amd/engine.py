@@ -36,6 +36,16 @@ dense KV_critical buffers that louiskv_retrieve gathers; for a host pool the
 default keeps them as a cache of pool rows (louiskv_retrieve_delta), so a
 retrieval moves only the rows the previous selection did not hold.
 
+With pool_bits=4 the pool (in device memory, rows listed) holds every row in
+4-bit floating point: louiskv_pack_pool_q4, louiskv_segment_output_q4 and
+louiskv_sparse_decode_attn_rows_q4 take the places of their counterparts.  Index
+vectors and the local window stay in full precision, so selections are those of
+a full-precision pool; the attended keys and values are rounded.
+
+prompt_attention() is the attention of the prompt's own queries over selected
+blocks of its keys (louiskv_page_prefill, louiskv_retrieve_blocks,
+louiskv_sparse_prefill_attn), for a whole prompt or a chunk of it.
+
 EngineConfig also selects the ablation baselines of Appendix D.3 and
 Appendix B: trigger="stride" (louiskv_fire_every in place of the boundary
 test), index="pages" (louiskv_page_prefill in place of the clustering) and
@@ -135,8 +145,15 @@ class LouisKVEngine:
                  keep_scores: bool = False, out_dtype: Optional[torch.dtype] = None,
                  zero_copy: Optional[bool] = None, delta: Optional[bool] = None,
                  prefill_chunk: Optional[int] = None, copy_engine: bool = True, fuse_prologue: bool = True,
-                 fused_step: Optional[bool] = None, cache_rows: Optional[int] = None):
+                 fused_step: Optional[bool] = None, cache_rows: Optional[int] = None, pool_bits: int = 16):
         self.cfg = cfg
+        if pool_bits not in (4, 16):
+            raise ValueError(f"pool_bits={pool_bits}: 16 (the engine's dtype) or 4")
+        self.q4 = pool_bits == 4
+        if self.q4 and (pool_on_host or zero_copy is False or delta or cache_rows is not None or fused_step
+                        or prefill_chunk is not None or cfg.selection != "group"):
+            raise ValueError("a 4-bit pool is built for device memory with listed rows and group-consistent selection, "
+                             "clustered in one pass, stepped by the stage calls")
         self.dtype = dtype
         self.device = torch.device(device)
         self.pool_on_host = pool_on_host
@@ -179,7 +196,11 @@ class LouisKVEngine:
         self.unit_size = torch.zeros(S, cap, **i32)
         self.assign = torch.zeros(S, cfg.prompt_len, **i32)
         self.perm = torch.zeros(S, cfg.prompt_len, **i32)
-        if pool_on_host:
+        if self.q4:
+            self.k_pool = self.v_pool = None
+            self.codes = torch.empty(S, cfg.pool_rows, 128, dtype=torch.uint8, device=dev)
+            self.scales = torch.empty(S, cfg.pool_rows, 8, dtype=torch.uint8, device=dev)
+        elif pool_on_host:
             self.k_pool = torch.empty(S, cfg.pool_rows, d, dtype=dtype, pin_memory=True)
             self.v_pool = torch.empty(S, cfg.pool_rows, d, dtype=dtype, pin_memory=True)
         else:
@@ -245,7 +266,9 @@ class LouisKVEngine:
                                        **u8)
         elif self.zero_copy:
             self.ws_retrieve = torch.empty(L.retrieve_rows_workspace_size(S, cap), **u8)
-            self.ws_attn = torch.empty(max(L.sparse_decode_attn_rows_workspace_size(S, g, rows, cfg.window), 1), **u8)
+            size = (L.sparse_decode_attn_rows_q4_workspace_size if self.q4
+                    else L.sparse_decode_attn_rows_workspace_size)
+            self.ws_attn = torch.empty(max(size(S, g, rows, cfg.window), 1), **u8)
         elif self.delta:
             self.ws_retrieve = torch.empty(L.retrieve_delta_workspace_size(S, cap, rows), **u8)
             self.ws_attn = torch.empty(max(L.sparse_decode_attn_rows_workspace_size(S, g, rows, cfg.window), 1), **u8)
@@ -261,7 +284,7 @@ class LouisKVEngine:
         step_shape_ok = (cfg.segments == "fixed" and cfg.trigger == "boundary" and not self.per_head
                          and cfg.n_q_heads // cfg.n_kv_heads in (1, 2, 4, 8))
         self._fused_cached = step_shape_ok and self.cached
-        self._fused_ok = step_shape_ok and ((self.zero_copy and not pool_on_host) or self._fused_cached)
+        self._fused_ok = step_shape_ok and not self.q4 and ((self.zero_copy and not pool_on_host) or self._fused_cached)
         if fused_step and not self._fused_ok:
             raise ValueError("the fused decode step needs fixed segments, group-consistent selection and either "
                              "zero-copy retrieval over a device pool or an LRU cache of pool rows")
@@ -321,6 +344,8 @@ class LouisKVEngine:
                            self.k_pool, self.v_pool, pool_on_host=self.pool_on_host)
             if pack_event is not None:
                 pack_event.record()
+            if self.q4:
+                L.pack_pool_q4(prompt_keys, prompt_values, None, self.codes, self.scales)
         elif self.prefill_chunk is not None:
             if iter_events is not None or pack_event is not None:
                 raise ValueError("the pipelined prefill takes no iteration or pack events")
@@ -335,8 +360,11 @@ class LouisKVEngine:
                               workspace=self.ws_prefill)
             if pack_event is not None:
                 pack_event.record()
-            L.pack_pool(prompt_keys, prompt_values, self.perm, self.k_pool, self.v_pool,
-                        pool_on_host=self.pool_on_host)
+            if self.q4:
+                L.pack_pool_q4(prompt_keys, prompt_values, self.perm, self.codes, self.scales)
+            else:
+                L.pack_pool(prompt_keys, prompt_values, self.perm, self.k_pool, self.v_pool,
+                            pool_on_host=self.pool_on_host)
         if self.seg_state is not None:
             L.segment_state_init(self.seg_state, c.window, c.n_clusters)
         if self.delta:
@@ -345,8 +373,34 @@ class LouisKVEngine:
             self.slot_step.fill_(-1)
         self.t = 0
 
+    def prompt_attention(self, q: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, q_start: int = 0,
+                         block_len: int = 64, q_block: int = 64, n_first: int = 1, n_recent: int = 4,
+                         n_top: int = 24, out: Optional[torch.Tensor] = None,
+                         lse_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Causal attention of the prompt tokens q_start .. q_start + n_q - 1 (q [G][Hq][n_q][d]) over selected
+        blocks of the keys and values so far ([S][n][d], n >= q_start + n_q): every tile of q_block queries
+        attends to the first n_first blocks of block_len keys, its own and the n_recent before them, and the n_top
+        others with the largest scores of their mean keys.  Returns out [G][Hq][n_q][d] (allocated if not given)."""
+        h = self.cfg.n_kv_heads
+        s, n, d = keys.shape
+        n_q = q.shape[2]
+        i32 = dict(dtype=torch.int32, device=q.device)
+        n_blocks = -(-n // block_len)
+        cap = L.retrieve_blocks_cap(n, q_block, block_len, n_first, n_recent, n_top)
+        if cap < 1:
+            raise ValueError(f"block_len={block_len} q_block={q_block} n_first={n_first} n_recent={n_recent} n_top={n_top}")
+        reps = torch.empty(s, n_blocks, d, dtype=torch.float32, device=q.device)
+        spans = torch.empty(2, s, n_blocks, **i32)
+        L.page_prefill(keys, block_len, reps, spans[0], spans[1])
+        sel = torch.empty(s, -(-n_q // q_block), cap, **i32)
+        n_sel = torch.empty(sel.shape[:2], **i32)
+        L.retrieve_blocks(q, h, reps, n, q_start, q_block, block_len, n_first, n_recent, n_top, sel, n_sel)
+        out = torch.empty_like(q) if out is None else out
+        L.sparse_prefill_attn(q, h, keys, values, n, q_start, q_block, block_len, sel, n_sel, out, lse_out)
+        return out
+
     # ------------------------------------------------------- layer by layer
-    _PER_SLICE = ("reps", "unit_start", "unit_size", "assign", "perm", "k_pool", "v_pool", "k_local", "v_local",
+    _PER_SLICE = ("reps", "unit_start", "unit_size", "assign", "perm", "k_pool", "v_pool", "codes", "scales", "k_local", "v_local",
                   "sel_rows", "sel_rows_step", "k_buf", "v_buf", "buf_row", "slot_step", "slot_list",
                   "n_fetched", "sel_units", "n_sel_units", "n_sel", "scores", "seg_state")
     _PER_GROUP = ("q_ref", "fire", "r", "out", "lse")
@@ -378,7 +432,9 @@ class LouisKVEngine:
         if n not in self._view_ws_attn:
             gs = c.n_q_heads // h
             rows = max(c.budget, 1)
-            if self.zero_copy or self.delta:
+            if self.q4:
+                need = L.sparse_decode_attn_rows_q4_workspace_size(h * n, gs, rows, c.window)
+            elif self.zero_copy or self.delta:
                 need = L.sparse_decode_attn_rows_workspace_size(h * n, gs, rows, c.window)
             else:
                 need = L.sparse_decode_attn_workspace_size(h * n, gs, rows, c.window)
@@ -447,6 +503,9 @@ class LouisKVEngine:
             self.t += 1
             return
         fused = self.fuse_prologue and c.trigger == "boundary" and self.seg_state is None
+        if self.q4 and fused:
+            # a step that evicts stores with its own call, which writes the 4-bit pool
+            fused = L.window_info(t, c.window, c.seg_len)[0] < 0
         if c.trigger == "stride":
             L.fire_every(self.fire, t, c.stride)
         elif fused:
@@ -476,7 +535,10 @@ class LouisKVEngine:
                        self.k_pool, self.v_pool, c.budget, self.sel_units, self.n_sel_units, self.n_sel,
                        self.k_buf, self.v_buf, fire=self.fire, pool_on_host=self.pool_on_host,
                        scores_out=self.scores, workspace=self.ws_retrieve)
-        if not fused:
+        if not fused and self.q4:
+            L.segment_output_q4(k_t, v_t, self.k_local, self.v_local, t, c.seg_len, self.reps, self.unit_start,
+                                self.unit_size, c.n_clusters, self.codes, self.scales, c.prompt_len)
+        elif not fused:
             L.segment_output(k_t, v_t, self.k_local, self.v_local, t, c.seg_len, self.reps, self.unit_start,
                              self.unit_size, c.n_clusters, self.k_pool, self.v_pool, c.prompt_len,
                              pool_on_host=self.pool_on_host)
@@ -485,6 +547,10 @@ class LouisKVEngine:
             L.sparse_decode_attn_rows_per_head(q_t, c.n_kv_heads, self.k_pool, self.v_pool, self.sel_rows,
                                                self.n_sel, self.k_local, self.v_local, local_start, n_local,
                                                self.out, self.lse, workspace=self.ws_attn)
+        elif self.q4:
+            L.sparse_decode_attn_rows_q4(q_t, c.n_kv_heads, self.codes, self.scales, self.sel_rows, self.n_sel,
+                                         self.k_local, self.v_local, local_start, n_local, self.out, self.lse,
+                                         workspace=self.ws_attn)
         elif self.zero_copy:
             L.sparse_decode_attn_rows(q_t, c.n_kv_heads, self.k_pool, self.v_pool, self.sel_rows, self.n_sel,
                                       self.k_local, self.v_local, local_start, n_local, self.out, self.lse,
@@ -517,6 +583,15 @@ class LouisKVEngine:
                            c.window, self.k_pool, self.v_pool, c.budget, self.sel_units, self.n_sel_units,
                            self.n_sel, self.k_buf, self.v_buf, fire=self.fire, pool_on_host=self.pool_on_host,
                            scores_out=self.scores, workspace=self.ws_retrieve)
+        if self.q4:
+            L.segment_output_boundary_q4(k_t, v_t, self.k_local, self.v_local, t, c.seg_len, self.fire, self.seg_state,
+                                         self.reps, self.unit_start, self.unit_size, c.n_clusters, c.n_kv_heads,
+                                         self.codes, self.scales, c.prompt_len)
+            L.sparse_decode_attn_rows_q4_seg(q_t, c.n_kv_heads, self.codes, self.scales, self.sel_rows, self.n_sel,
+                                             self.k_local, self.v_local, self.seg_state, t + 1, self.out, self.lse,
+                                             workspace=self.ws_attn)
+            self.t += 1
+            return
         L.segment_output_boundary(k_t, v_t, self.k_local, self.v_local, t, c.seg_len, self.fire, self.seg_state,
                                   self.reps, self.unit_start, self.unit_size, c.n_clusters, c.n_kv_heads,
                                   self.k_pool, self.v_pool, c.prompt_len, pool_on_host=self.pool_on_host)

@@ -187,3 +187,14 @@ def test_python_calls_check_shapes():
     with pytest.raises(ValueError, match="contiguous"):
         c = torch.zeros(2, 10, 256, dtype=torch.uint8)[..., :128]
         L.pack_pool_q4(k, k, None, c, torch.zeros(2, 10, 8, dtype=torch.uint8))
+
+
+def test_engine_refuses_what_a_4_bit_pool_is_not_built_for():
+    from paper_2510_11292_amd.engine import EngineConfig, LouisKVEngine
+    cfg = EngineConfig(n_slices=2, n_kv_heads=2, n_q_heads=8, prompt_len=64, n_clusters=4, n_iters=1, gen_len=8,
+                       seg_len=4, budget=16, window=8, tau=0.9)
+    for kw in (dict(pool_bits=8), dict(pool_bits=4, pool_on_host=True), dict(pool_bits=4, zero_copy=False),
+               dict(pool_bits=4, fused_step=True), dict(pool_bits=4, cache_rows=64), dict(pool_bits=4, prefill_chunk=1),
+               dict(pool_bits=4, delta=True)):
+        with pytest.raises(ValueError, match="4-bit pool|pool_bits"):
+            LouisKVEngine(cfg, torch.bfloat16, "cpu", **kw)
