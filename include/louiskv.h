@@ -26,6 +26,11 @@
  *   louiskv_sparse_decode_attn_rows  the same over listed pool rows
  *                                                   (Section 3.1 attention;
  *                                                    Algorithm 1 decode loop)
+ *   louiskv_*_q4                the pool in 4-bit floating point: its writes,
+ *                               dense reads and the attention over listed rows
+ *   louiskv_retrieve_blocks, louiskv_sparse_prefill_attn
+ *                               the prompt's own attention over selected blocks
+ *                               of its keys
  *
  * Conventions shared by every call
  * --------------------------------
