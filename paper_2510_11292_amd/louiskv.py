@@ -696,6 +696,13 @@ def pack_pool(keys, values, perm, k_pool, v_pool=None, pool_on_host: bool = Fals
 Q4_MAX_POOL_ROWS = 1 << 24
 
 
+def _ws_bytes(workspace: Optional[torch.Tensor], device, size: int):
+    """The workspace and its bytes; one of `size` where none is given, none where none is needed."""
+    if workspace is not None:
+        return workspace, workspace.nbytes
+    return (torch.empty(size, dtype=torch.uint8, device=device), size) if size else (None, 0)
+
+
 def _pool_q4(codes, scales, n_slices: int) -> int:
     """Rows per slice of a 4-bit pool (codes [S][rows][128], scales [S][rows][8], uint8)."""
     a, b = codes.shape, scales.shape
@@ -710,7 +717,7 @@ def pack_pool_q4(keys, values, perm, codes, scales, stream=None):
     """Prompt K/V rows quantised into a 4-bit pool in perm order (perm None: token order)."""
     s, n, d = keys.shape
     rows = _pool_q4(codes, scales, s)
-    _check(_native().pack_pool_q4(keys, values, _dtype_code(keys), s, n, d, perm, codes, scales, rows, stream))
+    _check(_native().pack_pool_q4(keys, values, _one_dtype(keys, values), s, n, d, perm, codes, scales, rows, stream))
 
 
 def gather_rows_q4(codes, scales, sel_rows, n_sel, k_buf, v_buf, stream=None):
@@ -719,7 +726,7 @@ def gather_rows_q4(codes, scales, sel_rows, n_sel, k_buf, v_buf, stream=None):
     s, n, d = k_buf.shape
     rows = _pool_q4(codes, scales, s)
     _check(_native().gather_rows_q4(codes, scales, s, rows, d, sel_rows, n_sel, n, k_buf, v_buf,
-                                    _dtype_code(k_buf), stream))
+                                    _one_dtype(k_buf, v_buf), stream))
 
 
 def segment_output_q4(k_new, v_new, k_local, v_local, step: int, seg_len: int, reps, unit_start, unit_size,
@@ -728,7 +735,7 @@ def segment_output_q4(k_new, v_new, k_local, v_local, step: int, seg_len: int, r
     s, d = k_new.shape
     rows = _pool_q4(codes, scales, s) if codes is not None else 0
     _check(_native().segment_output_q4(
-        k_new, v_new, _dtype_code(k_new), s, d, k_local, v_local, k_local.shape[1],
+        k_new, v_new, _one_dtype(k_new, v_new, k_local, v_local), s, d, k_local, v_local, k_local.shape[1],
         step, seg_len, reps, unit_start, unit_size, reps.shape[1], n_clusters,
         codes, scales, rows, prompt_len, stream))
 
@@ -740,7 +747,7 @@ def segment_output_boundary_q4(k_new, v_new, k_local, v_local, step: int, seg_ma
     s, d = k_new.shape
     rows = _pool_q4(codes, scales, s) if codes is not None else 0
     _check(_native().segment_output_boundary_q4(
-        k_new, v_new, _dtype_code(k_new), s, n_kv_heads, d, k_local, v_local,
+        k_new, v_new, _one_dtype(k_new, v_new, k_local, v_local), s, n_kv_heads, d, k_local, v_local,
         k_local.shape[1], step, seg_max, fire, seg_state, reps, unit_start,
         unit_size, reps.shape[1], n_clusters, codes, scales, rows, prompt_len, stream))
 
@@ -759,10 +766,12 @@ def sparse_decode_attn_rows_q4(q, n_kv_heads: int, codes, scales, sel_rows, n_se
     budget = sel_rows.shape[1]
     window = k_local.shape[1]
     rows = _pool_q4(codes, scales, s)
-    ws, wsb = _ws(workspace, q.device, sparse_decode_attn_rows_q4_workspace_size, s, gs, budget, window, d)
+    lib = _native()
+    ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else
+                        lib.sparse_decode_attn_rows_q4_workspace_size(s, gs, d, budget, window))
     sc = (1.0 / d ** 0.5) if scale is None else scale
-    _check(_native().sparse_decode_attn_rows_q4(
-        q, _dtype_code(q), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel, budget,
+    _check(lib.sparse_decode_attn_rows_q4(
+        q, _one_dtype(q, k_local, v_local), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel, budget,
         k_local, v_local, window, local_start, n_local, out, _dtype_code(out), lse_out, ws, wsb, stream))
 
 
@@ -776,10 +785,12 @@ def sparse_decode_attn_rows_q4_seg(q, n_kv_heads: int, codes, scales, sel_rows, 
     budget = sel_rows.shape[1]
     window = k_local.shape[1]
     rows = _pool_q4(codes, scales, s)
-    ws, wsb = _ws(workspace, q.device, sparse_decode_attn_rows_q4_workspace_size, s, gs, budget, window, d)
+    lib = _native()
+    ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else
+                        lib.sparse_decode_attn_rows_q4_workspace_size(s, gs, d, budget, window))
     sc = (1.0 / d ** 0.5) if scale is None else scale
-    _check(_native().sparse_decode_attn_rows_q4_seg(
-        q, _dtype_code(q), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel, budget,
+    _check(lib.sparse_decode_attn_rows_q4_seg(
+        q, _one_dtype(q, k_local, v_local), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel, budget,
         k_local, v_local, window, seg_state, n_tokens, out, _dtype_code(out), lse_out, ws, wsb, stream))
 
 
@@ -790,15 +801,29 @@ def retrieve_blocks_cap(n_keys: int, q_block: int, block_len: int, n_first: int,
     return _native().retrieve_blocks_cap(n_keys, q_block, block_len, n_first, n_recent, n_top)
 
 
+def _lists(sel_blocks, n_sel_blocks, s: int, n_q: int, q_block: int) -> None:
+    a, b = sel_blocks.shape, (s, -(-n_q // max(q_block, 1)))
+    if (len(a) != 3 or a[:2] != b or n_sel_blocks.shape != b
+            or not (sel_blocks.dtype is n_sel_blocks.dtype is torch.int32)):
+        raise ValueError(f"sel_blocks {tuple(a)} {sel_blocks.dtype} and n_sel_blocks {tuple(n_sel_blocks.shape)} "
+                         f"{n_sel_blocks.dtype} are not int32 lists of {s} slices' {b[1]} tiles")
+
+
+def _one_dtype(first, *more) -> int:
+    """The dtype code that tensors of one element type share."""
+    for t in more:
+        if t.dtype is not first.dtype:
+            raise TypeError(f"tensors of one call differ in dtype: {first.dtype}, {t.dtype}")
+    return _dtype_code(first)
+
+
 def retrieve_blocks(q, n_kv_heads: int, reps, n_keys: int, q_start: int, q_block: int, block_len: int, n_first: int,
                     n_recent: int, n_top: int, sel_blocks, n_sel_blocks, stream=None):
     """The key blocks that every tile of q_block queries attends to: q [G][Hq][n_q][d], reps [S][blocks..][d] (the
     mean keys, as page_prefill makes them), sel_blocks [S][tiles][cap], n_sel_blocks [S][tiles]."""
     g, hq, n_q, d = q.shape
     s = g * n_kv_heads
-    if tuple(sel_blocks.shape[:2]) != (s, -(-n_q // max(q_block, 1))) or n_sel_blocks.shape != sel_blocks.shape[:2]:
-        raise ValueError(f"sel_blocks {tuple(sel_blocks.shape)} and n_sel_blocks {tuple(n_sel_blocks.shape)} do not "
-                         f"hold a list for each of {s} slices' {-(-n_q // max(q_block, 1))} tiles")
+    _lists(sel_blocks, n_sel_blocks, s, n_q, q_block)
     _check(_native().retrieve_blocks(
         q, _dtype_code(q), s, n_kv_heads, hq // n_kv_heads, n_q, d, reps, reps.shape[1], n_keys, q_start, q_block,
         block_len, n_first, n_recent, n_top, sel_blocks, sel_blocks.shape[2], n_sel_blocks, stream))
@@ -816,12 +841,15 @@ def sparse_prefill_attn(q, n_kv_heads: int, keys, values, n_keys: int, q_start: 
     g, hq, n_q, d = q.shape
     s = g * n_kv_heads
     gs = hq // n_kv_heads
-    if tuple(sel_blocks.shape[:2]) != (s, -(-n_q // max(q_block, 1))) or n_sel_blocks.shape != sel_blocks.shape[:2]:
-        raise ValueError(f"sel_blocks {tuple(sel_blocks.shape)} and n_sel_blocks {tuple(n_sel_blocks.shape)} do not "
-                         f"hold a list for each of {s} slices' {-(-n_q // max(q_block, 1))} tiles")
+    _lists(sel_blocks, n_sel_blocks, s, n_q, q_block)
+    if keys.shape != values.shape or keys.shape[0] != s or out.shape != q.shape:
+        raise ValueError(f"keys {tuple(keys.shape)}, values {tuple(values.shape)} of {s} slices, out {tuple(out.shape)} "
+                         f"as q {tuple(q.shape)} expected")
     cap = sel_blocks.shape[2]
-    ws, wsb = _ws(workspace, q.device, sparse_prefill_attn_workspace_size, s, gs, n_q, q_block, block_len, cap, d)
+    lib = _native()
+    ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else
+                        lib.sparse_prefill_attn_workspace_size(s, gs, n_q, d, q_block, block_len, cap))
     sc = (1.0 / d ** 0.5) if scale is None else scale
-    _check(_native().sparse_prefill_attn(
-        q, _dtype_code(q), s, n_kv_heads, gs, n_q, d, float(sc), keys, values, keys.shape[1], n_keys, q_start,
+    _check(lib.sparse_prefill_attn(
+        q, _one_dtype(q, keys, values), s, n_kv_heads, gs, n_q, d, float(sc), keys, values, keys.shape[1], n_keys, q_start,
         q_block, block_len, sel_blocks, cap, n_sel_blocks, out, _dtype_code(out), lse_out, ws, wsb, stream))

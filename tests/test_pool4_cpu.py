@@ -180,10 +180,20 @@ def test_python_calls_check_shapes():
         L.gather_rows_q4(torch.zeros(2, 10, 128, dtype=torch.uint8), torch.zeros(2, 9, 8, dtype=torch.uint8), None, None, k, k)
     q = torch.zeros(1, 4, 100, 128)
     sel, n = torch.zeros(2, 3, 4, dtype=torch.int32), torch.zeros(2, 3, dtype=torch.int32)
-    with pytest.raises(ValueError, match="lists|list for each"):
+    with pytest.raises(ValueError, match="lists"):
         L.retrieve_blocks(q, 2, torch.zeros(2, 8, 128), 100, 0, 64, 16, 0, 0, 1, sel, n)
-    with pytest.raises(ValueError, match="lists|list for each"):
+    with pytest.raises(ValueError, match="lists"):
         L.sparse_prefill_attn(q, 2, k, k, 100, 0, 64, 16, sel, n, q)
+    good = torch.zeros(2, 2, 4, dtype=torch.int32), torch.zeros(2, 2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="lists"):
+        L.sparse_prefill_attn(q, 2, k, k, 10, 0, 64, 16, good[0].long(), good[1], q)
+    with pytest.raises(ValueError, match="expected"):
+        L.sparse_prefill_attn(q, 2, k, k[:1], 10, 0, 64, 16, *good, q)
+    with pytest.raises(TypeError, match="differ in dtype"):
+        L.sparse_prefill_attn(q, 2, k, k.bfloat16(), 10, 0, 64, 16, *good, q)
+    with pytest.raises(TypeError, match="differ in dtype"):
+        L.pack_pool_q4(k, k.bfloat16(), None, torch.zeros(2, 10, 128, dtype=torch.uint8),
+                       torch.zeros(2, 10, 8, dtype=torch.uint8))
     with pytest.raises(ValueError, match="contiguous"):
         c = torch.zeros(2, 10, 256, dtype=torch.uint8)[..., :128]
         L.pack_pool_q4(k, k, None, c, torch.zeros(2, 10, 8, dtype=torch.uint8))
