@@ -893,11 +893,11 @@ int louiskv_sparse_decode_attn_rows_per_head(const void* q, int32_t dtype, int64
  *
  * Format      The d = 128 channels of a row are four blocks of 32.  A block has
  *             the scale 2^E with the smallest E in [-125, 125] for which
- *             max|x| <= 7 * 2^E (125 if there is none), and an element is the nearest of 0, 0.5, 1, 1.5,
- *             2, 3, 4, 6 times the scale, with its sign (ties to the even code;
- *             more than 6 scales become 6): below 7 * 2^125 no element is
- *             off by more than one scale, half the widest step.  A block with an infinity or NaN
- *             reads as 32 NaN.
+ *             max|x| <= 7 * 2^E (125 if there is none), and an element is the
+ *             nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the scale, with its
+ *             sign (ties to the even code; more than 6 scales become 6): below
+ *             7 * 2^125 no element is off by more than one scale, half the widest
+ *             step.  A block with an infinity or NaN reads as 32 NaN.
  * codes       [n_slices][pool_rows][128] uint8, 16-byte aligned: bytes 0..63 of
  *             a row its key, 64..127 its value.  A byte holds channel 2i in its
  *             low and 2i+1 in its high four bits, each a sign and the 3-bit index
@@ -906,7 +906,11 @@ int louiskv_sparse_decode_attn_rows_per_head(const void* q, int32_t dtype, int64
  *             four key blocks, then of the four value blocks; 255 for a block
  *             that is not finite.  Finite blocks have bytes 2 to 252; others mean
  *             nothing.
- * Limit       pool_rows <= LOUISKV_Q4_MAX_POOL_ROWS (LOUISKV_ERR_SHAPE).
+ * Limit       pool_rows <= LOUISKV_Q4_MAX_POOL_ROWS (LOUISKV_ERR_SHAPE); a list and
+ *             the window of one slice together at most twice that.
+ * Alignment   of these calls' and the block calls' element buffers (queries,
+ *             keys, values, windows, index vectors of the blocks, workspaces): 16
+ *             bytes (LOUISKV_ERR_UNSUPPORTED, LOUISKV_ERR_WORKSPACE).
  */
 #define LOUISKV_Q4_MAX_POOL_ROWS (1 << 24)
 
@@ -1029,8 +1033,8 @@ int louiskv_sparse_decode_attn_rows_q4_seg(const void* q, int32_t dtype, int64_t
  */
 
 /* Entries a tile's list can need: min(ceil(n_keys / block_len), n_first +
- * n_recent + n_top + blocks that q_block tokens can touch); 0 for sizes that
- * louiskv_retrieve_blocks refuses. */
+ * n_recent + n_top + blocks that q_block tokens can touch); 0 for a q_block, a
+ * block_len or counts that louiskv_retrieve_blocks refuses. */
 size_t louiskv_retrieve_blocks_cap(int32_t n_keys, int32_t q_block, int32_t block_len,
                                    int32_t n_first, int32_t n_recent, int32_t n_top);
 
@@ -1042,7 +1046,7 @@ size_t louiskv_retrieve_blocks_cap(int32_t n_keys, int32_t q_block, int32_t bloc
  *             the tile's blocks, ascending; entries behind them stay as they were.
  * n_sel_blocks out [n_slices][n_tiles] int32.
  * Requires 1 <= group_size <= 8, 1 <= q_block <= 128, block_len 16, 32, 64, 128
- * or 256, q_start >= 0, q_start + n_q <= n_keys, at most 8192 blocks,
+ * or 256, q_start >= 0, q_start + n_q <= n_keys <= 2^30, at most 8192 blocks,
  * blocks <= units_cap and sel_cap >= louiskv_retrieve_blocks_cap().
  */
 int louiskv_retrieve_blocks(const void* q, int32_t dtype, int64_t n_slices,
@@ -1071,7 +1075,8 @@ size_t louiskv_sparse_prefill_attn_workspace_size(int64_t n_slices, int32_t grou
  * workspace   louiskv_sparse_prefill_attn_workspace_size() bytes (partials where
  *             few tiles have their lists split over several blocks), may be 0.
  * Arithmetic as louiskv_sparse_decode_attn_rows_q4; group_size 1, 2, 4 or 8,
- * other sizes as louiskv_retrieve_blocks, sel_cap >= 1.
+ * other sizes as louiskv_retrieve_blocks (but any number of blocks), sel_cap >= 1,
+ * sel_cap * block_len <= 2^30.
  */
 int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t n_slices,
                                 int32_t n_kv_heads, int32_t group_size, int32_t n_q,

@@ -107,10 +107,20 @@ PyObject* guarded(F&& f) {
   }
 }
 
-template <int kStreams, class R, class... A, std::size_t... I>
+// Refuses a tensor that a kernel on the current device should not be handed.
+void check_device(PyObject* o) {
+  if (!THPVariable_Check(o)) return;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.is_cuda() && t.get_device() == c10::hip::current_device()) return;
+  PyErr_SetString(PyExc_ValueError, "libLouisKV needs tensors on the current device");
+  throw PyError();
+}
+
+template <int kStreams, bool kDeviceOnly, class R, class... A, std::size_t... I>
 PyObject* call(R (*fn)(A...), PyObject* const* args, std::index_sequence<I...>) {
   constexpr std::size_t n = sizeof...(A);
   std::tuple<A...> a{convert<A>(args[I], I + kStreams >= n)...};   // braces: converted in order
+  if constexpr (kDeviceOnly) (check_device(args[I]), ...);
   R r;
   Py_BEGIN_ALLOW_THREADS
   r = fn(std::get<I>(a)...);
@@ -125,13 +135,13 @@ constexpr std::size_t arity(R (*)(A...)) { return sizeof...(A); }
 template <class R, class... A>
 std::index_sequence_for<A...> indices(R (*)(A...)) { return {}; }
 
-template <auto kFn, int kStreams>
+template <auto kFn, int kStreams, bool kDeviceOnly = false>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != (Py_ssize_t)arity(kFn)) {
     PyErr_Format(PyExc_TypeError, "takes %zu arguments, got %zd", arity(kFn), n);
     return nullptr;
   }
-  return guarded([&] { return call<kStreams>(kFn, args, decltype(indices(kFn)){}); });
+  return guarded([&] { return call<kStreams, kDeviceOnly>(kFn, args, decltype(indices(kFn)){}); });
 }
 
 // (evicted segment, segments evicted, live tokens, ring slot of the oldest), or the status
@@ -151,6 +161,10 @@ PyObject* window_info(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define LKV_ENTRY(name, streams) \
   {#name, reinterpret_cast<PyCFunction>(&entry<&louiskv_##name, streams>), METH_FASTCALL, nullptr}
+
+// a call of which every tensor is in device memory
+#define LKV_DEVICE_ENTRY(name) \
+  {#name, reinterpret_cast<PyCFunction>(&entry<&louiskv_##name, 1, true>), METH_FASTCALL, nullptr}
 
 PyMethodDef methods[] = {
     {"window_info", reinterpret_cast<PyCFunction>(&window_info), METH_FASTCALL, nullptr},
@@ -194,17 +208,17 @@ PyMethodDef methods[] = {
     LKV_ENTRY(page_prefill, 1),
     LKV_ENTRY(retrieve_rows_per_head, 1),
     LKV_ENTRY(sparse_decode_attn_rows_per_head, 1),
-    LKV_ENTRY(pack_pool_q4, 1),
-    LKV_ENTRY(gather_rows_q4, 1),
-    LKV_ENTRY(segment_output_q4, 1),
-    LKV_ENTRY(segment_output_boundary_q4, 1),
+    LKV_DEVICE_ENTRY(pack_pool_q4),
+    LKV_DEVICE_ENTRY(gather_rows_q4),
+    LKV_DEVICE_ENTRY(segment_output_q4),
+    LKV_DEVICE_ENTRY(segment_output_boundary_q4),
     LKV_ENTRY(sparse_decode_attn_rows_q4_workspace_size, 0),
-    LKV_ENTRY(sparse_decode_attn_rows_q4, 1),
-    LKV_ENTRY(sparse_decode_attn_rows_q4_seg, 1),
+    LKV_DEVICE_ENTRY(sparse_decode_attn_rows_q4),
+    LKV_DEVICE_ENTRY(sparse_decode_attn_rows_q4_seg),
     LKV_ENTRY(retrieve_blocks_cap, 0),
-    LKV_ENTRY(retrieve_blocks, 1),
+    LKV_DEVICE_ENTRY(retrieve_blocks),
     LKV_ENTRY(sparse_prefill_attn_workspace_size, 0),
-    LKV_ENTRY(sparse_prefill_attn, 1),
+    LKV_DEVICE_ENTRY(sparse_prefill_attn),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -10,6 +10,7 @@ namespace {
 
 constexpr int kMaxBlocks = 8192;    // key blocks a tile's selection ranks
 constexpr int kMaxTile = 128;       // queries of a tile
+constexpr int kMaxKeys = 1 << 30;   // of a sequence, and of a list
 
 // ------------------------------------------------------------------ selection
 
@@ -751,9 +752,10 @@ int check_sizes(int64_t n_slices, int32_t n_kv_heads, int32_t n_q, int32_t d, in
   if (q_block < 1 || q_block > kMaxTile || log2_block(block_len) < 0)
     return fail(LOUISKV_ERR_UNSUPPORTED, "q_block=%d must be in [1, %d], block_len=%d one of 16, 32, 64, 128, 256",
                 q_block, kMaxTile, block_len);
+  if (n_keys > kMaxKeys) return fail(LOUISKV_ERR_SHAPE, "n_keys=%d exceeds %d", n_keys, kMaxKeys);
   if (n_q < 1 || n_keys < 1 || q_start < 0 || (int64_t)q_start + n_q > n_keys)
     return fail(LOUISKV_ERR_SHAPE, "queries q_start=%d .. +%d must be among the n_keys=%d tokens", q_start, n_q, n_keys);
-  if (n_slices * (((int64_t)n_q + q_block - 1) / q_block) > INT32_MAX)
+  if (n_slices > kMaxGrid || n_slices * (((int64_t)n_q + q_block - 1) / q_block) > kMaxGrid)
     return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   return LOUISKV_OK;
 }
@@ -784,6 +786,7 @@ extern "C" int louiskv_retrieve_blocks(const void* q, int32_t dtype, int64_t n_s
   if (st) return st;
   if ((st = check_sizes(n_slices, n_kv_heads, n_q, d, n_keys, q_start, q_block, block_len))) return st;
   if (group_size < 1 || group_size > 8) return fail(LOUISKV_ERR_UNSUPPORTED, "group_size=%d must be 1 to 8", group_size);
+  if (!aligned16(q, reps)) return fail(LOUISKV_ERR_UNSUPPORTED, "q and reps must be 16-byte aligned");
   if (n_first < 0 || n_recent < 0 || n_top < 0)
     return fail(LOUISKV_ERR_SHAPE, "n_first=%d n_recent=%d n_top=%d", n_first, n_recent, n_top);
   const int blocks = (int)(((int64_t)n_keys + block_len - 1) / block_len);
@@ -830,7 +833,9 @@ extern "C" int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t
   if ((st = check_sizes(n_slices, n_kv_heads, n_q, d, n_keys, q_start, q_block, block_len))) return st;
   if (group_size != 1 && group_size != 2 && group_size != 4 && group_size != 8)
     return fail(LOUISKV_ERR_UNSUPPORTED, "group_size=%d must be 1, 2, 4 or 8", group_size);
-  if (key_rows < n_keys || sel_cap < 1)
+  if (!aligned16(q, keys, values, out))
+    return fail(LOUISKV_ERR_UNSUPPORTED, "q, keys, values and out must be 16-byte aligned");
+  if (key_rows < n_keys || sel_cap < 1 || (int64_t)sel_cap * block_len > kMaxKeys)
     return fail(LOUISKV_ERR_SHAPE, "key_rows=%lld n_keys=%d sel_cap=%d", (long long)key_rows, n_keys, sel_cap);
   PrefillArgs a;
   a.q = q; a.group_size = group_size; a.n_q = n_q; a.scale = scale; a.keys = keys; a.values = values;
@@ -838,17 +843,16 @@ extern "C" int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t
   a.sel = sel_blocks; a.sel_cap = sel_cap; a.n_sel = n_sel_blocks; a.n_tiles = (n_q - 1) / q_block + 1; a.n_split = 1;
   a.part = nullptr; a.out = out; a.out_bf16 = out_dtype == LOUISKV_BF16; a.lse_out = lse_out;
   const int64_t n_rows = n_slices * group_size * n_q;
-  if ((n_rows + 15) / 16 > INT32_MAX) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   const int rows = std::min(q_block, n_q) * group_size, per = block_rows(rows), row_groups = (rows + per - 1) / per;
   const int n_split = prefill_splits(n_slices, group_size, n_q, q_block, block_len, sel_cap);
   const size_t need = part_bytes(n_rows, n_split);
-  if (need > 0 && (!workspace || workspace_bytes < need))
-    return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, workspace_bytes);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+    return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, 16-byte aligned, got %zu", need, workspace_bytes);
   hipStream_t hs = as_stream(stream);
   a.n_split = n_split;
   a.part = static_cast<float*>(workspace);
   const int64_t n_blocks = n_slices * a.n_tiles * row_groups * n_split;
-  if (n_blocks > INT32_MAX) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
+  if (n_blocks > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   if (dtype == LOUISKV_BF16) {
     switch (per) {
       case 256: launch_prefill<uint16_t, 8, 1>(a, row_groups, n_blocks, hs); break;

@@ -8,6 +8,13 @@ namespace louiskv {
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2E = 1.4426950408889634f;
 
+// Blocks of up to 512 threads that one launch can hold: 2^32 - 1 threads.
+constexpr int64_t kMaxGrid = (1 << 23) - 1;
+
+// Whether kernels may read (or write) these in 16-byte pieces.
+template <class... P>
+bool aligned16(const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 15) == 0; }
+
 // A partial: the maximum of its base-2 logits (-inf: no key), the sum of
 // 2^(logit - max) and the weighted sum of the value rows.  Partials of row r are
 // part[r][0..n_parts-1].
@@ -27,8 +34,8 @@ __device__ __forceinline__ float inv_sum(float l) { return l == 0.f ? 0.f : 1.f 
 __device__ __forceinline__ float lse_of(float m, float l) { return kLn2 * (max_base(m) + log2f(l)); }
 
 // One wave per row; lane k holds dims 2k, 2k + 1.  Lane c loads the maximum and sum
-// of part c; a batch of parts' weighted sums is on its way meanwhile (17 parts,
-// four loads at a time: 4.2 us).
+// of part c; a batch of parts' weighted sums is on its way meanwhile (32 rows of 17
+// parts: 3.6 us, most of it the trips to memory; four loads at a time, 4.2).
 constexpr int kMergeParts = 16;
 template <class TO>
 __global__ __launch_bounds__(256)

@@ -283,7 +283,6 @@ void store_q4_kernel(const T* __restrict__ k_new, const T* __restrict__ v_new, T
 
 struct AttnQ4 {
   const void* q;
-  int n_kv_heads;
   float scale;
   const uint8_t* codes;
   const uint8_t* scales;
@@ -785,6 +784,7 @@ int attn_q4(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads, 
   int st = check_dtype(dtype);
   if (st || (st = check_dtype(out_dtype))) return st;
   if (d != kHeadDim) return fail(LOUISKV_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", d);
+  if (!aligned16(q, k_local, v_local)) return fail(LOUISKV_ERR_UNSUPPORTED, "q, k_local and v_local must be 16-byte aligned");
   if (n_kv_heads < 1 || n_slices < 1 || n_slices % n_kv_heads != 0)
     return fail(LOUISKV_ERR_SHAPE, "n_slices=%lld must be a positive multiple of n_kv_heads=%d", (long long)n_slices,
                 n_kv_heads);
@@ -795,13 +795,13 @@ int attn_q4(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads, 
     return fail(LOUISKV_ERR_SHAPE, "budget=%d window=%d local_start=%d n_local=%d", budget, window, local_start, n_local);
   if (budget > 0 && (st = check_pool(codes, scales, pool_rows))) return st;
   const int n_chunks = attn_q4_chunks(n_slices, budget, window);
-  if (n_slices * n_chunks > INT32_MAX || n_slices * group_size > INT32_MAX)
+  if (n_slices > kMaxGrid || (int64_t)budget + window > LOUISKV_Q4_MAX_POOL_ROWS * 2)
     return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   const size_t need = part_bytes(n_slices * group_size, n_chunks);
-  if (need > 0 && (!workspace || workspace_bytes < need))
-    return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, workspace_bytes);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+    return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, 16-byte aligned, got %zu", need, workspace_bytes);
   AttnQ4 a;
-  a.q = q; a.n_kv_heads = n_kv_heads; a.scale = scale; a.codes = codes; a.scales = scales; a.pool_rows = pool_rows;
+  a.q = q; a.scale = scale; a.codes = codes; a.scales = scales; a.pool_rows = pool_rows;
   a.rows = sel_rows; a.n_sel = n_sel; a.budget = budget; a.k_local = k_local; a.v_local = v_local;
   a.window = std::max(window, 1); a.local_start = window > 0 ? local_start : 0; a.n_local = n_local;
   a.seg_state = seg_state; a.n_tokens = n_tokens; a.n_chunks = n_chunks; a.part = static_cast<float*>(workspace);
@@ -826,6 +826,7 @@ extern "C" int louiskv_pack_pool_q4(const void* keys, const void* values, int32_
   int st = check_dtype(dtype);
   if (st) return st;
   if (d != kHeadDim) return fail(LOUISKV_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", d);
+  if (!aligned16(keys, values)) return fail(LOUISKV_ERR_UNSUPPORTED, "keys and values must be 16-byte aligned");
   if (n_slices < 1 || n_slices > INT32_MAX || n_tokens < 1)
     return fail(LOUISKV_ERR_SHAPE, "n_slices=%lld n_tokens=%d", (long long)n_slices, n_tokens);
   if ((st = check_pool(codes, scales, pool_rows))) return st;
@@ -852,6 +853,7 @@ extern "C" int louiskv_gather_rows_q4(const uint8_t* codes, const uint8_t* scale
   int st = check_dtype(dtype);
   if (st) return st;
   if (d != kHeadDim) return fail(LOUISKV_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", d);
+  if (!aligned16(k_buf, v_buf)) return fail(LOUISKV_ERR_UNSUPPORTED, "k_buf and v_buf must be 16-byte aligned");
   if (n_slices < 1 || n_slices > INT32_MAX || buf_rows < 1)
     return fail(LOUISKV_ERR_SHAPE, "n_slices=%lld buf_rows=%d", (long long)n_slices, buf_rows);
   if ((st = check_pool(codes, scales, pool_rows))) return st;
@@ -881,7 +883,9 @@ extern "C" int louiskv_segment_output_q4(const void* k_new, const void* v_new, i
   int st = check_dtype(dtype);
   if (st) return st;
   if (d != kHeadDim) return fail(LOUISKV_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", d);
-  if (n_slices < 1 || n_slices > INT32_MAX) return fail(LOUISKV_ERR_SHAPE, "n_slices=%lld", (long long)n_slices);
+  if (!aligned16(k_new, v_new, k_local, v_local))
+    return fail(LOUISKV_ERR_UNSUPPORTED, "k_new, v_new, k_local and v_local must be 16-byte aligned");
+  if (n_slices < 1 || n_slices > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "n_slices=%lld", (long long)n_slices);
   if (codes && (st = check_pool(codes, scales, pool_rows))) return st;
   int32_t ev = -1;
   if ((st = louiskv_window_info(step, window, seg_len, &ev, nullptr, nullptr, nullptr))) return st;
@@ -911,7 +915,9 @@ extern "C" int louiskv_segment_output_boundary_q4(const void* k_new, const void*
   int st = check_dtype(dtype);
   if (st) return st;
   if (d != kHeadDim) return fail(LOUISKV_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", d);
-  if (n_kv_heads < 1 || n_slices < 1 || n_slices % n_kv_heads != 0 || n_slices > INT32_MAX)
+  if (!aligned16(k_new, v_new, k_local, v_local))
+    return fail(LOUISKV_ERR_UNSUPPORTED, "k_new, v_new, k_local and v_local must be 16-byte aligned");
+  if (n_kv_heads < 1 || n_slices < 1 || n_slices % n_kv_heads != 0 || n_slices > kMaxGrid)
     return fail(LOUISKV_ERR_SHAPE, "n_slices=%lld must be a positive multiple of n_kv_heads=%d", (long long)n_slices,
                 n_kv_heads);
   if (window < 2 || seg_max < 1 || seg_max >= window)

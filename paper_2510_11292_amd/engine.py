@@ -388,7 +388,8 @@ class LouisKVEngine:
         n_blocks = -(-n // block_len)
         cap = L.retrieve_blocks_cap(n, q_block, block_len, n_first, n_recent, n_top)
         if cap < 1:
-            raise ValueError(f"block_len={block_len} q_block={q_block} n_first={n_first} n_recent={n_recent} n_top={n_top}")
+            raise ValueError(f"block_len={block_len} q_block={q_block} n_first={n_first} n_recent={n_recent} "
+                             f"n_top={n_top}")
         reps = torch.empty(s, n_blocks, d, dtype=torch.float32, device=q.device)
         spans = torch.empty(2, s, n_blocks, **i32)
         L.page_prefill(keys, block_len, reps, spans[0], spans[1])
@@ -400,9 +401,9 @@ class LouisKVEngine:
         return out
 
     # ------------------------------------------------------- layer by layer
-    _PER_SLICE = ("reps", "unit_start", "unit_size", "assign", "perm", "k_pool", "v_pool", "codes", "scales", "k_local", "v_local",
-                  "sel_rows", "sel_rows_step", "k_buf", "v_buf", "buf_row", "slot_step", "slot_list",
-                  "n_fetched", "sel_units", "n_sel_units", "n_sel", "scores", "seg_state")
+    _PER_SLICE = ("reps", "unit_start", "unit_size", "assign", "perm", "k_pool", "v_pool", "codes", "scales",
+                  "k_local", "v_local", "sel_rows", "sel_rows_step", "k_buf", "v_buf", "buf_row", "slot_step",
+                  "slot_list", "n_fetched", "sel_units", "n_sel_units", "n_sel", "scores", "seg_state")
     _PER_GROUP = ("q_ref", "fire", "r", "out", "lse")
 
     def group_view(self, g: int, n: int = 1) -> "LouisKVEngine":

@@ -696,11 +696,38 @@ def pack_pool(keys, values, perm, k_pool, v_pool=None, pool_on_host: bool = Fals
 Q4_MAX_POOL_ROWS = 1 << 24
 
 
-def _ws_bytes(workspace: Optional[torch.Tensor], device, size: int):
-    """The workspace and its bytes; one of `size` where none is given, none where none is needed."""
+def _one_dtype(first, *more) -> int:
+    """The dtype code that tensors of one element type share."""
+    for t in more:
+        if t.dtype is not first.dtype:
+            raise TypeError(f"tensors of one call differ in dtype: {first.dtype}, {t.dtype}")
+    return _dtype_code(first)
+
+
+def _ws_bytes(workspace: Optional[torch.Tensor], device, size: int, stream):
+    """The workspace and its bytes; one of `size` where none is given, none where none is needed.  It is memory of
+    the stream that the call runs on: the caller's own work may take it over only behind that."""
     if workspace is not None:
         return workspace, workspace.nbytes
-    return (torch.empty(size, dtype=torch.uint8, device=device), size) if size else (None, 0)
+    if not size:
+        return None, 0
+    if stream is None:
+        return torch.empty(size, dtype=torch.uint8, device=device), size
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        return torch.empty(size, dtype=torch.uint8, device=device), size
+
+
+def _sizes(**tensors) -> None:
+    """Raises unless every (tensor, shape) has that shape; None tensors are not given."""
+    for name, (t, shape) in tensors.items():
+        if t is not None and t.shape != shape:
+            raise ValueError(f"{name} {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def _int32(*tensors) -> None:
+    for t in tensors:
+        if t is not None and t.dtype is not torch.int32:
+            raise TypeError(f"lists and tables are int32, got {t.dtype}")
 
 
 def _pool_q4(codes, scales, n_slices: int) -> int:
@@ -717,6 +744,8 @@ def pack_pool_q4(keys, values, perm, codes, scales, stream=None):
     """Prompt K/V rows quantised into a 4-bit pool in perm order (perm None: token order)."""
     s, n, d = keys.shape
     rows = _pool_q4(codes, scales, s)
+    _sizes(values=(values, (s, n, d)), perm=(perm, (s, n)))
+    _int32(perm)
     _check(_native().pack_pool_q4(keys, values, _one_dtype(keys, values), s, n, d, perm, codes, scales, rows, stream))
 
 
@@ -725,8 +754,17 @@ def gather_rows_q4(codes, scales, sel_rows, n_sel, k_buf, v_buf, stream=None):
     them (None: all), into k_buf and v_buf [S][n][d]."""
     s, n, d = k_buf.shape
     rows = _pool_q4(codes, scales, s)
+    _sizes(v_buf=(v_buf, (s, n, d)), sel_rows=(sel_rows, (s, n)), n_sel=(n_sel, (s,)))
+    _int32(sel_rows, n_sel)
     _check(_native().gather_rows_q4(codes, scales, s, rows, d, sel_rows, n_sel, n, k_buf, v_buf,
                                     _one_dtype(k_buf, v_buf), stream))
+
+
+def _store_sizes(s: int, d: int, v_new, k_local, v_local, reps, unit_start, unit_size) -> None:
+    local, units = (s, k_local.shape[1], d), (s, reps.shape[1])
+    _sizes(v_new=(v_new, (s, d)), k_local=(k_local, local), v_local=(v_local, local), reps=(reps, units + (d,)),
+           unit_start=(unit_start, units), unit_size=(unit_size, units))
+    _int32(unit_start, unit_size)
 
 
 def segment_output_q4(k_new, v_new, k_local, v_local, step: int, seg_len: int, reps, unit_start, unit_size,
@@ -734,6 +772,7 @@ def segment_output_q4(k_new, v_new, k_local, v_local, step: int, seg_len: int, r
     """segment_output with the evicted rows quantised into a 4-bit pool."""
     s, d = k_new.shape
     rows = _pool_q4(codes, scales, s) if codes is not None else 0
+    _store_sizes(s, d, v_new, k_local, v_local, reps, unit_start, unit_size)
     _check(_native().segment_output_q4(
         k_new, v_new, _one_dtype(k_new, v_new, k_local, v_local), s, d, k_local, v_local, k_local.shape[1],
         step, seg_len, reps, unit_start, unit_size, reps.shape[1], n_clusters,
@@ -746,6 +785,8 @@ def segment_output_boundary_q4(k_new, v_new, k_local, v_local, step: int, seg_ma
     """segment_output_boundary with the evicted rows quantised into a 4-bit pool."""
     s, d = k_new.shape
     rows = _pool_q4(codes, scales, s) if codes is not None else 0
+    _store_sizes(s, d, v_new, k_local, v_local, reps, unit_start, unit_size)
+    _int32(seg_state)
     _check(_native().segment_output_boundary_q4(
         k_new, v_new, _one_dtype(k_new, v_new, k_local, v_local), s, n_kv_heads, d, k_local, v_local,
         k_local.shape[1], step, seg_max, fire, seg_state, reps, unit_start,
@@ -756,23 +797,38 @@ def sparse_decode_attn_rows_q4_workspace_size(n_slices, group_size, budget, wind
     return _native().sparse_decode_attn_rows_q4_workspace_size(n_slices, group_size, d, budget, window)
 
 
+def _groups(hq: int, n_kv_heads: int) -> int:
+    """Query heads that share a KV head."""
+    if hq % n_kv_heads:
+        raise ValueError(f"{hq} query heads are not a multiple of {n_kv_heads} KV heads")
+    return hq // n_kv_heads
+
+
+def _rows_sizes(s: int, q, out, lse_out, sel_rows, n_sel, k_local, v_local) -> None:
+    local = (s, k_local.shape[1], q.shape[2])
+    _sizes(out=(out, q.shape), lse_out=(lse_out, q.shape[:2]), sel_rows=(sel_rows, (s, sel_rows.shape[-1])),
+           n_sel=(n_sel, (s,)), k_local=(k_local, local), v_local=(v_local, local))
+    _int32(sel_rows, n_sel)
+
+
 def sparse_decode_attn_rows_q4(q, n_kv_heads: int, codes, scales, sel_rows, n_sel, k_local, v_local,
                                local_start: int, n_local: int, out, lse_out=None, scale: Optional[float] = None,
                                workspace=None, stream=None):
     """sparse_decode_attn_rows over a 4-bit pool."""
     g, hq, d = q.shape
-    s = n_sel.shape[0]
-    gs = hq // n_kv_heads
+    s = g * n_kv_heads
+    gs = _groups(hq, n_kv_heads)
+    _rows_sizes(s, q, out, lse_out, sel_rows, n_sel, k_local, v_local)
     budget = sel_rows.shape[1]
     window = k_local.shape[1]
     rows = _pool_q4(codes, scales, s)
     lib = _native()
     ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else
-                        lib.sparse_decode_attn_rows_q4_workspace_size(s, gs, d, budget, window))
+                        lib.sparse_decode_attn_rows_q4_workspace_size(s, gs, d, budget, window), stream)
     sc = (1.0 / d ** 0.5) if scale is None else scale
     _check(lib.sparse_decode_attn_rows_q4(
-        q, _one_dtype(q, k_local, v_local), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel, budget,
-        k_local, v_local, window, local_start, n_local, out, _dtype_code(out), lse_out, ws, wsb, stream))
+        q, _one_dtype(q, k_local, v_local), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel,
+        budget, k_local, v_local, window, local_start, n_local, out, _dtype_code(out), lse_out, ws, wsb, stream))
 
 
 def sparse_decode_attn_rows_q4_seg(q, n_kv_heads: int, codes, scales, sel_rows, n_sel, k_local, v_local, seg_state,
@@ -780,18 +836,19 @@ def sparse_decode_attn_rows_q4_seg(q, n_kv_heads: int, codes, scales, sel_rows, 
                                    stream=None):
     """sparse_decode_attn_rows_seg over a 4-bit pool."""
     g, hq, d = q.shape
-    s = n_sel.shape[0]
-    gs = hq // n_kv_heads
+    s = g * n_kv_heads
+    gs = _groups(hq, n_kv_heads)
+    _rows_sizes(s, q, out, lse_out, sel_rows, n_sel, k_local, v_local)
     budget = sel_rows.shape[1]
     window = k_local.shape[1]
     rows = _pool_q4(codes, scales, s)
     lib = _native()
     ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else
-                        lib.sparse_decode_attn_rows_q4_workspace_size(s, gs, d, budget, window))
+                        lib.sparse_decode_attn_rows_q4_workspace_size(s, gs, d, budget, window), stream)
     sc = (1.0 / d ** 0.5) if scale is None else scale
     _check(lib.sparse_decode_attn_rows_q4_seg(
-        q, _one_dtype(q, k_local, v_local), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel, budget,
-        k_local, v_local, window, seg_state, n_tokens, out, _dtype_code(out), lse_out, ws, wsb, stream))
+        q, _one_dtype(q, k_local, v_local), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel,
+        budget, k_local, v_local, window, seg_state, n_tokens, out, _dtype_code(out), lse_out, ws, wsb, stream))
 
 
 # ---------------------------------------------------------------- the prompt's attention over selected blocks
@@ -809,14 +866,6 @@ def _lists(sel_blocks, n_sel_blocks, s: int, n_q: int, q_block: int) -> None:
                          f"{n_sel_blocks.dtype} are not int32 lists of {s} slices' {b[1]} tiles")
 
 
-def _one_dtype(first, *more) -> int:
-    """The dtype code that tensors of one element type share."""
-    for t in more:
-        if t.dtype is not first.dtype:
-            raise TypeError(f"tensors of one call differ in dtype: {first.dtype}, {t.dtype}")
-    return _dtype_code(first)
-
-
 def retrieve_blocks(q, n_kv_heads: int, reps, n_keys: int, q_start: int, q_block: int, block_len: int, n_first: int,
                     n_recent: int, n_top: int, sel_blocks, n_sel_blocks, stream=None):
     """The key blocks that every tile of q_block queries attends to: q [G][Hq][n_q][d], reps [S][blocks..][d] (the
@@ -824,8 +873,9 @@ def retrieve_blocks(q, n_kv_heads: int, reps, n_keys: int, q_start: int, q_block
     g, hq, n_q, d = q.shape
     s = g * n_kv_heads
     _lists(sel_blocks, n_sel_blocks, s, n_q, q_block)
+    _sizes(reps=(reps, (s, reps.shape[1], d)))
     _check(_native().retrieve_blocks(
-        q, _dtype_code(q), s, n_kv_heads, hq // n_kv_heads, n_q, d, reps, reps.shape[1], n_keys, q_start, q_block,
+        q, _dtype_code(q), s, n_kv_heads, _groups(hq, n_kv_heads), n_q, d, reps, reps.shape[1], n_keys, q_start, q_block,
         block_len, n_first, n_recent, n_top, sel_blocks, sel_blocks.shape[2], n_sel_blocks, stream))
 
 
@@ -840,16 +890,15 @@ def sparse_prefill_attn(q, n_kv_heads: int, keys, values, n_keys: int, q_start: 
     values [S][rows >= n_keys][d], the lists as retrieve_blocks writes them."""
     g, hq, n_q, d = q.shape
     s = g * n_kv_heads
-    gs = hq // n_kv_heads
+    gs = _groups(hq, n_kv_heads)
     _lists(sel_blocks, n_sel_blocks, s, n_q, q_block)
-    if keys.shape != values.shape or keys.shape[0] != s or out.shape != q.shape:
-        raise ValueError(f"keys {tuple(keys.shape)}, values {tuple(values.shape)} of {s} slices, out {tuple(out.shape)} "
-                         f"as q {tuple(q.shape)} expected")
+    kv = (s, keys.shape[1], d)
+    _sizes(keys=(keys, kv), values=(values, kv), out=(out, q.shape), lse_out=(lse_out, q.shape[:3]))
     cap = sel_blocks.shape[2]
     lib = _native()
     ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else
-                        lib.sparse_prefill_attn_workspace_size(s, gs, n_q, d, q_block, block_len, cap))
+                        lib.sparse_prefill_attn_workspace_size(s, gs, n_q, d, q_block, block_len, cap), stream)
     sc = (1.0 / d ** 0.5) if scale is None else scale
     _check(lib.sparse_prefill_attn(
-        q, _one_dtype(q, keys, values), s, n_kv_heads, gs, n_q, d, float(sc), keys, values, keys.shape[1], n_keys, q_start,
-        q_block, block_len, sel_blocks, cap, n_sel_blocks, out, _dtype_code(out), lse_out, ws, wsb, stream))
+        q, _one_dtype(q, keys, values), s, n_kv_heads, gs, n_q, d, float(sc), keys, values, keys.shape[1], n_keys,
+        q_start, q_block, block_len, sel_blocks, cap, n_sel_blocks, out, _dtype_code(out), lse_out, ws, wsb, stream))

@@ -356,3 +356,34 @@ def test_two_streams_and_a_replayed_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(eager[n], cap[n]) for n in eager), i
+
+
+def test_a_workspace_of_the_call_is_memory_of_its_stream():
+    """Without a workspace the call takes one that the caller's stream does not reuse while it runs."""
+    l, size = L(), 3 << 20
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        ws, n = l._ws_bytes(None, DEV, size, stream)
+        at = ws.data_ptr()
+        assert n == size and torch.cuda.current_stream() != side
+        del ws
+        other = torch.empty(size, dtype=torch.uint8, device=DEV)
+        assert other.data_ptr() != at
+        del other
+    rng = np.random.default_rng(12)
+    s, g, budget = 2, 4, 700
+    codes, scales = (x.to(DEV) for x in pool_of(rng, s, 800))
+    sel = torch.from_numpy(rng.integers(0, 800, (s, budget)).astype(np.int32)).to(DEV)
+    n_sel = torch.full((s,), budget, dtype=torch.int32, device=DEV)
+    q = torch.randn(1, s * g, 128, device=DEV).bfloat16()
+    loc = torch.randn(s, 16, 128, device=DEV).bfloat16()
+    assert l.sparse_decode_attn_rows_q4_workspace_size(s, g, budget, 16) > 0
+    outs = [torch.zeros_like(q) for _ in range(3)]
+    torch.cuda.synchronize()
+    for out, stream in zip(outs, (None, side, side.cuda_stream)):
+        l.sparse_decode_attn_rows_q4(q, s, codes, scales, sel, n_sel, loc, loc, 0, 16, out, stream=stream)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    with pytest.raises(l.LouisKVError, match="aligned"):     # a view that starts in the middle of 16 bytes
+        odd = torch.zeros(s * g * 128 + 4, device=DEV, dtype=torch.bfloat16)[4:].view(1, s * g, 128)
+        l.sparse_decode_attn_rows_q4(odd, s, codes, scales, sel, n_sel, loc, loc, 0, 16, outs[0])

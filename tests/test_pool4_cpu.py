@@ -199,6 +199,90 @@ def test_python_calls_check_shapes():
         L.pack_pool_q4(k, k, None, c, torch.zeros(2, 10, 8, dtype=torch.uint8))
 
 
+def test_unaligned_buffers_and_sizes_behind_the_index_range_are_refused(lib):
+    odd, ws = P(4104), 1 << 20
+    base = [D16, D16, 1, 2, 64, 128, None, D16, D16, 64, None]
+    _statuses(lib.louiskv_pack_pool_q4, base, [({0: odd}, UNSUPPORTED), ({1: odd}, UNSUPPORTED)])
+    base = [D16, D16, 2, 64, 128, None, None, 64, D16, D16, 1, None]
+    _statuses(lib.louiskv_gather_rows_q4, base, [({8: odd}, UNSUPPORTED), ({9: odd}, UNSUPPORTED)])
+    base = [D16, D16, 1, 8, 128, D16, D16, 64, 64, 32, D16, D16, D16, 10, 9, D16, D16, 132, 100, None]
+    _statuses(lib.louiskv_segment_output_q4, base,
+              [({i: odd}, UNSUPPORTED) for i in (0, 1, 5, 6)] + [({3: 1 << 23}, SHAPE)])
+    base = [D16, D16, 1, 8, 8, 128, D16, D16, 64, 0, 16, None, D16, D16, D16, D16, 20, 10, D16, D16, 200, 100, None]
+    _statuses(lib.louiskv_segment_output_boundary_q4, base,
+              [({i: odd}, UNSUPPORTED) for i in (0, 1, 6, 7)] + [({3: 1 << 23}, SHAPE)])
+    base = [D16, 1, 8, 8, 4, 128, 0.1, D16, D16, 4096, D16, D16, 2048, D16, D16, 128, 0, 128, D16, 1, None, D16, ws, None]
+    _statuses(lib.louiskv_sparse_decode_attn_rows_q4, base,
+              [({i: odd}, UNSUPPORTED) for i in (0, 13, 14)] + [({21: odd}, WORKSPACE), ({3: 1 << 23}, SHAPE),
+                                                                ({12: 1 << 25}, SHAPE), ({15: (1 << 31) - 1}, SHAPE)])
+    base = [D16, 1, 8, 8, 4, 500, 128, D16, 32, 2000, 1500, 64, 64, 1, 2, 4, D16, 9, D16, None]
+    _statuses(lib.louiskv_retrieve_blocks, base, [
+        ({0: odd}, UNSUPPORTED), ({7: odd}, UNSUPPORTED), ({9: (1 << 30) + 1}, SHAPE), ({2: 1 << 20}, SHAPE)])
+    size = lib.louiskv_sparse_prefill_attn_workspace_size(8, 4, 64, 128, 64, 64, 9)
+    assert size > 0
+    base = [D16, 1, 8, 8, 4, 64, 128, 0.1, D16, D16, 2000, 2000, 1500, 64, 64, D16, 9, D16, D16, 1, None, D16, size, None]
+    _statuses(lib.louiskv_sparse_prefill_attn, base, [({i: odd}, UNSUPPORTED) for i in (0, 8, 9, 18)] + [
+        ({21: odd}, WORKSPACE), ({22: size - 1}, WORKSPACE), ({16: (1 << 24) + 1}, SHAPE),
+        ({10: 1 << 31, 11: (1 << 30) + 1}, SHAPE), ({2: 1 << 23}, SHAPE)])
+
+
+def test_python_calls_refuse_sizes_types_and_host_memory():
+    from paper_2510_11292_amd import louiskv as L
+    i32, u8 = dict(dtype=torch.int32), dict(dtype=torch.uint8)
+    k, loc = torch.zeros(2, 10, 128), torch.zeros(2, 4, 128)
+    pool = torch.zeros(2, 10, 128, **u8), torch.zeros(2, 10, 8, **u8)
+    perm, sel, n_sel = torch.zeros(2, 10, **i32), torch.zeros(2, 5, **i32), torch.zeros(2, **i32)
+    q, out, ws = torch.zeros(1, 4, 128), torch.zeros(1, 4, 128), torch.zeros(1 << 20, **u8)
+    new, reps, table = torch.zeros(2, 128), torch.zeros(2, 6, 128), torch.zeros(2, 6, **i32)
+
+    def pack(values=k, perm=perm):
+        L.pack_pool_q4(k, values, perm, *pool, stream=0)
+
+    def gather(sel=perm, n=n_sel, v=k):
+        L.gather_rows_q4(*pool, sel, n, k, v, stream=0)
+
+    def store(v_new=new, v_local=loc, start=table):
+        L.segment_output_q4(new, v_new, loc, v_local, 0, 2, reps, start, table, 3, *pool, stream=0)
+
+    def bound(state=torch.zeros(2, 12, **i32), size=table):
+        L.segment_output_boundary_q4(new, new, loc, loc, 0, 2, None, state, reps, table, size, 3, 2, stream=0)
+
+    def attn(q=q, out=out, lse=None, sel=sel, n=n_sel, loc=loc):
+        L.sparse_decode_attn_rows_q4(q, 2, *pool, sel, n, loc, loc, 0, 4, out, lse, workspace=ws, stream=0)
+
+    def seg(out=out, n=n_sel):
+        L.sparse_decode_attn_rows_q4_seg(q, 2, *pool, sel, n, loc, loc, torch.zeros(2, 12, **i32), 3, out, workspace=ws,
+                                         stream=0)
+    qp, lists = torch.zeros(1, 4, 7, 128), (torch.zeros(2, 1, 3, **i32), torch.zeros(2, 1, **i32))
+
+    def blocks(q=qp, reps=reps):
+        L.retrieve_blocks(q, 2, reps, 10, 3, 16, 16, 1, 1, 1, *lists, stream=0)
+
+    def prompt(q=qp, values=k, out=qp, lse=None):
+        L.sparse_prefill_attn(q, 2, k, values, 10, 3, 16, 16, *lists, out, lse, workspace=ws, stream=0)
+    for call, kw in ((pack, dict(values=k[:, :9])), (pack, dict(perm=perm[:1])), (gather, dict(sel=perm[:, :9])),
+                     (gather, dict(n=n_sel[:1])), (gather, dict(v=k[:, :9])), (store, dict(v_new=new[:1])),
+                     (store, dict(v_local=loc[:, :3])), (store, dict(start=table[:, :5])), (bound, dict(size=table[:1])),
+                     (attn, dict(out=out[:, :3])), (attn, dict(lse=out[..., 0][:, :3])), (attn, dict(sel=sel[:1])),
+                     (attn, dict(n=n_sel[:1])), (attn, dict(loc=loc[:1])), (seg, dict(n=n_sel[:1])),
+                     (blocks, dict(reps=reps[:1])), (prompt, dict(values=k[:, :9])), (prompt, dict(out=qp[:, :3])),
+                     (prompt, dict(lse=qp[..., :3, 0]))):
+        with pytest.raises(ValueError, match="expected"):
+            call(**kw)
+    for call, kw in ((pack, dict(perm=perm.long())), (gather, dict(sel=perm.long())), (gather, dict(n=n_sel.float())),
+                     (store, dict(start=table.long())), (bound, dict(state=torch.zeros(2, 12))),
+                     (attn, dict(sel=sel.long())), (seg, dict(n=n_sel.long()))):
+        with pytest.raises(TypeError, match="int32"):
+            call(**kw)
+    for call in (attn, blocks, prompt):
+        with pytest.raises(ValueError, match="multiple"):
+            call(**({"q": q[:, :3], "out": out[:, :3]} if call is attn else {"q": qp[:, :3].contiguous()}
+                    | ({"out": qp[:, :3]} if call is prompt else {})))
+    for call in (pack, gather, store, bound, attn, seg, blocks, prompt):   # every size is right: host memory is what is left
+        with pytest.raises(ValueError, match="current device"):
+            call()
+
+
 def test_engine_refuses_what_a_4_bit_pool_is_not_built_for():
     from paper_2510_11292_amd.engine import EngineConfig, LouisKVEngine
     cfg = EngineConfig(n_slices=2, n_kv_heads=2, n_q_heads=8, prompt_len=64, n_clusters=4, n_iters=1, gen_len=8,
