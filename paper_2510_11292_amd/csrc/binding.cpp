@@ -15,6 +15,7 @@
 //   numbers    int, bool or float
 // The status (or size) comes back as an int, text as a str; the GIL is released
 // for the call.
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <c10/hip/HIPStream.h>
 
@@ -159,6 +160,36 @@ PyObject* window_info(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// expect(name, tensor or None, shape, dtype or None, ...): raises at the first
+// tensor that is of another shape (ValueError) or element type (TypeError).
+PyObject* expect(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    for (Py_ssize_t i = 0; i + 4 <= n; i += 4) {
+      PyObject *o = args[i + 1], *shape = args[i + 2], *dtype = args[i + 3];
+      if (o == Py_None) continue;
+      if (!THPVariable_Check(o) || !PyTuple_Check(shape)) {
+        PyErr_Format(PyExc_TypeError, "%U: a tensor and the tuple of its sizes", args[i]);
+        throw PyError();
+      }
+      const at::Tensor& t = THPVariable_Unpack(o);
+      bool same = t.dim() == PyTuple_GET_SIZE(shape);
+      for (int64_t k = 0; same && k < t.dim(); ++k) same = t.size(k) == to_int(PyTuple_GET_ITEM(shape, k));
+      if (!same) {
+        PyObject* got = PyObject_GetAttrString(o, "shape");
+        if (!got) throw PyError();
+        PyErr_Format(PyExc_ValueError, "%U: %R, expected %R", args[i], got, shape);
+        Py_DECREF(got);
+        throw PyError();
+      }
+      if (dtype != Py_None && (!THPDtype_Check(dtype) || t.scalar_type() != reinterpret_cast<THPDtype*>(dtype)->scalar_type)) {
+        PyErr_Format(PyExc_TypeError, "%U and this call differ in dtype: %R expected", args[i], dtype);
+        throw PyError();
+      }
+    }
+    Py_RETURN_NONE;
+  });
+}
+
 #define LKV_ENTRY(name, streams) \
   {#name, reinterpret_cast<PyCFunction>(&entry<&louiskv_##name, streams>), METH_FASTCALL, nullptr}
 
@@ -167,6 +198,7 @@ PyObject* window_info(PyObject*, PyObject* const* args, Py_ssize_t n) {
   {#name, reinterpret_cast<PyCFunction>(&entry<&louiskv_##name, 1, true>), METH_FASTCALL, nullptr}
 
 PyMethodDef methods[] = {
+    {"expect", reinterpret_cast<PyCFunction>(&expect), METH_FASTCALL, nullptr},
     {"window_info", reinterpret_cast<PyCFunction>(&window_info), METH_FASTCALL, nullptr},
     LKV_ENTRY(abi_version, 0),
     LKV_ENTRY(status_str, 0),

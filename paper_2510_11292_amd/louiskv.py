@@ -696,14 +696,6 @@ def pack_pool(keys, values, perm, k_pool, v_pool=None, pool_on_host: bool = Fals
 Q4_MAX_POOL_ROWS = 1 << 24
 
 
-def _one_dtype(first, *more) -> int:
-    """The dtype code that tensors of one element type share."""
-    for t in more:
-        if t.dtype is not first.dtype:
-            raise TypeError(f"tensors of one call differ in dtype: {first.dtype}, {t.dtype}")
-    return _dtype_code(first)
-
-
 def _ws_bytes(workspace: Optional[torch.Tensor], device, size: int, stream):
     """The workspace and its bytes; one of `size` where none is given, none where none is needed.  It is memory of
     the stream that the call runs on: the caller's own work may take it over only behind that."""
@@ -717,26 +709,11 @@ def _ws_bytes(workspace: Optional[torch.Tensor], device, size: int, stream):
         return torch.empty(size, dtype=torch.uint8, device=device), size
 
 
-def _sizes(**tensors) -> None:
-    """Raises unless every (tensor, shape) has that shape; None tensors are not given."""
-    for name, (t, shape) in tensors.items():
-        if t is not None and t.shape != shape:
-            raise ValueError(f"{name} {tuple(t.shape)}, expected {tuple(shape)}")
-
-
-def _int32(*tensors) -> None:
-    for t in tensors:
-        if t is not None and t.dtype is not torch.int32:
-            raise TypeError(f"lists and tables are int32, got {t.dtype}")
-
-
 def _pool_q4(codes, scales, n_slices: int) -> int:
-    """Rows per slice of a 4-bit pool (codes [S][rows][128], scales [S][rows][8], uint8)."""
-    a, b = codes.shape, scales.shape
-    rows = a[1] if len(a) == 3 else -1
-    if a != (n_slices, rows, 128) or b != (n_slices, rows, 8) or not (codes.dtype is scales.dtype is torch.uint8):
-        raise ValueError(f"a 4-bit pool of {n_slices} slices is codes [{n_slices}][rows][128] and scales "
-                         f"[{n_slices}][rows][8], uint8: got {tuple(a)} {codes.dtype}, {tuple(b)} {scales.dtype}")
+    """Rows per slice of a 4-bit pool."""
+    rows = codes.shape[1]
+    _native().expect("codes of a 4-bit pool", codes, (n_slices, rows, 128), torch.uint8,
+                     "scales of a 4-bit pool", scales, (n_slices, rows, 8), torch.uint8)
     return rows
 
 
@@ -744,9 +721,9 @@ def pack_pool_q4(keys, values, perm, codes, scales, stream=None):
     """Prompt K/V rows quantised into a 4-bit pool in perm order (perm None: token order)."""
     s, n, d = keys.shape
     rows = _pool_q4(codes, scales, s)
-    _sizes(values=(values, (s, n, d)), perm=(perm, (s, n)))
-    _int32(perm)
-    _check(_native().pack_pool_q4(keys, values, _one_dtype(keys, values), s, n, d, perm, codes, scales, rows, stream))
+    lib = _native()
+    lib.expect("values", values, (s, n, d), keys.dtype, "perm", perm, (s, n), torch.int32)
+    _check(lib.pack_pool_q4(keys, values, _dtype_code(keys), s, n, d, perm, codes, scales, rows, stream))
 
 
 def gather_rows_q4(codes, scales, sel_rows, n_sel, k_buf, v_buf, stream=None):
@@ -754,17 +731,19 @@ def gather_rows_q4(codes, scales, sel_rows, n_sel, k_buf, v_buf, stream=None):
     them (None: all), into k_buf and v_buf [S][n][d]."""
     s, n, d = k_buf.shape
     rows = _pool_q4(codes, scales, s)
-    _sizes(v_buf=(v_buf, (s, n, d)), sel_rows=(sel_rows, (s, n)), n_sel=(n_sel, (s,)))
-    _int32(sel_rows, n_sel)
-    _check(_native().gather_rows_q4(codes, scales, s, rows, d, sel_rows, n_sel, n, k_buf, v_buf,
-                                    _one_dtype(k_buf, v_buf), stream))
+    lib = _native()
+    lib.expect("v_buf", v_buf, (s, n, d), k_buf.dtype, "sel_rows", sel_rows, (s, n), torch.int32,
+               "n_sel", n_sel, (s,), torch.int32)
+    _check(lib.gather_rows_q4(codes, scales, s, rows, d, sel_rows, n_sel, n, k_buf, v_buf, _dtype_code(k_buf),
+                              stream))
 
 
-def _store_sizes(s: int, d: int, v_new, k_local, v_local, reps, unit_start, unit_size) -> None:
-    local, units = (s, k_local.shape[1], d), (s, reps.shape[1])
-    _sizes(v_new=(v_new, (s, d)), k_local=(k_local, local), v_local=(v_local, local), reps=(reps, units + (d,)),
-           unit_start=(unit_start, units), unit_size=(unit_size, units))
-    _int32(unit_start, unit_size)
+def _store_sizes(k_new, v_new, k_local, v_local, window: int, reps, unit_start, unit_size, cap: int) -> None:
+    s, d = k_new.shape
+    t = k_new.dtype
+    _native().expect("v_new", v_new, (s, d), t, "k_local", k_local, (s, window, d), t,
+                     "v_local", v_local, (s, window, d), t, "reps", reps, (s, cap, d), torch.float32,
+                     "unit_start", unit_start, (s, cap), torch.int32, "unit_size", unit_size, (s, cap), torch.int32)
 
 
 def segment_output_q4(k_new, v_new, k_local, v_local, step: int, seg_len: int, reps, unit_start, unit_size,
@@ -772,11 +751,11 @@ def segment_output_q4(k_new, v_new, k_local, v_local, step: int, seg_len: int, r
     """segment_output with the evicted rows quantised into a 4-bit pool."""
     s, d = k_new.shape
     rows = _pool_q4(codes, scales, s) if codes is not None else 0
-    _store_sizes(s, d, v_new, k_local, v_local, reps, unit_start, unit_size)
+    window, cap = k_local.shape[1], reps.shape[1]
+    _store_sizes(k_new, v_new, k_local, v_local, window, reps, unit_start, unit_size, cap)
     _check(_native().segment_output_q4(
-        k_new, v_new, _one_dtype(k_new, v_new, k_local, v_local), s, d, k_local, v_local, k_local.shape[1],
-        step, seg_len, reps, unit_start, unit_size, reps.shape[1], n_clusters,
-        codes, scales, rows, prompt_len, stream))
+        k_new, v_new, _dtype_code(k_new), s, d, k_local, v_local, window, step, seg_len, reps, unit_start, unit_size,
+        cap, n_clusters, codes, scales, rows, prompt_len, stream))
 
 
 def segment_output_boundary_q4(k_new, v_new, k_local, v_local, step: int, seg_max: int, fire, seg_state, reps,
@@ -785,12 +764,12 @@ def segment_output_boundary_q4(k_new, v_new, k_local, v_local, step: int, seg_ma
     """segment_output_boundary with the evicted rows quantised into a 4-bit pool."""
     s, d = k_new.shape
     rows = _pool_q4(codes, scales, s) if codes is not None else 0
-    _store_sizes(s, d, v_new, k_local, v_local, reps, unit_start, unit_size)
-    _int32(seg_state)
+    window, cap = k_local.shape[1], reps.shape[1]
+    _store_sizes(k_new, v_new, k_local, v_local, window, reps, unit_start, unit_size, cap)
+    _native().expect("seg_state", seg_state, (s, segment_state_ints(window)), torch.int32)
     _check(_native().segment_output_boundary_q4(
-        k_new, v_new, _one_dtype(k_new, v_new, k_local, v_local), s, n_kv_heads, d, k_local, v_local,
-        k_local.shape[1], step, seg_max, fire, seg_state, reps, unit_start,
-        unit_size, reps.shape[1], n_clusters, codes, scales, rows, prompt_len, stream))
+        k_new, v_new, _dtype_code(k_new), s, n_kv_heads, d, k_local, v_local, window, step, seg_max, fire, seg_state,
+        reps, unit_start, unit_size, cap, n_clusters, codes, scales, rows, prompt_len, stream))
 
 
 def sparse_decode_attn_rows_q4_workspace_size(n_slices, group_size, budget, window, d=128) -> int:
@@ -804,11 +783,12 @@ def _groups(hq: int, n_kv_heads: int) -> int:
     return hq // n_kv_heads
 
 
-def _rows_sizes(s: int, q, out, lse_out, sel_rows, n_sel, k_local, v_local) -> None:
-    local = (s, k_local.shape[1], q.shape[2])
-    _sizes(out=(out, q.shape), lse_out=(lse_out, q.shape[:2]), sel_rows=(sel_rows, (s, sel_rows.shape[-1])),
-           n_sel=(n_sel, (s,)), k_local=(k_local, local), v_local=(v_local, local))
-    _int32(sel_rows, n_sel)
+def _rows_sizes(s: int, q, out, lse_out, sel_rows, n_sel, budget: int, k_local, v_local, window: int) -> None:
+    shape = g, hq, d = q.shape
+    t = q.dtype
+    _native().expect("out", out, shape, None, "lse_out", lse_out, (g, hq), torch.float32,
+                     "sel_rows", sel_rows, (s, budget), torch.int32, "n_sel", n_sel, (s,), torch.int32,
+                     "k_local", k_local, (s, window, d), t, "v_local", v_local, (s, window, d), t)
 
 
 def sparse_decode_attn_rows_q4(q, n_kv_heads: int, codes, scales, sel_rows, n_sel, k_local, v_local,
@@ -818,16 +798,15 @@ def sparse_decode_attn_rows_q4(q, n_kv_heads: int, codes, scales, sel_rows, n_se
     g, hq, d = q.shape
     s = g * n_kv_heads
     gs = _groups(hq, n_kv_heads)
-    _rows_sizes(s, q, out, lse_out, sel_rows, n_sel, k_local, v_local)
-    budget = sel_rows.shape[1]
-    window = k_local.shape[1]
+    budget, window = sel_rows.shape[1], k_local.shape[1]
+    _rows_sizes(s, q, out, lse_out, sel_rows, n_sel, budget, k_local, v_local, window)
     rows = _pool_q4(codes, scales, s)
     lib = _native()
     ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else
                         lib.sparse_decode_attn_rows_q4_workspace_size(s, gs, d, budget, window), stream)
     sc = (1.0 / d ** 0.5) if scale is None else scale
     _check(lib.sparse_decode_attn_rows_q4(
-        q, _one_dtype(q, k_local, v_local), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel,
+        q, _dtype_code(q), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel,
         budget, k_local, v_local, window, local_start, n_local, out, _dtype_code(out), lse_out, ws, wsb, stream))
 
 
@@ -838,16 +817,16 @@ def sparse_decode_attn_rows_q4_seg(q, n_kv_heads: int, codes, scales, sel_rows, 
     g, hq, d = q.shape
     s = g * n_kv_heads
     gs = _groups(hq, n_kv_heads)
-    _rows_sizes(s, q, out, lse_out, sel_rows, n_sel, k_local, v_local)
-    budget = sel_rows.shape[1]
-    window = k_local.shape[1]
+    budget, window = sel_rows.shape[1], k_local.shape[1]
+    _rows_sizes(s, q, out, lse_out, sel_rows, n_sel, budget, k_local, v_local, window)
+    _native().expect("seg_state", seg_state, (s, segment_state_ints(window)), torch.int32)
     rows = _pool_q4(codes, scales, s)
     lib = _native()
     ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else
                         lib.sparse_decode_attn_rows_q4_workspace_size(s, gs, d, budget, window), stream)
     sc = (1.0 / d ** 0.5) if scale is None else scale
     _check(lib.sparse_decode_attn_rows_q4_seg(
-        q, _one_dtype(q, k_local, v_local), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel,
+        q, _dtype_code(q), s, n_kv_heads, gs, d, float(sc), codes, scales, rows, sel_rows, n_sel,
         budget, k_local, v_local, window, seg_state, n_tokens, out, _dtype_code(out), lse_out, ws, wsb, stream))
 
 
@@ -873,10 +852,10 @@ def retrieve_blocks(q, n_kv_heads: int, reps, n_keys: int, q_start: int, q_block
     g, hq, n_q, d = q.shape
     s = g * n_kv_heads
     _lists(sel_blocks, n_sel_blocks, s, n_q, q_block)
-    _sizes(reps=(reps, (s, reps.shape[1], d)))
+    _native().expect("reps", reps, (s, reps.shape[1], d), torch.float32)
     _check(_native().retrieve_blocks(
-        q, _dtype_code(q), s, n_kv_heads, _groups(hq, n_kv_heads), n_q, d, reps, reps.shape[1], n_keys, q_start, q_block,
-        block_len, n_first, n_recent, n_top, sel_blocks, sel_blocks.shape[2], n_sel_blocks, stream))
+        q, _dtype_code(q), s, n_kv_heads, _groups(hq, n_kv_heads), n_q, d, reps, reps.shape[1], n_keys, q_start,
+        q_block, block_len, n_first, n_recent, n_top, sel_blocks, sel_blocks.shape[2], n_sel_blocks, stream))
 
 
 def sparse_prefill_attn_workspace_size(n_slices, group_size, n_q, q_block, block_len, sel_cap, d=128) -> int:
@@ -893,12 +872,13 @@ def sparse_prefill_attn(q, n_kv_heads: int, keys, values, n_keys: int, q_start: 
     gs = _groups(hq, n_kv_heads)
     _lists(sel_blocks, n_sel_blocks, s, n_q, q_block)
     kv = (s, keys.shape[1], d)
-    _sizes(keys=(keys, kv), values=(values, kv), out=(out, q.shape), lse_out=(lse_out, q.shape[:3]))
+    _native().expect("keys", keys, kv, q.dtype, "values", values, kv, q.dtype, "out", out, q.shape, None,
+                     "lse_out", lse_out, q.shape[:3], torch.float32)
     cap = sel_blocks.shape[2]
     lib = _native()
     ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else
                         lib.sparse_prefill_attn_workspace_size(s, gs, n_q, d, q_block, block_len, cap), stream)
     sc = (1.0 / d ** 0.5) if scale is None else scale
     _check(lib.sparse_prefill_attn(
-        q, _one_dtype(q, keys, values), s, n_kv_heads, gs, n_q, d, float(sc), keys, values, keys.shape[1], n_keys,
+        q, _dtype_code(q), s, n_kv_heads, gs, n_q, d, float(sc), keys, values, keys.shape[1], n_keys,
         q_start, q_block, block_len, sel_blocks, cap, n_sel_blocks, out, _dtype_code(out), lse_out, ws, wsb, stream))
