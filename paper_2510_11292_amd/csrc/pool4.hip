@@ -95,7 +95,10 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
 
 // Rows are taken 32 to a block: 32 lanes a row, 16 for its key and 16 for its
 // value, eight channels each, so that a wave's code stores are two whole 128-byte
-// rows.  Blocks stride over the (slice, 32 rows) chunks.
+// rows.  A block takes one (slice, 32 rows) chunk; blocks that stride over several
+// lose their loads' time in between (64 slices of 32768 bfloat16 rows, written and
+// read back, 2.73 GB: 498 us, 5.5 TB/s; eight blocks a compute unit 540, 64 of them
+// 511).  Both are bound by memory: a copy of that size reaches 4.8 to 5.2 TB/s.
 constexpr int kRowsPerChunk = 32;
 constexpr int kRowsInFlight = 4;   // of a wave's lane half
 
@@ -173,7 +176,8 @@ constexpr int kNUnits = 0, kWinFirst = 1, kHead = 2, kCount = 3, kOverflow = 4, 
 // a time.  The rows of the segment that leaves go to the pool and into eight
 // float64 partial means per channel, then the new token enters its slot, which
 // is the first of the rows that left: the barrier and the wait before it keep
-// every wave's reads ahead of that write.
+// every wave's reads ahead of that write.  Bound by latency: 8 slices with a segment
+// of 32 tokens 4.4 us, 1024 slices (32 MB) 6.6 us.
 template <class T, bool kSeg>
 __global__ __launch_bounds__(256)
 void store_q4_kernel(const T* __restrict__ k_new, const T* __restrict__ v_new, T* __restrict__ k_local,
@@ -351,8 +355,11 @@ __device__ __forceinline__ void merge_waves(const AttnQ4& a, const float (*s_m)[
 // ---- float32: vector ALUs
 
 // Block (slice, chunk): softmax over the chunk's share of the slice's rows, one
-// pass, 16 lanes a row (lane sub owns channels 8 sub..+7).  Every 16-lane group keeps its own running maximum, sum and weighted
-// sum; they are joined at the end.
+// pass, 16 lanes a row (lane sub owns channels 8 sub..+7), four rows of a group on
+// their way.  Every 16-lane group keeps its own running maximum, sum and weighted
+// sum; they are joined at the end.  Bound by the vector ALUs: a row and head take 16
+// fused multiply-adds, 16 products and the sum over 16 lanes (8 slices of 1300 rows
+// with 8 heads: 16.3 us and 3.9 for the merge).
 constexpr int kAttnWaves = 8;
 
 template <int G>
@@ -490,8 +497,12 @@ constexpr float kGrow = 8.0f;   // base-2 logits may pass the base by this much 
 //           them, paired by byte permutes, is the operand of the i-th product, whose
 //           columns are channels 8 c + i.
 // Rows are loaded 16 bytes a lane, five loads a tile; the values' words and the
-// scales change lanes through LDS.  (Loaded where they are used, in twenty loads of
-// 1 and 4 bytes, rows came at 4.9 TB/s however many were in flight.)
+// scales change lanes through LDS (loaded where they are used, in twenty loads of
+// 1 and 4 bytes, the time was the same).  Weights are rounded to bfloat16 for the second
+// product, half a step or 2^-8 of each at most; their sum is of the unrounded ones.
+// 256 slices of 2148 rows, 4 heads (86.5 MB): 20.0 us, 4.3 TB/s, of which 6 to 7 us pass
+// before the first rows arrive and after the last; more rows come at 5.4 TB/s.  Sixteen
+// waves a block spill (61 us), the list staged in LDS 20.7.
 template <int G>
 __global__ __launch_bounds__(kAttnWaves * 64)
 void attn_q4_mfma_kernel(const AttnQ4 a) {
@@ -743,11 +754,8 @@ int check_pool(const void* codes, const void* scales, int64_t pool_rows) {
   return LOUISKV_OK;
 }
 
-// Blocks of a launch that strides over chunks of rows: eight a compute unit.
-unsigned stride_grid(int64_t n_chunks) {
-  const int cus = device_cu_count();
-  return (unsigned)std::min<int64_t>(n_chunks, 8 * (int64_t)(cus > 0 ? cus : 256));
-}
+// Blocks of a launch over chunks of rows: one a chunk, as far as a launch holds them.
+unsigned chunk_grid(int64_t n_chunks) { return (unsigned)std::min(n_chunks, kMaxGrid); }
 
 int store_q4(const void* k_new, const void* v_new, int32_t dtype, int64_t n_slices, void* k_local, void* v_local,
              int32_t window, int32_t step, int32_t seg_len, int32_t evict, const uint8_t* fire, int32_t n_kv_heads,
@@ -835,11 +843,11 @@ extern "C" int louiskv_pack_pool_q4(const void* keys, const void* values, int32_
   const int per = (n_tokens + kRowsPerChunk - 1) / kRowsPerChunk;
   const int64_t n = n_slices * per;
   if (dtype == LOUISKV_BF16)
-    pack_q4_kernel<uint16_t><<<stride_grid(n), 256, 0, as_stream(stream)>>>(
+    pack_q4_kernel<uint16_t><<<chunk_grid(n), 256, 0, as_stream(stream)>>>(
         static_cast<const uint16_t*>(keys), static_cast<const uint16_t*>(values), perm, n_tokens, n, per, codes,
         scales, pool_rows);
   else
-    pack_q4_kernel<float><<<stride_grid(n), 256, 0, as_stream(stream)>>>(
+    pack_q4_kernel<float><<<chunk_grid(n), 256, 0, as_stream(stream)>>>(
         static_cast<const float*>(keys), static_cast<const float*>(values), perm, n_tokens, n, per, codes, scales,
         pool_rows);
   LKV_CHECK_LAUNCH();
@@ -862,11 +870,11 @@ extern "C" int louiskv_gather_rows_q4(const uint8_t* codes, const uint8_t* scale
   const int per = (int)(((int64_t)buf_rows + kRowsPerChunk - 1) / kRowsPerChunk);
   const int64_t n = n_slices * per;
   if (dtype == LOUISKV_BF16)
-    gather_q4_kernel<uint16_t><<<stride_grid(n), 256, 0, as_stream(stream)>>>(
+    gather_q4_kernel<uint16_t><<<chunk_grid(n), 256, 0, as_stream(stream)>>>(
         codes, scales, pool_rows, sel_rows, n_sel, buf_rows, n, per, static_cast<uint16_t*>(k_buf),
         static_cast<uint16_t*>(v_buf));
   else
-    gather_q4_kernel<float><<<stride_grid(n), 256, 0, as_stream(stream)>>>(
+    gather_q4_kernel<float><<<chunk_grid(n), 256, 0, as_stream(stream)>>>(
         codes, scales, pool_rows, sel_rows, n_sel, buf_rows, n, per, static_cast<float*>(k_buf),
         static_cast<float*>(v_buf));
   LKV_CHECK_LAUNCH();
