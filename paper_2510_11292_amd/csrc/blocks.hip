@@ -275,9 +275,21 @@ constexpr float kGrow = 8.0f;   // base-2 logits may pass the base by this much 
 // 32K tokens).  A wave computes S^T = K Q^T for 32 keys, so that a lane holds
 // 16 scores of one query row; their exponentials are, unmoved, the B operand of
 // O^T += V^T P^T, whose A operand comes from LDS through transposing reads.  The
-// running base, sum and the rescale are then a lane's own.
+// running base, sum and the rescale are then a lane's own; the sums are rescaled
+// only where a score passes the base by 2^8.
 // float32: the same with 32 positions a stage and products of two channels or keys
 // at a time, k index = half of the wave; the scores need no rounding.
+//
+// A layer of 32K tokens (8 slices x 512 tiles of 256 rows, 30 blocks of 64 keys, 985
+// GFLOP): 1.10 ms, 0.89 PFLOP/s, where a large product reaches 1.35; in float32 a layer
+// of 8192 tokens 2.0 ms, 114 TFLOP/s of 153.  For each 32 rows by 32 keys a wave has 16
+// products (512 cycles), 16 exponentials and 80 other vector operations, and reads
+// 16 KB of LDS.  Two waves of a SIMD alternate between them, and overlap in part: the
+// same instructions without a dependency between the pairs take 1.02 ms, the
+// products and LDS reads alone 0.74.  64 rows a wave would halve the LDS reads, but its
+// accumulators do not fit beside the rest (copies between the register files:
+// 1.60 ms); phases kept apart by barriers 1.35 ms, a maximum over 64 keys at a time
+// 1.16, the next 32 keys' scores between the exponentials 1.11 to 1.13.
 constexpr int kStageBytes = 16384;   // of the keys, and of the values
 
 template <class T, int WR, int WK>
@@ -706,29 +718,50 @@ void prefill_kernel(const PrefillArgs a, int row_groups, int64_t n_blocks) {
     }
 }
 
-template <class T, int WR, int WK>
-void launch_prefill(const PrefillArgs& a, int row_groups, int64_t n_blocks, hipStream_t s) {
-  prefill_kernel<T, WR, WK><<<(unsigned)n_blocks, WR * WK * 64, 0, s>>>(a, row_groups, n_blocks);
-}
-
 int check_dtype(int dtype) {
   if (dtype != LOUISKV_F32 && dtype != LOUISKV_BF16) return fail(LOUISKV_ERR_DTYPE, "unknown dtype %d", dtype);
   return LOUISKV_OK;
 }
 
-// Rows (tokens by heads) that a block of the matrix-core kernel takes, for tiles of
-// `rows`.
-int block_rows(int rows) { return rows > 128 ? 256 : rows > 64 ? 128 : rows > 32 ? 64 : 32; }
+// How a call is cut into blocks of waves.  A block takes all rows of a tile, up to
+// 256, as long as there are 256 blocks for the chip (8 slices in tiles of 64 tokens
+// by 4 heads: of 8192 tokens 256 rows a block 276 us, 64 rows 343; of 1024 tokens 256
+// rows and lists in four parts 76 us, 64 rows and whole lists 49).  Where that is
+// not enough the lists are split for 512 blocks (256 tokens: 28.7 us; 256 blocks
+// 30.7, 1024 blocks 35.6), into parts of two stages or more, so that the next one is
+// under way (one token, 2112 keys: 9.6 us; one stage 10.7, four 11.2), and of four
+// keys a row (two in float32), so that writing and reading the partials moves half
+// of the keys' bytes at most (64 tokens, 2112 keys: 17.5 us; half 22.4, twice 19.1).
+// 256 slices of one token stay whole: 53 us; split in two 50, but the same
+// rule takes 141 us for 75 with 2048 tokens.
+struct Cut {
+  int rows;         // rows (tokens by heads) of a tile that a block takes: 64, 128 or 256
+  int row_groups;   // blocks of a tile
+  int splits;       // parts of a tile's list
+  int64_t blocks;
+};
+constexpr int kFullGrid = 256, kSplitGrid = 512;
+Cut cut_of(int64_t n_slices, int group_size, int n_q, int q_block, int block_len, int sel_cap, int dtype) {
+  const int rows = std::min(q_block, n_q) * group_size, stage_keys = dtype == LOUISKV_BF16 ? 64 : 32;
+  const int64_t tiles = n_slices * (((int64_t)n_q + q_block - 1) / q_block);
+  Cut c;
+  auto take = [&](int per) {
+    c.rows = per;
+    c.row_groups = (rows + per - 1) / per;
+    c.blocks = tiles * c.row_groups;
+  };
+  take(rows > 128 ? 256 : rows > 64 ? 128 : 64);
+  while (c.rows > 64 && c.blocks < kFullGrid) take(c.rows / 2);
+  const int part_keys = std::max(2 * stage_keys, std::min(rows, c.rows) * stage_keys / 16);
+  const int64_t by_keys = std::max<int64_t>(1, (int64_t)sel_cap * block_len / part_keys);
+  c.splits = c.blocks >= kFullGrid ? 1 : (int)std::min<int64_t>(by_keys, kSplitGrid / c.blocks);
+  c.blocks *= c.splits;
+  return c;
+}
 
-// Parts that a tile's list is split into: one where there are tiles for the chip;
-// otherwise enough blocks for it, with 128 keys or more in each.
-constexpr int kFullGrid = 256, kSplitGrid = 512, kSplitKeys = 128;
-int prefill_splits(int64_t n_slices, int group_size, int n_q, int q_block, int block_len, int sel_cap) {
-  const int rows = std::min(q_block, n_q) * group_size, per = block_rows(rows);
-  const int64_t blocks = n_slices * (((int64_t)n_q + q_block - 1) / q_block) * ((rows + per - 1) / per);
-  if (blocks >= kFullGrid) return 1;
-  const int64_t by_keys = std::max<int64_t>(1, (int64_t)sel_cap * block_len / kSplitKeys);
-  return (int)std::min<int64_t>(by_keys, kSplitGrid / blocks);
+template <class T, int WR, int WK>
+void launch_prefill(const PrefillArgs& a, const Cut& c, hipStream_t s) {
+  prefill_kernel<T, WR, WK><<<(unsigned)c.blocks, WR * WK * 64, 0, s>>>(a, c.row_groups, c.blocks);
 }
 
 int log2_block(int block_len) {
@@ -817,7 +850,8 @@ extern "C" size_t louiskv_sparse_prefill_attn_workspace_size(int64_t n_slices, i
   if (n_slices < 1 || group_size < 1 || n_q < 1 || q_block < 1 || q_block > kMaxTile || log2_block(block_len) < 0 ||
       sel_cap < 1)
     return 0;
-  return part_bytes(n_slices * group_size * n_q, prefill_splits(n_slices, group_size, n_q, q_block, block_len, sel_cap));
+  auto parts = [&](int dtype) { return cut_of(n_slices, group_size, n_q, q_block, block_len, sel_cap, dtype).splits; };
+  return part_bytes(n_slices * group_size * n_q, std::max(parts(LOUISKV_BF16), parts(LOUISKV_F32)));
 }
 
 extern "C" int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads,
@@ -843,32 +877,29 @@ extern "C" int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t
   a.sel = sel_blocks; a.sel_cap = sel_cap; a.n_sel = n_sel_blocks; a.n_tiles = (n_q - 1) / q_block + 1; a.n_split = 1;
   a.part = nullptr; a.out = out; a.out_bf16 = out_dtype == LOUISKV_BF16; a.lse_out = lse_out;
   const int64_t n_rows = n_slices * group_size * n_q;
-  const int rows = std::min(q_block, n_q) * group_size, per = block_rows(rows), row_groups = (rows + per - 1) / per;
-  const int n_split = prefill_splits(n_slices, group_size, n_q, q_block, block_len, sel_cap);
-  const size_t need = part_bytes(n_rows, n_split);
+  const Cut c = cut_of(n_slices, group_size, n_q, q_block, block_len, sel_cap, dtype);
+  const size_t need =
+      louiskv_sparse_prefill_attn_workspace_size(n_slices, group_size, n_q, d, q_block, block_len, sel_cap);
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
     return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, 16-byte aligned, got %zu", need, workspace_bytes);
   hipStream_t hs = as_stream(stream);
-  a.n_split = n_split;
+  a.n_split = c.splits;
   a.part = static_cast<float*>(workspace);
-  const int64_t n_blocks = n_slices * a.n_tiles * row_groups * n_split;
-  if (n_blocks > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
+  if (c.blocks > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   if (dtype == LOUISKV_BF16) {
-    switch (per) {
-      case 256: launch_prefill<uint16_t, 8, 1>(a, row_groups, n_blocks, hs); break;
-      case 128: launch_prefill<uint16_t, 4, 1>(a, row_groups, n_blocks, hs); break;
-      case 64: launch_prefill<uint16_t, 2, 2>(a, row_groups, n_blocks, hs); break;
-      default: launch_prefill<uint16_t, 1, 2>(a, row_groups, n_blocks, hs); break;
+    switch (c.rows) {
+      case 256: launch_prefill<uint16_t, 8, 1>(a, c, hs); break;
+      case 128: launch_prefill<uint16_t, 4, 1>(a, c, hs); break;
+      default: launch_prefill<uint16_t, 2, 2>(a, c, hs); break;
     }
   } else {
-    switch (per) {
-      case 256: launch_prefill<float, 8, 1>(a, row_groups, n_blocks, hs); break;
-      case 128: launch_prefill<float, 4, 1>(a, row_groups, n_blocks, hs); break;
-      case 64: launch_prefill<float, 2, 1>(a, row_groups, n_blocks, hs); break;
-      default: launch_prefill<float, 1, 1>(a, row_groups, n_blocks, hs); break;
+    switch (c.rows) {
+      case 256: launch_prefill<float, 8, 1>(a, c, hs); break;
+      case 128: launch_prefill<float, 4, 1>(a, c, hs); break;
+      default: launch_prefill<float, 2, 1>(a, c, hs); break;
     }
   }
   LKV_CHECK_LAUNCH();
-  if (n_split == 1) return LOUISKV_OK;
-  return merge_parts(a.part, n_split, n_rows, out, out_dtype, lse_out, hs);
+  if (c.splits == 1) return LOUISKV_OK;
+  return merge_parts(a.part, c.splits, n_rows, out, out_dtype, lse_out, hs);
 }
