@@ -354,12 +354,25 @@ __device__ __forceinline__ void merge_waves(const AttnQ4& a, const float (*s_m)[
 
 // ---- float32: vector ALUs
 
+// a's lower and b's upper halves (32) of the wave, or even and odd quarters (16), are
+// added to the others: a's sums in the lower half (even quarters), b's in the upper.
+template <int kLanes>
+__device__ __forceinline__ float swap_add(float a, float b) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  u32x2 r;
+  if constexpr (kLanes == 32) r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  else r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // Block (slice, chunk): softmax over the chunk's share of the slice's rows, one
 // pass, 16 lanes a row (lane sub owns channels 8 sub..+7), four rows of a group on
 // their way.  Every 16-lane group keeps its own running maximum, sum and weighted
-// sum; they are joined at the end.  Bound by the vector ALUs: a row and head take 16
-// fused multiply-adds, 16 products and the sum over 16 lanes (8 slices of 1300 rows
-// with 8 heads: 16.3 us and 3.9 for the merge).
+// sum; they are joined at the end.  Two rows share a rescale (one each: 256 slices of
+// 2148 rows, 4 heads, 71 us; two 48; four 47, but more idle work where rows are few).
+// Bound by the vector ALUs, 27 operations a row and head and lane, where there are many
+// rows; by trips to memory where few (8 slices of 1300 rows, 8 heads: 12.1 us with the
+// merge; the wave's groups joined by shuffles 17.5).
 constexpr int kAttnWaves = 8;
 
 template <int G>
@@ -367,7 +380,7 @@ __global__ __launch_bounds__(kAttnWaves * 64)
 void attn_q4_kernel(const AttnQ4 a) {
   constexpr int kGroups = kAttnWaves * 4;
   __shared__ float s_m[kAttnWaves][G], s_l[kAttnWaves][G];
-  __shared__ float s_acc[kAttnWaves][G][kHeadDim];
+  __shared__ __align__(16) float s_acc[kAttnWaves][G][kHeadDim];
   const int64_t s = blockIdx.x / a.n_chunks;
   const int chunk = (int)(blockIdx.x - s * a.n_chunks);
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, sub = tid & 15, grp = tid >> 4;
@@ -392,22 +405,35 @@ void attn_q4_kernel(const AttnQ4 a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[j][e] = 0.f;
   }
-  auto attend = [&](const float (&k)[8], const float (&v)[8]) {
+  // Two of a group's rows, of which n are there (the other repeats one of them): their
+  // scores, one rescale for both, and their values.
+  auto attend = [&](const float (&k)[2][8], const float (&v)[2][8], int n) {
 #pragma unroll
     for (int j = 0; j < G; ++j) {
-      float d = 0.f;
+      float p[2], mn = m[j];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d = fmaf(q[j][e], k[e], d);
-      d = row16_add(d);
-      const float mn = fmaxf(m[j], d), base = max_base(mn);
-      const float c = __builtin_amdgcn_exp2f(m[j] - base), p = __builtin_amdgcn_exp2f(d - base);
+      for (int u = 0; u < 2; ++u) {
+        float d = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d = fmaf(q[j][e], k[u][e], d);
+        p[u] = u < n ? row16_add(d) : -__builtin_inff();
+        mn = fmaxf(mn, p[u]);
+      }
+      const float base = max_base(mn), c = __builtin_amdgcn_exp2f(m[j] - base);
       m[j] = mn;
-      l[j] = l[j] * c + p;
+      l[j] *= c;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[j][e] = fmaf(acc[j][e], c, p * v[e]);
+      for (int e = 0; e < 8; ++e) acc[j][e] *= c;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float y = __builtin_amdgcn_exp2f(p[u] - base);
+        l[j] += y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[j][e] = fmaf(y, v[u][e], acc[j][e]);
+      }
     }
   };
-  // kRows of a group's rows on their way together: their list entries, then their codes
+  // kRows of a group's rows are on their way together: list entries, then codes
   constexpr int kRows = 4;
   const int p1 = min(r1, nsel);
   for (int r = r0 + grp; r < p1; r += kRows * kGroups) {
@@ -424,23 +450,30 @@ void attn_q4_kernel(const AttnQ4 a) {
       ks[u] = a.scales[row[u] * kScaleBytes + (sub >> 2)];
       vs[u] = a.scales[row[u] * kScaleBytes + 4 + (sub >> 2)];
     }
+    const int n = (p1 - r + kGroups - 1) / kGroups;
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      if (r + u * kGroups >= p1) break;
-      float k[8], v[8];
-      expand8(kc[u], scale_of(ks[u]), k);
-      expand8(vc[u], scale_of(vs[u]), v);
-      attend(k, v);
+    for (int u = 0; u < kRows; u += 2) {
+      if (u >= n) break;
+      float k[2][8], v[2][8];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        expand8(kc[u + x], scale_of(ks[u + x]), k[x]);
+        expand8(vc[u + x], scale_of(vs[u + x]), v[x]);
+      }
+      attend(k, v, n - u);
     }
   }
-  for (int r = max(r0, nsel) + grp; r < r1; r += kGroups) {
-    int slot = local_start + (r - nsel);
-    slot -= slot >= a.window ? a.window : 0;
-    const size_t o = ((size_t)s * a.window + slot) * kHeadDim + 8 * sub;
-    float k[8], v[8];
-    load8(static_cast<const float*>(a.k_local) + o, k);
-    load8(static_cast<const float*>(a.v_local) + o, v);
-    attend(k, v);
+  for (int r = max(r0, nsel) + grp; r < r1; r += 2 * kGroups) {
+    float k[2][8], v[2][8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      int slot = local_start + (min(r + u * kGroups, r1 - 1) - nsel);
+      slot -= slot >= a.window ? a.window : 0;
+      const size_t o = ((size_t)s * a.window + slot) * kHeadDim + 8 * sub;
+      load8(static_cast<const float*>(a.k_local) + o, k[u]);
+      load8(static_cast<const float*>(a.v_local) + o, v[u]);
+    }
+    attend(k, v, (r1 - r + kGroups - 1) / kGroups);
   }
   // the wave's four groups, then its totals into LDS
 #pragma unroll
@@ -451,13 +484,14 @@ void attn_q4_kernel(const AttnQ4 a) {
     float ll = l[j] * c;
     ll += __shfl_xor(ll, 16, kWave);
     ll += __shfl_xor(ll, 32, kWave);
+    // halves, then quarters of the wave change places with another channel's: what is
+    // left of eight sums over four lanes is channels 2 h and 2 h + 1 in lane 16 h + sub
+    float x[4], y[2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float x = acc[j][e] * c;
-      x += __shfl_xor(x, 16, kWave);
-      x += __shfl_xor(x, 32, kWave);
-      if (lane < 16) s_acc[w][j][8 * sub + e] = x;
-    }
+    for (int e = 0; e < 4; ++e) x[e] = swap_add<32>(acc[j][e] * c, acc[j][e + 4] * c);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) y[e] = swap_add<16>(x[e], x[e + 2]);
+    *reinterpret_cast<float2*>(&s_acc[w][j][8 * sub + 2 * (lane >> 4)]) = make_float2(y[0], y[1]);
     if (lane == 0) {
       s_m[w][j] = mm;
       s_l[w][j] = ll;
@@ -508,7 +542,7 @@ __global__ __launch_bounds__(kAttnWaves * 64)
 void attn_q4_mfma_kernel(const AttnQ4 a) {
   constexpr int NW = kAttnWaves;
   __shared__ float s_m[NW][G], s_l[NW][G];
-  __shared__ float s_acc[NW][G][kHeadDim];
+  __shared__ __align__(16) float s_acc[NW][G][kHeadDim];
   __shared__ __align__(16) uint32_t s_v[NW][32 * 16 + 7 * 16], s_sc[NW][64];
   // word of a tile's row in s_v: 16 more after every four rows, so that a read of
   // rows 4 h + j by the four groups of lanes falls into different banks
@@ -712,13 +746,15 @@ void attn_q4_mfma_kernel(const AttnQ4 a) {
 }
 
 // Chunks of a slice's rows: blocks for the chip, with the rows that a block has in
-// flight at once, a half tile a wave (8 slices of 2148 rows, attention alone: 128
-// rows a block 5.8 us, 256 rows 7.0; 256 slices: one chunk 20 us, two and their
-// merge 25).
-constexpr int kTargetBlocks = 256, kMinRows = 128;
-int attn_q4_chunks(int64_t S, int budget, int window) {
+// flight at once: in bfloat16 a half tile a wave (8 slices of 2148 rows, attention
+// alone: 128 rows a block 5.8 us, 256 rows 7.0; 256 slices: one chunk 20 us, two and
+// their merge 25), in float32 two rows a group (8 slices of 2148 rows with the merge:
+// 64 rows a block 9.7 us, 128 rows 10.3).
+constexpr int kTargetBlocks = 256;
+int attn_q4_chunks(int64_t S, int budget, int window, int dtype) {
+  const int min_rows = dtype == LOUISKV_BF16 ? 128 : 64;
   const int64_t cap = (int64_t)budget + window;
-  const int64_t by_rows = std::max<int64_t>(1, (cap + kMinRows - 1) / kMinRows);
+  const int64_t by_rows = std::max<int64_t>(1, (cap + min_rows - 1) / min_rows);
   const int64_t by_grid = std::max<int64_t>(1, kTargetBlocks / S);
   return (int)std::min(by_rows, by_grid);
 }
@@ -802,10 +838,10 @@ int attn_q4(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads, 
       (window > 0 && (local_start < 0 || local_start >= window)))
     return fail(LOUISKV_ERR_SHAPE, "budget=%d window=%d local_start=%d n_local=%d", budget, window, local_start, n_local);
   if (budget > 0 && (st = check_pool(codes, scales, pool_rows))) return st;
-  const int n_chunks = attn_q4_chunks(n_slices, budget, window);
+  const int n_chunks = attn_q4_chunks(n_slices, budget, window, dtype);
   if (n_slices > kMaxGrid || (int64_t)budget + window > LOUISKV_Q4_MAX_POOL_ROWS * 2)
     return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
-  const size_t need = part_bytes(n_slices * group_size, n_chunks);
+  const size_t need = louiskv_sparse_decode_attn_rows_q4_workspace_size(n_slices, group_size, d, budget, window);
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
     return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, 16-byte aligned, got %zu", need, workspace_bytes);
   AttnQ4 a;
@@ -945,7 +981,9 @@ extern "C" size_t louiskv_sparse_decode_attn_rows_q4_workspace_size(int64_t n_sl
                                                                     int32_t budget, int32_t window) {
   (void)d;
   if (n_slices < 1 || group_size < 1 || budget < 0 || window < 0) return 0;
-  return part_bytes(n_slices * group_size, attn_q4_chunks(n_slices, budget, window));
+  const int parts = std::max(attn_q4_chunks(n_slices, budget, window, LOUISKV_BF16),
+                             attn_q4_chunks(n_slices, budget, window, LOUISKV_F32));
+  return part_bytes(n_slices * group_size, parts);
 }
 
 extern "C" int louiskv_sparse_decode_attn_rows_q4(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads,
