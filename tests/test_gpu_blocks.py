@@ -245,3 +245,51 @@ def test_replayed_graph_and_two_streams():
         torch.cuda.synchronize()
         for n in ("sel", "n", "out", "lse"):
             assert torch.equal(eager[n], cap_[n]) and torch.equal(eager[n], other[n]), (i, n)
+
+
+MANY = [  # enough tiles for blocks of 256 and 128 rows; groups, kv, g, n_q, n_k, tile, block, cap
+    (16, 8, 4, 130, 400, 64, 32, 9), (40, 4, 8, 70, 300, 33, 16, 8), (64, 2, 8, 40, 333, 16, 64, 5),
+    (160, 1, 1, 200, 200, 128, 128, 2), (130, 1, 8, 130, 500, 128, 64, 7),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", MANY, ids=[f"{c[0] * c[1]}x{c[2]}x{c[3]}t{c[5]}b{c[6]}" for c in MANY])
+def test_attention_of_many_tiles(dtype, case):
+    groups, kv, g, n_q, n_k, tile, block, cap = case
+    s, dt = groups * kv, DT[dtype]
+    rng = np.random.default_rng(n_k)
+    gen = torch.Generator(device=DEV).manual_seed(n_q)
+    q = (2 * torch.randn(groups, kv * g, n_q, 128, generator=gen, device=DEV)).to(dt)
+    keys, values = (torch.randn(s, n_k, 128, generator=gen, device=DEV).to(dt) for _ in range(2))
+    sel, n = lists_for(rng, s, n_q, n_k, tile, block, cap, True)
+    out, lse = run_attn(q, kv, keys, values, n_k, tile, block, sel, n, dt)
+    for i in (0, groups // 2, groups - 1):
+        a, b = slice(i, i + 1), slice(i * kv, (i + 1) * kv)
+        worst = check_against_oracle(q[a], kv, keys[b], values[b], n_k, tile, block, sel[b], n[b], out[a], lse[a],
+                                     dtype == "bf16")
+        print(f"{case} {dtype}, group {i}: largest error {worst:.3f} of the bound", flush=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tile,g", [(64, 4), (128, 8), (32, 4)])
+def test_later_keys_do_not_reach_a_query_of_many_tiles(dtype, tile, g):
+    """As above where the blocks take more rows: 150 sequences, one of them with bad keys behind its queries."""
+    dt, n, groups, block = DT[dtype], 200, 150, 32
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    q = torch.randn(groups, g, n, 128, generator=gen, device=DEV).to(dt)
+    keys, values = (torch.randn(groups, n, 128, generator=gen, device=DEV).to(dt) for _ in range(2))
+    nb, tiles = -(-n // block), -(-n // tile)
+    sel = np.tile(np.arange(nb, dtype=np.int32), (groups, tiles, 1))
+    cnt = np.full((groups, tiles), nb, dtype=np.int32)
+    ref, ref_lse = run_attn(q, 1, keys, values, n, tile, block, sel, cnt, torch.float32)
+    assert not torch.isnan(ref).any()
+    for at, bad in ((77, float("nan")), (130, -float("inf"))):
+        k2, v2 = keys.clone(), values.clone()
+        k2[70, at + 40:], v2[70, at:at + 40, 5:90] = bad, bad
+        out, lse = run_attn(q, 1, k2, v2, n, tile, block, sel, cnt, torch.float32)
+        assert torch.equal(out[70, :, :at], ref[70, :, :at]) and torch.equal(lse[70, :, :at], ref_lse[70, :, :at])
+        assert not torch.isfinite(out[70, :, at:at + 40, 5:90]).any()
+        assert torch.equal(out[70, :, :at + 40, 90:], ref[70, :, :at + 40, 90:])
+        others = torch.arange(groups, device=DEV) != 70
+        assert torch.equal(out[others], ref[others]) and torch.equal(lse[others], ref_lse[others])
