@@ -9,7 +9,9 @@
 // each argument is converted in place:
 //   pointers   a tensor (must be contiguous) or None (NULL); an array of
 //              handles (void* const*) is passed by its address.  Numbers are
-//              refused where a tensor belongs: a kernel would read there
+//              refused where a tensor belongs: a kernel would read there.  The
+//              calls of LKV_DEVICE_ENTRY also refuse tensors that are not in
+//              the current device's memory
 //   stream     the last parameter(s): None (the current stream), a
 //              torch.cuda.Stream or a handle
 //   numbers    int, bool or float

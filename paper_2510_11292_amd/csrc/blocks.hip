@@ -847,8 +847,8 @@ extern "C" size_t louiskv_sparse_prefill_attn_workspace_size(int64_t n_slices, i
                                                              int32_t d, int32_t q_block, int32_t block_len,
                                                              int32_t sel_cap) {
   (void)d;
-  if (n_slices < 1 || group_size < 1 || n_q < 1 || q_block < 1 || q_block > kMaxTile || log2_block(block_len) < 0 ||
-      sel_cap < 1)
+  if (n_slices < 1 || n_slices > kMaxGrid || group_size < 1 || group_size > 8 || n_q < 1 || q_block < 1 ||
+      q_block > kMaxTile || log2_block(block_len) < 0 || sel_cap < 1)
     return 0;
   auto parts = [&](int dtype) { return cut_of(n_slices, group_size, n_q, q_block, block_len, sel_cap, dtype).splits; };
   return part_bytes(n_slices * group_size * n_q, std::max(parts(LOUISKV_BF16), parts(LOUISKV_F32)));

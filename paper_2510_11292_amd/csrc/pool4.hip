@@ -980,7 +980,7 @@ extern "C" int louiskv_segment_output_boundary_q4(const void* k_new, const void*
 extern "C" size_t louiskv_sparse_decode_attn_rows_q4_workspace_size(int64_t n_slices, int32_t group_size, int32_t d,
                                                                     int32_t budget, int32_t window) {
   (void)d;
-  if (n_slices < 1 || group_size < 1 || budget < 0 || window < 0) return 0;
+  if (n_slices < 1 || n_slices > kMaxGrid || group_size < 1 || group_size > 8 || budget < 0 || window < 0) return 0;
   const int parts = std::max(attn_q4_chunks(n_slices, budget, window, LOUISKV_BF16),
                              attn_q4_chunks(n_slices, budget, window, LOUISKV_F32));
   return part_bytes(n_slices * group_size, parts);

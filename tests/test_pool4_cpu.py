@@ -226,6 +226,14 @@ def test_unaligned_buffers_and_sizes_behind_the_index_range_are_refused(lib):
         ({10: 1 << 31, 11: (1 << 30) + 1}, SHAPE), ({2: 1 << 23}, SHAPE)])
 
 
+def test_workspace_sizes_of_what_the_calls_refuse_are_zero(lib):
+    size, big = lib.louiskv_sparse_prefill_attn_workspace_size, (1 << 31) - 1
+    assert size(8, 8, 64, 128, 64, 64, 9) > 0 and size(8, 8, 64, 128, 64, 64, big) > 0
+    assert size(8, big, 64, 128, 64, 64, 9) == size(1 << 62, 4, 64, 128, 64, 64, 9) == size(8, 4, 64, 128, 129, 64, 9) == 0
+    size = lib.louiskv_sparse_decode_attn_rows_q4_workspace_size
+    assert size(8, 8, 128, big, 128) > 0 and size(8, big, 128, 64, 128) == size(1 << 62, 4, 128, 64, 128) == 0
+
+
 def test_python_calls_refuse_sizes_types_and_host_memory():
     from paper_2510_11292_amd import louiskv as L
     i32, u8 = dict(dtype=torch.int32), dict(dtype=torch.uint8)
