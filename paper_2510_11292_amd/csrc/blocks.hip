@@ -246,9 +246,11 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // Waits for every copy and LDS access of the wave, then for the block's waves.
 __device__ __forceinline__ void sync_stage() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// 64 lanes copy 16 bytes each from base + off (per lane) to LDS lds + 16 * lane.
+// 64 lanes copy 16 bytes each from base + off (per lane) to LDS lds + 16 * lane.  The
+// copy reads M0 one wait state after its write at the earliest.
 __device__ __forceinline__ void copy_to_lds(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds)
+               : "memory", "m0");
 }
 
 typedef __attribute__((address_space(3))) char* lds_ptr;

@@ -181,13 +181,17 @@ static_assert(kBf16StageTiles * kTileC <= 64, "one 64-lane copy carries a stage'
 // header it cannot tell the ring buffers apart and drains every copy in
 // flight (vmcnt(0)) once per pass of the ring.  Written this way the compiler
 // sees no memory operation, and the sweep's explicit vmcnt waits and barriers
-// are the only synchronisation, as intended.
+// are the only synchronisation, as intended.  The compiler does not look into the
+// text either: the wait state between the write of M0 and the copy that reads it
+// is the s_nop.
 __device__ __forceinline__ void dma_16b(const void* base, uint32_t lane_off, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(base), "s"(lds_addr)
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(base),
+               "s"(lds_addr)
                : "memory", "m0");
 }
 __device__ __forceinline__ void dma_4b(const void* base, uint32_t lane_off, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1" ::"v"(lane_off), "s"(base), "s"(lds_addr)
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(lane_off), "s"(base),
+               "s"(lds_addr)
                : "memory", "m0");
 }
 
