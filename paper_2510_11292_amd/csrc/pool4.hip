@@ -472,6 +472,9 @@ void attn_q4_kernel(const AttnQ4 a) {
       const size_t o = ((size_t)s * a.window + slot) * kHeadDim + 8 * sub;
       load8(static_cast<const float*>(a.k_local) + o, k[u]);
       load8(static_cast<const float*>(a.v_local) + o, v[u]);
+      // a repeated row weighs 0, and 0 times an infinity would be NaN
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[u][e] = r + u * kGroups < r1 ? v[u][e] : 0.f;
     }
     attend(k, v, (r1 - r + kGroups - 1) / kGroups);
   }
@@ -713,6 +716,11 @@ void attn_q4_mfma_kernel(const AttnQ4 a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       v[j] = *reinterpret_cast<const uint4*>(vl + (size_t)slot(16 * (j >> 2) + 4 * h + (j & 3)) * kHeadDim + 8 * c);
+    if (n_win - 32 * t < 32) {               // a repeated row weighs 0, and 0 times an infinity would be NaN
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (32 * t + 16 * (j >> 2) + 4 * h + (j & 3) >= n_win) v[j] = make_uint4(0, 0, 0, 0);
+    }
     attend(sc, v, n_win - 32 * t);
   }
   for (int t = w; t < n_pool_tiles; t += 2 * NW) {

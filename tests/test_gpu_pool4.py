@@ -253,6 +253,39 @@ def test_attention_values_that_are_not_finite(dtype):
     assert (n64(out).reshape(s, g, 128)[2] == 0).all() and np.isneginf(n64(lse).reshape(s, g)[2]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_local", [1, 15, 31, 33, 45, 64])
+@pytest.mark.parametrize("budget", [0, 37, 700])
+def test_infinite_window_values(dtype, n_local, budget):
+    """An infinity among the window's values gives its channel an infinity wherever it stands, in the newest row too,
+    which a last tile that it does not fill repeats; other channels keep their bits."""
+    rng = np.random.default_rng(n_local + budget)
+    s, g, rows, window, start, dt = 3, 4, 800, 64, 21, DT[dtype]
+    codes, scales = (x.to(DEV) for x in pool_of(rng, s, rows))
+    sel = torch.from_numpy(rng.integers(0, rows, (s, budget)).astype(np.int32)).to(DEV)
+    n_sel = torch.full((s,), budget, dtype=torch.int32, device=DEV)
+    # scores stay within a few units: no weight is lost beside another
+    q = torch.from_numpy(0.1 * rng.standard_normal((1, s * g, 128))).to(dt).to(DEV)
+    kl, vl = (torch.from_numpy(rng.standard_normal((s, window, 128))).to(dt).to(DEV) for _ in range(2))
+
+    def attend(v):
+        out, lse = torch.zeros(1, s * g, 128, device=DEV), torch.zeros(1, s * g, device=DEV)
+        L().sparse_decode_attn_rows_q4(q, s, codes, scales, sel, n_sel, kl, v, start, n_local, out, lse)
+        return out.view(s, g, 128), lse
+    ref, ref_lse = attend(vl)
+    assert torch.isfinite(ref).all()
+    for at in {0, n_local // 2, n_local - 1}:
+        slot, bad = (start + at) % window, vl.clone()
+        bad[1, slot, 3], bad[1, slot, 77], bad[2, slot, 127] = float("inf"), -float("inf"), float("nan")
+        out, lse = attend(bad)
+        assert (out[1, :, 3] == float("inf")).all() and (out[1, :, 77] == -float("inf")).all(), at
+        assert torch.isnan(out[2, :, 127]).all()
+        keep = torch.ones(s, 128, dtype=torch.bool, device=DEV)
+        keep[1, 3] = keep[1, 77] = keep[2, 127] = False
+        keep = keep[:, None].expand(s, g, 128)
+        assert torch.equal(out[keep], ref[keep]) and torch.equal(lse, ref_lse), at
+
+
 def test_attention_with_per_slice_windows():
     l = L()
     rng = np.random.default_rng(9)
