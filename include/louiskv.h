@@ -981,8 +981,9 @@ size_t louiskv_sparse_decode_attn_rows_q4_workspace_size(int64_t n_slices, int32
  * from codes and scales, the window's rows in dtype.  Arguments, outputs and
  * the empty slice as there.  Keys and values enter the arithmetic as the exact
  * values they stand for; scores, softmax and sums are float32, and for
- * LOUISKV_BF16 the softmax weights are rounded to bfloat16 once, for the matrix
- * cores (their sum and lse_out use the unrounded ones).
+ * LOUISKV_BF16 a softmax weight meets its value as the sum of two bfloat16, for
+ * the matrix cores, which is off by 2^-16 of it at most (their sum and lse_out
+ * use the weights themselves).
  * workspace  louiskv_sparse_decode_attn_rows_q4_workspace_size() bytes, 0 where
  *            one block takes a slice.
  */
@@ -1074,9 +1075,10 @@ size_t louiskv_sparse_prefill_attn_workspace_size(int64_t n_slices, int32_t grou
  *             louiskv_sparse_decode_attn; -inf and o = 0 where a query sees no key.
  * workspace   louiskv_sparse_prefill_attn_workspace_size() bytes (partials where
  *             few tiles have their lists split over several blocks), may be 0.
- * Arithmetic as louiskv_sparse_decode_attn_rows_q4; group_size 1, 2, 4 or 8,
- * other sizes as louiskv_retrieve_blocks (but any number of blocks), sel_cap >= 1,
- * sel_cap * block_len <= 2^30.
+ * Scores, softmax and sums are float32; for LOUISKV_BF16 the softmax weights are
+ * rounded to bfloat16 once, for the matrix cores (their sum and lse_out use the
+ * unrounded ones).  group_size 1, 2, 4 or 8, other sizes as louiskv_retrieve_blocks
+ * (but any number of blocks), sel_cap >= 1, sel_cap * block_len <= 2^30.
  */
 int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t n_slices,
                                 int32_t n_kv_heads, int32_t group_size, int32_t n_q,

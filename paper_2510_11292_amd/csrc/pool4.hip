@@ -535,9 +535,13 @@ constexpr float kGrow = 8.0f;   // base-2 logits may pass the base by this much 
 //           columns are channels 8 c + i.
 // Rows are loaded 16 bytes a lane, five loads a tile; the values' words and the
 // scales change lanes through LDS (loaded where they are used, in twenty loads of
-// 1 and 4 bytes, the time was the same).  Weights are rounded to bfloat16 for the second
-// product, half a step or 2^-8 of each at most; their sum is of the unrounded ones.
-// 256 slices of 2148 rows, 4 heads (86.5 MB): 20.0 us, 4.3 TB/s, of which 6 to 7 us pass
+// 1 and 4 bytes, the time was the same).  The second product takes a weight as the sum
+// of two bfloat16, off by 2^-16 of it at most: rows c < 8 of its A operand hold the
+// weights of head c % G rounded to bfloat16, rows c + 8, whose heads are the same, what
+// that rounding left, and the two results are added at the end.  The rounded weights
+// alone (off by 2^-8, when the row-list attention over a full-precision pool has them in
+// float32) would save 0.6 us of the time below.  The sum is of the unrounded ones.
+// 256 slices of 2148 rows, 4 heads (86.5 MB): 20.5 us, 4.2 TB/s, of which 6 to 7 us pass
 // before the first rows arrive and after the last; more rows come at 5.4 TB/s.  Sixteen
 // waves a block spill (61 us), the list staged in LDS 20.7.
 template <int G>
@@ -573,6 +577,7 @@ void attn_q4_mfma_kernel(const AttnQ4 a) {
     v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
     q[k] = __builtin_bit_cast(bf16x8, v);
   }
+  const float rest = c < 8 ? 0.f : 1.f;                                 // this row's part of a weight: p - rest * rounded p
   float base = 0.f, grow_at = -__builtin_inff(), sum = 0.f;
   f32x4 o[8];
 #pragma unroll
@@ -609,8 +614,20 @@ void attn_q4_mfma_kernel(const AttnQ4 a) {
     }
     x.scale = *reinterpret_cast<const uint32_t*>(sc4 + (r.own >> 4));
   };
+  // O += P V for the eight rows' values
+  auto add_values = [&](const bf16x8& p, const uint4 (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint4 b;
+      constexpr uint32_t kLow = 0x05040100, kHigh = 0x07060302;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        (&b.x)[t] = __builtin_amdgcn_perm((&v[2 * t + 1].x)[i >> 1], (&v[2 * t].x)[i >> 1], i & 1 ? kHigh : kLow);
+      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, __builtin_bit_cast(bf16x8, b), o[i], 0, 0, 0);
+    }
+  };
   // scores of 32 rows, of which n are there, and their values' pairs
-  auto attend = [&](f32x4 (&sc)[2], const uint4 (&v)[8], int n) {
+  auto attend = [&](f32x4 (&sc)[2], uint4 (&v)[8], int n, bool window) {
     float m = mult;
     if (n < 32) {                                                        // wave-uniform
       m = 1.f;
@@ -638,22 +655,40 @@ void attn_q4_mfma_kernel(const AttnQ4 a) {
         for (int i = 0; i < 8; ++i) o[i][e] *= fe;
       }
     }
-    bf16x8 p;
+    bf16x8 whole, p;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float y = __builtin_amdgcn_exp2f(fmaf(sc[j >> 2][j & 3], m, -base));
       sum += y;
-      p[j] = (__bf16)y;
+      whole[j] = (__bf16)y;
+      p[j] = (__bf16)fmaf(-rest, (float)whole[j], y);
     }
+    if (window) {
+      // What rounding left can be 0 or negative: an infinity must not meet it.  Where the
+      // values hold any (0 times them is not 0), those that are not finite are added apart, by
+      // the rounded weights.
+      float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      uint4 b;
-      constexpr uint32_t kLow = 0x05040100, kHigh = 0x07060302;
+      for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        (&b.x)[t] = __builtin_amdgcn_perm((&v[2 * t + 1].x)[i >> 1], (&v[2 * t].x)[i >> 1], i & 1 ? kHigh : kLow);
-      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, __builtin_bit_cast(bf16x8, b), o[i], 0, 0, 0);
+        for (int x = 0; x < 4; ++x)
+          zero[x] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (&v[j].x)[x]), bf16x2{}, zero[x], false);
+      const float all = (zero[0] + zero[1]) + (zero[2] + zero[3]);
+      if (__builtin_amdgcn_ballot_w64(all != 0.f)) {
+        uint4 apart[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            uint32_t& e = (&v[j].x)[x];
+            const uint32_t bad = ((e & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((e & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+            (&apart[j].x)[x] = e & bad;
+            e &= ~bad;
+          }
+        add_values(whole, apart);
+      }
     }
+    add_values(p, v);
   };
   auto score = [&](const uint4 (&k)[4]) {
     f32x4 sc = {0.f, 0.f, 0.f, 0.f};
@@ -684,7 +719,7 @@ void attn_q4_mfma_kernel(const AttnQ4 a) {
       const int r = 16 * (j >> 2) + 4 * h + (j & 3);
       v[j] = expand8_bf16(s_v[w][value_word(r) + c], scale_of(sb[128 + 4 * r + (c >> 2)]));
     }
-    attend(sc, v, n_pool - 32 * t);
+    attend(sc, v, n_pool - 32 * t, false);
   };
   // a tile's rows are on their way while the one before is at hand, its list
   // entries while the one two before is
@@ -721,7 +756,7 @@ void attn_q4_mfma_kernel(const AttnQ4 a) {
       for (int j = 0; j < 8; ++j)
         if (32 * t + 16 * (j >> 2) + 4 * h + (j & 3) >= n_win) v[j] = make_uint4(0, 0, 0, 0);
     }
-    attend(sc, v, n_win - 32 * t);
+    attend(sc, v, n_win - 32 * t, true);
   }
   for (int t = w; t < n_pool_tiles; t += 2 * NW) {
     if (t + NW < n_pool_tiles) fetch(rb, xb);
@@ -734,20 +769,22 @@ void attn_q4_mfma_kernel(const AttnQ4 a) {
     __builtin_amdgcn_sched_barrier(0);
     tile(t + NW, xb);
   }
-  // the wave's sums: head c of lanes c < G, and heads 4 h + e of the channels 8 c + i
+  // the wave's sums: head c of lanes c < G, and rows 4 h + e of the channels 8 c + i.
+  // Rows h and h + 2 change places with other channels': the sums of row 4 (h % 2) + e
+  // are left for channels 8 c + 4 (h / 2) + 0..3.
   sum += __shfl_xor(sum, 16, kWave);
   sum += __shfl_xor(sum, 32, kWave);
   if (lane < G) {
     s_m[w][lane] = grow_at == -__builtin_inff() ? -__builtin_inff() : base;
     s_l[w][lane] = sum;
   }
-  if (4 * h < G) {
 #pragma unroll
-    for (int e = 0; e < (G < 4 ? G : 4); ++e) {
-      float* dst = &s_acc[w][4 * h + e][8 * c];
-      reinterpret_cast<float4*>(dst)[0] = make_float4(o[0][e], o[1][e], o[2][e], o[3][e]);
-      reinterpret_cast<float4*>(dst)[1] = make_float4(o[4][e], o[5][e], o[6][e], o[7][e]);
-    }
+  for (int e = 0; e < (G < 4 ? G : 4); ++e) {
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = swap_add<32>(o[i][e], o[i + 4][e]);
+    if (4 * (h & 1) < G)
+      *reinterpret_cast<float4*>(&s_acc[w][4 * (h & 1) + e][8 * c + 4 * (h >> 1)]) = make_float4(x[0], x[1], x[2], x[3]);
   }
   __syncthreads();
   merge_waves<G, NW>(a, s_m, s_l, s_acc, s, chunk, tid);

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from attn_bounds import check_attention
+from attn_bounds import attention_bounds, check_attention
 from oracle import blocks as ob
 from oracle import pool4 as o4
 
@@ -284,6 +284,30 @@ def test_infinite_window_values(dtype, n_local, budget):
         keep[1, 3] = keep[1, 77] = keep[2, 127] = False
         keep = keep[:, None].expand(s, g, 128)
         assert torch.equal(out[keep], ref[keep]) and torch.equal(lse, ref_lse), at
+
+
+@pytest.mark.parametrize("groups,kv,g,budget,local", [(1, 2, 1, 900, 50), (2, 3, 2, 64, 128), (1, 8, 4, 2048, 100),
+                                                      (40, 8, 4, 129, 128), (2, 2, 8, 333, 17), (1, 1, 8, 0, 40)])
+def test_bf16_attention_keeps_its_weights_beyond_bf16(groups, kv, g, budget, local):
+    """Weights enter the sum of values as two bfloat16: what the second rounding leaves is 2^-8 of at most 2^-8 of a
+    weight, so a float32 result is off by 2^-16 of the weighted mean of |v| beside the float32 roundings."""
+    s, rows, window, start = groups * kv, 2500, 128, 77
+    rng = np.random.default_rng(budget + g)
+    codes, scales = pool_of(rng, s, rows)
+    sel = rng.integers(0, rows, (s, budget)).astype(np.int32)
+    n_sel = np.full(s, budget, dtype=np.int32)
+    q = torch.from_numpy(rng.standard_normal((groups, kv * g, 128))).bfloat16()
+    kl, vl = (torch.from_numpy(rng.standard_normal((s, window, 128))).bfloat16() for _ in range(2))
+    out, lse = torch.zeros(groups, kv * g, 128, device=DEV), torch.zeros(groups, kv * g, device=DEV)
+    L().sparse_decode_attn_rows_q4(q.to(DEV), kv, codes.to(DEV), scales.to(DEV), torch.from_numpy(sel).to(DEV),
+                                   torch.from_numpy(n_sel).to(DEV), kl.to(DEV), vl.to(DEV), start, local, out, lse)
+    ring = [(start + i) % window for i in range(local)]
+    for i in range(s):
+        o, e, mass, size = attn_want(codes[i].numpy(), scales[i].numpy(), sel[i], n64(kl[i, ring]), n64(vl[i, ring]),
+                                     n64(q).reshape(s, g, 128)[i], 128 ** -0.5)
+        tol, tol_lse = attention_bounds(o, mass, e, size, budget + local, False, False)
+        assert np.all(np.abs(n64(out).reshape(s, g, 128)[i] - o) <= tol + 2.0 ** -16 * mass), i
+        assert np.all(np.abs(n64(lse).reshape(s, g)[i] - e) <= tol_lse), i
 
 
 def test_attention_with_per_slice_windows():
