@@ -766,7 +766,9 @@ def segment_output_boundary_q4(k_new, v_new, k_local, v_local, step: int, seg_ma
     rows = _pool_q4(codes, scales, s) if codes is not None else 0
     window, cap = k_local.shape[1], reps.shape[1]
     _store_sizes(k_new, v_new, k_local, v_local, window, reps, unit_start, unit_size, cap)
-    _native().expect("seg_state", seg_state, (s, segment_state_ints(window)), torch.int32)
+    boolean = fire is not None and fire.dtype is torch.bool      # bytes 0 and 1, as uint8 holds them
+    _native().expect("seg_state", seg_state, (s, segment_state_ints(window)), torch.int32,
+                     "fire", fire, (s // max(n_kv_heads, 1),), torch.bool if boolean else torch.uint8)
     _check(_native().segment_output_boundary_q4(
         k_new, v_new, _dtype_code(k_new), s, n_kv_heads, d, k_local, v_local, window, step, seg_max, fire, seg_state,
         reps, unit_start, unit_size, cap, n_clusters, codes, scales, rows, prompt_len, stream))

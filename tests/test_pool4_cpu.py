@@ -291,6 +291,28 @@ def test_python_calls_refuse_sizes_types_and_host_memory():
             call()
 
 
+def test_boundary_store_checks_the_groups_decisions():
+    """fire holds a byte for each group: fewer would be read past their end, wider numbers as the wrong bytes."""
+    from paper_2510_11292_amd import louiskv as L
+    i32, u8 = dict(dtype=torch.int32), dict(dtype=torch.uint8)
+    new, loc, reps, table = torch.zeros(6, 128), torch.zeros(6, 4, 128), torch.zeros(6, 6, 128), torch.zeros(6, 6, **i32)
+
+    def store(fire):
+        L.segment_output_boundary_q4(new, new, loc, loc, 0, 2, fire, torch.zeros(6, 12, **i32), reps, table, table, 3, 2,
+                                     stream=0)
+    for n in (0, 2, 4, 6):
+        with pytest.raises(ValueError, match="fire.*expected"):
+            store(torch.zeros(n, **u8))
+    with pytest.raises(ValueError, match="fire.*expected"):
+        store(torch.zeros(3, 1, **u8))
+    for dtype in (torch.int32, torch.float32, torch.int8):
+        with pytest.raises(TypeError, match="fire.*uint8"):
+            store(torch.zeros(3, dtype=dtype))
+    for fire in (None, torch.zeros(3, **u8), torch.zeros(3, dtype=torch.bool)):   # host memory is what is left to refuse
+        with pytest.raises(ValueError, match="current device"):
+            store(fire)
+
+
 def test_engine_refuses_what_a_4_bit_pool_is_not_built_for():
     from paper_2510_11292_amd.engine import EngineConfig, LouisKVEngine
     cfg = EngineConfig(n_slices=2, n_kv_heads=2, n_q_heads=8, prompt_len=64, n_clusters=4, n_iters=1, gen_len=8,
