@@ -385,11 +385,11 @@ class LouisKVEngine:
         s, n, d = keys.shape
         n_q = q.shape[2]
         i32 = dict(dtype=torch.int32, device=q.device)
-        n_blocks = -(-n // block_len)
         cap = L.retrieve_blocks_cap(n, q_block, block_len, n_first, n_recent, n_top)
         if cap < 1:
             raise ValueError(f"block_len={block_len} q_block={q_block} n_first={n_first} n_recent={n_recent} "
                              f"n_top={n_top}")
+        n_blocks = -(-n // block_len)
         reps = torch.empty(s, n_blocks, d, dtype=torch.float32, device=q.device)
         spans = torch.empty(2, s, n_blocks, **i32)
         L.page_prefill(keys, block_len, reps, spans[0], spans[1])

@@ -322,3 +322,17 @@ def test_engine_refuses_what_a_4_bit_pool_is_not_built_for():
                dict(pool_bits=4, delta=True)):
         with pytest.raises(ValueError, match="4-bit pool|pool_bits"):
             LouisKVEngine(cfg, torch.bfloat16, "cpu", **kw)
+
+
+def test_prompt_attention_refuses_its_sizes():
+    from paper_2510_11292_amd.engine import EngineConfig, LouisKVEngine
+    cfg = EngineConfig(n_slices=2, n_kv_heads=2, n_q_heads=8, prompt_len=64, n_clusters=4, n_iters=1, gen_len=8,
+                       seg_len=4, budget=16, window=8, tau=0.9)
+    eng = LouisKVEngine(cfg, torch.float32, "cpu")
+    q, k = torch.zeros(1, 8, 64, 128), torch.zeros(2, 64, 128)
+    for kw in (dict(block_len=0), dict(block_len=-64), dict(block_len=48), dict(q_block=0), dict(q_block=129),
+               dict(n_first=-1), dict(n_recent=-1), dict(n_top=-1)):
+        with pytest.raises(ValueError, match="block_len="):
+            eng.prompt_attention(q, k, k, **kw)
+    with pytest.raises(ValueError, match="block_len="):
+        eng.prompt_attention(q, k[:, :0], k[:, :0])
