@@ -14,7 +14,8 @@
 //              the current device's memory
 //   stream     the last parameter(s): None (the current stream), a
 //              torch.cuda.Stream or a handle
-//   numbers    int, bool or float
+//   numbers    int, bool or float; an int that a 32-bit parameter cannot hold is
+//              refused rather than cut to its lower bits
 // The status (or size) comes back as an int, text as a str; the GIL is released
 // for the call.
 #include <torch/csrc/Dtype.h>
@@ -93,7 +94,12 @@ T convert(PyObject* o, bool stream) {
     if (v == -1.0 && PyErr_Occurred()) throw PyError();
     return (T)v;
   } else {
-    return (T)to_int(o);
+    const int64_t v = to_int(o);
+    if (sizeof(T) < sizeof(int64_t) && (int64_t)(T)v != v) {
+      PyErr_Format(PyExc_OverflowError, "%lld does not fit a %d-bit argument", (long long)v, (int)(8 * sizeof(T)));
+      throw PyError();
+    }
+    return (T)v;
   }
 }
 

@@ -336,3 +336,21 @@ def test_prompt_attention_refuses_its_sizes():
             eng.prompt_attention(q, k, k, **kw)
     with pytest.raises(ValueError, match="block_len="):
         eng.prompt_attention(q, k[:, :0], k[:, :0])
+
+
+def test_numbers_that_an_argument_cannot_hold_are_refused():
+    """Cut to 32 bits, a token count of 2^32 + 100 would be one of 100."""
+    from paper_2510_11292_amd import louiskv as L
+    big = 1 << 32
+    assert L.retrieve_blocks_cap((1 << 31) - 1, 64, 64, 1, 4, 24) == 31
+    for args in ((big + 100, 64, 64, 1, 4, 24), (100, 64, big + 64, 1, 4, 24), (100, 64, 64, 1, 4, 1 << 31),
+                 (-big + 100, 64, 64, 1, 4, 24)):
+        with pytest.raises(OverflowError, match="32-bit"):
+            L.retrieve_blocks_cap(*args)
+    q, k = torch.zeros(1, 4, 7, 128), torch.zeros(2, 10, 128)
+    lists = torch.zeros(2, 1, 3, dtype=torch.int32), torch.zeros(2, 1, dtype=torch.int32)
+    with pytest.raises(OverflowError, match="32-bit"):
+        L.sparse_prefill_attn(q, 2, k, k, big + 10, 3, 16, 16, *lists, q, workspace=k, stream=0)
+    with pytest.raises(OverflowError, match="32-bit"):
+        L.sparse_prefill_attn(q, 2, k, k, 10, big + 3, 16, 16, *lists, q, workspace=k, stream=0)
+    assert L.sparse_decode_attn_rows_q4_workspace_size(big + 8, 4, 100, 10) == 0     # 64 bits there: more slices than fit
