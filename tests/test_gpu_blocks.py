@@ -166,6 +166,19 @@ def test_later_keys_do_not_reach_a_query(dtype, tile, block, g):
                 assert torch.equal(out[..., 90:], ref[..., 90:]) and torch.equal(lse, ref_lse)
 
 
+@pytest.mark.parametrize("bits", [0x7fc00000, 0x7fffffff, -1, 0x7f800001])
+@pytest.mark.parametrize("n", [40, 600])     # whole lists, and lists in parts, whose merge rounds
+def test_a_nan_of_any_bits_stays_one_in_a_bf16_output(bits, n):
+    q, keys, values = torch.randn(1, 4, 40, 128, device=DEV), torch.randn(1, n, 128, device=DEV), torch.randn(1, n, 128, device=DEV)
+    values.view(torch.int32)[0, 7, 5] = torch.tensor(bits, dtype=torch.int32)
+    nb = -(-n // 16)
+    out, _ = run_attn(q, 1, keys, values, n, 64, 16, np.arange(nb, dtype=np.int32).reshape(1, 1, nb),
+                      np.full((1, 1), nb, dtype=np.int32), torch.bfloat16)
+    want = torch.zeros(1, 4, 40, 128, dtype=torch.bool, device=DEV)
+    want[..., max(0, 7 - (n - 40)):, 5] = True
+    assert torch.equal(torch.isnan(out), want)
+
+
 def test_scores_of_minus_infinity_weigh_nothing():
     q = torch.ones(1, 2, 40, 128, device=DEV).bfloat16()
     keys = torch.zeros(1, 40, 128, device=DEV).bfloat16()

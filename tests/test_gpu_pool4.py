@@ -310,6 +310,25 @@ def test_bf16_attention_keeps_its_weights_beyond_bf16(groups, kv, g, budget, loc
         assert np.all(np.abs(n64(lse).reshape(s, g)[i] - e) <= tol_lse), i
 
 
+@pytest.mark.parametrize("bits", [0x7fc00000, 0x7fffffff, -1, 0x7f800001, -0x7fffff])
+@pytest.mark.parametrize("budget", [1, 900])     # one block a slice and several, whose merge rounds
+def test_a_nan_of_any_bits_stays_one_in_a_bf16_output(bits, budget):
+    s, g, rng = 2, 4, np.random.default_rng(2)
+    codes, scales = (x.to(DEV) for x in pool_of(rng, s, 50))
+    nan = torch.tensor([bits], dtype=torch.int32, device=DEV).view(torch.float32)
+    q = torch.randn(1, s * g, 128, device=DEV)
+    loc = torch.randn(s, 16, 128, device=DEV)
+    loc.view(torch.int32)[1, 7, 5] = nan.view(torch.int32)[0]
+    sel = torch.from_numpy(rng.integers(0, 50, (s, budget)).astype(np.int32)).to(DEV)
+    n_sel = torch.full((s,), budget, dtype=torch.int32, device=DEV)
+    kl = torch.randn(s, 16, 128, device=DEV)
+    out = torch.zeros(1, s * g, 128, dtype=torch.bfloat16, device=DEV)
+    L().sparse_decode_attn_rows_q4(q, s, codes, scales, sel, n_sel, kl, loc, 0, 16, out)
+    want = torch.zeros(s, g, 128, dtype=torch.bool, device=DEV)
+    want[1, :, 5] = True
+    assert torch.equal(torch.isnan(out.view(s, g, 128)), want)
+
+
 def test_attention_with_per_slice_windows():
     l = L()
     rng = np.random.default_rng(9)
