@@ -909,8 +909,10 @@ int louiskv_sparse_decode_attn_rows_per_head(const void* q, int32_t dtype, int64
  * Limit       pool_rows <= LOUISKV_Q4_MAX_POOL_ROWS (LOUISKV_ERR_SHAPE); a list and
  *             the window of one slice together at most twice that.
  * Alignment   of these calls' and the block calls' element buffers (queries,
- *             keys, values, windows, index vectors of the blocks, workspaces): 16
- *             bytes (LOUISKV_ERR_UNSUPPORTED, LOUISKV_ERR_WORKSPACE).
+ *             keys, values, windows, index vectors of the blocks, workspaces,
+ *             the outputs of louiskv_gather_rows_q4 and
+ *             louiskv_sparse_prefill_attn): 16 bytes (LOUISKV_ERR_UNSUPPORTED,
+ *             LOUISKV_ERR_WORKSPACE).
  */
 #define LOUISKV_Q4_MAX_POOL_ROWS (1 << 24)
 

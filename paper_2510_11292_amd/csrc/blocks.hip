@@ -278,20 +278,28 @@ constexpr float kGrow = 8.0f;   // base-2 logits may pass the base by this much 
 // 16 scores of one query row; their exponentials are, unmoved, the B operand of
 // O^T += V^T P^T, whose A operand comes from LDS through transposing reads.  The
 // running base, sum and the rescale are then a lane's own; the sums are rescaled
-// only where a score passes the base by 2^8.
+// only where a score passes the base by 2^8.  The exponentials are rounded to bfloat16
+// for that product, 2^-8 of each at most, while their sum takes them unrounded: unlike in
+// the decode attention no column of the product is idle, and what the rounding leaves
+// would cost a second one, half as many products again (results are off by 2.0e-3 of
+// their size; the rounding of a bfloat16 result alone is 1.7e-3 of it).
 // float32: the same with 32 positions a stage and products of two channels or keys
-// at a time, k index = half of the wave; the scores need no rounding.
+// at a time, k index = half of the wave; the weights need no rounding.  The kernels for
+// 256 and 128 rows keep 26 and 30 registers in scratch memory; the loop's reloads wait for
+// the copies in flight as well (vmcnt counts in order), which undoes the overlap of
+// copies and products in part.
 //
 // A layer of 32K tokens (8 slices x 512 tiles of 256 rows, 30 blocks of 64 keys, 985
-// GFLOP): 1.10 ms, 0.89 PFLOP/s, where a large product reaches 1.35; in float32 a layer
-// of 8192 tokens 2.0 ms, 114 TFLOP/s of 153.  For each 32 rows by 32 keys a wave has 16
-// products (512 cycles), 16 exponentials and 80 other vector operations, and reads
-// 16 KB of LDS.  Two waves of a SIMD alternate between them, and overlap in part: the
-// same instructions without a dependency between the pairs take 1.02 ms, the
-// products and LDS reads alone 0.74.  64 rows a wave would halve the LDS reads, but its
-// accumulators do not fit beside the rest (copies between the register files:
-// 1.60 ms); phases kept apart by barriers 1.35 ms, a maximum over 64 keys at a time
-// 1.16, the next 32 keys' scores between the exponentials 1.11 to 1.13.
+// GFLOP): 1.10 to 1.19 ms, 0.89 to 0.83 PFLOP/s, on parts where a large product reaches
+// 1.35 and 1.30; in float32 a layer of 8192 tokens 1.92 ms, 117 TFLOP/s of 154.  For each
+// 32 rows by 32 keys a wave has 16 products (512 cycles), 16 exponentials and 80 other
+// vector operations, and reads 16 KB of LDS.  Two waves of a SIMD alternate between them,
+// and overlap in part: where the layer took 1.10 ms, the same instructions without a
+// dependency between the pairs took 1.02, the products and LDS reads alone 0.74.  64 rows
+// a wave would halve the LDS reads, but its accumulators do not fit beside the rest (copies
+// between the register files: 1.60 ms); phases kept apart by barriers 1.35 ms, a maximum
+// over 64 keys at a time 1.16, the next 32 keys' scores between the exponentials 1.11 to
+// 1.13.
 constexpr int kStageBytes = 16384;   // of the keys, and of the values
 
 template <class T, int WR, int WK>

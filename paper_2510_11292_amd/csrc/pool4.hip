@@ -176,8 +176,9 @@ constexpr int kNUnits = 0, kWinFirst = 1, kHead = 2, kCount = 3, kOverflow = 4, 
 // a time.  The rows of the segment that leaves go to the pool and into eight
 // float64 partial means per channel, then the new token enters its slot, which
 // is the first of the rows that left: the barrier and the wait before it keep
-// every wave's reads ahead of that write.  Bound by latency: 8 slices with a segment
-// of 32 tokens 4.4 us, 1024 slices (32 MB) 6.6 us.
+// every wave's reads ahead of that write.  Bound by latency: a lane group's rows, four of
+// a segment of 32, are read one after another, each read behind the stores of the row
+// before (8 slices with a segment of 32 tokens 4.4 us, 1024 slices, 22 MB, 6.9 us).
 template <class T, bool kSeg>
 __global__ __launch_bounds__(256)
 void store_q4_kernel(const T* __restrict__ k_new, const T* __restrict__ v_new, T* __restrict__ k_local,
@@ -541,9 +542,11 @@ constexpr float kGrow = 8.0f;   // base-2 logits may pass the base by this much 
 // that rounding left, and the two results are added at the end.  The rounded weights
 // alone (off by 2^-8, when the row-list attention over a full-precision pool has them in
 // float32) would save 0.6 us of the time below.  The sum is of the unrounded ones.
-// 256 slices of 2148 rows, 4 heads (86.5 MB): 20.5 us, 4.2 TB/s, of which 6 to 7 us pass
-// before the first rows arrive and after the last; more rows come at 5.4 TB/s.  Sixteen
-// waves a block spill (61 us), the list staged in LDS 20.7.
+// 256 slices of 2148 rows, 4 heads (86.5 MB): 20.6 us, 4.2 TB/s; of 4196 rows 32.9 us, so
+// that some 8 us pass before the first rows arrive and after the last and the others come
+// at 6.0 TB/s; of 8292 rows (307 MB, more than the last cache holds) 67 us.  Sixteen waves
+// a block spill (61 us for 20.0, with the weights rounded once), the list staged in LDS
+// is no faster (20.7).
 template <int G>
 __global__ __launch_bounds__(kAttnWaves * 64)
 void attn_q4_mfma_kernel(const AttnQ4 a) {
@@ -791,10 +794,10 @@ void attn_q4_mfma_kernel(const AttnQ4 a) {
 }
 
 // Chunks of a slice's rows: blocks for the chip, with the rows that a block has in
-// flight at once: in bfloat16 a half tile a wave (8 slices of 2148 rows, attention
-// alone: 128 rows a block 5.8 us, 256 rows 7.0; 256 slices: one chunk 20 us, two and
-// their merge 25), in float32 two rows a group (8 slices of 2148 rows with the merge:
-// 64 rows a block 9.7 us, 128 rows 10.3).
+// flight at once: in bfloat16 a half tile a wave (8 slices of 2148 rows with the merge:
+// 128 rows a block 8.9 us, 256 rows 9.3; 256 slices: one chunk 20.6 us, two and their
+// merge 27.1), in float32 two rows a group (8 slices of 2148 rows with the merge: 64 rows
+// a block 9.8 us, 128 rows 10.5).
 constexpr int kTargetBlocks = 256;
 int attn_q4_chunks(int64_t S, int budget, int window, int dtype) {
   const int min_rows = dtype == LOUISKV_BF16 ? 128 : 64;

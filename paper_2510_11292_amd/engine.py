@@ -380,7 +380,11 @@ class LouisKVEngine:
         """Causal attention of the prompt tokens q_start .. q_start + n_q - 1 (q [G][Hq][n_q][d]) over selected
         blocks of the keys and values so far ([S][n][d], n >= q_start + n_q): every tile of q_block queries
         attends to the first n_first blocks of block_len keys, its own and the n_recent before them, and the n_top
-        others with the largest scores of their mean keys.  Returns out [G][Hq][n_q][d] (allocated if not given)."""
+        others with the largest scores of their mean keys.  Returns out [G][Hq][n_q][d] (allocated if not given).
+
+        keys and values may be whole buffers that later chunks are written to: rows behind a query never reach its
+        result, whatever they hold.  Every call computes the mean keys of all n rows; a caller that has many short
+        chunks or single tokens keeps them and calls louiskv.retrieve_blocks and louiskv.sparse_prefill_attn itself."""
         h = self.cfg.n_kv_heads
         s, n, d = keys.shape
         n_q = q.shape[2]

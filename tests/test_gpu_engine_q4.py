@@ -154,3 +154,20 @@ def test_prompt_attention(dtype):
     assert (sparse.float() - dense.float()).abs().max() > tol
     with pytest.raises(ValueError):
         eng.prompt_attention(q, keys, values, block_len=48)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_prompt_attention_over_a_buffer_that_is_still_filling(dtype):
+    """Rows behind the queries, here NaN and infinities, change nothing: chunks and tokens read one whole buffer."""
+    wl, data, mk = engines(dtype)
+    eng = mk(pool_bits=4)
+    c = eng.cfg
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    q = torch.randn(c.n_groups, c.n_q_heads, c.prompt_len, 128, generator=gen, device=DEV).to(dtype)
+    kw = dict(block_len=32, q_block=32, n_top=4, n_recent=1)
+    for a, b in ((320, 451), (451, 452), (500, 600)):
+        keys, values = data.prompt_keys.clone(), data.prompt_values.clone()
+        keys[:, b:], values[:, b:] = float("nan"), float("inf")
+        qc = q[:, :, a:b].contiguous()
+        short = eng.prompt_attention(qc, keys[:, :b].contiguous(), values[:, :b].contiguous(), a, **kw)
+        assert torch.isfinite(short).all() and torch.equal(eng.prompt_attention(qc, keys, values, a, **kw), short), (a, b)
