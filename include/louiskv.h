@@ -31,6 +31,11 @@
  *   louiskv_retrieve_blocks, louiskv_sparse_prefill_attn
  *                               the prompt's own attention over selected blocks
  *                               of its keys
+ *   louiskv_shared_prefix_attn  attention of sequences that share a prefix, or
+ *                               over caches of bounded size
+ *   louiskv_attn_weights, louiskv_evict_rows, louiskv_store_evict
+ *                               such a cache: it keeps the rows that gathered the
+ *                               most attention weight
  *
  * Conventions shared by every call
  * --------------------------------
@@ -1091,6 +1096,144 @@ int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t n_slices,
                                 const int32_t* n_sel_blocks, void* out, int32_t out_dtype,
                                 float* lse_out, void* workspace, size_t workspace_bytes,
                                 void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Sequences that share a prefix, and caches of bounded size                  */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Sequences that continue one prefix (samples of one prompt, questions about one
+ * document) attend to its rows, which are held and read once for all of them, and
+ * to rows of their own.  A sequence's own rows can be a cache of bounded size, from
+ * which the rows of least accumulated attention weight leave; with prefix_rows = 0
+ * that is all there is.  Own rows lie in any order of positions, but those of the
+ * last tokens come last, in order.
+ *
+ * Alignment   of these calls' element buffers (queries, keys, values, outputs) and
+ *             workspaces: 16 bytes (LOUISKV_ERR_UNSUPPORTED, LOUISKV_ERR_WORKSPACE).
+ * Limits      group_size 1 to 8; rows of a slice, and queries of all sequences
+ *             that share a prefix slice (times group_size): at most 2^30.
+ */
+
+size_t louiskv_shared_prefix_attn_workspace_size(int64_t n_slices, int64_t n_prefix_slices,
+                                                 int32_t group_size, int32_t n_q, int32_t d,
+                                                 int64_t prefix_rows, int64_t own_rows,
+                                                 int32_t with_weights);
+
+/*
+ * Attention of the last n_q tokens of every sequence (n_q = 1: a decode step):
+ * o = softmax(q [K_prefix : K_own]^T * scale) [V_prefix : V_own].  Query t of slice s
+ * sees the rows 0..n_prefix-1 of prefix slice s % n_prefix_slices (slices are ordered
+ * sequence by sequence, so that this is the slice's layer and KV head) and its own
+ * rows 0..n_own[s]-n_q+t.
+ *
+ * q           [n_groups][n_kv_heads*group_size][n_q][d] dtype.
+ * k_prefix, v_prefix [n_prefix_slices][prefix_rows][d] dtype; NULL, and
+ *             n_prefix_slices not looked at, with prefix_rows = 0.  n_prefix_slices
+ *             is a multiple of n_kv_heads that divides n_slices.
+ * n_prefix    [n_prefix_slices] int32 (clamped into [0, prefix_rows]), or NULL:
+ *             prefix_rows.
+ * k_own, v_own [n_slices][own_rows][d] dtype; NULL with own_rows = 0.
+ * n_own       [n_slices] int32 (clamped into [0, own_rows]), or NULL: own_rows.
+ * weights     in/out [n_slices][own_rows] float32 or NULL: to the entry of every own
+ *             row the sum over the queries that see it and the group's heads of its
+ *             softmax weight is added.  Entries from n_own on are left alone.
+ * out         [n_groups][n_kv_heads*group_size][n_q][d] in out_dtype.
+ * lse_out     [n_groups][n_kv_heads*group_size][n_q] float32 or NULL, as
+ *             louiskv_sparse_decode_attn; -inf and o = 0 where a query sees no row.
+ * Rows that a query does not see do not reach its result, whatever they hold.
+ * Scores, softmax, sums and weights are float32; for LOUISKV_BF16 the softmax
+ * weights meet the values rounded to bfloat16, for the matrix cores (their sums,
+ * lse_out and `weights` use the unrounded ones).
+ * workspace   louiskv_shared_prefix_attn_workspace_size() bytes, may be 0;
+ *             with_weights != 0 where weights are given.
+ */
+int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t n_slices,
+                               int32_t n_kv_heads, int32_t group_size, int32_t n_q,
+                               int32_t d, float scale, const void* k_prefix,
+                               const void* v_prefix, int64_t n_prefix_slices,
+                               int64_t prefix_rows, const int32_t* n_prefix,
+                               const void* k_own, const void* v_own, int64_t own_rows,
+                               const int32_t* n_own, float* weights, void* out,
+                               int32_t out_dtype, float* lse_out, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+size_t louiskv_attn_weights_workspace_size(int64_t n_slices, int32_t group_size, int32_t n_q,
+                                           int32_t d, int64_t key_rows);
+
+/*
+ * The attention weight that the last n_q tokens give to each key, from any
+ * attention's lse: weights[s][i] += the sum over the group's heads and the queries t
+ * that see row i (i <= n_keys[s] - n_q + t) of exp(q . k_i * scale - lse), float32.
+ * A query whose lse is -inf adds nothing.
+ *
+ * q           [n_groups][n_kv_heads*group_size][n_q][d] dtype.
+ * keys        [n_slices][key_rows][d] dtype.
+ * n_keys      [n_slices] int32 (clamped into [0, key_rows]), or NULL: key_rows.
+ * lse         [n_groups][n_kv_heads*group_size][n_q] float32.
+ * weights     in/out [n_slices][key_rows] float32; entries from n_keys on are left
+ *             alone.
+ * workspace   louiskv_attn_weights_workspace_size() bytes, may be 0.
+ */
+int louiskv_attn_weights(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads,
+                         int32_t group_size, int32_t n_q, int32_t d, float scale,
+                         const void* keys, int64_t key_rows, const int32_t* n_keys,
+                         const float* lse, float* weights, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+size_t louiskv_evict_rows_workspace_size(int64_t n_slices, int64_t rows, int64_t n_keep);
+
+/*
+ * Of each slice's n rows m = min(n, n_keep) stay: those with a position below n_first
+ * or from n_seen - n_recent on, then the ones of largest weight, equal weights the
+ * higher row; a NaN counts as less than every number.  (Should more than m rows have
+ * protected positions, the higher rows stay.)  Row i < m of the smaller cache is
+ * row i if that stays, otherwise the k-th staying row from m on, where i is the k-th
+ * row below m that leaves: in place nothing else moves.
+ *
+ * weights     [n_slices][rows] float32.
+ * pos, n_seen [n_slices][rows] and [n_slices] int32: each row's position and the
+ *             tokens so far; both NULL: a row's number, and n.
+ * n_rows      [n_slices] int32 (clamped into [0, rows]), or NULL: rows.
+ * k, v        [n_slices][rows][d] dtype.
+ * k_to, v_to  out [n_slices][rows_to][d] dtype, weights_to, pos_to [n_slices][rows_to]
+ *             float32 and int32 (each may be NULL): rows 0..m-1 are written, others
+ *             stay as they were.  Each is the buffer that it is taken from
+ *             (rows_to = rows then) or one that does not overlap any other.
+ * n_rows_to   out [n_slices] int32: m.  May be n_rows.
+ * Requires 0 <= n_first + n_recent <= n_keep <= rows_to and n_keep >= 1.
+ * workspace   louiskv_evict_rows_workspace_size() bytes.
+ */
+int louiskv_evict_rows(const float* weights, const int32_t* pos, const int32_t* n_rows,
+                       const int32_t* n_seen, int32_t dtype, int64_t n_slices, int32_t d,
+                       int64_t rows, int64_t n_keep, int32_t n_first, int32_t n_recent,
+                       const void* k, const void* v, void* k_to, void* v_to,
+                       float* weights_to, int32_t* pos_to, int64_t rows_to,
+                       int32_t* n_rows_to, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
+size_t louiskv_store_evict_workspace_size(int64_t n_slices, int64_t rows, int32_t n_new,
+                                          int64_t budget);
+
+/*
+ * n_new tokens enter each slice's cache of at most `budget` rows:
+ * louiskv_evict_rows in place to budget - n_new rows, then the new rows behind those
+ * that stay, in order, with weight 0 and the positions n_seen, n_seen + 1, ...
+ *
+ * k_new, v_new [n_slices][n_new][d] dtype.
+ * k, v        in/out [n_slices][rows][d] dtype; weights, pos in/out [n_slices][rows].
+ * n_rows      in/out [n_slices] int32: rows held, then min(n_rows, budget - n_new) + n_new.
+ * n_seen      in/out [n_slices] int32: tokens so far, then n_new more (below 2^31).
+ *             Both 0 before the first call.  The counts are on the device, so that
+ *             a captured call stores the next token at every replay.
+ * Requires n_new >= 1, 0 <= n_first + n_recent <= budget - n_new, budget <= rows.
+ * workspace   louiskv_store_evict_workspace_size() bytes, may be 0.
+ */
+int louiskv_store_evict(const void* k_new, const void* v_new, int32_t dtype,
+                        int64_t n_slices, int32_t n_new, int32_t d, void* k, void* v,
+                        float* weights, int32_t* pos, int32_t* n_rows, int32_t* n_seen,
+                        int64_t rows, int64_t budget, int32_t n_first, int32_t n_recent,
+                        void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

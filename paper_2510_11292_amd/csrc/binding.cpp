@@ -259,6 +259,14 @@ PyMethodDef methods[] = {
     LKV_DEVICE_ENTRY(retrieve_blocks),
     LKV_ENTRY(sparse_prefill_attn_workspace_size, 0),
     LKV_DEVICE_ENTRY(sparse_prefill_attn),
+    LKV_ENTRY(shared_prefix_attn_workspace_size, 0),
+    LKV_DEVICE_ENTRY(shared_prefix_attn),
+    LKV_ENTRY(attn_weights_workspace_size, 0),
+    LKV_DEVICE_ENTRY(attn_weights),
+    LKV_ENTRY(evict_rows_workspace_size, 0),
+    LKV_DEVICE_ENTRY(evict_rows),
+    LKV_ENTRY(store_evict_workspace_size, 0),
+    LKV_DEVICE_ENTRY(store_evict),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -156,6 +156,19 @@ _SIGS = {
     "louiskv_sparse_prefill_attn": (ctypes.c_int, [
         _P, _I32, _I64, _I32, _I32, _I32, _I32, _F, _P, _P, _I64, _I32, _I32, _I32, _I32,
         _P, _I32, _P, _P, _I32, _P, _P, _SZ, _P]),
+    "louiskv_shared_prefix_attn_workspace_size": (_SZ, [_I64, _I64, _I32, _I32, _I32, _I64, _I64, _I32]),
+    "louiskv_shared_prefix_attn": (ctypes.c_int, [
+        _P, _I32, _I64, _I32, _I32, _I32, _I32, _F, _P, _P, _I64, _I64, _P, _P, _P, _I64, _P, _P,
+        _P, _I32, _P, _P, _SZ, _P]),
+    "louiskv_attn_weights_workspace_size": (_SZ, [_I64, _I32, _I32, _I32, _I64]),
+    "louiskv_attn_weights": (ctypes.c_int, [
+        _P, _I32, _I64, _I32, _I32, _I32, _I32, _F, _P, _I64, _P, _P, _P, _P, _SZ, _P]),
+    "louiskv_evict_rows_workspace_size": (_SZ, [_I64, _I64, _I64]),
+    "louiskv_evict_rows": (ctypes.c_int, [
+        _P, _P, _P, _P, _I32, _I64, _I32, _I64, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _I64, _P, _P, _SZ, _P]),
+    "louiskv_store_evict_workspace_size": (_SZ, [_I64, _I64, _I32, _I64]),
+    "louiskv_store_evict": (ctypes.c_int, [
+        _P, _P, _I32, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _I64, _I64, _I32, _I32, _P, _SZ, _P]),
 }
 
 EXPORTED = sorted(_SIGS)
@@ -884,3 +897,117 @@ def sparse_prefill_attn(q, n_kv_heads: int, keys, values, n_keys: int, q_start: 
     _check(lib.sparse_prefill_attn(
         q, _dtype_code(q), s, n_kv_heads, gs, n_q, d, float(sc), keys, values, keys.shape[1], n_keys,
         q_start, q_block, block_len, sel_blocks, cap, n_sel_blocks, out, _dtype_code(out), lse_out, ws, wsb, stream))
+
+
+# ---------------------------------------------------------------- sequences that share a prefix, bounded caches
+
+def shared_prefix_attn_workspace_size(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows,
+                                      with_weights: bool, d=128) -> int:
+    return _native().shared_prefix_attn_workspace_size(n_slices, n_prefix_slices, group_size, n_q, d, prefix_rows,
+                                                       own_rows, int(with_weights))
+
+
+def _queries(q):
+    """(groups, query heads, tokens, d) of queries [G][Hq][n_q][d], or [G][Hq][d] of one token."""
+    shape = q.shape
+    if len(shape) == 3:
+        return shape[0], shape[1], 1, shape[2]
+    if len(shape) == 4:
+        return tuple(shape)
+    raise ValueError(f"queries {tuple(shape)}: [groups][query heads][tokens][d], or [groups][query heads][d]")
+
+
+def shared_prefix_attn(q, n_kv_heads: int, k_prefix, v_prefix, n_prefix, k_own, v_own, n_own, out, lse_out=None,
+                       weights=None, scale: Optional[float] = None, workspace=None, stream=None):
+    """Attention of every sequence's last tokens over rows that all sequences share and rows of its own: q and out
+    [G][Hq][n_q][d] (or [G][Hq][d] for one token), k_prefix and v_prefix [Sp][rows][d] (None: no prefix), k_own and
+    v_own [S][rows][d] (None: no own rows), n_prefix [Sp] and n_own [S] the rows held (None: all).  weights [S][rows]
+    float32: each own row's softmax weight, summed over queries and heads, is added."""
+    g, hq, n_q, d = _queries(q)
+    s = g * n_kv_heads
+    gs = _groups(hq, n_kv_heads)
+    if k_prefix is None and (v_prefix is not None or n_prefix is not None):
+        raise ValueError("v_prefix and n_prefix belong to k_prefix, which is None")
+    if k_own is None and (v_own is not None or n_own is not None or weights is not None):
+        raise ValueError("v_own, n_own and weights belong to k_own, which is None")
+    sp, p_rows = (k_prefix.shape[0], k_prefix.shape[1]) if k_prefix is not None else (s, 0)
+    rows = k_own.shape[1] if k_own is not None else 0
+    t = q.dtype
+    lib = _native()
+    lib.expect("k_prefix", k_prefix, (sp, p_rows, d), t, "v_prefix", v_prefix, (sp, p_rows, d), t,
+               "n_prefix", n_prefix, (sp,), torch.int32, "k_own", k_own, (s, rows, d), t, "v_own", v_own, (s, rows, d), t,
+               "n_own", n_own, (s,), torch.int32, "weights", weights, (s, rows), torch.float32,
+               "out", out, tuple(q.shape), None, "lse_out", lse_out, tuple(q.shape[:-1]), torch.float32)
+    ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else lib.shared_prefix_attn_workspace_size(
+        s, sp, gs, n_q, d, p_rows, rows, int(weights is not None)), stream)
+    sc = (1.0 / d ** 0.5) if scale is None else scale
+    _check(lib.shared_prefix_attn(
+        q, _dtype_code(q), s, n_kv_heads, gs, n_q, d, float(sc), k_prefix, v_prefix, sp, p_rows, n_prefix, k_own, v_own,
+        rows, n_own, weights, out, _dtype_code(out), lse_out, ws, wsb, stream))
+
+
+def attn_weights_workspace_size(n_slices, group_size, n_q, key_rows, d=128) -> int:
+    return _native().attn_weights_workspace_size(n_slices, group_size, n_q, d, key_rows)
+
+
+def attn_weights(q, n_kv_heads: int, keys, n_keys, lse, weights, scale: Optional[float] = None, workspace=None,
+                 stream=None):
+    """The attention weight that the last n_q tokens give to each key, summed over tokens and heads, is added to
+    weights [S][rows] float32: q [G][Hq][n_q][d] (or [G][Hq][d]), keys [S][rows][d], n_keys [S] (None: all rows), lse
+    as an attention call wrote it for q."""
+    g, hq, n_q, d = _queries(q)
+    s, rows = g * n_kv_heads, keys.shape[1]
+    gs = _groups(hq, n_kv_heads)
+    lib = _native()
+    lib.expect("keys", keys, (s, rows, d), q.dtype, "n_keys", n_keys, (s,), torch.int32,
+               "lse", lse, tuple(q.shape[:-1]), torch.float32, "weights", weights, (s, rows), torch.float32)
+    ws, wsb = _ws_bytes(workspace, q.device, 0 if workspace is not None else
+                        lib.attn_weights_workspace_size(s, gs, n_q, d, rows), stream)
+    sc = (1.0 / d ** 0.5) if scale is None else scale
+    _check(lib.attn_weights(q, _dtype_code(q), s, n_kv_heads, gs, n_q, d, float(sc), keys, rows, n_keys, lse, weights,
+                            ws, wsb, stream))
+
+
+def evict_rows_workspace_size(n_slices, rows, n_keep) -> int:
+    return _native().evict_rows_workspace_size(n_slices, rows, n_keep)
+
+
+def evict_rows(weights, pos, n_rows, n_seen, n_keep: int, n_first: int, n_recent: int, k, v, k_to, v_to, weights_to,
+               pos_to, n_rows_to, workspace=None, stream=None):
+    """The n_keep rows of largest weight (positions below n_first and the last n_recent always among them) of k and v
+    [S][rows][d] into k_to and v_to [S][rows_to][d], with their weights and positions; in place where an output is its
+    input.  pos [S][rows] and n_seen [S] None: positions are row numbers; n_rows [S] None: all rows."""
+    s, rows, d = k.shape
+    rows_to = k_to.shape[1]
+    t, f32, i32 = k.dtype, torch.float32, torch.int32
+    lib = _native()
+    lib.expect("v", v, (s, rows, d), t, "k_to", k_to, (s, rows_to, d), t, "v_to", v_to, (s, rows_to, d), t,
+               "weights", weights, (s, rows), f32, "pos", pos, (s, rows), i32, "n_rows", n_rows, (s,), i32,
+               "n_seen", n_seen, (s,), i32, "weights_to", weights_to, (s, rows_to), f32,
+               "pos_to", pos_to, (s, rows_to), i32, "n_rows_to", n_rows_to, (s,), i32)
+    ws, wsb = _ws_bytes(workspace, k.device, 0 if workspace is not None else
+                        lib.evict_rows_workspace_size(s, rows, n_keep), stream)
+    _check(lib.evict_rows(weights, pos, n_rows, n_seen, _dtype_code(k), s, d, rows, n_keep, n_first, n_recent, k, v,
+                          k_to, v_to, weights_to, pos_to, rows_to, n_rows_to, ws, wsb, stream))
+
+
+def store_evict_workspace_size(n_slices, rows, n_new, budget) -> int:
+    return _native().store_evict_workspace_size(n_slices, rows, n_new, budget)
+
+
+def store_evict(k_new, v_new, k, v, weights, pos, n_rows, n_seen, budget: int, n_first: int, n_recent: int,
+                workspace=None, stream=None):
+    """New tokens k_new and v_new [S][d] or [S][n_new][d] enter caches k and v [S][rows][d] of at most `budget` rows;
+    the lightest rows leave for them.  weights, pos [S][rows], n_rows and n_seen [S] are updated."""
+    s, rows, d = k.shape
+    n_new = 1 if k_new.dim() == 2 else k_new.shape[1]
+    new = (s, d) if k_new.dim() == 2 else (s, n_new, d)
+    t, i32 = k.dtype, torch.int32
+    lib = _native()
+    lib.expect("k_new", k_new, new, t, "v_new", v_new, new, t, "v", v, (s, rows, d), t,
+               "weights", weights, (s, rows), torch.float32, "pos", pos, (s, rows), i32, "n_rows", n_rows, (s,), i32,
+               "n_seen", n_seen, (s,), i32)
+    ws, wsb = _ws_bytes(workspace, k.device, 0 if workspace is not None else
+                        lib.store_evict_workspace_size(s, rows, n_new, budget), stream)
+    _check(lib.store_evict(k_new, v_new, _dtype_code(k), s, n_new, d, k, v, weights, pos, n_rows, n_seen, rows, budget,
+                           n_first, n_recent, ws, wsb, stream))

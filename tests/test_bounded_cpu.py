@@ -1,0 +1,176 @@
+"""Shared prefixes and bounded caches without a GPU: the oracle's rules, and what the calls refuse before any launch."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import blocks as ob
+from oracle import prefix as op
+
+P = ctypes.c_void_p
+NULL, SHAPE, DTYPE, UNSUPPORTED, WORKSPACE = 1, 2, 3, 4, 5
+D16, ODD = P(4096), P(4104)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2510_11292_amd import louiskv
+    return louiskv.load_library()
+
+
+def refused(fn, base, table):
+    for change, want in table:
+        args = list(base)
+        for i, v in change.items():
+            args[i] = v
+        got = fn(*args)
+        assert got == want, f"{change}: {got}, expected {want}"
+
+
+# ------------------------------------------------------------------- the oracle
+
+def test_weights_are_the_columns_of_the_attention():
+    rng = np.random.default_rng(0)
+    q, k, v = rng.standard_normal((6, 8)), rng.standard_normal((11, 8)), rng.standard_normal((11, 3))
+    see = np.arange(11)[None] <= 4 + np.arange(6)[:, None]
+    see[2] = False
+    out, lse, _, _ = ob.masked_attention(q, k, v, see, 0.3)
+    w, size = op.row_weights(q, k, see, lse, 0.3)
+    x = np.where(see, q @ k.T * 0.3, -np.inf)
+    rows = [0, 1, 3, 4, 5]
+    p = np.exp(x[rows]) / np.exp(x[rows]).sum(1, keepdims=True)
+    np.testing.assert_allclose(w, p.sum(0), rtol=1e-12)
+    np.testing.assert_allclose(p @ v, out[rows], rtol=1e-12)
+    assert abs(w.sum() - 5) < 1e-12 and (size >= 0).all()
+
+
+def test_rows_that_stay_by_hand():
+    pos = list(range(6))
+    # row 0 is protected (first), 5 (recent); of 1..4 the two lightest leave: 2 and 4
+    assert op.rows_that_stay([0.0, 3.0, 1.0, 2.0, 0.5, 0.0], pos, 6, 6, 4, 1, 1) == [0, 1, 5, 3]
+    # equal weights: the lower rows leave
+    assert op.rows_that_stay([1.0] * 6, pos, 6, 6, 3, 0, 0) == [3, 4, 5]
+    assert op.rows_that_stay([1.0] * 6, pos, 6, 6, 3, 1, 0) == [0, 4, 5]
+    nan = float("nan")
+    assert op.rows_that_stay([nan, -np.inf, 0.0, nan], pos, 4, 4, 2, 0, 0) == [2, 1]
+    assert op.rows_that_stay([-0.0, 0.0], pos, 2, 2, 1, 0, 0) == [1]
+    # fewer rows than fit: all stay where they are; none kept
+    assert op.rows_that_stay([1.0, 2.0], pos, 2, 2, 5, 0, 1) == [0, 1]
+    assert op.rows_that_stay([1.0, 2.0], pos, 2, 2, 0, 0, 0) == []
+    # positions, not rows, are protected
+    assert op.rows_that_stay([5.0, 1.0, 1.0, 9.0], [7, 9, 0, 8], 4, 10, 2, 1, 1) == [2, 1]
+
+
+# ------------------------------------------------------------------- refusals
+
+def test_attention_refuses(lib):
+    size = lib.louiskv_shared_prefix_attn_workspace_size
+    ws = size(32, 8, 4, 1, 128, 4096, 600, 1)
+    assert ws > 0 and size(0, 8, 4, 1, 128, 4096, 600, 1) == size(32, 8, 9, 1, 128, 4096, 600, 1) == 0
+    assert size(32, 8, 4, 0, 128, 4096, 600, 1) == size(32, 5, 4, 1, 128, 4096, 600, 1) == size(32, 8, 4, 1, 128, -1, 600, 1) == 0
+    assert size(32, 8, 4, 1, 128, 4096, (1 << 30) + 1, 1) == size(1 << 62, 8, 4, 1, 128, 4096, 600, 1) == 0
+    #       q    dt S   kv g  nq d    scale kp   vp  Sp rows  np   ko   vo   rows no  w    out odt lse ws   bytes
+    base = [D16, 1, 32, 8, 4, 1, 128, 0.1, D16, D16, 8, 4096, None, D16, D16, 600, D16, D16, D16, 1, None, D16, ws, None]
+    refused(lib.louiskv_shared_prefix_attn, base, [
+        ({0: None}, NULL), ({18: None}, NULL), ({8: None}, NULL), ({9: None}, NULL), ({13: None}, NULL), ({14: None}, NULL),
+        ({1: 2}, DTYPE), ({19: -1}, DTYPE), ({6: 64}, UNSUPPORTED), ({4: 0}, UNSUPPORTED), ({4: 9}, UNSUPPORTED),
+        ({2: 0}, SHAPE), ({2: 33}, SHAPE), ({3: 0}, SHAPE), ({3: 5}, SHAPE), ({5: 0}, SHAPE), ({5: 1 << 30}, SHAPE),
+        ({2: 1 << 40}, SHAPE), ({10: 0}, SHAPE), ({10: 4}, SHAPE), ({10: 24}, SHAPE), ({11: -1}, SHAPE),
+        ({11: (1 << 30) + 1}, SHAPE), ({15: -1}, SHAPE), ({15: (1 << 30) + 1}, SHAPE),
+        ({0: ODD}, UNSUPPORTED), ({8: ODD}, UNSUPPORTED), ({9: ODD}, UNSUPPORTED), ({13: ODD}, UNSUPPORTED),
+        ({14: ODD}, UNSUPPORTED), ({18: ODD}, UNSUPPORTED), ({21: None}, WORKSPACE), ({21: ODD}, WORKSPACE),
+        ({22: ws - 1}, WORKSPACE)])
+
+
+def test_weights_refuse(lib):
+    size = lib.louiskv_attn_weights_workspace_size
+    assert size(0, 4, 64, 128, 4096) == size(8, 9, 64, 128, 4096) == size(8, 4, 0, 128, 4096) == size(8, 4, 64, 128, -1) == 0
+    ws = size(8, 4, 64, 128, 4096)
+    #       q    dt S  kv g  nq  d    scale keys rows n    lse  w    ws   bytes
+    base = [D16, 1, 8, 8, 4, 64, 128, 0.1, D16, 4096, D16, D16, D16, D16, ws, None]
+    refused(lib.louiskv_attn_weights, base, [
+        ({0: None}, NULL), ({8: None}, NULL), ({11: None}, NULL), ({12: None}, NULL), ({1: 7}, DTYPE),
+        ({6: 256}, UNSUPPORTED), ({4: 12}, UNSUPPORTED), ({2: 12}, SHAPE), ({5: 0}, SHAPE), ({9: 0}, SHAPE),
+        ({9: (1 << 30) + 1}, SHAPE), ({0: ODD}, UNSUPPORTED), ({8: ODD}, UNSUPPORTED)]
+        + ([({13: None}, WORKSPACE), ({14: ws - 1}, WORKSPACE)] if ws else []))
+
+
+def test_eviction_refuses(lib):
+    size = lib.louiskv_evict_rows_workspace_size
+    ws = size(8, 4096, 512)
+    assert ws > 0 and size(0, 4096, 512) == size(8, 0, 512) == size(8, 4096, 0) == size(1 << 62, 4096, 512) == 0
+    a = [P(1 << 30 | i << 26) for i in range(1, 12)]        # buffers far from each other
+    #       w     pos  n     seen  dt S  d    rows  keep fst rec k     v     k_to  v_to  w_to  p_to  to   n_to  ws    bytes
+    base = [a[0], a[1], a[2], a[3], 1, 8, 128, 4096, 512, 4, 64, a[4], a[5], a[6], a[7], a[8], a[9], 600, a[10], D16, ws, None]
+    refused(lib.louiskv_evict_rows, base, [
+        ({0: None}, NULL), ({11: None}, NULL), ({12: None}, NULL), ({13: None}, NULL), ({14: None}, NULL), ({18: None}, NULL),
+        ({1: None}, NULL), ({3: None}, NULL), ({4: 4}, DTYPE), ({6: 64}, UNSUPPORTED), ({5: 0}, SHAPE), ({7: 0}, SHAPE),
+        ({7: (1 << 30) + 1}, SHAPE), ({8: 0}, SHAPE), ({8: 601}, SHAPE), ({9: -1}, SHAPE), ({10: -1}, SHAPE),
+        ({9: 449}, SHAPE), ({10: (1 << 31) - 1}, SHAPE), ({5: 1 << 23}, SHAPE), ({11: P((1 << 30) + 8)}, UNSUPPORTED),
+        # a part of another buffer, the same buffer with another number of rows, another input's buffer
+        ({13: P(a[4].value + 4096)}, SHAPE), ({13: a[4]}, SHAPE), ({13: a[5]}, SHAPE), ({14: a[6]}, SHAPE),
+        ({15: a[4]}, SHAPE), ({18: a[3]}, SHAPE), ({18: a[8]}, SHAPE),
+        ({19: None}, WORKSPACE), ({19: ODD}, WORKSPACE), ({20: ws - 1}, WORKSPACE)])
+
+
+def test_store_refuses(lib):
+    size = lib.louiskv_store_evict_workspace_size
+    assert size(0, 600, 1, 512) == size(8, 600, 0, 512) == size(8, 600, 1, 601) == size(8, 600, 9, 8) == 0
+    ws = size(8, 600, 3, 512)
+    #       kn   vn   dt S  new d    k    v    w    pos  n    seen rows bud  fst rec ws  bytes
+    base = [D16, D16, 1, 8, 3, 128, D16, D16, D16, D16, D16, D16, 600, 512, 4, 64, D16, ws, None]
+    refused(lib.louiskv_store_evict, base, [
+        *[({i: None}, NULL) for i in (0, 1, 6, 7, 8, 9, 10, 11)], ({2: -1}, DTYPE), ({5: 96}, UNSUPPORTED), ({3: 0}, SHAPE),
+        ({4: 0}, SHAPE), ({4: 513}, SHAPE), ({13: 601}, SHAPE), ({13: 2}, SHAPE), ({12: (1 << 30) + 1}, SHAPE),
+        ({14: 446}, SHAPE), ({15: 506}, SHAPE), ({14: -1}, SHAPE), ({15: -1}, SHAPE), ({0: ODD}, UNSUPPORTED),
+        ({7: ODD}, UNSUPPORTED)] + ([({16: None}, WORKSPACE), ({17: ws - 1}, WORKSPACE)] if ws else []))
+
+
+def test_python_calls_refuse_sizes_types_and_host_memory():
+    from paper_2510_11292_amd import louiskv as L
+    i32 = dict(dtype=torch.int32)
+    q, kp, ko, out = torch.zeros(3, 4, 2, 128), torch.zeros(2, 9, 128), torch.zeros(6, 5, 128), torch.zeros(3, 4, 2, 128)
+    n_p, n_o, w, lse = torch.zeros(2, **i32), torch.zeros(6, **i32), torch.zeros(6, 5), torch.zeros(3, 4, 2)
+    pos, ws = torch.zeros(6, 5, **i32), torch.zeros(1 << 16, dtype=torch.uint8)
+
+    def attn(q=q, kp=kp, vp=kp, n_p=n_p, ko=ko, vo=ko, n_o=n_o, out=out, lse=lse, w=w):
+        L.shared_prefix_attn(q, 2, kp, vp, n_p, ko, vo, n_o, out, lse, weights=w, workspace=ws, stream=0)
+
+    def weights(keys=ko, n=n_o, lse=lse, w=w):
+        L.attn_weights(q, 2, keys, n, lse, w, workspace=ws, stream=0)
+
+    def evict(w=w, pos=pos, n=n_o, seen=n_o, v=ko, to=ko, w_to=w, pos_to=pos, n_to=n_o):
+        L.evict_rows(w, pos, n, seen, 3, 1, 1, ko, v, to, ko, w_to, pos_to, n_to, workspace=ws, stream=0)
+
+    def store(new=ko[:, :1], v_new=ko[:, :1], v=ko, w=w, pos=pos, n=n_o, seen=n_o):
+        L.store_evict(new.contiguous(), v_new, ko, v, w, pos, n, seen, 4, 1, 1, workspace=ws, stream=0)
+    for call, kw in ((attn, dict(vp=kp[:, :8])), (attn, dict(n_p=n_p[:1])), (attn, dict(vo=ko[:5])), (attn, dict(ko=ko[:5])),
+                     (attn, dict(n_o=n_o[:5])), (attn, dict(out=out[:, :3])), (attn, dict(lse=lse[0])),
+                     (attn, dict(w=w[:, :4])), (weights, dict(keys=ko[:4])), (weights, dict(n=n_o[:1])),
+                     (weights, dict(lse=lse[:2])), (weights, dict(w=w[:, :3])), (evict, dict(w=w[:1])), (evict, dict(pos=pos[:1])),
+                     (evict, dict(v=ko[:5])), (evict, dict(n=n_o[:1])), (evict, dict(seen=n_o[:1])), (evict, dict(w_to=w[:1])),
+                     (evict, dict(pos_to=pos[:1])), (evict, dict(n_to=n_o[:1])), (evict, dict(to=ko[:, :4])),
+                     (store, dict(v_new=ko[:, :2])), (store, dict(v=ko[:5])), (store, dict(w=w[:5])), (store, dict(pos=pos[:5])),
+                     (store, dict(n=n_o[:5])), (store, dict(seen=n_o[:5]))):
+        with pytest.raises(ValueError, match="expected"):
+            call(**kw)
+    for call, kw in ((attn, dict(n_o=n_o.long())), (attn, dict(n_p=n_p.float())), (attn, dict(kp=kp.bfloat16())),
+                     (attn, dict(w=w.double())), (weights, dict(n=n_o.long())), (weights, dict(w=w.bfloat16())),
+                     (weights, dict(lse=lse.double())), (evict, dict(pos=pos.long())), (evict, dict(w=w.bfloat16())),
+                     (evict, dict(n_to=n_o.long())), (store, dict(v_new=ko[:, :1].bfloat16())), (store, dict(n=n_o.long()))):
+        with pytest.raises(TypeError, match="expected"):
+            call(**kw)
+    with pytest.raises(ValueError, match="multiple"):
+        attn(q=torch.zeros(3, 3, 2, 128), out=torch.zeros(3, 3, 2, 128), lse=None)
+    for kw in (dict(kp=None), dict(kp=None, vp=None), dict(ko=None, vo=None), dict(ko=None, vo=None, w=None)):
+        with pytest.raises(ValueError, match="None"):
+            attn(**kw)
+    with pytest.raises(ValueError, match="queries"):
+        attn(q=q[0, 0])
+    for call in (attn, weights, evict, store):      # every size is right: host memory is what is left
+        with pytest.raises(ValueError, match="current device|contiguous"):
+            call()
+    with pytest.raises(TypeError, match="dtype"):
+        h = torch.float16
+        L.shared_prefix_attn(q.to(h), 2, kp.to(h), kp.to(h), None, None, None, None, out, stream=0)
