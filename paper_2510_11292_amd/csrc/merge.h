@@ -38,11 +38,8 @@ __device__ __forceinline__ float lse_of(float m, float l) { return kLn2 * (max_b
 // parts: 3.6 us, most of it the trips to memory; four loads at a time, 4.2).
 constexpr int kMergeParts = 16;
 template <class TO>
-__global__ __launch_bounds__(256)
-void merge_parts_kernel(const float* __restrict__ part, int n_parts, int64_t n_rows, TO* __restrict__ out,
-                        float* __restrict__ lse_out) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= n_rows) return;
+__device__ __forceinline__ void merge_row(const float* __restrict__ part, int n_parts, int64_t row,
+                                          TO* __restrict__ out, float* __restrict__ lse_out) {
   const int lane = threadIdx.x & 63;
   const float* p = part + (size_t)row * n_parts * kPartFloats;
   float2 x[kMergeParts];
@@ -78,6 +75,14 @@ void merge_parts_kernel(const float* __restrict__ part, int n_parts, int64_t n_r
   store_from_f32(out + (size_t)row * kHeadDim, 2 * lane, a0 * inv);
   store_from_f32(out + (size_t)row * kHeadDim, 2 * lane + 1, a1 * inv);
   if (lse_out && lane == 0) lse_out[row] = lse_of(m, l);
+}
+
+template <class TO>
+__global__ __launch_bounds__(256)
+void merge_parts_kernel(const float* __restrict__ part, int n_parts, int64_t n_rows, TO* __restrict__ out,
+                        float* __restrict__ lse_out) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row < n_rows) merge_row(part, n_parts, row, out, lse_out);
 }
 
 inline int merge_parts(const float* part, int n_parts, int64_t n_rows, void* out, int out_dtype, float* lse_out,

@@ -1,26 +1,36 @@
 // Attention of sequences that share a prefix (or of caches of bounded size), and the
 // weight that queries give to each key.
+#include <type_traits>
+
 #include "common.h"
 #include "merge.h"
+#include "tiles.h"
 
 namespace louiskv {
 namespace {
 
 constexpr int64_t kMaxRows = 1 << 30;   // rows of a slice, queries of a prefix slice
 
+// The rows of a prefix, or of the slices' own caches.
+struct Side {
+  const void* k;
+  const void* v;
+  const int32_t* n;
+  int rows;
+  int row_groups, splits;   // blocks that a slice's queries, and parts that its keys, are cut into
+};
+
 struct AttnArgs {
   const void* q;
-  int group_size, n_q;
+  int group_size, n_q, n_seqs;
   float scale;
-  const void* k_prefix;
-  const void* v_prefix;
   int64_t n_prefix_slices;
-  int prefix_rows;
-  const int32_t* n_prefix;
-  const void* k_own;
-  const void* v_own;
-  int own_rows;
-  const int32_t* n_own;
+  Side prefix, own;
+  int64_t prefix_blocks;
+  int n_parts;              // of a query: the prefix's, then its own rows'
+  float* part;
+  float* logits;            // [slices][group_size * n_q][logit_stride], base 2, or NULL
+  int logit_stride;
   void* out;
   int out_bf16;
   float* lse_out;
@@ -36,63 +46,575 @@ __device__ __forceinline__ float at(const void* p, int64_t r, int c) {
   return load_as_f32(static_cast<const T*>(p), r * kHeadDim + c);
 }
 
-// Block: one query.  Its waves take every fourth 64 rows, a row a lane for the
-// scores, two channels a lane for the sums.
+constexpr int kTile = 32;            // keys of a product
+constexpr int kBlockWaves = 4;
+constexpr int kStage = 64;           // keys of a stage that the block's waves share
+constexpr float kGrow = 8.0f;        // base-2 logits may pass the base by this much before the sums are rescaled
+template <class T> constexpr int kRowBytes = kHeadDim * sizeof(T);
+// keys and values of a tile for each wave, or of two stages
+template <class T> constexpr int kRingBytes = kBlockWaves * kTile * 2 * kRowBytes<T>;
+
+// A block's place: the queries and keys that it attends.
+struct Place {
+  int64_t s;         // slice, or prefix slice
+  int rgrp, split;
+  int n_rows;        // queries of the (prefix) slice
+  int64_t kv_row;    // first row of the slice in k and v
+  int n;             // rows held
+};
+
+template <bool kOwn>
+__device__ __forceinline__ Place place_of(const AttnArgs& a, int64_t id) {
+  const Side& x = kOwn ? a.own : a.prefix;
+  if (!kOwn && a.prefix_blocks >= 64) {
+    // blocks that read the same keys go to one XCD (blocks are dealt to the eight in turn)
+    const int64_t per = a.prefix_blocks >> 3, rest = a.prefix_blocks & 7, xcd = id & 7;
+    id = xcd * per + min<int64_t>(xcd, rest) + (id >> 3);
+  }
+  Place p;
+  p.rgrp = (int)(id % x.row_groups);
+  id /= x.row_groups;
+  p.split = (int)(id % x.splits);
+  p.s = id / x.splits;
+  p.n_rows = a.group_size * a.n_q * (kOwn ? 1 : a.n_seqs);
+  p.kv_row = p.s * x.rows;
+  p.n = length_of(x.n, p.s, x.rows);
+  return p;
+}
+
+// Query r of a place as its row in q and out.
+template <bool kOwn>
+__device__ __forceinline__ int64_t query_row(const AttnArgs& a, const Place& p, int r) {
+  const int per = a.group_size * a.n_q;
+  if (kOwn) return p.s * per + r;
+  const int seq = r / per;
+  return ((int64_t)seq * a.n_prefix_slices + p.s) * per + (r - seq * per);
+}
+
+// Keys that query r of a place sees.
+template <bool kOwn>
+__device__ __forceinline__ int limit_of(const AttnArgs& a, const Place& p, int r) {
+  return kOwn ? max(0, p.n - a.n_q + r % a.n_q + 1) : p.n;
+}
+
+// The fewest and most keys that queries r0..r1 see.
+template <bool kOwn>
+__device__ __forceinline__ void limits_of(const AttnArgs& a, const Place& p, int r0, int r1, int& least, int& most) {
+  const bool wraps = kOwn && r0 / a.n_q != r1 / a.n_q;
+  least = wraps ? max(0, p.n - a.n_q + 1) : limit_of<kOwn>(a, p, r0);
+  most = wraps ? p.n : limit_of<kOwn>(a, p, r1);
+}
+
+typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8;
+typedef const __attribute__((address_space(3))) f32x4* lds_f32x4;
+typedef const __attribute__((address_space(3))) float* lds_f32;
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+
+// A wave's 32 queries, a lane (of two) a query n = lane % 32: S^T = K Q^T of 32 keys leaves
+// the lane 16 scores, of keys (i & 3) + 8 (i >> 2) + 4 h with h = lane / 32, and their
+// exponentials are, unmoved, the B operand of O^T += V^T P^T.
 template <class T>
-__global__ __launch_bounds__(256)
-void attn_kernel(const AttnArgs a) {
-  __shared__ float s_q[kHeadDim];
-  __shared__ float s_o[4][kHeadDim], s_m[4], s_l[4];
-  const int64_t row = blockIdx.x, s = row / (a.group_size * a.n_q);
-  const int t = (int)(row % a.n_q), lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  if (threadIdx.x < kHeadDim) s_q[threadIdx.x] = at<T>(a.q, row, threadIdx.x) * (a.scale * kLog2E);
-  __syncthreads();
-  const int64_t ps = a.prefix_rows ? s % a.n_prefix_slices : 0;
-  const int np = a.prefix_rows ? length_of(a.n_prefix, ps, a.prefix_rows) : 0;
-  const int own = max(0, length_of(a.n_own, s, a.own_rows) - a.n_q + t + 1);
-  float m = -__builtin_inff(), l = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int part = 0; part < 2; ++part) {
-    const int n = part ? own : np;
-    const void* k = part ? a.k_own : a.k_prefix;
-    const void* v = part ? a.v_own : a.v_prefix;
-    const int64_t r0 = part ? s * a.own_rows : ps * a.prefix_rows;
-    for (int i0 = 64 * w; i0 < n; i0 += 256) {
-      const int i = min(i0 + lane, n - 1);
-      float x = 0.f;
-      for (int c = 0; c < kHeadDim; ++c) x += s_q[c] * at<T>(k, r0 + i, c);
-      if (i0 + lane >= n) x = -__builtin_inff();
-      const float mm = fmaxf(m, wave_max(x)), f = exp2f(max_base(m) - max_base(mm));
-      const float p = exp2f(x - max_base(mm));
-      m = mm;
-      l = l * f + p;
-      o0 *= f;
-      o1 *= f;
-      for (int j = 0; j < min(64, n - i0); ++j) {
-        const float pj = __shfl(p, j, kWave);
-        o0 += pj * at<T>(v, r0 + i0 + j, 2 * lane);
-        o1 += pj * at<T>(v, r0 + i0 + j, 2 * lane + 1);
+struct Wave {
+  static constexpr bool kBf16 = sizeof(T) == 2;
+  typedef typename std::conditional<kBf16, bf16x8, f32x4>::type QPiece;
+  typedef typename std::conditional<kBf16, bf16x8[8], int>::type Keys;       // float32: read where they are used
+  typedef typename std::conditional<kBf16, s16x8[2][4], int>::type Values;
+  typedef typename std::conditional<kBf16, bf16x8[2], f32x16>::type Weights;
+  static constexpr int kQ = kBf16 ? 8 : 16;
+
+  int lane, h, n;
+  QPiece q[kQ];              // 16-byte pieces 2 c + h (bfloat16) or 16 h + c (float32)
+  float mult;                // |scale| log2(e); the queries' signs are flipped where the scale is negative
+  int limit;                 // keys that the lane's query sees
+  f32x16 o[4];
+  float base = 0.f, grow_at = -__builtin_inff(), sum = 0.f;
+  uint32_t k_at[8], v_at[4][2];   // LDS addresses of the lane's reads in a tile at address 0
+
+  __device__ __forceinline__ void init(const AttnArgs& a, int64_t row, int lim) {
+    lane = threadIdx.x & 63;
+    h = lane >> 5;
+    n = lane & 31;
+    limit = lim;
+    const float qs = a.scale * kLog2E;
+    const uint32_t flip = qs < 0.f ? (kBf16 ? 0x80008000u : 0x80000000u) : 0u;
+    mult = fabsf(qs);
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + row * kHeadDim);
+#pragma unroll
+    for (int c = 0; c < kQ; ++c) {
+      uint4 v = src[kBf16 ? 2 * c + h : 16 * h + c];
+      v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
+      q[c] = __builtin_bit_cast(QPiece, v);
+    }
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  }
+
+  // bfloat16: pieces 2 c + h of key n, and of the values rows 4 h + 0..3 and, in the
+  // second, those + 8 (the same swizzle but for bit 1) of channels 32 dt + 0..31.
+  // float32: pieces 16 h + c of key n, and channel n % 4 of piece n / 4 (+ 8 dt) of rows
+  // 4 h + i.
+  __device__ __forceinline__ void addresses(uint32_t k0, uint32_t v0) {
+    constexpr int kRow = kRowBytes<T>;
+    if constexpr (kBf16) {
+      const uint32_t kp = (h ^ swizzle<T>(n & 15)) << 4, kr = k0 + n * kRow;
+      const int j4 = (lane & 15) >> 2, xp = (((lane >> 4) & 1) << 1) | ((lane & 3) >> 1);
+      const uint32_t v1 = v0 + (4 * h + j4) * kRow + ((lane & 1) << 3), vp = ((j4 << 2) | (xp ^ h)) << 4;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) k_at[c] = kr + (kp ^ (c << 5));
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        v_at[dt][0] = v1 + (vp ^ (dt << 6));
+        v_at[dt][1] = v1 + 8 * kRow + (vp ^ (dt << 6) ^ 32);
       }
+    } else {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) k_at[c] = k0 + n * kRow + h * 256 + ((c ^ swizzle<T>(n & 15)) << 4);   // and ^ 128 for c + 8
+      // row (i & 3) + 8 (i >> 2) + 4 h: its swizzle is (i & 3) | (i >> 2 & 1) << 2 | h << 3
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+        v_at[dt][0] = v0 + 4 * h * kRow + (((8 * dt + (n >> 2)) ^ (h << 3)) << 4) + ((n & 3) << 2);
     }
   }
-  l = wave_sum(l);
-  s_m[w] = m;
-  s_l[w] = l;
-  s_o[w][2 * lane] = o0;
-  s_o[w][2 * lane + 1] = o1;
-  __syncthreads();
-  if (threadIdx.x >= kHeadDim) return;
-  m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  float o = 0.f;
-  l = 0.f;
-  for (int i = 0; i < 4; ++i) {
-    const float f = exp2f(s_m[i] - max_base(m));
-    l += s_l[i] * f;
-    o += s_o[i][threadIdx.x] * f;
+
+  __device__ __forceinline__ void load_keys(uint32_t off, Keys& kf) {
+    if constexpr (kBf16) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) kf[c] = *(lds_bf16x8)(uintptr_t)(k_at[c] + off);
+    }
   }
-  o *= inv_sum(l);
-  if (a.out_bf16) store_from_f32(static_cast<uint16_t*>(a.out) + row * kHeadDim, threadIdx.x, o);
-  else store_from_f32(static_cast<float*>(a.out) + row * kHeadDim, threadIdx.x, o);
-  if (a.lse_out && threadIdx.x == 0) a.lse_out[row] = lse_of(m, l);
+  __device__ __forceinline__ void load_values(uint32_t off, Values& vf) {
+    if constexpr (kBf16) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+          const uint32_t x = off + 16 * k * kRowBytes<T>;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(v_at[dt][0] + x));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(v_at[dt][1] + x));
+          vf[k][dt] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+  }
+  __device__ __forceinline__ f32x16 scores(uint32_t off, const Keys& kf) {
+    f32x16 sc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+    if constexpr (kBf16) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], q[c], sc, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {
+        const f32x4 k = *(lds_f32x4)(uintptr_t)((k_at[c & 7] ^ (c >> 3 << 7)) + off);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[c][e], sc, 0, 0, 0);
+      }
+    }
+    return sc;
+  }
+  // Raises the base where a lane's scores pass it.
+  __device__ __forceinline__ void rebase(float top) {
+    if (!__builtin_amdgcn_ballot_w64(top > grow_at)) return;
+    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    const bool grows = top > grow_at;
+    // before the first finite score the sums are 0 (or NaN): any factor does
+    const float f = grows && grow_at != -__builtin_inff() ? __builtin_amdgcn_exp2f(base - top) : 1.f;
+    base = grows ? top : base;
+    grow_at = grows ? top + kGrow : grow_at;
+    sum *= f;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) o[dt] *= f;
+  }
+  // Scores of keys p0.. as base-2 logits (-inf where the query does not see the key) if
+  // kMask, and their weights.  low: the lane's weights are what the rounding to bfloat16
+  // leaves over.
+  template <bool kLow>
+  __device__ __forceinline__ void soften(f32x16& sc, int p0, bool masked, bool low, Weights& pb) {
+    float m = mult;
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = p0 + (i & 3) + 8 * (i >> 2) + 4 * h;
+        sc[i] = key < limit ? sc[i] * mult : -__builtin_inff();
+      }
+      m = 1.f;
+    }
+    float top = sc[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
+    rebase(top * m);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], m, -base));
+      sum += p;
+      if constexpr (kBf16) {
+        __bf16 b = (__bf16)p;
+        if constexpr (kLow) b = low ? (__bf16)(p - (float)b) : b;
+        pb[i >> 3][i & 7] = b;
+      } else {
+        pb[i] = p;
+      }
+    }
+    if (!masked) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] *= mult;      // dead where nobody stores the logits
+    }
+  }
+  __device__ __forceinline__ void add_values(uint32_t off, const Values& vf, const Weights& pb) {
+    if constexpr (kBf16) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k][dt]), pb[k], o[dt], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+          const uint32_t x = v_at[dt][0] + ((i & 3) + 8 * (i >> 2)) * kRowBytes<T>;
+          const float v = *(lds_f32)(uintptr_t)((x ^ (((i & 3) | ((i >> 2) & 1) << 2) << 4)) + off);
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, pb[i], o[dt], 0, 0, 0);
+        }
+    }
+  }
+  // A value that is not finite, of row `key`, to the queries that see it.
+  __device__ __forceinline__ void add_not_finite(const void* v, int64_t row, int key, bool skip) {
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float f = at<T>(v, row, 32 * dt + (i & 3) + 8 * (i >> 2) + 4 * h);
+        o[dt][i] += key < limit && !skip && !__builtin_isfinite(f) ? f : 0.f;
+      }
+  }
+};
+
+// Rows first..first + kN - 1 of a slice (row0 its first, n rows held; rows from n on repeat
+// the last) to LDS, permuted as `swizzle` says.
+template <class T, int kN>
+__device__ __forceinline__ void copy_rows(const void* p, int64_t row0, int first, int n, uint32_t lds) {
+  constexpr int kRow = kRowBytes<T>, kPieces = kRow / 16, kRows = 1024 / kRow;   // rows of one copy of 64 x 16 bytes
+  const int lane = threadIdx.x & 63, from = min(first, n - 1);
+  const char* base = static_cast<const char*>(p) + (row0 + from) * kRow;
+#pragma unroll
+  for (int c = 0; c < kN / kRows; ++c) {
+    const int r = c * kRows + lane / kPieces;
+    copy_to_lds(base, min(r, n - 1 - from) * kRow + (((lane % kPieces) ^ swizzle<T>(r)) << 4), lds + c * 1024);
+  }
+}
+
+// Makes values that are not finite 0 in kBytes of LDS that this wave's lanes share;
+// whether there were any.
+template <class T, int kBytes>
+__device__ __forceinline__ bool clear_not_finite(char* p) {
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < kBytes / 1024; ++i) {
+    uint4* v = reinterpret_cast<uint4*>(p + i * 1024) + (threadIdx.x & 63);
+    uint4 u = *v;
+    uint32_t* e = &u.x;
+    bool bad = false;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const bool b0 = sizeof(T) == 2 && (e[c] & 0x7f80u) == 0x7f80u, b1 = (e[c] & 0x7f800000u) == 0x7f800000u;
+      e[c] &= (b0 ? 0xffff0000u : ~0u) & (b1 ? (sizeof(T) == 2 ? 0x0000ffffu : 0u) : ~0u);
+      bad |= b0 | b1;
+    }
+    if (bad) *v = u;
+    any |= bad;
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  return any;
+}
+
+// 16 channels of a query's sums, 32 dt + (i & 3) + 8 (i >> 2) + 4 h, as results or as a part.
+__device__ __forceinline__ void store_sums(const AttnArgs& a, int64_t row, int part, int dt, int h, const f32x16& o,
+                                           float m, float l) {
+  if (a.n_parts > 1) {
+    float* p = a.part + (row * a.n_parts + part) * kPartFloats;
+    if (dt == 0 && h == 0) *reinterpret_cast<float2*>(p) = make_float2(m, l);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2)
+      *reinterpret_cast<float2*>(p + 2 + 32 * dt + (i & 3) + 8 * (i >> 2) + 4 * h) = make_float2(o[i], o[i + 1]);
+    return;
+  }
+  const float inv = inv_sum(l);
+  if (a.lse_out && dt == 0 && h == 0) a.lse_out[row] = lse_of(m, l);
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) {
+    const size_t x = row * kHeadDim + 32 * dt + 2 * i + 4 * h;
+    const float y0 = o[i] * inv, y1 = o[i + 1] * inv, y2 = o[i + 2] * inv, y3 = o[i + 3] * inv;
+    if (a.out_bf16) {
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + x) =
+          make_uint2(f32_to_bf16(y0) | (uint32_t)f32_to_bf16(y1) << 16, f32_to_bf16(y2) | (uint32_t)f32_to_bf16(y3) << 16);
+    } else {
+      *reinterpret_cast<float4*>(static_cast<float*>(a.out) + x) = make_float4(y0, y1, y2, y3);
+    }
+  }
+}
+
+// Up to 32 queries: every wave takes every fourth 32 keys, through its own place in LDS.
+// Up to 16 (bfloat16): lanes n and n + 16 hold the same query, and the second's weights
+// are what rounding the first's leaves over.
+template <class T, bool kOwn>
+__device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* s_ring, float* s_m, float* s_l) {
+  constexpr int kTileBytes = kTile * kRowBytes<T>;
+  const Side& x = kOwn ? a.own : a.prefix;
+  const Place p = place_of<kOwn>(a, id);
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r0 = p.rgrp * 32, n_rows = min(32, p.n_rows - r0);
+  const bool twice = Wave<T>::kBf16 && n_rows <= 16, low = twice && (lane & 16);
+  const int r = r0 + min(lane & (twice ? 15 : 31), n_rows - 1);
+  int least, most;
+  limits_of<kOwn>(a, p, r0, r0 + n_rows - 1, least, most);
+  const int tiles = (most + kTile - 1) / kTile;
+  const int t0 = (int)((int64_t)tiles * p.split / x.splits), t1 = (int)((int64_t)tiles * (p.split + 1) / x.splits);
+  const uint32_t slot = __builtin_amdgcn_readfirstlane(lds_addr(s_ring) + w * 2 * kTileBytes);
+  auto copy = [&](int tile) {
+    copy_rows<T, kTile>(x.k, p.kv_row, tile * kTile, p.n, slot);
+    copy_rows<T, kTile>(x.v, p.kv_row, tile * kTile, p.n, slot + kTileBytes);
+  };
+  Wave<T> f;
+  f.init(a, query_row<kOwn>(a, p, r), limit_of<kOwn>(a, p, r));
+  f.addresses(slot, slot + kTileBytes);
+#pragma unroll
+  for (int c = 0; c < Wave<T>::kQ; ++c) asm volatile("" : "+v"(f.q[c]));   // the queries are in before the copies start
+  if (t0 + w < t1) copy(t0 + w);
+  bool bad = false;
+  for (int tile = t0 + w; tile < t1; tile += kBlockWaves) {
+    const int p0 = tile * kTile;
+    const bool masked = p0 + kTile > least;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // values that a query may not see must not reach it: 0 * inf is NaN
+    if (masked) bad |= __builtin_amdgcn_ballot_w64(clear_not_finite<T, kTileBytes>(s_ring + (w * 2 + 1) * kTileBytes)) != 0;
+    typename Wave<T>::Keys kf;
+    typename Wave<T>::Values vf;
+    typename Wave<T>::Weights pb;
+    f.load_keys(0, kf);
+    f.load_values(0, vf);
+    const bool more = tile + kBlockWaves < t1;
+    if constexpr (Wave<T>::kBf16) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (more) copy(tile + kBlockWaves);       // all of this tile is in registers
+    }
+    f32x16 sc = f.scores(0, kf);
+    f.template soften<Wave<T>::kBf16>(sc, p0, masked, low, pb);
+    if (kOwn && a.logits && f.n < n_rows) {
+      float* to = a.logits + (p.s * p.n_rows + r) * a.logit_stride + p0 + 4 * f.h;
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<float4*>(to + 2 * i) = make_float4(sc[i], sc[i + 1], sc[i + 2], sc[i + 3]);
+    }
+    f.add_values(0, vf, pb);
+    if constexpr (!Wave<T>::kBf16) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (more) copy(tile + kBlockWaves);
+    }
+  }
+  if (bad) {                                    // rare
+#pragma unroll 1
+    for (int tile = t0 + w; tile < t1; tile += kBlockWaves) {
+      if (tile * kTile + kTile <= least) continue;
+#pragma unroll 1
+      for (int key = tile * kTile; key < min(tile * kTile + kTile, most); ++key)
+        f.add_not_finite(x.v, p.kv_row + key, key, low);
+    }
+  }
+  // the waves' sums, in their places in LDS; wave w joins channels 32 w..
+  const float m = f.grow_at == -__builtin_inff() ? -__builtin_inff() : f.base;
+  const float total = f.sum + __shfl_xor(f.sum, 32, kWave);
+  float* mine = reinterpret_cast<float*>(s_ring + w * 2 * kTileBytes) + lane;
+#pragma unroll
+  for (int i = 0; i < 64; ++i) mine[i * 64] = f.o[i >> 4][i & 15];
+  if (f.h == 0) {
+    s_m[w * 32 + f.n] = m;
+    s_l[w * 32 + f.n] = total;
+  }
+  __syncthreads();
+  float mm = s_m[f.n];
+#pragma unroll
+  for (int i = 1; i < kBlockWaves; ++i) mm = fmaxf(mm, s_m[i * 32 + f.n]);
+  float l = 0.f;
+  f32x16 o;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) o[i] = 0.f;
+#pragma unroll
+  for (int v = 0; v < kBlockWaves; ++v) {
+    const float e = __builtin_amdgcn_exp2f(s_m[v * 32 + f.n] - max_base(mm));
+    l += s_l[v * 32 + f.n] * e;
+    const float* from = reinterpret_cast<const float*>(s_ring + v * 2 * kTileBytes) + w * 16 * 64;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float y = from[i * 64 + lane];
+      if (twice) y += from[i * 64 + (lane ^ 16)];
+      o[i] += y * e;
+    }
+  }
+  if (f.n >= n_rows) return;
+  store_sums(a, query_row<kOwn>(a, p, r), (kOwn && a.prefix_blocks ? a.prefix.splits : 0) + p.split, w, f.h, o, mm, l);
+}
+
+// Up to 32 WR queries, 32 a wave; the waves share stages of 64 keys (two places in LDS, one
+// in flight), WR = 2 in halves.
+template <class T, int WR, bool kOwn>
+__device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char* s_ring, int* s_bad) {
+  constexpr int kRow = kRowBytes<T>, kHalf = kStage * kRow, WK = kBlockWaves / WR;
+  const Side& x = kOwn ? a.own : a.prefix;
+  const Place p = place_of<kOwn>(a, id);
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = w % WR, wk = w / WR;
+  const int b0 = p.rgrp * WR * 32, b1 = min(b0 + WR * 32, p.n_rows) - 1;     // the block's queries
+  const int r0 = min(b0 + wr * 32, p.n_rows - 1), r1 = min(r0 + 31, p.n_rows - 1);
+  const int r = min(b0 + wr * 32 + (lane & 31), p.n_rows - 1);
+  int least, most, w_least, w_most;
+  limits_of<kOwn>(a, p, b0, b1, least, most);
+  limits_of<kOwn>(a, p, r0, r1, w_least, w_most);
+  const int stages = (most + kStage - 1) / kStage;
+  const int st0 = (int)((int64_t)stages * p.split / x.splits), st1 = (int)((int64_t)stages * (p.split + 1) / x.splits);
+  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr(s_ring));
+  // a wave's share: 16 rows
+  auto copy = [&](int st, int place) {
+    const uint32_t to = ring + place * 2 * kHalf + w * 16 * kRow;
+    copy_rows<T, 16>(x.k, p.kv_row, st * kStage + w * 16, p.n, to);
+    copy_rows<T, 16>(x.v, p.kv_row, st * kStage + w * 16, p.n, to + kHalf);
+  };
+  Wave<T> f;
+  f.init(a, query_row<kOwn>(a, p, r), limit_of<kOwn>(a, p, r));
+  f.addresses(ring, ring + kHalf);
+#pragma unroll
+  for (int c = 0; c < Wave<T>::kQ; ++c) asm volatile("" : "+v"(f.q[c]));   // the queries are in before the copies start
+  if (threadIdx.x == 0) *s_bad = 0;
+  __syncthreads();
+  if (st0 < st1) copy(st0, 0);
+  // Stage st, which lies at place `at` of the ring (a constant where it is inlined).
+  auto stage = [&](int st, int place) {
+    const int p0 = st * kStage;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (p0 + kStage > least) {                  // block-uniform
+      if (clear_not_finite<T, 16 * kRow>(s_ring + place * 2 * kHalf + kHalf + w * 16 * kRow)) *s_bad = 1;
+    }
+    sync_stage();                               // the stage is in LDS; the other place is free
+    if (st + 1 < st1) copy(st + 1, place ^ 1);
+    typename Wave<T>::Keys kf;
+    typename Wave<T>::Values vf;
+    typename Wave<T>::Weights pb;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (WK == 2 && half != wk) continue;
+      const int k0 = p0 + half * kTile;
+      if (k0 >= w_most) continue;
+      const uint32_t off = place * 2 * kHalf + half * kTile * kRow;
+      f.load_keys(off, kf);
+      f32x16 sc = f.scores(off, kf);
+      f.load_values(off, vf);
+      f.template soften<false>(sc, k0, k0 + kTile > w_least, false, pb);
+      f.add_values(off, vf, pb);
+    }
+  };
+  for (int st = st0; st < st1; st += 2) {
+    stage(st, 0);
+    if (st + 1 < st1) stage(st + 1, 1);
+  }
+  sync_stage();
+  if (*s_bad) {                                 // block-uniform, rare
+#pragma unroll 1
+    for (int st = st0; st < st1; ++st) {
+      if (st * kStage + kStage <= least) continue;
+#pragma unroll 1
+      for (int key = st * kStage; key < min(st * kStage + kStage, w_most); ++key)
+        if (WK == 1 || (key / kTile) % 2 == wk) f.add_not_finite(x.v, p.kv_row + key, key, false);
+    }
+  }
+  float m = f.grow_at == -__builtin_inff() ? -__builtin_inff() : f.base;
+  float total = f.sum + __shfl_xor(f.sum, 32, kWave);
+  if constexpr (WK == 2) {
+    // wk = 1 leaves its sums in LDS, wk = 0 adds them
+    float* mine = reinterpret_cast<float*>(s_ring) + wr * 66 * 64 + lane;
+    __syncthreads();                            // every wave has read s_bad and its last stage
+    if (wk == 1) {
+#pragma unroll
+      for (int i = 0; i < 64; ++i) mine[i * 64] = f.o[i >> 4][i & 15];
+      mine[64 * 64] = m;
+      mine[65 * 64] = total;
+    }
+    __syncthreads();
+    if (wk == 1) return;
+    const float m1 = mine[64 * 64], mm = fmaxf(m, m1);
+    const float f0 = __builtin_amdgcn_exp2f(m - max_base(mm)), f1 = __builtin_amdgcn_exp2f(m1 - max_base(mm));
+    m = mm;
+    total = total * f0 + mine[65 * 64] * f1;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) f.o[i >> 4][i & 15] = f.o[i >> 4][i & 15] * f0 + mine[i * 64] * f1;
+  }
+  if (b0 + wr * 32 + f.n > b1) return;
+  const int64_t row = query_row<kOwn>(a, p, r);
+  const int part = (kOwn && a.prefix_blocks ? a.prefix.splits : 0) + p.split;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) store_sums(a, row, part, dt, f.h, f.o[dt], m, total);
+}
+
+// Blocks of the prefix (WP waves of queries), then of the own rows (WO).
+template <class T, int WP, int WO>
+__global__ __launch_bounds__(kBlockWaves * 64, sizeof(T) == 2 ? 2 : 1)
+void attn_kernel(const AttnArgs a) {
+  __shared__ __align__(256) char s_ring[kRingBytes<T>];
+  __shared__ float s_m[kBlockWaves * 32], s_l[kBlockWaves * 32];
+  __shared__ int s_bad;
+  const int64_t id = blockIdx.x;
+  if (id < a.prefix_blocks) {
+    if constexpr (WP == 1) attend_few<T, false>(a, id, s_ring, s_m, s_l);
+    else attend_many<T, WP, false>(a, id, s_ring, &s_bad);
+  } else {
+    if constexpr (WO == 1) attend_few<T, true>(a, id - a.prefix_blocks, s_ring, s_m, s_l);
+    else attend_many<T, WO, true>(a, id - a.prefix_blocks, s_ring, &s_bad);
+  }
+}
+
+// How a call is cut into blocks.
+struct Cut {
+  int waves_p, waves_o;            // of queries of a block: 1, 2 or 4
+  int groups_p, groups_o;          // blocks that a slice's queries are cut into
+  int splits_p, splits_o;          // parts that its keys are cut into
+  int64_t blocks_p, blocks_o;
+  int n_parts() const { return splits_p + splits_o; }
+};
+constexpr int kGridBlocks = 512;
+Cut cut_of(int64_t n_slices, int64_t n_prefix_slices, int group_size, int n_q, int64_t prefix_rows, int64_t own_rows) {
+  Cut c{};
+  const int64_t mine = (int64_t)group_size * n_q, all = prefix_rows ? mine * (n_slices / n_prefix_slices) : 0;
+  auto waves = [](int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; };
+  auto groups = [](int64_t rows, int w) { return (int)((rows + 32 * w - 1) / (32 * w)); };
+  c.waves_o = waves(mine);
+  c.waves_p = std::max(waves(all), c.waves_o);
+  c.groups_o = groups(mine, c.waves_o);
+  c.groups_p = groups(all, c.waves_p);
+  const int64_t tiles_p = (prefix_rows + kTile - 1) / kTile, tiles_o = (own_rows + kTile - 1) / kTile;
+  const int64_t unit_p = prefix_rows ? n_prefix_slices * c.groups_p : 0, unit_o = own_rows ? n_slices * c.groups_o : 0;
+  const int64_t per = (unit_p * tiles_p + unit_o * tiles_o + kGridBlocks - 1) / kGridBlocks;
+  auto splits = [&](int64_t tiles, int w) {
+    const int64_t least = w == 1 ? 8 : 8 * w;
+    return (int)std::max<int64_t>(1, (tiles + std::max(per, least) - 1) / std::max(per, least));
+  };
+  c.splits_p = prefix_rows ? splits(tiles_p, c.waves_p) : 0;
+  c.splits_o = own_rows ? splits(tiles_o, c.waves_o) : 0;
+  c.blocks_p = unit_p * c.splits_p;
+  c.blocks_o = unit_o * c.splits_o;
+  return c;
+}
+
+template <class T>
+void launch_attn(const AttnArgs& a, const Cut& c, hipStream_t hs) {
+  const unsigned grid = (unsigned)(c.blocks_p + c.blocks_o);
+  switch (c.waves_p * 8 + c.waves_o) {
+    case 8 + 1: attn_kernel<T, 1, 1><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
+    case 16 + 1: attn_kernel<T, 2, 1><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
+    case 16 + 2: attn_kernel<T, 2, 2><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
+    case 32 + 1: attn_kernel<T, 4, 1><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
+    case 32 + 2: attn_kernel<T, 4, 2><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
+    default: attn_kernel<T, 4, 4><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
+  }
 }
 
 struct WeightArgs {
@@ -169,6 +691,21 @@ int check_workspace(const void* workspace, size_t bytes, size_t need) {
   return LOUISKV_OK;
 }
 
+// Neither a prefix nor own rows: every query sees nothing.
+__global__ void no_rows_kernel(void* out, int out_bf16, float* lse_out, int64_t n_rows) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;   // four channels
+  if (i >= n_rows * (kHeadDim / 4)) return;
+  if (out_bf16) static_cast<uint2*>(out)[i] = make_uint2(0, 0);
+  else static_cast<uint4*>(out)[i] = make_uint4(0, 0, 0, 0);
+  if (lse_out && i % (kHeadDim / 4) == 0) lse_out[i / (kHeadDim / 4)] = -__builtin_inff();
+}
+
+int no_rows(const AttnArgs& a, int64_t n_rows, hipStream_t hs) {
+  no_rows_kernel<<<(unsigned)((n_rows * (kHeadDim / 4) + 255) / 256), 256, 0, hs>>>(a.out, a.out_bf16, a.lse_out, n_rows);
+  LKV_CHECK_LAUNCH();
+  return LOUISKV_OK;
+}
+
 }  // namespace
 }  // namespace louiskv
 
@@ -182,7 +719,9 @@ extern "C" size_t louiskv_shared_prefix_attn_workspace_size(int64_t n_slices, in
   if (!served(n_slices, group_size, n_q, own_rows) || prefix_rows < 0 || prefix_rows > kMaxRows ||
       (prefix_rows > 0 && (n_prefix_slices < 1 || n_slices % n_prefix_slices != 0)))
     return 0;
-  return with_weights ? align_up((size_t)n_slices * group_size * n_q * sizeof(float), 256) : 0;
+  const int64_t rows = n_slices * group_size * n_q;
+  const Cut c = cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows);
+  return part_bytes(rows, c.n_parts()) + (with_weights ? align_up((size_t)rows * sizeof(float), 256) : 0);
 }
 
 extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads,
@@ -206,18 +745,25 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
   const size_t need = louiskv_shared_prefix_attn_workspace_size(n_slices, n_prefix_slices, group_size, n_q, d,
                                                                 prefix_rows, own_rows, weights != nullptr);
   if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
-  AttnArgs a;
+  const Cut c = cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows);
+  if (c.blocks_p + c.blocks_o > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
+  const int64_t n_rows = n_slices * group_size * n_q;
+  const size_t parts = part_bytes(n_rows, c.n_parts());
+  AttnArgs a{};
   a.q = q; a.group_size = group_size; a.n_q = n_q; a.scale = scale;
-  a.k_prefix = k_prefix; a.v_prefix = v_prefix; a.n_prefix_slices = prefix_rows ? n_prefix_slices : n_slices;
-  a.prefix_rows = (int)prefix_rows; a.n_prefix = n_prefix;
-  a.k_own = k_own; a.v_own = v_own; a.own_rows = (int)own_rows; a.n_own = n_own;
+  a.n_prefix_slices = prefix_rows ? n_prefix_slices : n_slices;
+  a.n_seqs = (int)(n_slices / a.n_prefix_slices);
+  a.prefix = {k_prefix, v_prefix, n_prefix, (int)prefix_rows, c.groups_p, c.splits_p};
+  a.own = {k_own, v_own, n_own, (int)own_rows, c.groups_o, c.splits_o};
+  a.prefix_blocks = c.blocks_p; a.n_parts = c.n_parts(); a.part = static_cast<float*>(workspace);
   a.out = out; a.out_bf16 = out_dtype == LOUISKV_BF16;
-  a.lse_out = lse_out ? lse_out : weights ? static_cast<float*>(workspace) : nullptr;
+  a.lse_out = lse_out ? lse_out : weights ? reinterpret_cast<float*>(static_cast<char*>(workspace) + parts) : nullptr;
   hipStream_t hs = as_stream(stream);
-  const unsigned grid = (unsigned)(n_slices * group_size * n_q);
-  if (dtype == LOUISKV_BF16) attn_kernel<uint16_t><<<grid, 256, 0, hs>>>(a);
-  else attn_kernel<float><<<grid, 256, 0, hs>>>(a);
+  if (a.n_parts == 0) return no_rows(a, n_rows, hs);
+  if (dtype == LOUISKV_BF16) launch_attn<uint16_t>(a, c, hs);
+  else launch_attn<float>(a, c, hs);
   LKV_CHECK_LAUNCH();
+  if (a.n_parts > 1 && (st = merge_parts(a.part, a.n_parts, n_rows, out, out_dtype, a.lse_out, hs))) return st;
   if (!weights || own_rows == 0) return LOUISKV_OK;
   WeightArgs wa;
   wa.q = q; wa.group_size = group_size; wa.n_q = n_q; wa.scale = scale; wa.keys = k_own; wa.key_rows = (int)own_rows;
