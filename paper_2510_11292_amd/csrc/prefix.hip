@@ -9,7 +9,8 @@
 namespace louiskv {
 namespace {
 
-constexpr int64_t kMaxRows = 1 << 30;   // rows of a slice, queries of a prefix slice
+constexpr int64_t kMaxRows = 1 << 30;      // of a slice
+constexpr int64_t kMaxQueries = 1 << 25;   // of a call, times heads
 
 // The rows of a prefix, or of the slices' own caches.
 struct Side {
@@ -626,36 +627,282 @@ struct WeightArgs {
   const int32_t* n_keys;
   const float* lse;
   float* weights;
+  int64_t n_slices;
+  int splits;        // parts of the queries
+  float* part;       // [splits][slices][key_rows] sums
 };
 
-// A thread a key.
+// Sums of softmax weights by key.  Block: keys, which stay in registers as the operand K^T
+// (KT 32-key tiles a wave), and a part of the queries that see them, 64 at a time through LDS
+// (two places, one in flight), the last tokens first, a token's heads together: blocks
+// of a slice begin with the same queries and meet them in the L2.  Q K^T leaves a lane 16
+// queries of one key, which it adds up.
+constexpr int kQueries = 64;                            // of a stage
+template <class T> constexpr int kKeyTiles = sizeof(T) == 2 ? 2 : 1;
+template <class T> constexpr int kBlockKeys = kBlockWaves * kKeyTiles<T> * kTile;
+
 template <class T>
-__global__ __launch_bounds__(256)
-void weights_kernel(const WeightArgs a, int blocks_per_slice) {
-  const int64_t s = blockIdx.x / blocks_per_slice;
-  const int i = (int)(blockIdx.x % blocks_per_slice) * 256 + threadIdx.x;
-  const int n = length_of(a.n_keys, s, a.key_rows);
-  if (i >= n) return;
-  float total = 0.f;
-  for (int j = 0; j < a.group_size; ++j)
-    for (int t = max(0, i - (n - a.n_q)); t < a.n_q; ++t) {
-      const int64_t row = (s * a.group_size + j) * a.n_q + t;
-      const float lse = a.lse[row];
-      if (lse == -__builtin_inff()) continue;
-      float x = 0.f;
-      for (int c = 0; c < kHeadDim; ++c) x += at<T>(a.q, row, c) * at<T>(a.keys, s * a.key_rows + i, c);
-      total += exp2f(x * (a.scale * kLog2E) - lse * kLog2E);
+__global__ __launch_bounds__(kBlockWaves * 64, 2)
+void weights_kernel(const WeightArgs a) {
+  constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int kRow = kRowBytes<T>, KT = kKeyTiles<T>, kPlace = kQueries * kRow;
+  __shared__ __align__(256) char s_ring[2][kPlace];
+  __shared__ float s_lse[2][kQueries];                  // -lse in base 2
+  __shared__ int s_limit[2][kQueries], s_dead[2];       // keys that a query sees; a stage with a query that adds nothing
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n32 = lane & 31;
+  int64_t id = blockIdx.x;
+  const int64_t s = id % a.n_slices;                    // slices are dealt to the XCDs
+  id /= a.n_slices;
+  const int split = (int)(id % a.splits), kb = (int)(id / a.splits) * kBlockKeys<T>;
+  const int n = length_of(a.n_keys, s, a.key_rows), g = a.group_size;
+  if (kb >= n) return;
+  const int first = max(0, kb - (n - a.n_q));           // the first token that sees one of the keys
+  const int total = (a.n_q - first) * g, stages = (total + kQueries - 1) / kQueries;
+  const int st0 = (int)((int64_t)stages * split / a.splits), st1 = (int)((int64_t)stages * (split + 1) / a.splits);
+  const int magic = 65536 / g + 1;                      // x / g = x * magic >> 16 for x below 80
+  const int wk0 = kb + w * KT * kTile;                  // the wave's first key
+
+  // K^T: 16-byte pieces 2 c + h (bfloat16) or 16 h + c (float32) of key n32 of each tile
+  typedef typename std::conditional<kBf16, bf16x8, f32x4>::type Piece;
+  constexpr int kPiecesOfLane = kBf16 ? 8 : 16;
+  Piece k[KT][kPiecesOfLane];
+#pragma unroll
+  for (int x = 0; x < KT; ++x) {
+    const int key = min(wk0 + x * kTile + n32, n - 1);
+    const Piece* from = reinterpret_cast<const Piece*>(static_cast<const T*>(a.keys) + (s * a.key_rows + key) * kHeadDim);
+#pragma unroll
+    for (int c = 0; c < kPiecesOfLane; ++c) k[x][c] = from[kBf16 ? 2 * c + h : 16 * h + c];
+  }
+
+  // Query r of stage st, the last token first, as its head and token; past the last one, that.
+  auto query = [&](int st, int r, int& head, int& token) {
+    const int base = st * kQueries, t = base / g, x = min(r, total - 1 - base) + base - t * g, dt = x * magic >> 16;
+    head = x - dt * g;
+    token = a.n_q - 1 - t - dt;
+  };
+  float lse_next = 0.f;
+  int limit_next = 0;
+  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr(s_ring));
+  const char* qs = static_cast<const char*>(a.q) + s * g * a.n_q * (int64_t)kRow;
+  auto copy = [&](int st, int place) {
+    constexpr int kPieces = kRow / 16, kRows = 1024 / kRow;
+#pragma unroll
+    for (int c = 0; c < 16 / kRows; ++c) {
+      const int r = w * 16 + c * kRows + lane / kPieces;
+      int head, token;
+      query(st, r, head, token);
+      const char* from = qs + ((int64_t)head * a.n_q + token) * kRow + (((lane % kPieces) ^ swizzle<T>(r & 15)) << 4);
+      const uint32_t to = ring + place * kPlace + (w * 16 + c * kRows) * kRow;
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory", "m0");
     }
-  a.weights[s * a.key_rows + i] += total;
+    if (w == 0) {
+      int head, token;
+      query(st, lane, head, token);
+      lse_next = a.lse[(s * g + head) * a.n_q + token];
+      limit_next = st * kQueries + lane < total ? n - a.n_q + token + 1 : 0;
+    }
+  };
+  uint32_t q_at[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    q_at[c] = kBf16 ? ring + n32 * kRow + ((h ^ swizzle<T>(n32 & 15)) << 4 ^ (c << 5))
+                    : ring + n32 * kRow + h * 256 + ((c ^ swizzle<T>(n32 & 15)) << 4);
+  const float qs2 = a.scale * kLog2E;
+  float sum[KT] = {};
+#pragma unroll
+  for (int x = 0; x < KT; ++x)
+#pragma unroll
+    for (int c = 0; c < kPiecesOfLane; ++c) asm volatile("" : "+v"(k[x][c]));   // the keys are in before the copies start
+  if (st0 < st1) copy(st0, 0);
+  auto stage = [&](int st, int place) {
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(lse_next), "+v"(limit_next)::"memory");
+    if (w == 0) {
+      const bool none = lse_next == -__builtin_inff() || limit_next <= 0;
+      s_lse[place][lane] = none ? -__builtin_inff() : -lse_next * kLog2E;
+      s_limit[place][lane] = none ? 0 : limit_next;
+      const bool any = __builtin_amdgcn_ballot_w64(none) != 0;
+      if (lane == 0) s_dead[place] = any;
+    }
+    sync_stage();
+    if (st + 1 < st1) copy(st + 1, place ^ 1);
+    const bool dead = __builtin_amdgcn_readfirstlane(s_dead[place]) != 0;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      // the tokens of the tile's last and first query bound what is seen
+      const int f0 = st * kQueries + half * 32, f1 = min(f0 + 31, total - 1);
+      if (f0 >= total) break;
+      const int most = n - f0 / g, least = n - f1 / g;
+      if (wk0 >= most) continue;
+      const uint32_t off = place * kPlace + half * 32 * kRow;
+      Piece q[kBf16 ? 8 : 1];
+      if constexpr (kBf16) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) q[c] = *(lds_bf16x8)(uintptr_t)(q_at[c] + off);
+      }
+      f32x4 nl[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) nl[i] = *reinterpret_cast<const f32x4*>(&s_lse[place][half * 32 + 8 * i + 4 * h]);
+#pragma unroll
+      for (int x = 0; x < KT; ++x) {
+        f32x16 sc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+        if constexpr (kBf16) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[c], k[x][c], sc, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            const f32x4 y = *(lds_f32x4)(uintptr_t)((q_at[c & 7] ^ (c >> 3 << 7)) + off);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(y[e], k[x][c][e], sc, 0, 0, 0);
+          }
+        }
+        const int key = wk0 + x * kTile + n32;
+        float part = 0.f;
+        if (dead || wk0 + x * kTile + kTile > least) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int limit = s_limit[place][half * 32 + (i & 3) + 8 * (i >> 2) + 4 * h];
+            part += key < limit ? __builtin_amdgcn_exp2f(fmaf(sc[i], qs2, nl[i >> 2][i & 3])) : 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) part += __builtin_amdgcn_exp2f(fmaf(sc[i], qs2, nl[i >> 2][i & 3]));
+        }
+        sum[x] += part;
+      }
+    }
+  };
+  for (int st = st0; st < st1; st += 2) {
+    stage(st, 0);
+    if (st + 1 < st1) stage(st + 1, 1);
+  }
+#pragma unroll
+  for (int x = 0; x < KT; ++x) {
+    const float y = sum[x] + __shfl_xor(sum[x], 32, kWave);
+    const int key = wk0 + x * kTile + n32;
+    if (h != 0 || key >= n) continue;
+    if (a.splits > 1) a.part[((int64_t)split * a.n_slices + s) * a.key_rows + key] = y;
+    else a.weights[s * a.key_rows + key] += y;
+  }
 }
 
-int launch_weights(const WeightArgs& a, int64_t n_slices, int dtype, hipStream_t hs) {
+// The parts' sums, four keys a thread.
+__global__ __launch_bounds__(256)
+void add_weights_kernel(const WeightArgs a, int blocks_per_slice) {
+  const int64_t s = blockIdx.x / blocks_per_slice;
+  const int i = (int)(blockIdx.x % blocks_per_slice) * 256 + threadIdx.x;
+  if (i >= length_of(a.n_keys, s, a.key_rows)) return;
+  float y = 0.f;
+#pragma unroll 4
+  for (int c = 0; c < a.splits; ++c) y += a.part[((int64_t)c * a.n_slices + s) * a.key_rows + i];
+  a.weights[s * a.key_rows + i] += y;
+}
+
+// Parts that the queries are cut into where few blocks of keys would leave the chip idle.
+int weight_splits(int64_t n_slices, int group_size, int n_q, int64_t key_rows) {
+  const int64_t blocks = n_slices * ((key_rows + kBlockKeys<uint16_t> - 1) / kBlockKeys<uint16_t>);
+  const int64_t stages = ((int64_t)group_size * n_q + kQueries - 1) / kQueries;
+  return blocks >= 512 ? 1 : (int)std::max<int64_t>(1, std::min({512 / std::max<int64_t>(blocks, 1), stages / 4, (int64_t)16}));
+}
+
+size_t weight_bytes(int64_t n_slices, int group_size, int n_q, int64_t key_rows) {
+  const int splits = weight_splits(n_slices, group_size, n_q, key_rows);
+  return splits > 1 ? align_up((size_t)splits * n_slices * key_rows * sizeof(float), 256) : 0;
+}
+
+int launch_weights(WeightArgs a, int dtype, void* workspace, hipStream_t hs) {
+  a.splits = weight_splits(a.n_slices, a.group_size, a.n_q, a.key_rows);
+  a.part = static_cast<float*>(workspace);
+  const int keys = dtype == LOUISKV_BF16 ? kBlockKeys<uint16_t> : kBlockKeys<float>;
+  const int64_t blocks = ((int64_t)a.key_rows + keys - 1) / keys, grid = a.n_slices * blocks * a.splits;
+  if (grid > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
+  if (dtype == LOUISKV_BF16) weights_kernel<uint16_t><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
+  else weights_kernel<float><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
+  LKV_CHECK_LAUNCH();
+  if (a.splits == 1) return LOUISKV_OK;
   const int per = (a.key_rows + 255) / 256;
-  const unsigned grid = (unsigned)(n_slices * per);
-  if (dtype == LOUISKV_BF16) weights_kernel<uint16_t><<<grid, 256, 0, hs>>>(a, per);
-  else weights_kernel<float><<<grid, 256, 0, hs>>>(a, per);
+  if (a.n_slices * per > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
+  add_weights_kernel<<<(unsigned)(a.n_slices * per), 256, 0, hs>>>(a, per);
   LKV_CHECK_LAUNCH();
   return LOUISKV_OK;
+}
+
+// Results of queries cut into parts, and weights of own rows from the logits that the
+// attention left.
+struct FinishArgs {
+  const float* part;
+  int n_parts;
+  int64_t n_rows;
+  void* out;
+  float* lse_out;
+  int64_t merge_blocks;
+  const float* logits;
+  int logit_stride, per_slice;    // queries of a slice, at most 32
+  const float* lse;               // natural, where there is one part
+  const int32_t* n_own;
+  int own_rows, chunks;           // blocks of a slice's rows
+  float* weights;
+};
+constexpr int kFinishKeys = 1024;   // of a block, four a thread
+
+// merge_blocks blocks of a query a wave, then `chunks` of each slice's rows.
+template <class TO>
+__global__ __launch_bounds__(256)
+void finish_kernel(const FinishArgs a) {
+  __shared__ float s_lse[32];
+  int64_t id = blockIdx.x;
+  if (id < a.merge_blocks) {
+    const int64_t row = id * 4 + (threadIdx.x >> 6);
+    if (row < a.n_rows) merge_row(a.part, a.n_parts, row, static_cast<TO*>(a.out), a.lse_out);
+    return;
+  }
+  id -= a.merge_blocks;
+  const int64_t s = id / a.chunks;
+  const int i = (int)(id - s * a.chunks) * kFinishKeys + 4 * threadIdx.x;
+  const int n = length_of(a.n_own, s, a.own_rows), r = threadIdx.x >> 3, j = threadIdx.x & 7;
+  // eight threads a query: its base-2 lse, infinite where it sees nothing
+  if (r < a.per_slice) {
+    float m = -__builtin_inff(), l = 0.f, lse2;
+    if (a.n_parts > 1) {
+      const float* p = a.part + (s * a.per_slice + r) * a.n_parts * kPartFloats;
+      for (int c = j; c < a.n_parts; c += 8) {
+        const float2 ml = *reinterpret_cast<const float2*>(p + (size_t)c * kPartFloats);
+        const float mm = fmaxf(m, ml.x);
+        l = l * __builtin_amdgcn_exp2f(m - max_base(mm)) + ml.y * __builtin_amdgcn_exp2f(ml.x - max_base(mm));
+        m = mm;
+      }
+      for (int o = 1; o < 8; o <<= 1) {
+        const float m1 = __shfl_xor(m, o, kWave), l1 = __shfl_xor(l, o, kWave), mm = fmaxf(m, m1);
+        l = l * __builtin_amdgcn_exp2f(m - max_base(mm)) + l1 * __builtin_amdgcn_exp2f(m1 - max_base(mm));
+        m = mm;
+      }
+      lse2 = l == 0.f ? __builtin_inff() : max_base(m) + log2f(l);
+    } else {
+      const float x = a.lse[s * a.per_slice + r];
+      lse2 = x == -__builtin_inff() ? __builtin_inff() : x * kLog2E;
+    }
+    if (j == 0) s_lse[r] = lse2;
+  }
+  __syncthreads();
+  if (i >= n) return;
+  const float* x = a.logits + s * a.per_slice * a.logit_stride + i;
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int q = 0; q < a.per_slice; ++q) {
+    const float4 v = *reinterpret_cast<const float4*>(x + (int64_t)q * a.logit_stride);
+    const float e = s_lse[q];
+    y.x += __builtin_amdgcn_exp2f(v.x - e);
+    y.y += __builtin_amdgcn_exp2f(v.y - e);
+    y.z += __builtin_amdgcn_exp2f(v.z - e);
+    y.w += __builtin_amdgcn_exp2f(v.w - e);
+  }
+  float* to = a.weights + s * a.own_rows + i;
+  to[0] += y.x;
+  if (i + 1 < n) to[1] += y.y;
+  if (i + 2 < n) to[2] += y.z;
+  if (i + 3 < n) to[3] += y.w;
 }
 
 int check_types(int dtype, int out_dtype) {
@@ -674,7 +921,7 @@ int check_sizes(int64_t n_slices, int32_t n_kv_heads, int32_t group_size, int32_
   if (n_q < 1 || rows < 0 || rows > kMaxRows)
     return fail(LOUISKV_ERR_SHAPE, "n_q=%d must be positive, rows=%lld at most %lld", n_q, (long long)rows,
                 (long long)kMaxRows);
-  if (n_slices > kMaxGrid || n_slices * group_size > kMaxRows / n_q)
+  if (n_slices > kMaxGrid || n_slices * group_size > kMaxQueries / n_q)
     return fail(LOUISKV_ERR_SHAPE, "%lld slices of %d heads and n_q=%d are too many queries for one call",
                 (long long)n_slices, group_size, n_q);
   return LOUISKV_OK;
@@ -682,13 +929,23 @@ int check_sizes(int64_t n_slices, int32_t n_kv_heads, int32_t group_size, int32_
 
 bool served(int64_t n_slices, int32_t group_size, int32_t n_q, int64_t rows) {
   return n_slices >= 1 && n_slices <= kMaxGrid && group_size >= 1 && group_size <= 8 && n_q >= 1 && rows >= 0 &&
-         rows <= kMaxRows && n_slices * group_size <= kMaxRows / n_q;
+         rows <= kMaxRows && n_slices * group_size <= kMaxQueries / n_q;
 }
 
 int check_workspace(const void* workspace, size_t bytes, size_t need) {
   if (need > 0 && (!workspace || bytes < need || !aligned16(workspace)))
     return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, 16-byte aligned, got %zu", need, bytes);
   return LOUISKV_OK;
+}
+
+// Own rows' weights take the logits that the attention leaves where a slice has up to 32
+// queries (8 bytes a row and query, written and read, against its key read again), and the
+// keys anew where it has more.
+int logit_stride(int64_t own_rows) { return (int)align_up((size_t)own_rows, kTile); }
+size_t weight_space(int64_t n_slices, int group_size, int n_q, int64_t own_rows, bool few) {
+  const size_t rows = (size_t)n_slices * group_size * n_q;
+  return align_up(rows * sizeof(float), 256) +
+         (few ? align_up(rows * logit_stride(own_rows) * sizeof(float), 256) : weight_bytes(n_slices, group_size, n_q, own_rows));
 }
 
 // Neither a prefix nor own rows: every query sees nothing.
@@ -721,7 +978,8 @@ extern "C" size_t louiskv_shared_prefix_attn_workspace_size(int64_t n_slices, in
     return 0;
   const int64_t rows = n_slices * group_size * n_q;
   const Cut c = cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows);
-  return part_bytes(rows, c.n_parts()) + (with_weights ? align_up((size_t)rows * sizeof(float), 256) : 0);
+  return part_bytes(rows, c.n_parts()) +
+         (with_weights ? weight_space(n_slices, group_size, n_q, own_rows, c.waves_o == 1) : 0);
 }
 
 extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads,
@@ -760,22 +1018,40 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
   a.lse_out = lse_out ? lse_out : weights ? reinterpret_cast<float*>(static_cast<char*>(workspace) + parts) : nullptr;
   hipStream_t hs = as_stream(stream);
   if (a.n_parts == 0) return no_rows(a, n_rows, hs);
+  char* rest = static_cast<char*>(workspace) + parts + align_up((size_t)n_rows * sizeof(float), 256);
+  const bool with_logits = weights && own_rows > 0 && c.waves_o == 1;
+  if (with_logits) {
+    a.logits = reinterpret_cast<float*>(rest);
+    a.logit_stride = logit_stride(own_rows);
+  }
   if (dtype == LOUISKV_BF16) launch_attn<uint16_t>(a, c, hs);
   else launch_attn<float>(a, c, hs);
   LKV_CHECK_LAUNCH();
+  if (with_logits) {
+    FinishArgs f{};
+    f.part = a.part; f.n_parts = a.n_parts; f.n_rows = n_rows; f.out = out; f.lse_out = a.lse_out;
+    f.merge_blocks = a.n_parts > 1 ? (n_rows + 3) / 4 : 0;
+    f.logits = a.logits; f.logit_stride = a.logit_stride; f.per_slice = group_size * n_q; f.lse = a.lse_out;
+    f.n_own = n_own; f.own_rows = (int)own_rows; f.chunks = (int)((own_rows + kFinishKeys - 1) / kFinishKeys);
+    f.weights = weights;
+    const int64_t grid = f.merge_blocks + n_slices * f.chunks;
+    if (a.out_bf16) finish_kernel<uint16_t><<<(unsigned)grid, 256, 0, hs>>>(f);
+    else finish_kernel<float><<<(unsigned)grid, 256, 0, hs>>>(f);
+    LKV_CHECK_LAUNCH();
+    return LOUISKV_OK;
+  }
   if (a.n_parts > 1 && (st = merge_parts(a.part, a.n_parts, n_rows, out, out_dtype, a.lse_out, hs))) return st;
   if (!weights || own_rows == 0) return LOUISKV_OK;
-  WeightArgs wa;
+  WeightArgs wa{};
   wa.q = q; wa.group_size = group_size; wa.n_q = n_q; wa.scale = scale; wa.keys = k_own; wa.key_rows = (int)own_rows;
-  wa.n_keys = n_own; wa.lse = a.lse_out; wa.weights = weights;
-  return launch_weights(wa, n_slices, dtype, hs);
+  wa.n_keys = n_own; wa.lse = a.lse_out; wa.weights = weights; wa.n_slices = n_slices;
+  return launch_weights(wa, dtype, rest, hs);
 }
 
 extern "C" size_t louiskv_attn_weights_workspace_size(int64_t n_slices, int32_t group_size, int32_t n_q, int32_t d,
                                                       int64_t key_rows) {
   (void)d;
-  if (!served(n_slices, group_size, n_q, key_rows)) return 0;
-  return 0;
+  return served(n_slices, group_size, n_q, key_rows) ? weight_bytes(n_slices, group_size, n_q, key_rows) : 0;
 }
 
 extern "C" int louiskv_attn_weights(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads,
@@ -789,8 +1065,8 @@ extern "C" int louiskv_attn_weights(const void* q, int32_t dtype, int64_t n_slic
   if (!aligned16(q, keys)) return fail(LOUISKV_ERR_UNSUPPORTED, "q and keys must be 16-byte aligned");
   const size_t need = louiskv_attn_weights_workspace_size(n_slices, group_size, n_q, d, key_rows);
   if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
-  WeightArgs a;
+  WeightArgs a{};
   a.q = q; a.group_size = group_size; a.n_q = n_q; a.scale = scale; a.keys = keys; a.key_rows = (int)key_rows;
-  a.n_keys = n_keys; a.lse = lse; a.weights = weights;
-  return launch_weights(a, n_slices, dtype, as_stream(stream));
+  a.n_keys = n_keys; a.lse = lse; a.weights = weights; a.n_slices = n_slices;
+  return launch_weights(a, dtype, workspace, as_stream(stream));
 }
