@@ -27,94 +27,232 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 }
 constexpr uint32_t kProtected = 0xffffffffu;   // above every ordered float
 
-constexpr int kPlanThreads = 256;
+// ------------------------------------------------------------------- which rows stay
 
-// Sum of x over the threads before this one; *total that of all.  Ends with a barrier.
-__device__ __forceinline__ int block_before(int x, int* total, int* s_part) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int v = x;
+// Rows of a slice as order keys: in registers, kValues a lane (a wave's rows are consecutive,
+// 64 at a time: row 64 (kValues w + j) + lane), or recomputed from memory where kValues
+// is 0 and a slice has more rows than that.
+template <int kThreads, int kValues>
+struct Rows {
+  static constexpr int kWaves = kThreads / 64;
+  const float* w;
+  const int32_t* pos;
+  int n, n_first, steps;
+  int64_t recent;
+  uint32_t key[kValues > 0 ? kValues : 1];
+
+  __device__ __forceinline__ uint32_t key_of(int p, float x) const {
+    return p < n_first || p >= recent ? kProtected : ordered(x);
+  }
+  __device__ __forceinline__ int row(int j) const {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    return 64 * ((kValues > 0 ? kValues : steps) * wave + j) + lane;
+  }
+  __device__ __forceinline__ uint32_t get(int j) const {
+    if constexpr (kValues > 0) return key[j];
+    const int i = row(j);
+    return i < n ? key_of(pos ? pos[i] : i, w[i]) : 0;
+  }
+  // f(j, row, key) for the lane's rows
+  template <class F>
+  __device__ __forceinline__ void each(F&& f) const {
+    if constexpr (kValues > 0) {
 #pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int y = __shfl_up(v, o, kWave);
-    if (lane >= o) v += y;
+      for (int j = 0; j < kValues; ++j) f(j, row(j), key[j]);
+    } else {
+      for (int j = 0; j < steps; ++j) f(j, row(j), get(j));
+    }
   }
-  if (lane == 63) s_part[w] = v;
-  __syncthreads();
-  int before = 0, all = 0;
-  for (int i = 0; i < kPlanThreads / 64; ++i) {
-    if (i < w) before += s_part[i];
-    all += s_part[i];
+  // The slice's rows; all loads are on their way together where they stay in registers.
+  __device__ __forceinline__ void load(const PlanArgs& a, int64_t s, int n_, int64_t seen) {
+    n = n_;
+    n_first = a.n_first;
+    w = a.weights + s * a.rows;
+    pos = a.pos ? a.pos + s * a.rows : nullptr;
+    recent = seen - a.n_recent;
+    steps = (n + 64 * kWaves - 1) / (64 * kWaves);
+    if constexpr (kValues > 0) {
+      constexpr int kAtOnce = kValues < 16 ? kValues : 16;
+#pragma unroll
+      for (int j0 = 0; j0 < kValues; j0 += kAtOnce) {
+        float x[kAtOnce];
+        int p[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+          const int i = min(row(j0 + j), n - 1);
+          x[j] = w[i];
+          p[j] = pos ? pos[i] : i;
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) key[j0 + j] = key_of(p[j], x[j]);
+      }
+    }
   }
+};
+
+constexpr int kDigit = 11, kBins = 1 << kDigit;   // 32 bits in digits of 11, 11 and 10: the first tells exponents apart
+template <int kThreads>
+struct Scratch {
+  int hist[kBins];
+  int part[kThreads / 64], part2[kThreads / 64];
+  int digit, need, equal;
+};
+
+// Sum of x over the waves before this one; every lane gives its wave's x.  Ends with a barrier
+// of its own use of `part` at the next call's first.
+template <int kThreads>
+__device__ __forceinline__ int waves_before(int x, int* part) {
+  const int wave = threadIdx.x >> 6;
   __syncthreads();
-  *total = all;
-  return before + v - x;
+  if ((threadIdx.x & 63) == 0) part[wave] = x;
+  __syncthreads();
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) before += i < wave ? part[i] : 0;
+  return before;
 }
 
-// Block: a slice.  The m-th largest key by digits of eight bits, then the rows above
-// it and the last of those that equal it stay.
-__global__ __launch_bounds__(kPlanThreads)
-void plan_kernel(const PlanArgs a) {
-  __shared__ int s_hist[256], s_part[kPlanThreads / 64], s_digit, s_need, s_equal;
-  const int64_t s = blockIdx.x;
-  const int tid = threadIdx.x;
-  const int n = a.n_rows ? max(0, min(a.n_rows[s], a.rows)) : a.rows;
-  const int m = min(n, a.n_keep);
-  const float* w = a.weights + s * a.rows;
-  const int32_t* pos = a.pos ? a.pos + s * a.rows : nullptr;
-  const int64_t recent = (int64_t)(a.pos ? a.n_seen[s] : n) - a.n_recent;
-  auto key = [&](int i) -> uint32_t {
-    const int p = pos ? pos[i] : i;
-    return p < a.n_first || p >= recent ? kProtected : ordered(w[i]);
-  };
-  if (tid == 0) a.kept[s] = m;
-  if (m == 0) return;
+// The m-th largest key of n (1 <= m <= n), how many rows have it and how many of those stay.
+template <int kThreads, int kValues>
+__device__ __forceinline__ uint32_t limit_key(const Rows<kThreads, kValues>& rows, int m, Scratch<kThreads>& x, int& need,
+                                              int& equal) {
+  constexpr int kPer = kBins / kThreads;
+  const int tid = threadIdx.x, lane = tid & 63;
   uint32_t prefix = 0, mask = 0;
-  int need = m, equal = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    s_hist[tid] = 0;
+  need = m;
+  for (int shift = 32 - kDigit;; shift = max(0, shift - kDigit)) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) x.hist[tid + e * kThreads] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += kPlanThreads) {
-      const uint32_t k = key(i);
-      if ((k & mask) == prefix) atomicAdd(&s_hist[(k >> shift) & 255], 1);
+    // the digit's bits that the mask does not hold already
+    rows.each([&](int, int i, uint32_t k) {
+      if (i < rows.n && (k & mask) == prefix) atomicAdd(&x.hist[(k >> shift) & (kBins - 1)], 1);
+    });
+    __syncthreads();
+    // bins from the top, kPer a thread; the digit at which the count reaches `need`
+    int c[kPer], mine = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      c[e] = x.hist[kBins - 1 - (tid * kPer + e)];
+      mine += c[e];
+    }
+    int before = mine;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int y = __shfl_up(before, o, kWave);
+      if (lane >= o) before += y;
+    }
+    const int wave_total = __shfl(before, 63, kWave);
+    before += waves_before<kThreads>(wave_total, x.part) - mine;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      if (before < need && before + c[e] >= need) {   // exactly one bin
+        x.digit = kBins - 1 - (tid * kPer + e);
+        x.need = need - before;
+        x.equal = c[e];
+      }
+      before += c[e];
     }
     __syncthreads();
-    int total;
-    const int c = s_hist[255 - tid], above = block_before(c, &total, s_part);
-    if (above < need && above + c >= need) {   // exactly one thread
-      s_digit = 255 - tid;
-      s_need = need - above;
-      s_equal = c;
-    }
+    prefix |= (uint32_t)x.digit << shift;
+    mask |= (uint32_t)(kBins - 1) << shift;
+    need = x.need;
+    equal = x.equal;
     __syncthreads();
-    prefix |= (uint32_t)s_digit << shift;
-    mask |= 255u << shift;
-    need = s_need;
-    equal = s_equal;
-    __syncthreads();
+    if (shift == 0) return prefix;
+    if (equal == need) return prefix;                  // all rows from this prefix on stay: the lowest key that has it
   }
-  // of `equal` rows at the limit the first equal - need leave
+}
+
+// A row's fate, by rank among those at the limit where only some of them stay: f(j, row, stays)
+// for the lane's rows, every lane in step.
+template <int kThreads, int kValues, class F>
+__device__ __forceinline__ void each_fate(const Rows<kThreads, kValues>& rows, uint32_t limit, int need, int equal,
+                                          Scratch<kThreads>& x, F&& f) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t below = (1ull << lane) - 1;
+  int rank = 0;
+  if (need < equal) {                                  // block-uniform
+    int mine = 0;
+    rows.each([&](int, int i, uint32_t k) { mine += __popcll(__ballot(i < rows.n && k == limit)); });
+    rank = waves_before<kThreads>(mine, x.part2);
+  }
+  rows.each([&](int j, int i, uint32_t k) {
+    bool stays = i < rows.n && k >= limit;
+    if (need < equal) {
+      const uint64_t eq = __ballot(i < rows.n && k == limit);
+      if (k == limit && rank + __popcll(eq & below) < equal - need) stays = false;
+      rank += __popcll(eq);
+    }
+    f(j, i, stays);
+  });
+}
+
+// Block: a slice.  Writes the row that each of the m rows is taken from.
+template <int kThreads, int kValues>
+__global__ __launch_bounds__(kThreads)
+void plan_kernel(const PlanArgs a) {
+  __shared__ Scratch<kThreads> x;
+  const int64_t s = blockIdx.x;
+  const int lane = threadIdx.x & 63;
+  const int n = a.n_rows ? max(0, min(a.n_rows[s], a.rows)) : a.rows, m = min(n, a.n_keep);
+  if (threadIdx.x == 0) a.kept[s] = m;
   int32_t* map = a.map + s * a.n_keep;
   int32_t* movers = a.movers + s * a.n_keep;
-  for (int pass = 0; pass < 2; ++pass) {
-    int seen = 0, found = 0;   // rows at the limit so far; movers (pass 0) or holes (pass 1) so far
-    for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
-      const int i = i0 + tid;
-      const uint32_t k = i < n ? key(i) : 0;
-      const bool eq = i < n && k == prefix;
-      int total;
-      const int rank = seen + block_before(eq, &total, s_part);
-      seen += total;
-      const bool stays = i < n && (k > prefix || (eq && rank >= equal - need));
-      const bool hit = pass == 0 ? stays && i >= m : i < m && !stays;
-      const int at = found + block_before(hit, &total, s_part);
-      found += total;
-      if (pass == 0 && hit) movers[at] = i;
-      if (pass == 1 && i < m) map[i] = hit ? movers[at] : i;
-    }
-    __threadfence_block();
-    __syncthreads();
+  if (m == n) {                                        // none leaves
+    for (int i = threadIdx.x; i < m; i += kThreads) map[i] = i;
+    return;
   }
+  if (m == 0) return;
+  Rows<kThreads, kValues> rows;
+  rows.load(a, s, n, a.pos ? a.n_seen[s] : n);
+  int need, equal;
+  const uint32_t limit = limit_key(rows, m, x, need, equal);
+  const uint64_t below = (1ull << lane) - 1;
+  uint32_t bits = 0;                                   // which of the lane's rows stay
+  if constexpr (kValues > 0)
+    each_fate(rows, limit, need, equal, x, [&](int j, int, bool stays) { bits |= (uint32_t)stays << j; });
+  auto each = [&](auto&& f) {
+    if constexpr (kValues > 0) {
+#pragma unroll
+      for (int j = 0; j < kValues; ++j) f(rows.row(j), (bits >> j & 1) != 0);
+    } else {
+      each_fate(rows, limit, need, equal, x, [&](int, int i, bool stays) { f(i, stays); });
+    }
+  };
+  int late = 0, gone = 0;                              // staying rows from m on, and leaving ones below m, of the wave
+  each([&](int i, bool stays) {
+    late += __popcll(__ballot(stays && i >= m));
+    gone += __popcll(__ballot(!stays && i < m));
+  });
+  late = waves_before<kThreads>(late, x.part);
+  gone = waves_before<kThreads>(gone, x.part);
+  each([&](int i, bool stays) {
+    const uint64_t l = __ballot(stays && i >= m);
+    if (stays && i >= m) movers[late + __popcll(l & below)] = i;
+    if (stays && i < m) map[i] = i;
+    late += __popcll(l);
+  });
+  __threadfence_block();
+  __syncthreads();
+  each([&](int i, bool stays) {
+    const uint64_t g = __ballot(!stays && i < m);
+    if (!stays && i < m) map[i] = movers[gone + __popcll(g & below)];
+    gone += __popcll(g);
+  });
 }
+
+int launch_plan(const PlanArgs& p, int64_t n_slices, hipStream_t hs) {
+  const unsigned grid = (unsigned)n_slices;
+  if (p.rows <= 2048) plan_kernel<256, 8><<<grid, 256, 0, hs>>>(p);
+  else if (p.rows <= 8192) plan_kernel<1024, 8><<<grid, 1024, 0, hs>>>(p);
+  else if (p.rows <= 32768) plan_kernel<1024, 32><<<grid, 1024, 0, hs>>>(p);
+  else plan_kernel<1024, 0><<<grid, 1024, 0, hs>>>(p);
+  LKV_CHECK_LAUNCH();
+  return LOUISKV_OK;
+}
+
+// ------------------------------------------------------------------- moves
 
 struct MoveArgs {
   const void* k;
@@ -125,38 +263,51 @@ struct MoveArgs {
   float* weights_to;
   const int32_t* pos;
   int32_t* pos_to;
-  int rows, rows_to, n_keep, row_bytes;
+  int rows, rows_to, n_keep;
   const int32_t* map;
   const int32_t* kept;
   int32_t* n_rows_to;
 };
 
-// A wave a row: 16-byte pieces of its key, then of its value.
+// Rows 8 a wave, their keys' and values' 16-byte pieces all on their way together.
+constexpr int kMoveRows = 8;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int kRowBytes>
 __global__ __launch_bounds__(256)
 void move_kernel(const MoveArgs a, int blocks_per_slice) {
+  constexpr int kPieces = kRowBytes / 16, kAtOnce = 64 / kPieces, kSteps = kMoveRows / kAtOnce;   // of keys, as of values
   const int64_t s = blockIdx.x / blocks_per_slice;
-  const int i = (int)(blockIdx.x % blocks_per_slice) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int i0 = ((int)(blockIdx.x % blocks_per_slice) * 4 + (threadIdx.x >> 6)) * kMoveRows, lane = threadIdx.x & 63;
   const int m = a.kept[s];
-  if (i == 0 && lane == 0 && a.n_rows_to) a.n_rows_to[s] = m;
-  if (i >= m) return;
-  const int from = a.map[s * a.n_keep + i];
-  const int64_t src = s * a.rows + from, dst = s * a.rows_to + i;
-  const bool moved = from != i;
-  const int pieces = a.row_bytes / 16;
-  for (int c = lane; c < 2 * pieces; c += kWave) {
-    const bool val = c >= pieces;
-    const int p = val ? c - pieces : c;
-    const char* x = static_cast<const char*>(val ? a.v : a.k);
-    char* y = static_cast<char*>(val ? a.v_to : a.k_to);
-    if (moved || x != y)
-      *reinterpret_cast<uint4*>(y + dst * a.row_bytes + 16 * p) =
-          *reinterpret_cast<const uint4*>(x + src * a.row_bytes + 16 * p);
+  if (i0 == 0 && lane == 0 && a.n_rows_to) a.n_rows_to[s] = m;
+  if (i0 >= m) return;
+  // lane j < 8: row i0 + j
+  const int mine = i0 + min(lane, kMoveRows - 1), from = a.map[s * a.n_keep + min(mine, m - 1)];
+  const int64_t src = s * a.rows, dst = s * a.rows_to;
+  const int piece = lane % kPieces * 16;
+  u32x4 k[kSteps] = {}, v[kSteps] = {};
+#pragma unroll
+  for (int j = 0; j < kSteps; ++j) {
+    const int r = j * kAtOnce + lane / kPieces, at = __shfl(from, r, kWave);
+    const bool there = i0 + r < m, moved = at != i0 + r;
+    const int64_t x = (src + at) * kRowBytes + piece;
+    if (there && (moved || a.k_to != a.k)) k[j] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.k) + x);
+    if (there && (moved || a.v_to != a.v)) v[j] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.v) + x);
   }
-  if (lane == 0 && a.weights_to && (moved || a.weights_to != a.weights)) a.weights_to[dst] = a.weights[src];
-  if (lane == 0 && a.pos_to && (moved || a.pos_to != a.pos)) a.pos_to[dst] = a.pos ? a.pos[src] : from;
+#pragma unroll
+  for (int j = 0; j < kSteps; ++j) {
+    const int r = j * kAtOnce + lane / kPieces, at = __shfl(from, r, kWave);
+    const bool there = i0 + r < m, moved = at != i0 + r;
+    const int64_t y = (dst + i0 + r) * kRowBytes + piece;
+    if (there && (moved || a.k_to != a.k)) *reinterpret_cast<u32x4*>(static_cast<char*>(a.k_to) + y) = k[j];
+    if (there && (moved || a.v_to != a.v)) *reinterpret_cast<u32x4*>(static_cast<char*>(a.v_to) + y) = v[j];
+  }
+  if (lane >= kMoveRows || mine >= m) return;
+  if (a.weights_to && (from != mine || a.weights_to != a.weights)) a.weights_to[dst + mine] = a.weights[src + from];
+  if (a.pos_to && (from != mine || a.pos_to != a.pos)) a.pos_to[dst + mine] = a.pos ? a.pos[src + from] : from;
 }
 
-struct AppendArgs {
+struct StoreArgs {
   const void* k_new;
   const void* v_new;
   void* k;
@@ -165,21 +316,23 @@ struct AppendArgs {
   int32_t* pos;
   int32_t* n_rows;
   int32_t* n_seen;
-  int n_new, rows, row_bytes;
+  int n_new;
   const int32_t* kept;
 };
 
-// Block: a slice.
+// The new rows behind the m that stay.  Block: a slice.
+template <int kRowBytes>
 __global__ __launch_bounds__(256)
-void append_kernel(const AppendArgs a) {
+void append_kernel(const StoreArgs a, int rows) {
+  constexpr int kPieces = kRowBytes / 16;
   const int64_t s = blockIdx.x;
-  const int m = a.kept[s], seen = a.n_seen[s], pieces = a.row_bytes / 16;
-  const int64_t dst = s * a.rows + m, src = s * a.n_new;
-  for (int64_t c = threadIdx.x; c < (int64_t)a.n_new * pieces; c += 256) {
-    reinterpret_cast<uint4*>(static_cast<char*>(a.k) + dst * a.row_bytes)[c] =
-        reinterpret_cast<const uint4*>(static_cast<const char*>(a.k_new) + src * a.row_bytes)[c];
-    reinterpret_cast<uint4*>(static_cast<char*>(a.v) + dst * a.row_bytes)[c] =
-        reinterpret_cast<const uint4*>(static_cast<const char*>(a.v_new) + src * a.row_bytes)[c];
+  const int m = a.kept[s], seen = a.n_seen[s];
+  const int64_t dst = s * rows + m, src = s * a.n_new;
+  for (int64_t c = threadIdx.x; c < (int64_t)a.n_new * kPieces; c += 256) {
+    reinterpret_cast<uint4*>(static_cast<char*>(a.k) + dst * kRowBytes)[c] =
+        reinterpret_cast<const uint4*>(static_cast<const char*>(a.k_new) + src * kRowBytes)[c];
+    reinterpret_cast<uint4*>(static_cast<char*>(a.v) + dst * kRowBytes)[c] =
+        reinterpret_cast<const uint4*>(static_cast<const char*>(a.v_new) + src * kRowBytes)[c];
   }
   for (int i = threadIdx.x; i < a.n_new; i += 256) {
     a.weights[dst + i] = 0.f;
@@ -190,6 +343,130 @@ void append_kernel(const AppendArgs a) {
     a.n_rows[s] = m + a.n_new;
     a.n_seen[s] = seen + a.n_new;
   }
+}
+
+// A store that at most 64 rows leave for, in one launch.  Block: a slice.  What a row
+// that moves, and a new one, holds is read beside the weights; the rows that leave are
+// found (one: the least key; more: by digits), and the staying rows among the last go
+// to their places in order.
+constexpr int kMostGone = 64;
+template <int kRowBytes, int kThreads, int kValues>
+__global__ __launch_bounds__(kThreads)
+void store_kernel(const PlanArgs a, const StoreArgs t) {
+  constexpr int kPieces = kRowBytes / 16;
+  __shared__ Scratch<kThreads> x;
+  __shared__ int s_gone[kMostGone], s_n_gone, s_hole[kMostGone], s_to[kMostGone];
+  const int64_t s = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int seen = t.n_seen[s], n = max(0, min(t.n_rows[s], a.rows)), m = min(n, a.n_keep), gone = n - m;
+  const int64_t row0 = s * a.rows;
+  Rows<kThreads, kValues> rows;
+  if (gone > 0) rows.load(a, s, n, seen);
+  // piece c of the last rows: of their keys, then of their values, row by row
+  auto last = [&](int c) -> uint4 {
+    const int r = c / (2 * kPieces), p = c % (2 * kPieces);
+    const char* from = static_cast<const char*>(p < kPieces ? t.k : t.v);
+    return *reinterpret_cast<const uint4*>(from + (row0 + m + r) * kRowBytes + p % kPieces * 16);
+  };
+  auto fresh = [&](int c) -> uint4 {
+    const int r = c / (2 * kPieces), p = c % (2 * kPieces);
+    const char* from = static_cast<const char*>(p < kPieces ? t.k_new : t.v_new);
+    return *reinterpret_cast<const uint4*>(from + (s * t.n_new + r) * kRowBytes + p % kPieces * 16);
+  };
+  auto put = [&](int row, int c, const uint4& u) {
+    const int p = c % (2 * kPieces);
+    char* to = static_cast<char*>(p < kPieces ? t.k : t.v);
+    *reinterpret_cast<uint4*>(to + (row0 + row) * kRowBytes + p % kPieces * 16) = u;
+  };
+  const int moves = gone * 2 * kPieces, news = t.n_new * 2 * kPieces;
+  uint4 move0 = make_uint4(0, 0, 0, 0), new0 = make_uint4(0, 0, 0, 0);
+  float w0 = 0.f;
+  int p0 = 0;
+  if (tid < moves) move0 = last(tid);
+  if (tid < news) new0 = fresh(tid);
+  if (tid < gone) {
+    w0 = t.weights[row0 + m + tid];
+    p0 = t.pos[row0 + m + tid];
+  }
+  if (gone > 0) {
+    if (tid == 0) s_n_gone = 0;
+    if (gone == 1) {
+      // the least key, of equal ones the lowest row
+      uint64_t least = ~0ull;
+      rows.each([&](int, int i, uint32_t k) {
+        if (i < n) least = min(least, (uint64_t)k << 32 | (uint32_t)i);
+      });
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) least = min(least, (uint64_t)__shfl_xor((unsigned long long)least, o, kWave));
+      uint64_t* s_least = reinterpret_cast<uint64_t*>(x.hist);
+      if (lane == 0) s_least[tid >> 6] = least;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kThreads / 64; ++i) least = min(least, s_least[i]);
+      if (tid == 0) s_gone[0] = (int)(uint32_t)least;
+    } else if (m > 0) {
+      int need, equal;
+      const uint32_t limit = limit_key(rows, m, x, need, equal);
+      each_fate(rows, limit, need, equal, x, [&](int, int i, bool stays) {
+        if (i < n && !stays) s_gone[atomicAdd(&s_n_gone, 1)] = i;
+      });
+    } else if (tid < gone) {
+      s_gone[tid] = tid;                               // all leave
+    }
+    __syncthreads();
+    if (tid < 64) {
+      // lane: a row that leaves, and a row of the last ones
+      const int e = lane < gone ? s_gone[lane] : INT32_MAX, c = m + lane;
+      int rank = 0;
+      bool leaves = false;
+      for (int j = 0; j < gone; ++j) {
+        const int y = __builtin_amdgcn_readlane(e, j);
+        rank += y < e;
+        leaves |= y == c;
+      }
+      if (e < m) s_hole[rank] = e;
+      const bool stays = lane < gone && !leaves;
+      const uint64_t b = __ballot(stays);
+      __builtin_amdgcn_wave_barrier();
+      if (lane < gone) s_to[lane] = stays ? s_hole[__popcll(b & ((1ull << lane) - 1))] : -1;
+    }
+    __syncthreads();
+    for (int c = tid; c < moves; c += kThreads) {
+      const int to = s_to[c / (2 * kPieces)];
+      if (to < 0) continue;
+      put(to, c, c == tid ? move0 : last(c));
+    }
+    if (tid < gone && s_to[tid] >= 0) {
+      t.weights[row0 + s_to[tid]] = w0;
+      t.pos[row0 + s_to[tid]] = p0;
+    }
+  }
+  __syncthreads();                                     // what is replaced below has been read, the counts too
+  for (int c = tid; c < news; c += kThreads) put(m + c / (2 * kPieces), c, c == tid ? new0 : fresh(c));
+  for (int i = tid; i < t.n_new; i += kThreads) {
+    t.weights[row0 + m + i] = 0.f;
+    t.pos[row0 + m + i] = seen + i;
+  }
+  if (tid == 0) {
+    t.n_rows[s] = m + t.n_new;
+    t.n_seen[s] = seen + t.n_new;
+  }
+}
+
+// The rows that can leave at once where a slice's buffer is full; whether one launch does.
+constexpr int kStoreRows = 32768;
+bool stores_at_once(int64_t rows, int64_t budget, int64_t n_new) {
+  return rows <= kStoreRows && rows - (budget - n_new) <= kMostGone;
+}
+
+template <int kRowBytes>
+int launch_store(const PlanArgs& p, const StoreArgs& t, int64_t n_slices, hipStream_t hs) {
+  const unsigned grid = (unsigned)n_slices;
+  if (p.rows <= 2048) store_kernel<kRowBytes, 256, 8><<<grid, 256, 0, hs>>>(p, t);
+  else if (p.rows <= 8192) store_kernel<kRowBytes, 1024, 8><<<grid, 1024, 0, hs>>>(p, t);
+  else store_kernel<kRowBytes, 1024, 32><<<grid, 1024, 0, hs>>>(p, t);
+  LKV_CHECK_LAUNCH();
+  return LOUISKV_OK;
 }
 
 size_t plan_bytes(int64_t n_slices, int64_t n_keep) {
@@ -223,9 +500,11 @@ int check_workspace(const void* workspace, size_t bytes, size_t need) {
   return LOUISKV_OK;
 }
 
-int launch_move(const MoveArgs& a, int64_t n_slices, hipStream_t hs) {
-  const int per = std::max(1, (a.n_keep + 3) / 4);
-  move_kernel<<<(unsigned)(n_slices * per), 256, 0, hs>>>(a, per);
+int launch_move(const MoveArgs& a, int64_t n_slices, int dtype, hipStream_t hs) {
+  const int per = std::max(1, (a.n_keep + 4 * kMoveRows - 1) / (4 * kMoveRows));
+  const unsigned grid = (unsigned)(n_slices * per);
+  if (dtype == LOUISKV_BF16) move_kernel<256><<<grid, 256, 0, hs>>>(a, per);
+  else move_kernel<512><<<grid, 256, 0, hs>>>(a, per);
   LKV_CHECK_LAUNCH();
   return LOUISKV_OK;
 }
@@ -285,19 +564,18 @@ extern "C" int louiskv_evict_rows(const float* weights, const int32_t* pos, cons
   p.n_first = n_first; p.n_recent = n_recent;
   carve(p, workspace, n_slices);
   hipStream_t hs = as_stream(stream);
-  plan_kernel<<<(unsigned)n_slices, kPlanThreads, 0, hs>>>(p);
-  LKV_CHECK_LAUNCH();
+  if ((st = launch_plan(p, n_slices, hs))) return st;
   MoveArgs mv;
   mv.k = k; mv.v = v; mv.k_to = k_to; mv.v_to = v_to; mv.weights = weights; mv.weights_to = weights_to; mv.pos = pos;
-  mv.pos_to = pos_to; mv.rows = (int)rows; mv.rows_to = (int)rows_to; mv.n_keep = (int)keep; mv.row_bytes = row_bytes;
+  mv.pos_to = pos_to; mv.rows = (int)rows; mv.rows_to = (int)rows_to; mv.n_keep = (int)keep;
   mv.map = p.map; mv.kept = p.kept; mv.n_rows_to = n_rows_to;
-  return launch_move(mv, n_slices, hs);
+  return launch_move(mv, n_slices, dtype, hs);
 }
 
 extern "C" size_t louiskv_store_evict_workspace_size(int64_t n_slices, int64_t rows, int32_t n_new, int64_t budget) {
   if (n_slices < 1 || n_slices > kMaxGrid || rows < 1 || rows > kMaxRows || n_new < 1 || budget < n_new || budget > rows)
     return 0;
-  return plan_bytes(n_slices, budget - n_new);
+  return stores_at_once(rows, budget, n_new) ? 0 : plan_bytes(n_slices, budget - n_new);
 }
 
 extern "C" int louiskv_store_evict(const void* k_new, const void* v_new, int32_t dtype, int64_t n_slices, int32_t n_new,
@@ -317,20 +595,25 @@ extern "C" int louiskv_store_evict(const void* k_new, const void* v_new, int32_t
   PlanArgs p;
   p.weights = weights; p.pos = pos; p.n_rows = n_rows; p.n_seen = n_seen; p.rows = (int)rows;
   p.n_keep = (int)(budget - n_new); p.n_first = n_first; p.n_recent = n_recent;
-  carve(p, workspace, n_slices);
+  StoreArgs t;
+  t.k_new = k_new; t.v_new = v_new; t.k = k; t.v = v; t.weights = weights; t.pos = pos; t.n_rows = n_rows;
+  t.n_seen = n_seen; t.n_new = n_new; t.kept = nullptr;
   hipStream_t hs = as_stream(stream);
-  plan_kernel<<<(unsigned)n_slices, kPlanThreads, 0, hs>>>(p);
-  LKV_CHECK_LAUNCH();
-  const int row_bytes = kHeadDim * (dtype == LOUISKV_BF16 ? 2 : 4);
+  const bool bf16 = dtype == LOUISKV_BF16;
+  if (stores_at_once(rows, budget, n_new)) {
+    p.map = p.movers = p.kept = nullptr;
+    return bf16 ? launch_store<256>(p, t, n_slices, hs) : launch_store<512>(p, t, n_slices, hs);
+  }
+  carve(p, workspace, n_slices);
+  if ((st = launch_plan(p, n_slices, hs))) return st;
   MoveArgs mv;
   mv.k = k; mv.v = v; mv.k_to = k; mv.v_to = v; mv.weights = weights; mv.weights_to = weights; mv.pos = pos;
-  mv.pos_to = pos; mv.rows = (int)rows; mv.rows_to = (int)rows; mv.n_keep = p.n_keep; mv.row_bytes = row_bytes;
+  mv.pos_to = pos; mv.rows = (int)rows; mv.rows_to = (int)rows; mv.n_keep = p.n_keep;
   mv.map = p.map; mv.kept = p.kept; mv.n_rows_to = nullptr;
-  if ((st = launch_move(mv, n_slices, hs))) return st;
-  AppendArgs ap;
-  ap.k_new = k_new; ap.v_new = v_new; ap.k = k; ap.v = v; ap.weights = weights; ap.pos = pos; ap.n_rows = n_rows;
-  ap.n_seen = n_seen; ap.n_new = n_new; ap.rows = (int)rows; ap.row_bytes = row_bytes; ap.kept = p.kept;
-  append_kernel<<<(unsigned)n_slices, 256, 0, hs>>>(ap);
+  if ((st = launch_move(mv, n_slices, dtype, hs))) return st;
+  t.kept = p.kept;
+  if (bf16) append_kernel<256><<<(unsigned)n_slices, 256, 0, hs>>>(t, (int)rows);
+  else append_kernel<512><<<(unsigned)n_slices, 256, 0, hs>>>(t, (int)rows);
   LKV_CHECK_LAUNCH();
   return LOUISKV_OK;
 }
