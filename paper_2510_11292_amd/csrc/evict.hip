@@ -90,10 +90,14 @@ struct Rows {
   }
 };
 
-constexpr int kDigit = 11, kBins = 1 << kDigit;   // 32 bits in digits of 11, 11 and 10: the first tells exponents apart
-template <int kThreads>
+// 32 bits in digits of 11, 11 and 10: the first tells exponents apart.  Where a
+// lane has many rows there are four counts a bin, so that lanes whose weights are alike meet
+// less often in one word (+ 1: in one bank).
+constexpr int kDigit = 11, kBins = 1 << kDigit, kCopyInts = kBins + 1;
+template <int kThreads, int kValues>
 struct Scratch {
-  int hist[kBins];
+  static constexpr int kCopies = kValues == 8 ? 1 : 4;
+  int hist[kCopies * kCopyInts];
   int part[kThreads / 64], part2[kThreads / 64];
   int digit, need, equal;
 };
@@ -114,26 +118,29 @@ __device__ __forceinline__ int waves_before(int x, int* part) {
 
 // The m-th largest key of n (1 <= m <= n), how many rows have it and how many of those stay.
 template <int kThreads, int kValues>
-__device__ __forceinline__ uint32_t limit_key(const Rows<kThreads, kValues>& rows, int m, Scratch<kThreads>& x, int& need,
+__device__ __forceinline__ uint32_t limit_key(const Rows<kThreads, kValues>& rows, int m, Scratch<kThreads, kValues>& x, int& need,
                                               int& equal) {
-  constexpr int kPer = kBins / kThreads;
+  constexpr int kPer = kBins / kThreads, kCopies = Scratch<kThreads, kValues>::kCopies;
   const int tid = threadIdx.x, lane = tid & 63;
   uint32_t prefix = 0, mask = 0;
   need = m;
   for (int shift = 32 - kDigit;; shift = max(0, shift - kDigit)) {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) x.hist[tid + e * kThreads] = 0;
+    for (int e = 0; e < kPer * kCopies; ++e) x.hist[tid + e * kThreads] = 0;
+    if (tid < kCopies) x.hist[kCopies * kBins + tid] = 0;
     __syncthreads();
     // the digit's bits that the mask does not hold already
     rows.each([&](int, int i, uint32_t k) {
-      if (i < rows.n && (k & mask) == prefix) atomicAdd(&x.hist[(k >> shift) & (kBins - 1)], 1);
+      if (i < rows.n && (k & mask) == prefix) atomicAdd(&x.hist[(lane & (kCopies - 1)) * kCopyInts + ((k >> shift) & (kBins - 1))], 1);
     });
     __syncthreads();
     // bins from the top, kPer a thread; the digit at which the count reaches `need`
     int c[kPer], mine = 0;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
-      c[e] = x.hist[kBins - 1 - (tid * kPer + e)];
+      c[e] = 0;
+#pragma unroll
+      for (int y = 0; y < kCopies; ++y) c[e] += x.hist[y * kCopyInts + kBins - 1 - (tid * kPer + e)];
       mine += c[e];
     }
     int before = mine;
@@ -168,7 +175,7 @@ __device__ __forceinline__ uint32_t limit_key(const Rows<kThreads, kValues>& row
 // for the lane's rows, every lane in step.
 template <int kThreads, int kValues, class F>
 __device__ __forceinline__ void each_fate(const Rows<kThreads, kValues>& rows, uint32_t limit, int need, int equal,
-                                          Scratch<kThreads>& x, F&& f) {
+                                          Scratch<kThreads, kValues>& x, F&& f) {
   const int lane = threadIdx.x & 63;
   const uint64_t below = (1ull << lane) - 1;
   int rank = 0;
@@ -192,7 +199,7 @@ __device__ __forceinline__ void each_fate(const Rows<kThreads, kValues>& rows, u
 template <int kThreads, int kValues>
 __global__ __launch_bounds__(kThreads)
 void plan_kernel(const PlanArgs a) {
-  __shared__ Scratch<kThreads> x;
+  __shared__ Scratch<kThreads, kValues> x;
   const int64_t s = blockIdx.x;
   const int lane = threadIdx.x & 63;
   const int n = a.n_rows ? max(0, min(a.n_rows[s], a.rows)) : a.rows, m = min(n, a.n_keep);
@@ -221,23 +228,35 @@ void plan_kernel(const PlanArgs a) {
     }
   };
   int late = 0, gone = 0;                              // staying rows from m on, and leaving ones below m, of the wave
-  each([&](int i, bool stays) {
-    late += __popcll(__ballot(stays && i >= m));
-    gone += __popcll(__ballot(!stays && i < m));
-  });
+  if constexpr (kValues > 0) {
+    // of the lane's rows the first `lows` are below m
+    const int lows = max(0, min(kValues, (m - rows.row(0) + 63) >> 6));
+    const uint32_t low = (uint32_t)((1ull << lows) - 1);
+    const int l = __popc(bits & ~low), g = lows - __popc(bits & low);
+    late = wave_sum_int(l);
+    gone = wave_sum_int(g);
+  } else {
+    each([&](int i, bool stays) {
+      late += __popcll(__ballot(stays && i >= m));
+      gone += __popcll(__ballot(!stays && i < m));
+    });
+  }
+  const bool any_late = late > 0;
   late = waves_before<kThreads>(late, x.part);
-  gone = waves_before<kThreads>(gone, x.part);
-  each([&](int i, bool stays) {
-    const uint64_t l = __ballot(stays && i >= m);
-    if (stays && i >= m) movers[late + __popcll(l & below)] = i;
-    if (stays && i < m) map[i] = i;
-    late += __popcll(l);
-  });
+  gone = waves_before<kThreads>(gone, x.part2);
+  if (kValues == 0 || any_late) {                      // of the wave
+    each([&](int i, bool stays) {
+      const uint64_t l = __ballot(stays && i >= m);
+      if (stays && i >= m) movers[late + __popcll(l & below)] = i;
+      late += __popcll(l);
+    });
+  }
   __threadfence_block();
   __syncthreads();
+  if (kValues > 0 && rows.row(0) - lane >= m) return;
   each([&](int i, bool stays) {
     const uint64_t g = __ballot(!stays && i < m);
-    if (!stays && i < m) map[i] = movers[gone + __popcll(g & below)];
+    if (i < m) map[i] = stays ? i : movers[gone + __popcll(g & below)];
     gone += __popcll(g);
   });
 }
@@ -354,7 +373,7 @@ template <int kRowBytes, int kThreads, int kValues>
 __global__ __launch_bounds__(kThreads)
 void store_kernel(const PlanArgs a, const StoreArgs t) {
   constexpr int kPieces = kRowBytes / 16;
-  __shared__ Scratch<kThreads> x;
+  __shared__ Scratch<kThreads, kValues> x;
   __shared__ int s_gone[kMostGone], s_n_gone, s_hole[kMostGone], s_to[kMostGone];
   const int64_t s = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63;
