@@ -15,7 +15,7 @@ struct PlanArgs {
   const int32_t* n_seen;
   int rows, n_keep, n_first, n_recent;
   int32_t* map;              // [slices][n_keep]: the row that each row is taken from
-  int32_t* movers;           // [slices][n_keep]: the staying rows from m on, ascending
+  int32_t* movers;           // [slices][n_keep]: the staying rows from m on, ascending (slices of more than kPlanRows)
   int32_t* kept;             // [slices]: m
 };
 
@@ -90,14 +90,13 @@ struct Rows {
   }
 };
 
-// 32 bits in digits of 11, 11 and 10: the first tells exponents apart.  Where a
-// lane has many rows there are four counts a bin, so that lanes whose weights are alike meet
-// less often in one word (+ 1: in one bank).
-constexpr int kDigit = 11, kBins = 1 << kDigit, kCopyInts = kBins + 1;
-template <int kThreads, int kValues>
+// 32 bits in digits of 11, 11 and 10: the first tells exponents apart.  (More counts a bin, so
+// that lanes whose weights are alike meet less often, took as long: 6.4 us for 32768 rows with
+// one, two, eight or sixteen.)
+constexpr int kDigit = 11, kBins = 1 << kDigit;
+template <int kThreads>
 struct Scratch {
-  static constexpr int kCopies = kValues == 8 ? 1 : 4;
-  int hist[kCopies * kCopyInts];
+  int hist[kBins];
   int part[kThreads / 64], part2[kThreads / 64];
   int digit, need, equal;
 };
@@ -118,29 +117,26 @@ __device__ __forceinline__ int waves_before(int x, int* part) {
 
 // The m-th largest key of n (1 <= m <= n), how many rows have it and how many of those stay.
 template <int kThreads, int kValues>
-__device__ __forceinline__ uint32_t limit_key(const Rows<kThreads, kValues>& rows, int m, Scratch<kThreads, kValues>& x, int& need,
+__device__ __forceinline__ uint32_t limit_key(const Rows<kThreads, kValues>& rows, int m, Scratch<kThreads>& x, int& need,
                                               int& equal) {
-  constexpr int kPer = kBins / kThreads, kCopies = Scratch<kThreads, kValues>::kCopies;
+  constexpr int kPer = kBins / kThreads;
   const int tid = threadIdx.x, lane = tid & 63;
   uint32_t prefix = 0, mask = 0;
   need = m;
   for (int shift = 32 - kDigit;; shift = max(0, shift - kDigit)) {
 #pragma unroll
-    for (int e = 0; e < kPer * kCopies; ++e) x.hist[tid + e * kThreads] = 0;
-    if (tid < kCopies) x.hist[kCopies * kBins + tid] = 0;
+    for (int e = 0; e < kPer; ++e) x.hist[tid + e * kThreads] = 0;
     __syncthreads();
     // the digit's bits that the mask does not hold already
     rows.each([&](int, int i, uint32_t k) {
-      if (i < rows.n && (k & mask) == prefix) atomicAdd(&x.hist[(lane & (kCopies - 1)) * kCopyInts + ((k >> shift) & (kBins - 1))], 1);
+      if (i < rows.n && (k & mask) == prefix) atomicAdd(&x.hist[(k >> shift) & (kBins - 1)], 1);
     });
     __syncthreads();
     // bins from the top, kPer a thread; the digit at which the count reaches `need`
     int c[kPer], mine = 0;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
-      c[e] = 0;
-#pragma unroll
-      for (int y = 0; y < kCopies; ++y) c[e] += x.hist[y * kCopyInts + kBins - 1 - (tid * kPer + e)];
+      c[e] = x.hist[kBins - 1 - (tid * kPer + e)];
       mine += c[e];
     }
     int before = mine;
@@ -175,7 +171,7 @@ __device__ __forceinline__ uint32_t limit_key(const Rows<kThreads, kValues>& row
 // for the lane's rows, every lane in step.
 template <int kThreads, int kValues, class F>
 __device__ __forceinline__ void each_fate(const Rows<kThreads, kValues>& rows, uint32_t limit, int need, int equal,
-                                          Scratch<kThreads, kValues>& x, F&& f) {
+                                          Scratch<kThreads>& x, F&& f) {
   const int lane = threadIdx.x & 63;
   const uint64_t below = (1ull << lane) - 1;
   int rank = 0;
@@ -199,13 +195,12 @@ __device__ __forceinline__ void each_fate(const Rows<kThreads, kValues>& rows, u
 template <int kThreads, int kValues>
 __global__ __launch_bounds__(kThreads)
 void plan_kernel(const PlanArgs a) {
-  __shared__ Scratch<kThreads, kValues> x;
+  __shared__ Scratch<kThreads> x;
   const int64_t s = blockIdx.x;
   const int lane = threadIdx.x & 63;
   const int n = a.n_rows ? max(0, min(a.n_rows[s], a.rows)) : a.rows, m = min(n, a.n_keep);
   if (threadIdx.x == 0) a.kept[s] = m;
   int32_t* map = a.map + s * a.n_keep;
-  int32_t* movers = a.movers + s * a.n_keep;
   if (m == n) {                                        // none leaves
     for (int i = threadIdx.x; i < m; i += kThreads) map[i] = i;
     return;
@@ -216,56 +211,72 @@ void plan_kernel(const PlanArgs a) {
   int need, equal;
   const uint32_t limit = limit_key(rows, m, x, need, equal);
   const uint64_t below = (1ull << lane) - 1;
-  uint32_t bits = 0;                                   // which of the lane's rows stay
-  if constexpr (kValues > 0)
-    each_fate(rows, limit, need, equal, x, [&](int j, int, bool stays) { bits |= (uint32_t)stays << j; });
-  auto each = [&](auto&& f) {
-    if constexpr (kValues > 0) {
-#pragma unroll
-      for (int j = 0; j < kValues; ++j) f(rows.row(j), (bits >> j & 1) != 0);
-    } else {
-      each_fate(rows, limit, need, equal, x, [&](int, int i, bool stays) { f(i, stays); });
-    }
-  };
-  int late = 0, gone = 0;                              // staying rows from m on, and leaving ones below m, of the wave
   if constexpr (kValues > 0) {
-    // of the lane's rows the first `lows` are below m
-    const int lows = max(0, min(kValues, (m - rows.row(0) + 63) >> 6));
-    const uint32_t low = (uint32_t)((1ull << lows) - 1);
-    const int l = __popc(bits & ~low), g = lows - __popc(bits & low);
-    late = wave_sum_int(l);
-    gone = wave_sum_int(g);
+    // which rows stay, a word 64 of them; a thread a word counts those from m on and the gaps below
+    constexpr int kWords = kThreads / 64 * kValues;
+    __shared__ uint64_t s_word[kWords];
+    __shared__ uint16_t s_gaps[kWords], s_mover[kWords * 32];
+    const int tid = threadIdx.x;
+    uint64_t word = 0;
+    each_fate(rows, limit, need, equal, x, [&](int j, int, bool stays) {
+      const uint64_t b = __ballot(stays);
+      if (lane == j) word = b;
+    });
+    if (lane < kValues) s_word[(tid >> 6) * kValues + lane] = word;
+    __syncthreads();
+    uint64_t late = 0;
+    int mine = 0;                                      // staying rows from m on, and gaps below m in the upper half
+    if (tid < kWords) {
+      const int lows = max(0, min(64, m - 64 * tid));
+      const uint64_t low = lows == 64 ? ~0ull : (1ull << lows) - 1;
+      late = s_word[tid] & ~low;
+      mine = __popcll(late) + (__popcll(~s_word[tid] & low) << 16);
+    }
+    int before = mine;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int y = __shfl_up(before, o, kWave);
+      if (lane >= o) before += y;
+    }
+    const int wave_total = __shfl(before, 63, kWave);
+    before += waves_before<kThreads>(wave_total, x.part) - mine;
+    if (tid < kWords) s_gaps[tid] = (uint16_t)(before >> 16);
+    for (int at = before & 0xffff; late; late &= late - 1) s_mover[at++] = (uint16_t)(64 * tid + __ffsll((unsigned long long)late) - 1);
+    __syncthreads();
+    for (int i = tid; i < m; i += kThreads) {
+      const uint64_t u = s_word[i >> 6];
+      map[i] = u >> (i & 63) & 1 ? i : s_mover[s_gaps[i >> 6] + __popcll(~u & ((1ull << (i & 63)) - 1))];
+    }
   } else {
-    each([&](int i, bool stays) {
+    int32_t* movers = a.movers + s * a.n_keep;
+    int late = 0, gone = 0;                            // staying rows from m on, and leaving ones below m, of the wave
+    each_fate(rows, limit, need, equal, x, [&](int, int i, bool stays) {
       late += __popcll(__ballot(stays && i >= m));
       gone += __popcll(__ballot(!stays && i < m));
     });
-  }
-  const bool any_late = late > 0;
-  late = waves_before<kThreads>(late, x.part);
-  gone = waves_before<kThreads>(gone, x.part2);
-  if (kValues == 0 || any_late) {                      // of the wave
-    each([&](int i, bool stays) {
+    late = waves_before<kThreads>(late, x.part);
+    gone = waves_before<kThreads>(gone, x.part);
+    each_fate(rows, limit, need, equal, x, [&](int, int i, bool stays) {
       const uint64_t l = __ballot(stays && i >= m);
       if (stays && i >= m) movers[late + __popcll(l & below)] = i;
       late += __popcll(l);
     });
+    __threadfence_block();
+    __syncthreads();
+    each_fate(rows, limit, need, equal, x, [&](int, int i, bool stays) {
+      const uint64_t g = __ballot(!stays && i < m);
+      if (i < m) map[i] = stays ? i : movers[gone + __popcll(g & below)];
+      gone += __popcll(g);
+    });
   }
-  __threadfence_block();
-  __syncthreads();
-  if (kValues > 0 && rows.row(0) - lane >= m) return;
-  each([&](int i, bool stays) {
-    const uint64_t g = __ballot(!stays && i < m);
-    if (i < m) map[i] = stays ? i : movers[gone + __popcll(g & below)];
-    gone += __popcll(g);
-  });
 }
 
+constexpr int kPlanRows = 32768;   // that a block holds in registers
 int launch_plan(const PlanArgs& p, int64_t n_slices, hipStream_t hs) {
   const unsigned grid = (unsigned)n_slices;
   if (p.rows <= 2048) plan_kernel<256, 8><<<grid, 256, 0, hs>>>(p);
   else if (p.rows <= 8192) plan_kernel<1024, 8><<<grid, 1024, 0, hs>>>(p);
-  else if (p.rows <= 32768) plan_kernel<1024, 32><<<grid, 1024, 0, hs>>>(p);
+  else if (p.rows <= kPlanRows) plan_kernel<1024, 32><<<grid, 1024, 0, hs>>>(p);
   else plan_kernel<1024, 0><<<grid, 1024, 0, hs>>>(p);
   LKV_CHECK_LAUNCH();
   return LOUISKV_OK;
@@ -373,7 +384,7 @@ template <int kRowBytes, int kThreads, int kValues>
 __global__ __launch_bounds__(kThreads)
 void store_kernel(const PlanArgs a, const StoreArgs t) {
   constexpr int kPieces = kRowBytes / 16;
-  __shared__ Scratch<kThreads, kValues> x;
+  __shared__ Scratch<kThreads> x;
   __shared__ int s_gone[kMostGone], s_n_gone, s_hole[kMostGone], s_to[kMostGone];
   const int64_t s = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -473,9 +484,8 @@ void store_kernel(const PlanArgs a, const StoreArgs t) {
 }
 
 // The rows that can leave at once where a slice's buffer is full; whether one launch does.
-constexpr int kStoreRows = 32768;
 bool stores_at_once(int64_t rows, int64_t budget, int64_t n_new) {
-  return rows <= kStoreRows && rows - (budget - n_new) <= kMostGone;
+  return rows <= kPlanRows && rows - (budget - n_new) <= kMostGone;
 }
 
 template <int kRowBytes>
@@ -488,15 +498,15 @@ int launch_store(const PlanArgs& p, const StoreArgs& t, int64_t n_slices, hipStr
   return LOUISKV_OK;
 }
 
-size_t plan_bytes(int64_t n_slices, int64_t n_keep) {
-  return align_up((size_t)n_slices * 4, 256) + 2 * align_up((size_t)n_slices * n_keep * 4, 256);
+size_t plan_bytes(int64_t n_slices, int64_t rows, int64_t n_keep) {
+  return align_up((size_t)n_slices * 4, 256) + (rows > kPlanRows ? 2 : 1) * align_up((size_t)n_slices * n_keep * 4, 256);
 }
 
 void carve(PlanArgs& p, void* workspace, int64_t n_slices) {
   Carver c(workspace);
   p.kept = c.take<int32_t>(n_slices);
   p.map = c.take<int32_t>((size_t)n_slices * p.n_keep);
-  p.movers = c.take<int32_t>((size_t)n_slices * p.n_keep);
+  p.movers = p.rows > kPlanRows ? c.take<int32_t>((size_t)n_slices * p.n_keep) : nullptr;
 }
 
 int check_sizes(int dtype, int64_t n_slices, int32_t d, int64_t rows, int64_t n_keep, int32_t n_first,
@@ -540,7 +550,7 @@ using namespace louiskv;
 
 extern "C" size_t louiskv_evict_rows_workspace_size(int64_t n_slices, int64_t rows, int64_t n_keep) {
   if (n_slices < 1 || n_slices > kMaxGrid || rows < 1 || rows > kMaxRows || n_keep < 1) return 0;
-  return plan_bytes(n_slices, std::min(rows, n_keep));
+  return plan_bytes(n_slices, rows, std::min(rows, n_keep));
 }
 
 extern "C" int louiskv_evict_rows(const float* weights, const int32_t* pos, const int32_t* n_rows,
@@ -594,7 +604,7 @@ extern "C" int louiskv_evict_rows(const float* weights, const int32_t* pos, cons
 extern "C" size_t louiskv_store_evict_workspace_size(int64_t n_slices, int64_t rows, int32_t n_new, int64_t budget) {
   if (n_slices < 1 || n_slices > kMaxGrid || rows < 1 || rows > kMaxRows || n_new < 1 || budget < n_new || budget > rows)
     return 0;
-  return stores_at_once(rows, budget, n_new) ? 0 : plan_bytes(n_slices, budget - n_new);
+  return stores_at_once(rows, budget, n_new) ? 0 : plan_bytes(n_slices, rows, budget - n_new);
 }
 
 extern "C" int louiskv_store_evict(const void* k_new, const void* v_new, int32_t dtype, int64_t n_slices, int32_t n_new,
