@@ -33,15 +33,13 @@ __device__ __forceinline__ float inv_sum(float l) { return l == 0.f ? 0.f : 1.f 
 // base-2 maximum and sum -> natural log of the softmax denominator
 __device__ __forceinline__ float lse_of(float m, float l) { return kLn2 * (max_base(m) + log2f(l)); }
 
-// One wave per row; lane k holds dims 2k, 2k + 1.  Lane c loads the maximum and sum
+// A wave joins n_parts parts of a row (at least one): their maximum m, and the sum l and, in
+// lane k, dims 2k and 2k + 1 of the weighted sums against it.  Lane c loads the maximum and sum
 // of part c; a batch of parts' weighted sums is on its way meanwhile (32 rows of 17
 // parts: 3.6 us, most of it the trips to memory; four loads at a time, 4.2).
 constexpr int kMergeParts = 16;
-template <class TO>
-__device__ __forceinline__ void merge_row(const float* __restrict__ part, int n_parts, int64_t row,
-                                          TO* __restrict__ out, float* __restrict__ lse_out) {
+__device__ __forceinline__ void join_parts(const float* __restrict__ p, int n_parts, float& m, float& l, float& a0, float& a1) {
   const int lane = threadIdx.x & 63;
-  const float* p = part + (size_t)row * n_parts * kPartFloats;
   float2 x[kMergeParts];
   auto load = [&](int c0) {
 #pragma unroll
@@ -50,11 +48,11 @@ __device__ __forceinline__ void merge_row(const float* __restrict__ part, int n_
   };
   float2 ml = *reinterpret_cast<const float2*>(p + (size_t)min(lane, n_parts - 1) * kPartFloats);
   load(0);
-  float m = ml.x;
+  m = ml.x;
   for (int c = kWave + lane; c < n_parts; c += kWave) m = fmaxf(m, p[(size_t)c * kPartFloats]);
   m = wave_max(m);
   const float base = max_base(m);
-  float l = 0.f, a0 = 0.f, a1 = 0.f;
+  l = 0.f, a0 = 0.f, a1 = 0.f;
   for (int c0 = 0; c0 < n_parts; c0 += kMergeParts) {
     if (c0 > 0) {
       load(c0);
@@ -71,6 +69,14 @@ __device__ __forceinline__ void merge_row(const float* __restrict__ part, int n_
         a1 += x[b].y * w;
       }
   }
+}
+
+template <class TO>
+__device__ __forceinline__ void merge_row(const float* __restrict__ part, int n_parts, int64_t row,
+                                          TO* __restrict__ out, float* __restrict__ lse_out) {
+  const int lane = threadIdx.x & 63;
+  float m, l, a0, a1;
+  join_parts(part + (size_t)row * n_parts * kPartFloats, n_parts, m, l, a0, a1);
   const float inv = inv_sum(l);
   store_from_f32(out + (size_t)row * kHeadDim, 2 * lane, a0 * inv);
   store_from_f32(out + (size_t)row * kHeadDim, 2 * lane + 1, a1 * inv);

@@ -29,9 +29,11 @@ struct AttnArgs {
   Side prefix, own;
   int64_t prefix_blocks;
   int n_parts;              // of a query: the prefix's, then its own rows'
+  int stream;               // rows that one block reads bypass the caches
   float* part;
   float* logits;            // [slices][group_size * n_q][logit_stride], base 2, or NULL
   int logit_stride;
+  float* weights;
   void* out;
   int out_bf16;
   float* lse_out;
@@ -296,15 +298,19 @@ struct Wave {
 // Rows first..first + kN - 1 of a slice (row0 its first, n rows held; rows from n on repeat
 // the last) to LDS, permuted as `swizzle` says.
 template <class T, int kN>
-__device__ __forceinline__ void copy_rows(const void* p, int64_t row0, int first, int n, uint32_t lds) {
+__device__ __forceinline__ void copy_rows(const void* p, int64_t row0, int first, int n, uint32_t lds, bool stream) {
   constexpr int kRow = kRowBytes<T>, kPieces = kRow / 16, kRows = 1024 / kRow;   // rows of one copy of 64 x 16 bytes
   const int lane = threadIdx.x & 63, from = min(first, n - 1);
   const char* base = static_cast<const char*>(p) + (row0 + from) * kRow;
+  auto copies = [&](auto&& copy) {
 #pragma unroll
-  for (int c = 0; c < kN / kRows; ++c) {
-    const int r = c * kRows + lane / kPieces;
-    copy_to_lds(base, min(r, n - 1 - from) * kRow + (((lane % kPieces) ^ swizzle<T>(r)) << 4), lds + c * 1024);
-  }
+    for (int c = 0; c < kN / kRows; ++c) {
+      const int r = c * kRows + lane / kPieces;
+      copy(base, min(r, n - 1 - from) * kRow + (((lane % kPieces) ^ swizzle<T>(r)) << 4), lds + c * 1024);
+    }
+  };
+  if (stream) copies([](const void* b, uint32_t off, uint32_t to) { stream_to_lds(b, off, to); });
+  else copies([](const void* b, uint32_t off, uint32_t to) { copy_to_lds(b, off, to); });
 }
 
 // Makes values that are not finite 0 in kBytes of LDS that this wave's lanes share;
@@ -357,6 +363,26 @@ __device__ __forceinline__ void store_sums(const AttnArgs& a, int64_t row, int p
   }
 }
 
+// Adds to the weights of rows i .. i + 3 of n what n_queries give them: 2^(logit - lse), lse
+// infinite where a query sees nothing.
+__device__ __forceinline__ void add_weights(const float* logits, int stride, int n_queries, const float* lse, int n, int i,
+                                            float* weights) {
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int q = 0; q < n_queries; ++q) {
+    const float4 v = *reinterpret_cast<const float4*>(logits + (int64_t)q * stride + i);
+    const float e = lse[q];
+    y.x += __builtin_amdgcn_exp2f(v.x - e);
+    y.y += __builtin_amdgcn_exp2f(v.y - e);
+    y.z += __builtin_amdgcn_exp2f(v.z - e);
+    y.w += __builtin_amdgcn_exp2f(v.w - e);
+  }
+  weights[i] += y.x;
+  if (i + 1 < n) weights[i + 1] += y.y;
+  if (i + 2 < n) weights[i + 2] += y.z;
+  if (i + 3 < n) weights[i + 3] += y.w;
+}
+
 // Up to 32 queries: every wave takes every fourth 32 keys, through its own place in LDS.
 // Up to 16 (bfloat16): lanes n and n + 16 hold the same query, and the second's weights
 // are what rounding the first's leaves over.
@@ -375,8 +401,8 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* 
   const int t0 = (int)((int64_t)tiles * p.split / x.splits), t1 = (int)((int64_t)tiles * (p.split + 1) / x.splits);
   const uint32_t slot = __builtin_amdgcn_readfirstlane(lds_addr(s_ring) + w * 2 * kTileBytes);
   auto copy = [&](int tile) {
-    copy_rows<T, kTile>(x.k, p.kv_row, tile * kTile, p.n, slot);
-    copy_rows<T, kTile>(x.v, p.kv_row, tile * kTile, p.n, slot + kTileBytes);
+    copy_rows<T, kTile>(x.k, p.kv_row, tile * kTile, p.n, slot, a.stream);
+    copy_rows<T, kTile>(x.v, p.kv_row, tile * kTile, p.n, slot + kTileBytes, a.stream);
   };
   Wave<T> f;
   f.init(a, query_row<kOwn>(a, p, r), limit_of<kOwn>(a, p, r));
@@ -454,8 +480,15 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* 
       o[i] += y * e;
     }
   }
-  if (f.n >= n_rows) return;
-  store_sums(a, query_row<kOwn>(a, p, r), (kOwn && a.prefix_blocks ? a.prefix.splits : 0) + p.split, w, f.h, o, mm, l);
+  if (f.n < n_rows)
+    store_sums(a, query_row<kOwn>(a, p, r), (kOwn && a.prefix_blocks ? a.prefix.splits : 0) + p.split, w, f.h, o, mm, l);
+  if (!kOwn || !a.logits || a.n_parts > 1) return;
+  // the block has seen all there is: its rows' weights from the logits that its waves left
+  if (w == 0 && f.h == 0) s_m[f.n] = l == 0.f ? __builtin_inff() : max_base(mm) + log2f(l);
+  __syncthreads();
+  const float* logits = a.logits + p.s * p.n_rows * a.logit_stride;
+  for (int i = threadIdx.x * 4; i < p.n; i += kBlockWaves * 64 * 4)
+    add_weights(logits, a.logit_stride, p.n_rows, s_m, p.n, i, a.weights + p.s * x.rows);
 }
 
 // Up to 32 WR queries, 32 a wave; the waves share stages of 64 keys (two places in LDS, one
@@ -478,8 +511,8 @@ __device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char*
   // a wave's share: 16 rows
   auto copy = [&](int st, int place) {
     const uint32_t to = ring + place * 2 * kHalf + w * 16 * kRow;
-    copy_rows<T, 16>(x.k, p.kv_row, st * kStage + w * 16, p.n, to);
-    copy_rows<T, 16>(x.v, p.kv_row, st * kStage + w * 16, p.n, to + kHalf);
+    copy_rows<T, 16>(x.k, p.kv_row, st * kStage + w * 16, p.n, to, a.stream && x.row_groups == 1);
+    copy_rows<T, 16>(x.v, p.kv_row, st * kStage + w * 16, p.n, to + kHalf, a.stream && x.row_groups == 1);
   };
   Wave<T> f;
   f.init(a, query_row<kOwn>(a, p, r), limit_of<kOwn>(a, p, r));
@@ -593,17 +626,26 @@ Cut cut_of(int64_t n_slices, int64_t n_prefix_slices, int group_size, int n_q, i
   c.groups_p = groups(all, c.waves_p);
   const int64_t tiles_p = (prefix_rows + kTile - 1) / kTile, tiles_o = (own_rows + kTile - 1) / kTile;
   const int64_t unit_p = prefix_rows ? n_prefix_slices * c.groups_p : 0, unit_o = own_rows ? n_slices * c.groups_o : 0;
-  const int64_t per = (unit_p * tiles_p + unit_o * tiles_o + kGridBlocks - 1) / kGridBlocks;
-  auto splits = [&](int64_t tiles, int w) {
-    const int64_t least = w == 1 ? 8 : 8 * w;
-    return (int)std::max<int64_t>(1, (tiles + std::max(per, least) - 1) / std::max(per, least));
-  };
-  c.splits_p = prefix_rows ? splits(tiles_p, c.waves_p) : 0;
-  c.splits_o = own_rows ? splits(tiles_o, c.waves_o) : 0;
+  // as many tiles a block as make kGridBlocks blocks or fewer of what they can be made of
+  int64_t per = (unit_p * tiles_p + unit_o * tiles_o + kGridBlocks - 1) / kGridBlocks;
+  for (;; ++per) {
+    auto splits = [&](int64_t tiles, int w) {
+      const int64_t each = std::max<int64_t>(per, 8 * w);
+      return (int)std::max<int64_t>(1, (tiles + each - 1) / each);
+    };
+    c.splits_p = prefix_rows ? splits(tiles_p, c.waves_p) : 0;
+    c.splits_o = own_rows ? splits(tiles_o, c.waves_o) : 0;
+    if (unit_p + unit_o > kGridBlocks / 2 || unit_p * c.splits_p + unit_o * c.splits_o <= kGridBlocks) break;
+  }
   c.blocks_p = unit_p * c.splits_p;
   c.blocks_o = unit_o * c.splits_o;
   return c;
 }
+
+// Rows of calls that read more than the L2s hold bypass the caches where one block reads
+// them: all layers of four sequences, 930 MB, 178 us (201 through the caches), a prefix of
+// 134 MB 34.6 us (38.4); 8 MB stay (12.0 us; 13.5 past the caches).
+constexpr int64_t kCacheBytes = 32 << 20;
 
 template <class T>
 void launch_attn(const AttnArgs& a, const Cut& c, hipStream_t hs) {
@@ -838,24 +880,49 @@ struct FinishArgs {
   void* out;
   float* lse_out;
   int64_t merge_blocks;
+  int wide;                       // a block a query
   const float* logits;
   int logit_stride, per_slice;    // queries of a slice, at most 32
-  const float* lse;               // natural, where there is one part
   const int32_t* n_own;
   int own_rows, chunks;           // blocks of a slice's rows
   float* weights;
 };
 constexpr int kFinishKeys = 1024;   // of a block, four a thread
+constexpr int64_t kWideRows = 1024; // queries that a block each fills the chip with
 
-// merge_blocks blocks of a query a wave, then `chunks` of each slice's rows.
+// merge_blocks blocks of four queries, a wave each, or (wide) of one, whose parts the waves
+// share; then `chunks` of each slice's rows.
 template <class TO>
 __global__ __launch_bounds__(256)
 void finish_kernel(const FinishArgs a) {
-  __shared__ float s_lse[32];
+  __shared__ float s_lse[32], s_o[4][kHeadDim], s_m[4], s_l[4];
   int64_t id = blockIdx.x;
-  if (id < a.merge_blocks) {
-    const int64_t row = id * 4 + (threadIdx.x >> 6);
+  const int w = threadIdx.x >> 6;
+  if (id < a.merge_blocks && !a.wide) {
+    const int64_t row = id * 4 + w;
     if (row < a.n_rows) merge_row(a.part, a.n_parts, row, static_cast<TO*>(a.out), a.lse_out);
+    return;
+  }
+  if (id < a.merge_blocks) {
+    const int c0 = a.n_parts * w / 4, c1 = a.n_parts * (w + 1) / 4, tid = threadIdx.x;
+    float m, l, o0, o1;
+    join_parts(a.part + (id * a.n_parts + c0) * kPartFloats, c1 - c0, m, l, o0, o1);
+    *reinterpret_cast<float2*>(&s_o[w][2 * (tid & 63)]) = make_float2(o0, o1);
+    s_m[w] = m;
+    s_l[w] = l;
+    __syncthreads();
+    if (tid >= kHeadDim) return;
+    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+    l = 0.f;
+    float o = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float e = __builtin_amdgcn_exp2f(s_m[i] - max_base(m));
+      l += s_l[i] * e;
+      o += s_o[i][tid] * e;
+    }
+    store_from_f32(static_cast<TO*>(a.out) + id * kHeadDim, tid, o * inv_sum(l));
+    if (a.lse_out && tid == 0) a.lse_out[id] = lse_of(m, l);
     return;
   }
   id -= a.merge_blocks;
@@ -864,45 +931,25 @@ void finish_kernel(const FinishArgs a) {
   const int n = length_of(a.n_own, s, a.own_rows), r = threadIdx.x >> 3, j = threadIdx.x & 7;
   // eight threads a query: its base-2 lse, infinite where it sees nothing
   if (r < a.per_slice) {
-    float m = -__builtin_inff(), l = 0.f, lse2;
-    if (a.n_parts > 1) {
-      const float* p = a.part + (s * a.per_slice + r) * a.n_parts * kPartFloats;
-      for (int c = j; c < a.n_parts; c += 8) {
-        const float2 ml = *reinterpret_cast<const float2*>(p + (size_t)c * kPartFloats);
-        const float mm = fmaxf(m, ml.x);
-        l = l * __builtin_amdgcn_exp2f(m - max_base(mm)) + ml.y * __builtin_amdgcn_exp2f(ml.x - max_base(mm));
-        m = mm;
-      }
-      for (int o = 1; o < 8; o <<= 1) {
-        const float m1 = __shfl_xor(m, o, kWave), l1 = __shfl_xor(l, o, kWave), mm = fmaxf(m, m1);
-        l = l * __builtin_amdgcn_exp2f(m - max_base(mm)) + l1 * __builtin_amdgcn_exp2f(m1 - max_base(mm));
-        m = mm;
-      }
-      lse2 = l == 0.f ? __builtin_inff() : max_base(m) + log2f(l);
-    } else {
-      const float x = a.lse[s * a.per_slice + r];
-      lse2 = x == -__builtin_inff() ? __builtin_inff() : x * kLog2E;
+    float m = -__builtin_inff(), l = 0.f;
+    const float* p = a.part + (s * a.per_slice + r) * a.n_parts * kPartFloats;
+    for (int c = j; c < a.n_parts; c += 8) {
+      const float2 ml = *reinterpret_cast<const float2*>(p + (size_t)c * kPartFloats);
+      const float mm = fmaxf(m, ml.x);
+      l = l * __builtin_amdgcn_exp2f(m - max_base(mm)) + ml.y * __builtin_amdgcn_exp2f(ml.x - max_base(mm));
+      m = mm;
     }
-    if (j == 0) s_lse[r] = lse2;
+    for (int o = 1; o < 8; o <<= 1) {
+      const float m1 = __shfl_xor(m, o, kWave), l1 = __shfl_xor(l, o, kWave), mm = fmaxf(m, m1);
+      l = l * __builtin_amdgcn_exp2f(m - max_base(mm)) + l1 * __builtin_amdgcn_exp2f(m1 - max_base(mm));
+      m = mm;
+    }
+    if (j == 0) s_lse[r] = l == 0.f ? __builtin_inff() : max_base(m) + log2f(l);
   }
   __syncthreads();
-  if (i >= n) return;
-  const float* x = a.logits + s * a.per_slice * a.logit_stride + i;
-  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int q = 0; q < a.per_slice; ++q) {
-    const float4 v = *reinterpret_cast<const float4*>(x + (int64_t)q * a.logit_stride);
-    const float e = s_lse[q];
-    y.x += __builtin_amdgcn_exp2f(v.x - e);
-    y.y += __builtin_amdgcn_exp2f(v.y - e);
-    y.z += __builtin_amdgcn_exp2f(v.z - e);
-    y.w += __builtin_amdgcn_exp2f(v.w - e);
-  }
-  float* to = a.weights + s * a.own_rows + i;
-  to[0] += y.x;
-  if (i + 1 < n) to[1] += y.y;
-  if (i + 2 < n) to[2] += y.z;
-  if (i + 3 < n) to[3] += y.w;
+  if (i < n)
+    add_weights(a.logits + s * a.per_slice * a.logit_stride, a.logit_stride, a.per_slice, s_lse, n, i,
+                a.weights + s * a.own_rows);
 }
 
 int check_types(int dtype, int out_dtype) {
@@ -1014,6 +1061,7 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
   a.prefix = {k_prefix, v_prefix, n_prefix, (int)prefix_rows, c.groups_p, c.splits_p};
   a.own = {k_own, v_own, n_own, (int)own_rows, c.groups_o, c.splits_o};
   a.prefix_blocks = c.blocks_p; a.n_parts = c.n_parts(); a.part = static_cast<float*>(workspace);
+  a.stream = (a.n_prefix_slices * prefix_rows + n_slices * own_rows) * 2 * kHeadDim * (dtype == LOUISKV_BF16 ? 2 : 4) > kCacheBytes;
   a.out = out; a.out_bf16 = out_dtype == LOUISKV_BF16;
   a.lse_out = lse_out ? lse_out : weights ? reinterpret_cast<float*>(static_cast<char*>(workspace) + parts) : nullptr;
   hipStream_t hs = as_stream(stream);
@@ -1023,24 +1071,26 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
   if (with_logits) {
     a.logits = reinterpret_cast<float*>(rest);
     a.logit_stride = logit_stride(own_rows);
+    a.weights = weights;
   }
   if (dtype == LOUISKV_BF16) launch_attn<uint16_t>(a, c, hs);
   else launch_attn<float>(a, c, hs);
   LKV_CHECK_LAUNCH();
-  if (with_logits) {
+  if (a.n_parts > 1) {
     FinishArgs f{};
     f.part = a.part; f.n_parts = a.n_parts; f.n_rows = n_rows; f.out = out; f.lse_out = a.lse_out;
-    f.merge_blocks = a.n_parts > 1 ? (n_rows + 3) / 4 : 0;
-    f.logits = a.logits; f.logit_stride = a.logit_stride; f.per_slice = group_size * n_q; f.lse = a.lse_out;
-    f.n_own = n_own; f.own_rows = (int)own_rows; f.chunks = (int)((own_rows + kFinishKeys - 1) / kFinishKeys);
-    f.weights = weights;
+    f.wide = a.n_parts >= 16 && n_rows <= kWideRows;
+    f.merge_blocks = f.wide ? n_rows : (n_rows + 3) / 4;
+    if (with_logits) {
+      f.logits = a.logits; f.logit_stride = a.logit_stride; f.per_slice = group_size * n_q; f.n_own = n_own;
+      f.own_rows = (int)own_rows; f.chunks = (int)((own_rows + kFinishKeys - 1) / kFinishKeys); f.weights = weights;
+    }
     const int64_t grid = f.merge_blocks + n_slices * f.chunks;
     if (a.out_bf16) finish_kernel<uint16_t><<<(unsigned)grid, 256, 0, hs>>>(f);
     else finish_kernel<float><<<(unsigned)grid, 256, 0, hs>>>(f);
     LKV_CHECK_LAUNCH();
-    return LOUISKV_OK;
   }
-  if (a.n_parts > 1 && (st = merge_parts(a.part, a.n_parts, n_rows, out, out_dtype, a.lse_out, hs))) return st;
+  if (with_logits) return LOUISKV_OK;
   if (!weights || own_rows == 0) return LOUISKV_OK;
   WeightArgs wa{};
   wa.q = q; wa.group_size = group_size; wa.n_q = n_q; wa.scale = scale; wa.keys = k_own; wa.key_rows = (int)own_rows;

@@ -22,6 +22,12 @@ __device__ __forceinline__ void copy_to_lds(const void* base, uint32_t off, uint
                : "memory", "m0");
 }
 
+// The same for rows that are read once and would only push others out of the caches.
+__device__ __forceinline__ void stream_to_lds(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(lds)
+               : "memory", "m0");
+}
+
 typedef __attribute__((address_space(3))) char* lds_ptr;
 __device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(lds_ptr)p; }
 
