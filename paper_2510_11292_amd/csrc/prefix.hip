@@ -400,35 +400,61 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* 
   const int tiles = (most + kTile - 1) / kTile;
   const int t0 = (int)((int64_t)tiles * p.split / x.splits), t1 = (int)((int64_t)tiles * (p.split + 1) / x.splits);
   const uint32_t slot = __builtin_amdgcn_readfirstlane(lds_addr(s_ring) + w * 2 * kTileBytes);
-  auto copy = [&](int tile) {
-    copy_rows<T, kTile>(x.k, p.kv_row, tile * kTile, p.n, slot, a.stream);
-    copy_rows<T, kTile>(x.v, p.kv_row, tile * kTile, p.n, slot + kTileBytes, a.stream);
+  auto copy_k = [&](int tile) { copy_rows<T, kTile>(x.k, p.kv_row, tile * kTile, p.n, slot, a.stream && x.row_groups == 1); };
+  auto copy_v = [&](int tile) {
+    copy_rows<T, kTile>(x.v, p.kv_row, tile * kTile, p.n, slot + kTileBytes, a.stream && x.row_groups == 1);
   };
   Wave<T> f;
   f.init(a, query_row<kOwn>(a, p, r), limit_of<kOwn>(a, p, r));
   f.addresses(slot, slot + kTileBytes);
+  // bfloat16: a tile's operands all fit the registers, so that the next one is under way during
+  // its arithmetic.  float32: the next keys follow the scores, the next values the sums.
+  constexpr bool kBf16 = Wave<T>::kBf16;
+  constexpr int kCopies = kTileBytes / 1024;
+  static_assert(kBf16 || kCopies == 16, "the waits below count copies");
+  if (t0 + w < t1) {
+    copy_k(t0 + w);
+    copy_v(t0 + w);
+  }
 #pragma unroll
-  for (int c = 0; c < Wave<T>::kQ; ++c) asm volatile("" : "+v"(f.q[c]));   // the queries are in before the copies start
-  if (t0 + w < t1) copy(t0 + w);
+  for (int c = 0; c < Wave<T>::kQ; ++c) asm volatile("" : "+v"(f.q[c]));   // waits for the queries here, not in the loop
   bool bad = false;
   for (int tile = t0 + w; tile < t1; tile += kBlockWaves) {
     const int p0 = tile * kTile;
-    const bool masked = p0 + kTile > least;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const bool masked = p0 + kTile > least, more = tile + kBlockWaves < t1;
     // values that a query may not see must not reach it: 0 * inf is NaN
-    if (masked) bad |= __builtin_amdgcn_ballot_w64(clear_not_finite<T, kTileBytes>(s_ring + (w * 2 + 1) * kTileBytes)) != 0;
+    auto clear = [&]() {
+      if (masked) bad |= __builtin_amdgcn_ballot_w64(clear_not_finite<T, kTileBytes>(s_ring + (w * 2 + 1) * kTileBytes)) != 0;
+    };
     typename Wave<T>::Keys kf;
     typename Wave<T>::Values vf;
     typename Wave<T>::Weights pb;
-    f.load_keys(0, kf);
-    f.load_values(0, vf);
-    const bool more = tile + kBlockWaves < t1;
-    if constexpr (Wave<T>::kBf16) {
+    if constexpr (kBf16) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      clear();
+      f.load_keys(0, kf);
+      f.load_values(0, vf);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (more) copy(tile + kBlockWaves);       // all of this tile is in registers
+      if (more) {
+        copy_k(tile + kBlockWaves);
+        copy_v(tile + kBlockWaves);
+      }
+    } else {
+      asm volatile("s_waitcnt vmcnt(16)" ::: "memory");        // all but the values
     }
     f32x16 sc = f.scores(0, kf);
-    f.template soften<Wave<T>::kBf16>(sc, p0, masked, low, pb);
+    if constexpr (!kBf16) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(sc[i]));    // the keys have been read
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (more) copy_k(tile + kBlockWaves);
+    }
+    f.template soften<kBf16>(sc, p0, masked, low, pb);
+    if constexpr (!kBf16) {
+      if (more) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");     // all but the next keys
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      clear();
+    }
     if (kOwn && a.logits && f.n < n_rows) {
       float* to = a.logits + (p.s * p.n_rows + r) * a.logit_stride + p0 + 4 * f.h;
 #pragma unroll
@@ -436,9 +462,9 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* 
         *reinterpret_cast<float4*>(to + 2 * i) = make_float4(sc[i], sc[i + 1], sc[i + 2], sc[i + 3]);
     }
     f.add_values(0, vf, pb);
-    if constexpr (!Wave<T>::kBf16) {
+    if constexpr (!kBf16) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (more) copy(tile + kBlockWaves);
+      if (more) copy_v(tile + kBlockWaves);
     }
   }
   if (bad) {                                    // rare
@@ -517,12 +543,12 @@ __device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char*
   Wave<T> f;
   f.init(a, query_row<kOwn>(a, p, r), limit_of<kOwn>(a, p, r));
   f.addresses(ring, ring + kHalf);
-#pragma unroll
-  for (int c = 0; c < Wave<T>::kQ; ++c) asm volatile("" : "+v"(f.q[c]));   // the queries are in before the copies start
   if (threadIdx.x == 0) *s_bad = 0;
   __syncthreads();
   if (st0 < st1) copy(st0, 0);
-  // Stage st, which lies at place `at` of the ring (a constant where it is inlined).
+#pragma unroll
+  for (int c = 0; c < Wave<T>::kQ; ++c) asm volatile("" : "+v"(f.q[c]));   // waits for the queries here, not in the loop
+  // Stage st, which lies at place `place` of the ring (a constant where it is inlined).
   auto stage = [&](int st, int place) {
     const int p0 = st * kStage;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -614,11 +640,13 @@ struct Cut {
   int64_t blocks_p, blocks_o;
   int n_parts() const { return splits_p + splits_o; }
 };
-constexpr int kGridBlocks = 512;
-Cut cut_of(int64_t n_slices, int64_t n_prefix_slices, int group_size, int n_q, int64_t prefix_rows, int64_t own_rows) {
+Cut cut_of(int64_t n_slices, int64_t n_prefix_slices, int group_size, int n_q, int64_t prefix_rows, int64_t own_rows,
+           int dtype) {
   Cut c{};
+  const bool bf16 = dtype == LOUISKV_BF16;
+  const int64_t resident = bf16 ? 512 : 256;      // blocks that the chip holds, two or one a CU
   const int64_t mine = (int64_t)group_size * n_q, all = prefix_rows ? mine * (n_slices / n_prefix_slices) : 0;
-  auto waves = [](int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; };
+  auto waves = [&](int64_t rows) { return rows <= (bf16 ? 32 : 128) ? 1 : bf16 && rows <= 64 ? 2 : 4; };
   auto groups = [](int64_t rows, int w) { return (int)((rows + 32 * w - 1) / (32 * w)); };
   c.waves_o = waves(mine);
   c.waves_p = std::max(waves(all), c.waves_o);
@@ -626,16 +654,16 @@ Cut cut_of(int64_t n_slices, int64_t n_prefix_slices, int group_size, int n_q, i
   c.groups_p = groups(all, c.waves_p);
   const int64_t tiles_p = (prefix_rows + kTile - 1) / kTile, tiles_o = (own_rows + kTile - 1) / kTile;
   const int64_t unit_p = prefix_rows ? n_prefix_slices * c.groups_p : 0, unit_o = own_rows ? n_slices * c.groups_o : 0;
-  // as many tiles a block as make kGridBlocks blocks or fewer of what they can be made of
-  int64_t per = (unit_p * tiles_p + unit_o * tiles_o + kGridBlocks - 1) / kGridBlocks;
+  // as many tiles a block as make no more blocks than are resident, where they can be so few
+  int64_t per = (unit_p * tiles_p + unit_o * tiles_o + resident - 1) / resident;
   for (;; ++per) {
     auto splits = [&](int64_t tiles, int w) {
-      const int64_t each = std::max<int64_t>(per, 8 * w);
+      const int64_t each = std::max<int64_t>(per, 4 * w);
       return (int)std::max<int64_t>(1, (tiles + each - 1) / each);
     };
     c.splits_p = prefix_rows ? splits(tiles_p, c.waves_p) : 0;
     c.splits_o = own_rows ? splits(tiles_o, c.waves_o) : 0;
-    if (unit_p + unit_o > kGridBlocks / 2 || unit_p * c.splits_p + unit_o * c.splits_o <= kGridBlocks) break;
+    if (unit_p + unit_o > resident / 2 || unit_p * c.splits_p + unit_o * c.splits_o <= resident) break;
   }
   c.blocks_p = unit_p * c.splits_p;
   c.blocks_o = unit_o * c.splits_o;
@@ -652,10 +680,16 @@ void launch_attn(const AttnArgs& a, const Cut& c, hipStream_t hs) {
   const unsigned grid = (unsigned)(c.blocks_p + c.blocks_o);
   switch (c.waves_p * 8 + c.waves_o) {
     case 8 + 1: attn_kernel<T, 1, 1><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
-    case 16 + 1: attn_kernel<T, 2, 1><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
-    case 16 + 2: attn_kernel<T, 2, 2><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
     case 32 + 1: attn_kernel<T, 4, 1><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
-    case 32 + 2: attn_kernel<T, 4, 2><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
+    case 16 + 1:
+      if constexpr (sizeof(T) == 2) attn_kernel<T, 2, 1><<<grid, kBlockWaves * 64, 0, hs>>>(a);
+      break;
+    case 16 + 2:
+      if constexpr (sizeof(T) == 2) attn_kernel<T, 2, 2><<<grid, kBlockWaves * 64, 0, hs>>>(a);
+      break;
+    case 32 + 2:
+      if constexpr (sizeof(T) == 2) attn_kernel<T, 4, 2><<<grid, kBlockWaves * 64, 0, hs>>>(a);
+      break;
     default: attn_kernel<T, 4, 4><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
   }
 }
@@ -751,11 +785,11 @@ void weights_kernel(const WeightArgs a) {
                     : ring + n32 * kRow + h * 256 + ((c ^ swizzle<T>(n32 & 15)) << 4);
   const float qs2 = a.scale * kLog2E;
   float sum[KT] = {};
+  if (st0 < st1) copy(st0, 0);
 #pragma unroll
   for (int x = 0; x < KT; ++x)
 #pragma unroll
-    for (int c = 0; c < kPiecesOfLane; ++c) asm volatile("" : "+v"(k[x][c]));   // the keys are in before the copies start
-  if (st0 < st1) copy(st0, 0);
+    for (int c = 0; c < kPiecesOfLane; ++c) asm volatile("" : "+v"(k[x][c]));   // waits for the keys here, not in the loop
   auto stage = [&](int st, int place) {
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(lse_next), "+v"(limit_next)::"memory");
     if (w == 0) {
@@ -989,10 +1023,11 @@ int check_workspace(const void* workspace, size_t bytes, size_t need) {
 // queries (8 bytes a row and query, written and read, against its key read again), and the
 // keys anew where it has more.
 int logit_stride(int64_t own_rows) { return (int)align_up((size_t)own_rows, kTile); }
-size_t weight_space(int64_t n_slices, int group_size, int n_q, int64_t own_rows, bool few) {
+bool keeps_logits(int group_size, int n_q) { return (int64_t)group_size * n_q <= 32; }
+size_t weight_space(int64_t n_slices, int group_size, int n_q, int64_t own_rows) {
   const size_t rows = (size_t)n_slices * group_size * n_q;
   return align_up(rows * sizeof(float), 256) +
-         (few ? align_up(rows * logit_stride(own_rows) * sizeof(float), 256) : weight_bytes(n_slices, group_size, n_q, own_rows));
+         (keeps_logits(group_size, n_q) ? align_up(rows * logit_stride(own_rows) * sizeof(float), 256) : weight_bytes(n_slices, group_size, n_q, own_rows));
 }
 
 // Neither a prefix nor own rows: every query sees nothing.
@@ -1024,9 +1059,9 @@ extern "C" size_t louiskv_shared_prefix_attn_workspace_size(int64_t n_slices, in
       (prefix_rows > 0 && (n_prefix_slices < 1 || n_slices % n_prefix_slices != 0)))
     return 0;
   const int64_t rows = n_slices * group_size * n_q;
-  const Cut c = cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows);
-  return part_bytes(rows, c.n_parts()) +
-         (with_weights ? weight_space(n_slices, group_size, n_q, own_rows, c.waves_o == 1) : 0);
+  auto parts = [&](int dtype) { return cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows, dtype).n_parts(); };
+  return part_bytes(rows, std::max(parts(LOUISKV_BF16), parts(LOUISKV_F32))) +
+         (with_weights ? weight_space(n_slices, group_size, n_q, own_rows) : 0);
 }
 
 extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads,
@@ -1050,7 +1085,7 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
   const size_t need = louiskv_shared_prefix_attn_workspace_size(n_slices, n_prefix_slices, group_size, n_q, d,
                                                                 prefix_rows, own_rows, weights != nullptr);
   if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
-  const Cut c = cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows);
+  const Cut c = cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows, dtype);
   if (c.blocks_p + c.blocks_o > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   const int64_t n_rows = n_slices * group_size * n_q;
   const size_t parts = part_bytes(n_rows, c.n_parts());
@@ -1067,7 +1102,7 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
   hipStream_t hs = as_stream(stream);
   if (a.n_parts == 0) return no_rows(a, n_rows, hs);
   char* rest = static_cast<char*>(workspace) + parts + align_up((size_t)n_rows * sizeof(float), 256);
-  const bool with_logits = weights && own_rows > 0 && c.waves_o == 1;
+  const bool with_logits = weights && own_rows > 0 && keeps_logits(group_size, n_q);
   if (with_logits) {
     a.logits = reinterpret_cast<float*>(rest);
     a.logit_stride = logit_stride(own_rows);
