@@ -66,10 +66,8 @@ struct Place {
   int n;             // rows held
 };
 
-template <bool kOwn>
-__device__ __forceinline__ Place place_of(const AttnArgs& a, int64_t id) {
-  const Side& x = kOwn ? a.own : a.prefix;
-  if (!kOwn && a.prefix_blocks >= 64) {
+__device__ __forceinline__ Place place_of(const AttnArgs& a, const Side& x, bool own, int64_t id) {
+  if (!own && a.prefix_blocks >= 64) {
     // blocks that read the same keys go to one XCD (blocks are dealt to the eight in turn)
     const int64_t per = a.prefix_blocks >> 3, rest = a.prefix_blocks & 7, xcd = id & 7;
     id = xcd * per + min<int64_t>(xcd, rest) + (id >> 3);
@@ -79,33 +77,30 @@ __device__ __forceinline__ Place place_of(const AttnArgs& a, int64_t id) {
   id /= x.row_groups;
   p.split = (int)(id % x.splits);
   p.s = id / x.splits;
-  p.n_rows = a.group_size * a.n_q * (kOwn ? 1 : a.n_seqs);
+  p.n_rows = a.group_size * a.n_q * (own ? 1 : a.n_seqs);
   p.kv_row = p.s * x.rows;
   p.n = length_of(x.n, p.s, x.rows);
   return p;
 }
 
 // Query r of a place as its row in q and out.
-template <bool kOwn>
-__device__ __forceinline__ int64_t query_row(const AttnArgs& a, const Place& p, int r) {
+__device__ __forceinline__ int64_t query_row(const AttnArgs& a, const Place& p, bool own, int r) {
   const int per = a.group_size * a.n_q;
-  if (kOwn) return p.s * per + r;
+  if (own) return p.s * per + r;
   const int seq = r / per;
   return ((int64_t)seq * a.n_prefix_slices + p.s) * per + (r - seq * per);
 }
 
 // Keys that query r of a place sees.
-template <bool kOwn>
-__device__ __forceinline__ int limit_of(const AttnArgs& a, const Place& p, int r) {
-  return kOwn ? max(0, p.n - a.n_q + r % a.n_q + 1) : p.n;
+__device__ __forceinline__ int limit_of(const AttnArgs& a, const Place& p, bool own, int r) {
+  return own ? max(0, p.n - a.n_q + r % a.n_q + 1) : p.n;
 }
 
 // The fewest and most keys that queries r0..r1 see.
-template <bool kOwn>
-__device__ __forceinline__ void limits_of(const AttnArgs& a, const Place& p, int r0, int r1, int& least, int& most) {
-  const bool wraps = kOwn && r0 / a.n_q != r1 / a.n_q;
-  least = wraps ? max(0, p.n - a.n_q + 1) : limit_of<kOwn>(a, p, r0);
-  most = wraps ? p.n : limit_of<kOwn>(a, p, r1);
+__device__ __forceinline__ void limits_of(const AttnArgs& a, const Place& p, bool own, int r0, int r1, int& least, int& most) {
+  const bool wraps = own && r0 / a.n_q != r1 / a.n_q;
+  least = wraps ? max(0, p.n - a.n_q + 1) : limit_of(a, p, own, r0);
+  most = wraps ? p.n : limit_of(a, p, own, r1);
 }
 
 typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8;
@@ -386,17 +381,17 @@ __device__ __forceinline__ void add_weights(const float* logits, int stride, int
 // Up to 32 queries: every wave takes every fourth 32 keys, through its own place in LDS.
 // Up to 16 (bfloat16): lanes n and n + 16 hold the same query, and the second's weights
 // are what rounding the first's leaves over.
-template <class T, bool kOwn>
-__device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* s_ring, float* s_m, float* s_l) {
+template <class T>
+__device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t id, char* s_ring, float* s_m, float* s_l) {
   constexpr int kTileBytes = kTile * kRowBytes<T>;
-  const Side& x = kOwn ? a.own : a.prefix;
-  const Place p = place_of<kOwn>(a, id);
+  const Side& x = own ? a.own : a.prefix;
+  const Place p = place_of(a, x, own, id);
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r0 = p.rgrp * 32, n_rows = min(32, p.n_rows - r0);
   const bool twice = Wave<T>::kBf16 && n_rows <= 16, low = twice && (lane & 16);
   const int r = r0 + min(lane & (twice ? 15 : 31), n_rows - 1);
   int least, most;
-  limits_of<kOwn>(a, p, r0, r0 + n_rows - 1, least, most);
+  limits_of(a, p, own, r0, r0 + n_rows - 1, least, most);
   const int tiles = (most + kTile - 1) / kTile;
   const int t0 = (int)((int64_t)tiles * p.split / x.splits), t1 = (int)((int64_t)tiles * (p.split + 1) / x.splits);
   const uint32_t slot = __builtin_amdgcn_readfirstlane(lds_addr(s_ring) + w * 2 * kTileBytes);
@@ -405,7 +400,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* 
     copy_rows<T, kTile>(x.v, p.kv_row, tile * kTile, p.n, slot + kTileBytes, a.stream && x.row_groups == 1);
   };
   Wave<T> f;
-  f.init(a, query_row<kOwn>(a, p, r), limit_of<kOwn>(a, p, r));
+  f.init(a, query_row(a, p, own, r), limit_of(a, p, own, r));
   f.addresses(slot, slot + kTileBytes);
   // bfloat16: a tile's operands all fit the registers, so that the next one is under way during
   // its arithmetic.  float32: the next keys follow the scores, the next values the sums.
@@ -455,7 +450,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* 
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       clear();
     }
-    if (kOwn && a.logits && f.n < n_rows) {
+    if (own && a.logits && f.n < n_rows) {
       float* to = a.logits + (p.s * p.n_rows + r) * a.logit_stride + p0 + 4 * f.h;
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
@@ -479,9 +474,14 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* 
   // the waves' sums, in their places in LDS; wave w joins channels 32 w..
   const float m = f.grow_at == -__builtin_inff() ? -__builtin_inff() : f.base;
   const float total = f.sum + __shfl_xor(f.sum, 32, kWave);
-  float* mine = reinterpret_cast<float*>(s_ring + w * 2 * kTileBytes) + lane;
+  // (a lane's 64 sums in 16-byte pieces, permuted so that sixteen lanes meet in no bank)
+  f32x4* mine = reinterpret_cast<f32x4*>(s_ring + w * 2 * kTileBytes) + lane * 16;
 #pragma unroll
-  for (int i = 0; i < 64; ++i) mine[i * 64] = f.o[i >> 4][i & 15];
+  for (int i = 0; i < 16; ++i) {
+    const f32x16& y = f.o[i >> 2];
+    const int e = (i & 3) * 4;
+    mine[i ^ (lane & 15)] = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
+  }
   if (f.h == 0) {
     s_m[w * 32 + f.n] = m;
     s_l[w * 32 + f.n] = total;
@@ -494,21 +494,22 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* 
   f32x16 o;
 #pragma unroll
   for (int i = 0; i < 16; ++i) o[i] = 0.f;
-#pragma unroll
+#pragma unroll 1
   for (int v = 0; v < kBlockWaves; ++v) {
     const float e = __builtin_amdgcn_exp2f(s_m[v * 32 + f.n] - max_base(mm));
     l += s_l[v * 32 + f.n] * e;
-    const float* from = reinterpret_cast<const float*>(s_ring + v * 2 * kTileBytes) + w * 16 * 64;
+    const f32x4* from = reinterpret_cast<const f32x4*>(s_ring + v * 2 * kTileBytes);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float y = from[i * 64 + lane];
-      if (twice) y += from[i * 64 + (lane ^ 16)];
-      o[i] += y * e;
+    for (int i = 0; i < 4; ++i) {
+      f32x4 y = from[lane * 16 + ((4 * w + i) ^ (lane & 15))];
+      if (twice) y += from[(lane ^ 16) * 16 + ((4 * w + i) ^ (lane & 15))];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[4 * i + c] += y[c] * e;
     }
   }
   if (f.n < n_rows)
-    store_sums(a, query_row<kOwn>(a, p, r), (kOwn && a.prefix_blocks ? a.prefix.splits : 0) + p.split, w, f.h, o, mm, l);
-  if (!kOwn || !a.logits || a.n_parts > 1) return;
+    store_sums(a, query_row(a, p, own, r), (own && a.prefix_blocks ? a.prefix.splits : 0) + p.split, w, f.h, o, mm, l);
+  if (!own || !a.logits || a.n_parts > 1) return;
   // the block has seen all there is: its rows' weights from the logits that its waves left
   if (w == 0 && f.h == 0) s_m[f.n] = l == 0.f ? __builtin_inff() : max_base(mm) + log2f(l);
   __syncthreads();
@@ -519,18 +520,18 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, int64_t id, char* 
 
 // Up to 32 WR queries, 32 a wave; the waves share stages of 64 keys (two places in LDS, one
 // in flight), WR = 2 in halves.
-template <class T, int WR, bool kOwn>
+template <class T, int WR, bool own>
 __device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char* s_ring, int* s_bad) {
   constexpr int kRow = kRowBytes<T>, kHalf = kStage * kRow, WK = kBlockWaves / WR;
-  const Side& x = kOwn ? a.own : a.prefix;
-  const Place p = place_of<kOwn>(a, id);
+  const Side& x = own ? a.own : a.prefix;
+  const Place p = place_of(a, x, own, id);
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = w % WR, wk = w / WR;
   const int b0 = p.rgrp * WR * 32, b1 = min(b0 + WR * 32, p.n_rows) - 1;     // the block's queries
   const int r0 = min(b0 + wr * 32, p.n_rows - 1), r1 = min(r0 + 31, p.n_rows - 1);
   const int r = min(b0 + wr * 32 + (lane & 31), p.n_rows - 1);
   int least, most, w_least, w_most;
-  limits_of<kOwn>(a, p, b0, b1, least, most);
-  limits_of<kOwn>(a, p, r0, r1, w_least, w_most);
+  limits_of(a, p, own, b0, b1, least, most);
+  limits_of(a, p, own, r0, r1, w_least, w_most);
   const int stages = (most + kStage - 1) / kStage;
   const int st0 = (int)((int64_t)stages * p.split / x.splits), st1 = (int)((int64_t)stages * (p.split + 1) / x.splits);
   const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr(s_ring));
@@ -541,7 +542,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char*
     copy_rows<T, 16>(x.v, p.kv_row, st * kStage + w * 16, p.n, to + kHalf, a.stream && x.row_groups == 1);
   };
   Wave<T> f;
-  f.init(a, query_row<kOwn>(a, p, r), limit_of<kOwn>(a, p, r));
+  f.init(a, query_row(a, p, own, r), limit_of(a, p, own, r));
   f.addresses(ring, ring + kHalf);
   if (threadIdx.x == 0) *s_bad = 0;
   __syncthreads();
@@ -609,8 +610,8 @@ __device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char*
     for (int i = 0; i < 64; ++i) f.o[i >> 4][i & 15] = f.o[i >> 4][i & 15] * f0 + mine[i * 64] * f1;
   }
   if (b0 + wr * 32 + f.n > b1) return;
-  const int64_t row = query_row<kOwn>(a, p, r);
-  const int part = (kOwn && a.prefix_blocks ? a.prefix.splits : 0) + p.split;
+  const int64_t row = query_row(a, p, own, r);
+  const int part = (own && a.prefix_blocks ? a.prefix.splits : 0) + p.split;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) store_sums(a, row, part, dt, f.h, f.o[dt], m, total);
 }
@@ -622,13 +623,17 @@ void attn_kernel(const AttnArgs a) {
   __shared__ __align__(256) char s_ring[kRingBytes<T>];
   __shared__ float s_m[kBlockWaves * 32], s_l[kBlockWaves * 32];
   __shared__ int s_bad;
-  const int64_t id = blockIdx.x;
-  if (id < a.prefix_blocks) {
-    if constexpr (WP == 1) attend_few<T, false>(a, id, s_ring, s_m, s_l);
-    else attend_many<T, WP, false>(a, id, s_ring, &s_bad);
+  const bool own = blockIdx.x >= a.prefix_blocks;
+  const int64_t id = own ? blockIdx.x - a.prefix_blocks : blockIdx.x;
+  if constexpr (WP == 1) {
+    // one code for both: such blocks run a few iterations, and what they run has to be fetched first
+    attend_few<T>(a, own, id, s_ring, s_m, s_l);
+  } else if (!own) {
+    attend_many<T, WP, false>(a, id, s_ring, &s_bad);
+  } else if constexpr (WO == 1) {
+    attend_few<T>(a, true, id, s_ring, s_m, s_l);
   } else {
-    if constexpr (WO == 1) attend_few<T, true>(a, id - a.prefix_blocks, s_ring, s_m, s_l);
-    else attend_many<T, WO, true>(a, id - a.prefix_blocks, s_ring, &s_bad);
+    attend_many<T, WO, true>(a, id, s_ring, &s_bad);
   }
 }
 
