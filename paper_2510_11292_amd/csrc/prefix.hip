@@ -713,20 +713,127 @@ struct WeightArgs {
   float* part;       // [splits][slices][key_rows] sums
 };
 
+// 32-key tiles of a wave as the operand K^T, and what 32 queries at a time add to their sums:
+// Q K^T leaves a lane 16 queries of one key, which it adds up.
+template <class T, int KT>
+struct KeyTiles {
+  static constexpr bool kBf16 = sizeof(T) == 2;
+  static constexpr int kPieces = kBf16 ? 8 : 16;       // 16-byte pieces 2 c + h (bfloat16) or 16 h + c (float32) of key n
+  typedef typename std::conditional<kBf16, bf16x8, f32x4>::type Piece;
+  Piece k[KT][kPieces];
+  float sum[KT];
+  int first;                                           // the first key
+
+  // Keys first.. of a slice of n (rows from n on repeat the last).
+  __device__ __forceinline__ void load(const void* keys, int64_t row0, int first_, int n) {
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    first = first_;
+#pragma unroll
+    for (int x = 0; x < KT; ++x) {
+      const int key = min(first + x * kTile + (lane & 31), n - 1);
+      const Piece* from = reinterpret_cast<const Piece*>(static_cast<const T*>(keys) + (row0 + key) * kHeadDim);
+#pragma unroll
+      for (int c = 0; c < kPieces; ++c) k[x][c] = from[kBf16 ? 2 * c + h : 16 * h + c];
+      sum[x] = 0.f;
+    }
+  }
+  // Waits for the keys here, not where they are used.
+  __device__ __forceinline__ void arrive() {
+#pragma unroll
+    for (int x = 0; x < KT; ++x)
+#pragma unroll
+      for (int c = 0; c < kPieces; ++c) asm volatile("" : "+v"(k[x][c]));
+  }
+  // LDS addresses of the lane's reads of a 32-query tile at `to`.
+  static __device__ __forceinline__ void addresses(uint32_t to, uint32_t (&q_at)[8]) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, r = lane & 31;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      q_at[c] = to + r * kRowBytes<T> + (kBf16 ? ((h ^ swizzle<T>(r & 15)) << 4) ^ (c << 5)
+                                               : h * 256 + ((c ^ swizzle<T>(r & 15)) << 4));
+  }
+  // The tile of queries `off` bytes on: their -lse in base 2, and the keys that each sees, of
+  // which the keys below `least` all do if none is `dead`.
+  __device__ __forceinline__ void weigh(const uint32_t (&q_at)[8], uint32_t off, const float* lse, const int* limits, int least,
+                                        bool dead, float scale) {
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    Piece q[kBf16 ? 8 : 1];
+    if constexpr (kBf16) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) q[c] = *(lds_bf16x8)(uintptr_t)(q_at[c] + off);
+    }
+    f32x4 nl[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) nl[i] = *reinterpret_cast<const f32x4*>(lse + 8 * i + 4 * h);
+#pragma unroll
+    for (int x = 0; x < KT; ++x) {
+      f32x16 sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      if constexpr (kBf16) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[c], k[x][c], sc, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+          const f32x4 y = *(lds_f32x4)(uintptr_t)((q_at[c & 7] ^ (c >> 3 << 7)) + off);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(y[e], k[x][c][e], sc, 0, 0, 0);
+        }
+      }
+      const int key = first + x * kTile + (lane & 31);
+      float part = 0.f;
+      if (dead || first + x * kTile + kTile > least) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          part += key < limits[(i & 3) + 8 * (i >> 2) + 4 * h]
+                      ? __builtin_amdgcn_exp2f(fmaf(sc[i], scale, nl[i >> 2][i & 3])) : 0.f;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) part += __builtin_amdgcn_exp2f(fmaf(sc[i], scale, nl[i >> 2][i & 3]));
+      }
+      sum[x] += part;
+    }
+  }
+  // f(key, sum) for the keys of the lanes below 32 that there are
+  template <class F>
+  __device__ __forceinline__ void each_sum(int n, F&& f) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int x = 0; x < KT; ++x) {
+      const float y = sum[x] + __shfl_xor(sum[x], 32, kWave);
+      const int key = first + x * kTile + (lane & 31);
+      if (lane < 32 && key < n) f(key, y);
+    }
+  }
+};
+
+// Query f of those of a slice that count, the last token first, a token's heads together:
+// x / g = x * magic >> 16 for x below 1024.
+struct QueryOrder {
+  int g, n_q, magic;
+  __device__ __forceinline__ QueryOrder(int g_, int n_q_) : g(g_), n_q(n_q_), magic(65536 / g_ + 1) {}
+  // query base + r (base uniform, r below 512) as its head and token
+  __device__ __forceinline__ void at(int base, int r, int& head, int& token) const {
+    const int t = base / g, x = r + base - t * g, dt = x * magic >> 16;
+    head = x - dt * g;
+    token = n_q - 1 - t - dt;
+  }
+};
+
 // Sums of softmax weights by key.  Block: keys, which stay in registers as the operand K^T
 // (KT 32-key tiles a wave), and a part of the queries that see them, 64 at a time through LDS
 // (two places, one in flight), the last tokens first, a token's heads together: blocks
 // of a slice begin with the same queries and meet them in the L2.  Q K^T leaves a lane 16
 // queries of one key, which it adds up.
 constexpr int kQueries = 64;                            // of a stage
-template <class T> constexpr int kKeyTiles = sizeof(T) == 2 ? 2 : 1;
-template <class T> constexpr int kBlockKeys = kBlockWaves * kKeyTiles<T> * kTile;
+constexpr int block_keys(int key_tiles) { return kBlockWaves * key_tiles * kTile; }
 
-template <class T>
-__global__ __launch_bounds__(kBlockWaves * 64, 2)
+template <class T, int KT>
+__global__ __launch_bounds__(kBlockWaves * 64, sizeof(T) == 2 ? KT == 2 ? 3 : 4 : 2)
 void weights_kernel(const WeightArgs a) {
   constexpr bool kBf16 = sizeof(T) == 2;
-  constexpr int kRow = kRowBytes<T>, KT = kKeyTiles<T>, kPlace = kQueries * kRow;
+  constexpr int kRow = kRowBytes<T>, kPlace = kQueries * kRow;
   __shared__ __align__(256) char s_ring[2][kPlace];
   __shared__ float s_lse[2][kQueries];                  // -lse in base 2
   __shared__ int s_limit[2][kQueries], s_dead[2];       // keys that a query sees; a stage with a query that adds nothing
@@ -734,32 +841,18 @@ void weights_kernel(const WeightArgs a) {
   int64_t id = blockIdx.x;
   const int64_t s = id % a.n_slices;                    // slices are dealt to the XCDs
   id /= a.n_slices;
-  const int split = (int)(id % a.splits), kb = (int)(id / a.splits) * kBlockKeys<T>;
+  const int split = (int)(id % a.splits), kb = (int)(id / a.splits) * block_keys(KT);
   const int n = length_of(a.n_keys, s, a.key_rows), g = a.group_size;
   if (kb >= n) return;
   const int first = max(0, kb - (n - a.n_q));           // the first token that sees one of the keys
   const int total = (a.n_q - first) * g, stages = (total + kQueries - 1) / kQueries;
   const int st0 = (int)((int64_t)stages * split / a.splits), st1 = (int)((int64_t)stages * (split + 1) / a.splits);
-  const int magic = 65536 / g + 1;                      // x / g = x * magic >> 16 for x below 80
+  const QueryOrder order(g, a.n_q);
   const int wk0 = kb + w * KT * kTile;                  // the wave's first key
-
-  // K^T: 16-byte pieces 2 c + h (bfloat16) or 16 h + c (float32) of key n32 of each tile
-  typedef typename std::conditional<kBf16, bf16x8, f32x4>::type Piece;
-  constexpr int kPiecesOfLane = kBf16 ? 8 : 16;
-  Piece k[KT][kPiecesOfLane];
-#pragma unroll
-  for (int x = 0; x < KT; ++x) {
-    const int key = min(wk0 + x * kTile + n32, n - 1);
-    const Piece* from = reinterpret_cast<const Piece*>(static_cast<const T*>(a.keys) + (s * a.key_rows + key) * kHeadDim);
-#pragma unroll
-    for (int c = 0; c < kPiecesOfLane; ++c) k[x][c] = from[kBf16 ? 2 * c + h : 16 * h + c];
-  }
-
-  // Query r of stage st, the last token first, as its head and token; past the last one, that.
-  auto query = [&](int st, int r, int& head, int& token) {
-    const int base = st * kQueries, t = base / g, x = min(r, total - 1 - base) + base - t * g, dt = x * magic >> 16;
-    head = x - dt * g;
-    token = a.n_q - 1 - t - dt;
+  KeyTiles<T, KT> keys;
+  keys.load(a.keys, s * a.key_rows, wk0, n);
+  auto query = [&](int st, int r, int& head, int& token) {   // past the last one, that
+    order.at(st * kQueries, min(r, total - 1 - st * kQueries), head, token);
   };
   float lse_next = 0.f;
   int limit_next = 0;
@@ -784,17 +877,9 @@ void weights_kernel(const WeightArgs a) {
     }
   };
   uint32_t q_at[8];
-#pragma unroll
-  for (int c = 0; c < 8; ++c)
-    q_at[c] = kBf16 ? ring + n32 * kRow + ((h ^ swizzle<T>(n32 & 15)) << 4 ^ (c << 5))
-                    : ring + n32 * kRow + h * 256 + ((c ^ swizzle<T>(n32 & 15)) << 4);
-  const float qs2 = a.scale * kLog2E;
-  float sum[KT] = {};
+  keys.addresses(ring, q_at);
   if (st0 < st1) copy(st0, 0);
-#pragma unroll
-  for (int x = 0; x < KT; ++x)
-#pragma unroll
-    for (int c = 0; c < kPiecesOfLane; ++c) asm volatile("" : "+v"(k[x][c]));   // waits for the keys here, not in the loop
+  keys.arrive();
   auto stage = [&](int st, int place) {
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(lse_next), "+v"(limit_next)::"memory");
     if (w == 0) {
@@ -814,58 +899,87 @@ void weights_kernel(const WeightArgs a) {
       if (f0 >= total) break;
       const int most = n - f0 / g, least = n - f1 / g;
       if (wk0 >= most) continue;
-      const uint32_t off = place * kPlace + half * 32 * kRow;
-      Piece q[kBf16 ? 8 : 1];
-      if constexpr (kBf16) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) q[c] = *(lds_bf16x8)(uintptr_t)(q_at[c] + off);
-      }
-      f32x4 nl[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) nl[i] = *reinterpret_cast<const f32x4*>(&s_lse[place][half * 32 + 8 * i + 4 * h]);
-#pragma unroll
-      for (int x = 0; x < KT; ++x) {
-        f32x16 sc;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
-        if constexpr (kBf16) {
-#pragma unroll
-          for (int c = 0; c < 8; ++c) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[c], k[x][c], sc, 0, 0, 0);
-        } else {
-#pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            const f32x4 y = *(lds_f32x4)(uintptr_t)((q_at[c & 7] ^ (c >> 3 << 7)) + off);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(y[e], k[x][c][e], sc, 0, 0, 0);
-          }
-        }
-        const int key = wk0 + x * kTile + n32;
-        float part = 0.f;
-        if (dead || wk0 + x * kTile + kTile > least) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int limit = s_limit[place][half * 32 + (i & 3) + 8 * (i >> 2) + 4 * h];
-            part += key < limit ? __builtin_amdgcn_exp2f(fmaf(sc[i], qs2, nl[i >> 2][i & 3])) : 0.f;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) part += __builtin_amdgcn_exp2f(fmaf(sc[i], qs2, nl[i >> 2][i & 3]));
-        }
-        sum[x] += part;
-      }
+      keys.weigh(q_at, place * kPlace + half * 32 * kRow, &s_lse[place][half * 32], &s_limit[place][half * 32], least, dead,
+                 a.scale * kLog2E);
     }
   };
   for (int st = st0; st < st1; st += 2) {
     stage(st, 0);
     if (st + 1 < st1) stage(st + 1, 1);
   }
-#pragma unroll
-  for (int x = 0; x < KT; ++x) {
-    const float y = sum[x] + __shfl_xor(sum[x], 32, kWave);
-    const int key = wk0 + x * kTile + n32;
-    if (h != 0 || key >= n) continue;
+  keys.each_sum(n, [&](int key, float y) {
     if (a.splits > 1) a.part[((int64_t)split * a.n_slices + s) * a.key_rows + key] = y;
     else a.weights[s * a.key_rows + key] += y;
+  });
+}
+
+// The same for up to kFewQueries queries, which stay in LDS while the keys pass: wave w of a
+// block takes every fourth group of KT tiles of the block's keys, the next group's on their
+// way meanwhile.
+template <class T> constexpr int kFewQueries = 65536 / kRowBytes<T>;
+template <class T, int KT>
+__global__ __launch_bounds__(kBlockWaves * 64, 2)
+void weights_few_kernel(const WeightArgs a) {
+  constexpr int kRow = kRowBytes<T>, kFew = kFewQueries<T>, kPieces = kRow / 16, kRows = 1024 / kRow;
+  __shared__ __align__(256) char s_q[kFew * kRow];
+  __shared__ float s_lse[kFew];                         // -lse in base 2
+  __shared__ int s_limit[kFew], s_dead;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t s = blockIdx.x % a.n_slices;
+  const int split = (int)(blockIdx.x / a.n_slices);     // of the keys
+  const int n = length_of(a.n_keys, s, a.key_rows), g = a.group_size, total = g * a.n_q;
+  const int groups = (n + KT * kTile - 1) / (KT * kTile);
+  const int g1 = (int)((int64_t)groups * (split + 1) / a.splits);
+  int at = (int)((int64_t)groups * split / a.splits) + w;
+  if (at - w >= g1) return;                             // block-uniform
+  const QueryOrder order(g, a.n_q);
+  KeyTiles<T, KT> keys, next;
+  keys.load(a.keys, s * a.key_rows, min(at, g1 - 1) * KT * kTile, n);
+  const int tiles = (total + 31) / 32;
+  const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(s_q));
+  const char* qs = static_cast<const char*>(a.q) + s * total * (int64_t)kRow;
+  for (int c = w; c < tiles * 32 / kRows; c += kBlockWaves) {
+    const int r = c * kRows + lane / kPieces;
+    int head, token;
+    order.at(0, min(r, total - 1), head, token);
+    const char* from = qs + ((int64_t)head * a.n_q + token) * kRow + (((lane % kPieces) ^ swizzle<T>(r & 15)) << 4);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(base + c * 1024);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory", "m0");
+  }
+  if (tid == 0) s_dead = 0;
+  __syncthreads();
+  for (int r = tid; r < tiles * 32; r += kBlockWaves * 64) {
+    int head, token;
+    order.at(0, min(r, total - 1), head, token);
+    const float lse = a.lse[(s * g + head) * a.n_q + token];
+    const int limit = r < total ? n - a.n_q + token + 1 : 0;
+    const bool none = lse == -__builtin_inff() || limit <= 0;
+    s_lse[r] = none ? -__builtin_inff() : -lse * kLog2E;
+    s_limit[r] = none ? 0 : limit;
+    if (none) s_dead = 1;
+  }
+  uint32_t q_at[8];
+  keys.addresses(base, q_at);
+  keys.arrive();
+  sync_stage();
+  const bool dead = __builtin_amdgcn_readfirstlane(s_dead) != 0;
+  auto group = [&](KeyTiles<T, KT>& k, KeyTiles<T, KT>& following) {
+    if (at + kBlockWaves < g1) following.load(a.keys, s * a.key_rows, (at + kBlockWaves) * KT * kTile, n);
+    float before[KT];
+#pragma unroll
+    for (int x = 0; x < KT; ++x) before[x] = a.weights[s * a.key_rows + min(k.first + x * kTile + (lane & 31), n - 1)];
+#pragma unroll 1
+    for (int t = 0; t < tiles; ++t) {
+      const int most = n - 32 * t / g, least = n - min(32 * t + 31, total - 1) / g;
+      if (k.first < most)
+        k.weigh(q_at, t * 32 * kRow, s_lse + 32 * t, s_limit + 32 * t, least, dead, a.scale * kLog2E);
+    }
+    k.each_sum(n, [&](int key, float y) { a.weights[s * a.key_rows + key] = before[(key - k.first) / kTile] + y; });
+    at += kBlockWaves;
+  };
+  while (at < g1) {
+    group(keys, next);
+    if (at < g1) group(next, keys);
   }
 }
 
@@ -881,26 +995,54 @@ void add_weights_kernel(const WeightArgs a, int blocks_per_slice) {
   a.weights[s * a.key_rows + i] += y;
 }
 
-// Parts that the queries are cut into where few blocks of keys would leave the chip idle.
-int weight_splits(int64_t n_slices, int group_size, int n_q, int64_t key_rows) {
-  const int64_t blocks = n_slices * ((key_rows + kBlockKeys<uint16_t> - 1) / kBlockKeys<uint16_t>);
+// How a call is cut: two key tiles a wave where a block has many stages of queries, and the
+// queries in parts until there are two rounds of blocks, the longer ones first (a block's first
+// keys are seen by the most queries).
+// Few queries stay in LDS, and the keys are cut instead (split of the keys).
+struct WeightCut { int key_tiles, splits; int64_t key_blocks; bool few; };
+WeightCut weight_cut(int64_t n_slices, int group_size, int n_q, int64_t key_rows, int dtype) {
+  WeightCut c{};
+  const int64_t rows = (int64_t)group_size * n_q;
+  if (rows <= (dtype == LOUISKV_BF16 ? kFewQueries<uint16_t> : kFewQueries<float>)) {
+    c.few = true;
+    c.key_tiles = 1;
+    c.key_blocks = 1;
+    const int64_t groups = (key_rows + kTile - 1) / kTile;
+    c.splits = (int)std::max<int64_t>(1, std::min((groups + kBlockWaves - 1) / kBlockWaves, 512 / n_slices));
+    return c;
+  }
   const int64_t stages = ((int64_t)group_size * n_q + kQueries - 1) / kQueries;
-  return blocks >= 512 ? 1 : (int)std::max<int64_t>(1, std::min({512 / std::max<int64_t>(blocks, 1), stages / 4, (int64_t)16}));
+  c.key_tiles = dtype == LOUISKV_BF16 && stages >= 32 ? 2 : 1;
+  c.key_blocks = (key_rows + block_keys(c.key_tiles) - 1) / block_keys(c.key_tiles);
+  const int64_t blocks = std::max<int64_t>(1, n_slices * c.key_blocks);
+  c.splits = (int)std::max<int64_t>(1, std::min({(1536 + blocks - 1) / blocks, stages / 4, (int64_t)16}));
+  return c;
 }
 
 size_t weight_bytes(int64_t n_slices, int group_size, int n_q, int64_t key_rows) {
-  const int splits = weight_splits(n_slices, group_size, n_q, key_rows);
-  return splits > 1 ? align_up((size_t)splits * n_slices * key_rows * sizeof(float), 256) : 0;
+  auto splits = [&](int dtype) {
+    const WeightCut c = weight_cut(n_slices, group_size, n_q, key_rows, dtype);
+    return c.few ? 1 : c.splits;
+  };
+  const int most = std::max(splits(LOUISKV_BF16), splits(LOUISKV_F32));
+  return most > 1 ? align_up((size_t)most * n_slices * key_rows * sizeof(float), 256) : 0;
 }
 
 int launch_weights(WeightArgs a, int dtype, void* workspace, hipStream_t hs) {
-  a.splits = weight_splits(a.n_slices, a.group_size, a.n_q, a.key_rows);
+  const WeightCut c = weight_cut(a.n_slices, a.group_size, a.n_q, a.key_rows, dtype);
+  a.splits = c.splits;
   a.part = static_cast<float*>(workspace);
-  const int keys = dtype == LOUISKV_BF16 ? kBlockKeys<uint16_t> : kBlockKeys<float>;
-  const int64_t blocks = ((int64_t)a.key_rows + keys - 1) / keys, grid = a.n_slices * blocks * a.splits;
+  const int64_t grid = a.n_slices * c.key_blocks * c.splits;
   if (grid > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
-  if (dtype == LOUISKV_BF16) weights_kernel<uint16_t><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
-  else weights_kernel<float><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
+  if (c.few) {
+    if (dtype == LOUISKV_BF16) weights_few_kernel<uint16_t, 1><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
+    else weights_few_kernel<float, 1><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
+    LKV_CHECK_LAUNCH();
+    return LOUISKV_OK;
+  }
+  if (dtype == LOUISKV_F32) weights_kernel<float, 1><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
+  else if (c.key_tiles == 1) weights_kernel<uint16_t, 1><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
+  else weights_kernel<uint16_t, 2><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
   LKV_CHECK_LAUNCH();
   if (a.splits == 1) return LOUISKV_OK;
   const int per = (a.key_rows + 255) / 256;
