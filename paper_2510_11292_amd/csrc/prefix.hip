@@ -914,11 +914,13 @@ void weights_kernel(const WeightArgs a) {
 }
 
 // The same for up to kFewQueries queries, which stay in LDS while the keys pass: wave w of a
-// block takes every fourth group of KT tiles of the block's keys, the next group's on their
-// way meanwhile.
+// block takes every eighth tile of the block's keys.  Four waves a SIMD wait for keys in turn
+// (64 queries, 32768 keys of 8 slices: 24.0 us; two waves with the next keys on their way
+// 26.8, with two tiles at a time 28.7).
+constexpr int kFewWaves = 8;
 template <class T> constexpr int kFewQueries = 65536 / kRowBytes<T>;
-template <class T, int KT>
-__global__ __launch_bounds__(kBlockWaves * 64, 2)
+template <class T>
+__global__ __launch_bounds__(kFewWaves * 64, 4)
 void weights_few_kernel(const WeightArgs a) {
   constexpr int kRow = kRowBytes<T>, kFew = kFewQueries<T>, kPieces = kRow / 16, kRows = 1024 / kRow;
   __shared__ __align__(256) char s_q[kFew * kRow];
@@ -928,17 +930,17 @@ void weights_few_kernel(const WeightArgs a) {
   const int64_t s = blockIdx.x % a.n_slices;
   const int split = (int)(blockIdx.x / a.n_slices);     // of the keys
   const int n = length_of(a.n_keys, s, a.key_rows), g = a.group_size, total = g * a.n_q;
-  const int groups = (n + KT * kTile - 1) / (KT * kTile);
+  const int groups = (n + kTile - 1) / kTile;
   const int g1 = (int)((int64_t)groups * (split + 1) / a.splits);
   int at = (int)((int64_t)groups * split / a.splits) + w;
   if (at - w >= g1) return;                             // block-uniform
   const QueryOrder order(g, a.n_q);
-  KeyTiles<T, KT> keys, next;
-  keys.load(a.keys, s * a.key_rows, min(at, g1 - 1) * KT * kTile, n);
+  KeyTiles<T, 1> keys;
+  keys.load(a.keys, s * a.key_rows, min(at, g1 - 1) * kTile, n);
   const int tiles = (total + 31) / 32;
   const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(s_q));
   const char* qs = static_cast<const char*>(a.q) + s * total * (int64_t)kRow;
-  for (int c = w; c < tiles * 32 / kRows; c += kBlockWaves) {
+  for (int c = w; c < tiles * 32 / kRows; c += kFewWaves) {
     const int r = c * kRows + lane / kPieces;
     int head, token;
     order.at(0, min(r, total - 1), head, token);
@@ -948,7 +950,7 @@ void weights_few_kernel(const WeightArgs a) {
   }
   if (tid == 0) s_dead = 0;
   __syncthreads();
-  for (int r = tid; r < tiles * 32; r += kBlockWaves * 64) {
+  for (int r = tid; r < tiles * 32; r += kFewWaves * 64) {
     int head, token;
     order.at(0, min(r, total - 1), head, token);
     const float lse = a.lse[(s * g + head) * a.n_q + token];
@@ -963,23 +965,19 @@ void weights_few_kernel(const WeightArgs a) {
   keys.arrive();
   sync_stage();
   const bool dead = __builtin_amdgcn_readfirstlane(s_dead) != 0;
-  auto group = [&](KeyTiles<T, KT>& k, KeyTiles<T, KT>& following) {
-    if (at + kBlockWaves < g1) following.load(a.keys, s * a.key_rows, (at + kBlockWaves) * KT * kTile, n);
-    float before[KT];
-#pragma unroll
-    for (int x = 0; x < KT; ++x) before[x] = a.weights[s * a.key_rows + min(k.first + x * kTile + (lane & 31), n - 1)];
+  while (at < g1) {
+    const int key = min(keys.first + (lane & 31), n - 1);
+    float* weight = a.weights + s * a.key_rows + key;
+    const float before = *weight;
 #pragma unroll 1
     for (int t = 0; t < tiles; ++t) {
       const int most = n - 32 * t / g, least = n - min(32 * t + 31, total - 1) / g;
-      if (k.first < most)
-        k.weigh(q_at, t * 32 * kRow, s_lse + 32 * t, s_limit + 32 * t, least, dead, a.scale * kLog2E);
+      if (keys.first < most)
+        keys.weigh(q_at, t * 32 * kRow, s_lse + 32 * t, s_limit + 32 * t, least, dead, a.scale * kLog2E);
     }
-    k.each_sum(n, [&](int key, float y) { a.weights[s * a.key_rows + key] = before[(key - k.first) / kTile] + y; });
-    at += kBlockWaves;
-  };
-  while (at < g1) {
-    group(keys, next);
-    if (at < g1) group(next, keys);
+    keys.each_sum(n, [&](int, float y) { *weight = before + y; });
+    at += kFewWaves;
+    if (at < g1) keys.load(a.keys, s * a.key_rows, at * kTile, n);
   }
 }
 
@@ -1008,7 +1006,7 @@ WeightCut weight_cut(int64_t n_slices, int group_size, int n_q, int64_t key_rows
     c.key_tiles = 1;
     c.key_blocks = 1;
     const int64_t groups = (key_rows + kTile - 1) / kTile;
-    c.splits = (int)std::max<int64_t>(1, std::min((groups + kBlockWaves - 1) / kBlockWaves, 512 / n_slices));
+    c.splits = (int)std::max<int64_t>(1, std::min((groups + kFewWaves - 1) / kFewWaves, 512 / n_slices));
     return c;
   }
   const int64_t stages = ((int64_t)group_size * n_q + kQueries - 1) / kQueries;
@@ -1035,8 +1033,8 @@ int launch_weights(WeightArgs a, int dtype, void* workspace, hipStream_t hs) {
   const int64_t grid = a.n_slices * c.key_blocks * c.splits;
   if (grid > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   if (c.few) {
-    if (dtype == LOUISKV_BF16) weights_few_kernel<uint16_t, 1><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
-    else weights_few_kernel<float, 1><<<(unsigned)grid, kBlockWaves * 64, 0, hs>>>(a);
+    if (dtype == LOUISKV_BF16) weights_few_kernel<uint16_t><<<(unsigned)grid, kFewWaves * 64, 0, hs>>>(a);
+    else weights_few_kernel<float><<<(unsigned)grid, kFewWaves * 64, 0, hs>>>(a);
     LKV_CHECK_LAUNCH();
     return LOUISKV_OK;
   }
