@@ -46,6 +46,13 @@ prompt_attention() is the attention of the prompt's own queries over selected
 blocks of its keys (louiskv_page_prefill, louiskv_retrieve_blocks,
 louiskv_sparse_prefill_attn), for a whole prompt or a chunk of it.
 
+BranchEngine is the other kind of cache: sequences that continue one prompt
+(samples of it, questions about it) attend to its rows, held once for all of them
+and, with prefix_budget, cut to those of most attention weight, and to caches of
+their own that keep at most `budget` rows, of which the lightest leaves for a
+new token (louiskv_shared_prefix_attn, louiskv_attn_weights,
+louiskv_evict_rows, louiskv_store_evict).
+
 EngineConfig also selects the ablation baselines of Appendix D.3 and
 Appendix B: trigger="stride" (louiskv_fire_every in place of the boundary
 test), index="pages" (louiskv_page_prefill in place of the clustering) and
@@ -630,3 +637,120 @@ class LouisKVEngine:
                          self.v_buf, self.buf_row, self.slot_list, fire=self.fire, seg_state=seg_state,
                          window=c.window, n_fetched=self.n_fetched, pool_on_host=self.pool_on_host,
                          scores_out=self.scores, workspace=self.ws_retrieve)
+
+
+# --------------------------------------------- sequences of one prompt, caches of bounded size
+
+@dataclass(frozen=True)
+class BranchConfig:
+    n_branches: int                       # sequences that continue the prompt
+    n_layers: int
+    n_kv_heads: int
+    n_q_heads: int
+    prompt_len: int
+    budget: int                           # rows of a branch's own cache, per (layer, KV head)
+    prefix_budget: Optional[int] = None   # prompt rows that are kept, per (layer, KV head); None: all
+    n_first: int = 4                      # of the prompt, and of a branch's own tokens: always kept
+    n_recent: int = 128                   # last tokens: always kept
+    n_new: int = 1                        # tokens of a step at most
+    head_dim: int = 128
+
+    @property
+    def n_prefix_slices(self) -> int:
+        return self.n_layers * self.n_kv_heads
+
+    @property
+    def n_slices(self) -> int:
+        return self.n_branches * self.n_prefix_slices
+
+    @property
+    def n_groups(self) -> int:
+        return self.n_branches * self.n_layers
+
+    @property
+    def cuts_prefix(self) -> bool:
+        return self.prefix_budget is not None and self.prefix_budget < self.prompt_len
+
+
+class BranchEngine:
+    """Sequences that continue one prompt, each with a cache of its own that keeps at most cfg.budget rows.
+
+    Groups are ordered branch by branch (group = branch * n_layers + layer), slices as in the library.  step() leaves
+    the counts on the device: a captured step is the next one at every replay."""
+
+    def __init__(self, cfg: BranchConfig, dtype: torch.dtype, device="cuda", out_dtype: Optional[torch.dtype] = None):
+        c = self.cfg = cfg
+        if min(c.n_branches, c.n_layers, c.n_kv_heads, c.prompt_len, c.n_new) < 1 or c.n_q_heads % c.n_kv_heads:
+            raise ValueError(f"{c}: sizes must be positive, query heads a multiple of the KV heads")
+        if c.n_first < 0 or c.n_recent < 0 or c.n_first + c.n_recent + c.n_new > c.budget:
+            raise ValueError(f"n_first={c.n_first} + n_recent={c.n_recent} + n_new={c.n_new} rows do not fit "
+                             f"budget={c.budget}")
+        if c.cuts_prefix and c.n_first + c.n_recent > c.prefix_budget:
+            raise ValueError(f"n_first={c.n_first} + n_recent={c.n_recent} rows do not fit "
+                             f"prefix_budget={c.prefix_budget}")
+        self.dtype = dtype
+        dev = self.device = torch.device(device)
+        s, sp, d = c.n_slices, c.n_prefix_slices, c.head_dim
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.k_prefix = self.v_prefix = self.n_prefix = self.pos_prefix = None
+        if c.cuts_prefix:
+            self.k_prefix, self.v_prefix = (torch.zeros(sp, c.prefix_budget, d, dtype=dtype, device=dev) for _ in range(2))
+            self.n_prefix, self.pos_prefix = torch.zeros(sp, **i32), torch.zeros(sp, c.prefix_budget, **i32)
+        self.k_own, self.v_own = (torch.zeros(s, c.budget, d, dtype=dtype, device=dev) for _ in range(2))
+        self.weights = torch.zeros(s, c.budget, dtype=torch.float32, device=dev)
+        self.pos = torch.zeros(s, c.budget, **i32)
+        self.n_rows, self.n_seen = torch.zeros(s, **i32), torch.zeros(s, **i32)
+        self.out = torch.zeros(c.n_groups, c.n_q_heads, d, dtype=out_dtype or dtype, device=dev)
+        self.lse = torch.zeros(c.n_groups, c.n_q_heads, dtype=torch.float32, device=dev)
+        g, rows = c.n_q_heads // c.n_kv_heads, c.prefix_budget if c.cuts_prefix else c.prompt_len
+        # of single tokens and full chunks; steps between them take memory of their own
+        self.ws = {t: (torch.empty(L.shared_prefix_attn_workspace_size(s, sp, g, t, rows, c.budget, True),
+                                   dtype=torch.uint8, device=dev),
+                       torch.empty(L.store_evict_workspace_size(s, c.budget, t, c.budget), dtype=torch.uint8, device=dev))
+                   for t in (1, c.n_new)}
+
+    def prefill(self, keys: torch.Tensor, values: torch.Tensor, q: Optional[torch.Tensor] = None,
+                lse: Optional[torch.Tensor] = None) -> None:
+        """The prompt's keys and values [n_layers * n_kv_heads][prompt_len][d]; the branches' caches are emptied.
+        Without a prefix_budget they are the prefix themselves (kept, not copied).  With one the rows of most weight
+        are copied, by the softmax weights of the prompt's last queries q [n_layers][Hq][n][d]: all of them, or a
+        window (64 is usual).  lse [n_layers][Hq][n]: of the attention that the caller has computed for q already;
+        without it this computes the queries' dense attention."""
+        c = self.cfg
+        if c.cuts_prefix:
+            if q is None:
+                raise ValueError("a prefix_budget needs queries of the prompt")
+            weights = torch.zeros(keys.shape[:2], dtype=torch.float32, device=keys.device)
+            if lse is None:
+                L.shared_prefix_attn(q, c.n_kv_heads, None, None, None, keys, values, None, torch.empty_like(q),
+                                     weights=weights)
+            else:
+                L.attn_weights(q, c.n_kv_heads, keys, None, lse, weights)
+            L.evict_rows(weights, None, None, None, c.prefix_budget, c.n_first, c.n_recent, keys, values, self.k_prefix,
+                         self.v_prefix, None, self.pos_prefix, self.n_prefix)
+        else:
+            want = (c.n_prefix_slices, c.prompt_len, c.head_dim)
+            if tuple(keys.shape) != want or tuple(values.shape) != want:
+                raise ValueError(f"keys {tuple(keys.shape)} and values {tuple(values.shape)}, expected {want}")
+            self.k_prefix, self.v_prefix = keys, values
+        self.n_rows.zero_()
+        self.n_seen.zero_()
+
+    def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """One token of every branch, q [G][Hq][d], k and v [S][d], or up to cfg.n_new at once, q [G][Hq][n][d], k and v
+        [S][n][d]: they enter the caches, from which the lightest rows leave, and attend to the prompt's rows and the
+        caches, whose weights they add to.  Returns self.out (one token), or out (allocated if not given)."""
+        c = self.cfg
+        if self.k_prefix is None:
+            raise RuntimeError("step() comes after prefill()")
+        n = 1 if k.dim() == 2 else k.shape[1]
+        if n > c.n_new:
+            raise ValueError(f"{n} tokens at once, n_new={c.n_new}")
+        ws, ws_store = self.ws.get(n, (None, None))
+        if out is None:
+            out = self.out if q.dim() == 3 else torch.empty(q.shape, dtype=self.out.dtype, device=q.device)
+        L.store_evict(k, v, self.k_own, self.v_own, self.weights, self.pos, self.n_rows, self.n_seen, c.budget, c.n_first,
+                      c.n_recent, workspace=ws_store)
+        L.shared_prefix_attn(q, c.n_kv_heads, self.k_prefix, self.v_prefix, self.n_prefix, self.k_own, self.v_own,
+                             self.n_rows, out, self.lse if q.dim() == 3 else None, weights=self.weights, workspace=ws)
+        return out

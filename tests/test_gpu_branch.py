@@ -1,0 +1,142 @@
+"""BranchEngine: sequences that continue one prompt, with caches of bounded size, step by step against plain attention in
+64 bits over the rows that the engine says it holds, and those rows against the eviction rule."""
+import pytest
+import torch
+
+from oracle import prefix as op
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+DEV = "cuda"
+
+
+def engine(dtype, **kw):
+    from paper_2510_11292_amd.engine import BranchConfig, BranchEngine
+    base = dict(n_branches=3, n_layers=2, n_kv_heads=2, n_q_heads=8, prompt_len=300, budget=40, n_first=2, n_recent=8)
+    base.update(kw)
+    return BranchEngine(BranchConfig(**base), DT[dtype], DEV, out_dtype=torch.float32)
+
+
+def prompt(e, gen, n_q):
+    c = e.cfg
+    keys, values = (torch.randn(c.n_prefix_slices, c.prompt_len, 128, generator=gen, device=DEV).to(e.dtype) for _ in range(2))
+    return keys, values, torch.randn(c.n_layers, c.n_q_heads, n_q, 128, generator=gen, device=DEV).to(e.dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cut", [None, 90])
+def test_steps(dtype, cut):
+    e = engine(dtype, prefix_budget=cut, n_new=3)
+    c, gen = e.cfg, torch.Generator(device=DEV).manual_seed(1)
+    keys, values, q = prompt(e, gen, 64)
+    e.prefill(keys, values, q)
+    kept = [list(range(c.prompt_len))] * c.n_prefix_slices
+    if cut:
+        x = torch.einsum("hgqd,hkd->hgqk", q.double().view(c.n_prefix_slices, 4, 64, 128), keys.double()) * 128 ** -0.5
+        hidden = torch.arange(300, device=DEV) > 300 - 64 + torch.arange(64, device=DEV)[:, None]
+        w = x.masked_fill(hidden, -float("inf")).softmax(-1).sum((1, 2))
+        kept = [sorted(e.pos_prefix[i].tolist()) for i in range(c.n_prefix_slices)]
+        for i in range(c.n_prefix_slices):
+            assert len(set(kept[i])) == cut and {0, 1} <= set(kept[i]) and set(range(292, 300)) <= set(kept[i])
+            want = set(op.rows_that_stay(w[i].tolist(), list(range(300)), 300, 300, cut, 2, 8))
+            # the two differ at most in rows whose weights in 64 bits are nearly equal
+            a, b = set(kept[i]) - want, want - set(kept[i])
+            assert not a or min(w[i, list(a)]) >= max(w[i, list(b)]) * (1 - 1e-4)
+            at = e.pos_prefix[i].long()
+            assert torch.equal(e.k_prefix[i], keys[i, at]) and torch.equal(e.v_prefix[i], values[i, at])
+    seen = 0
+    history_k = torch.zeros(c.n_slices, 0, 128, device=DEV, dtype=e.dtype)
+    history_v = history_k.clone()
+    for t in range(30):
+        n = (1, 1, 3, 2)[t % 4]
+        qt = torch.randn(c.n_groups, c.n_q_heads, n, 128, generator=gen, device=DEV).to(e.dtype)
+        kt, vt = (torch.randn(c.n_slices, n, 128, generator=gen, device=DEV).to(e.dtype) for _ in range(2))
+        history_k, history_v = torch.cat((history_k, kt), 1), torch.cat((history_v, vt), 1)
+        if t % 4 == 0:
+            out = e.step(qt[:, :, 0].contiguous(), kt[:, 0].contiguous(), vt[:, 0].contiguous()).unsqueeze(2)
+        else:
+            out = e.step(qt, kt, vt)
+        seen += n
+        assert (e.n_seen == seen).all() and (e.n_rows == min(seen, c.budget)).all()
+        rows = min(seen, c.budget)
+        for i in range(c.n_slices):
+            pos = e.pos[i, :rows].long()
+            assert len(set(pos.tolist())) == rows and pos[-n:].tolist() == list(range(seen - n, seen))
+            assert {0, 1} & set(range(seen)) <= set(pos.tolist())
+            k = torch.cat((keys[i % c.n_prefix_slices, kept[i % c.n_prefix_slices]], history_k[i, pos])).double()
+            v = torch.cat((values[i % c.n_prefix_slices, kept[i % c.n_prefix_slices]], history_v[i, pos])).double()
+            x = qt.view(c.n_slices, 4, n, 128)[i].double().reshape(4 * n, 128) @ k.t().contiguous() * 128 ** -0.5
+            hidden = torch.arange(len(k), device=DEV) > len(k) - n + torch.arange(n, device=DEV)[:, None]
+            p = x.view(4, n, -1).masked_fill(hidden, -float("inf")).softmax(-1)
+            got = out.view(c.n_slices, 4, n, 128)[i].double()
+            # weights rounded to bfloat16, 2^-8 of each; float32 sums else
+            tol = (2.0 ** -8 if dtype == "bf16" else 1e-5) * (p @ v.abs()) + 1e-5
+            assert ((got - p @ v).abs() <= tol).all(), (t, i)
+
+
+def test_weights_from_a_given_lse_select_the_same_rows():
+    for dtype in DT:
+        a, b = engine(dtype, prefix_budget=60), engine(dtype, prefix_budget=60)
+        gen = torch.Generator(device=DEV).manual_seed(2)
+        keys, values, q = prompt(a, gen, 300)
+        x = torch.einsum("hgqd,hkd->hgqk", q.double().view(4, 4, 300, 128), keys.double()) * 128 ** -0.5
+        x = x.masked_fill(torch.ones(300, 300, device=DEV, dtype=torch.bool).triu(1), -float("inf"))
+        a.prefill(keys, values, q)
+        b.prefill(keys, values, q, lse=x.logsumexp(-1).float().view(2, 8, 300))
+        w = x.softmax(-1).sum((1, 2))
+        for i in range(4):
+            one, two = set(a.pos_prefix[i].tolist()), set(b.pos_prefix[i].tolist())
+            diff = one ^ two
+            assert not diff or max(w[i, list(diff)]) <= min(w[i, list(diff)]) * (1 + 1e-4)
+
+
+def test_captured_steps_and_a_second_prefill():
+    """A captured step is the next one at every replay, beside eager work of another engine; prefill() starts again."""
+    a, b = engine("bf16", prefix_budget=100), engine("bf16", prefix_budget=100)
+    c, gen = a.cfg, torch.Generator(device=DEV).manual_seed(3)
+    keys, values, q = prompt(a, gen, 64)
+    new = [torch.zeros(c.n_groups, c.n_q_heads, 128, device=DEV).bfloat16(), *(torch.zeros(c.n_slices, 128, device=DEV).bfloat16() for _ in range(2))]
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    a.prefill(keys, values, q)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            a.step(*new)
+    for _ in range(2):
+        a.prefill(keys, values, q)
+        b.prefill(keys, values, q)
+        a.weights.zero_()
+        b.weights.zero_()
+        for t in range(60):
+            for x in new:
+                x.copy_(torch.randn(x.shape, generator=gen, device=DEV))
+            torch.cuda.synchronize()
+            graph.replay()
+            want = b.step(*new)
+            torch.cuda.synchronize()
+            assert torch.equal(a.out, want) and torch.equal(a.pos, b.pos) and torch.equal(a.lse, b.lse), t
+            assert (a.n_seen == t + 1).all()
+
+
+def test_refusals():
+    with pytest.raises(ValueError, match="budget"):
+        engine("bf16", budget=10)
+    with pytest.raises(ValueError, match="prefix_budget"):
+        engine("bf16", prefix_budget=9)
+    with pytest.raises(ValueError, match="positive"):
+        engine("bf16", n_q_heads=3)
+    e = engine("bf16", prefix_budget=50)
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    keys, values, q = prompt(e, gen, 4)
+    with pytest.raises(ValueError, match="queries"):
+        e.prefill(keys, values)
+    e.prefill(keys, values, q)
+    x = torch.zeros(e.cfg.n_groups, 8, 2, 128, device=DEV).bfloat16()
+    y = torch.zeros(e.cfg.n_slices, 2, 128, device=DEV).bfloat16()
+    with pytest.raises(ValueError, match="n_new"):
+        e.step(x, y, y)
+    e = engine("bf16")
+    with pytest.raises(RuntimeError, match="prefill"):
+        e.step(x[:, :, 0].contiguous(), y[:, 0].contiguous(), y[:, 0].contiguous())
+    with pytest.raises(ValueError, match="expected"):
+        e.prefill(keys[:, :299], values)
