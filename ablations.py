@@ -47,6 +47,9 @@ VARIANTS = {
     "pages 16": {"index": "pages", "page_len": 16, "seg_len": 16},
     "every-step clusters": {"trigger": "stride", "stride": 1},
     "every-step pages 16": {"trigger": "stride", "stride": 1, "index": "pages", "page_len": 16, "seg_len": 16},
+    # no retrieval: the prompt is cut to B rows by the first query's attention weights, the generated tokens are kept
+    # in a cache of W rows from which the one of least accumulated weight leaves
+    "eviction by weight": {"evict": True},
 }
 
 
@@ -100,7 +103,78 @@ def step_quality(eng, data, t, n_eval, topb):
     return recall, overlap
 
 
+def timed_loop(prefill, step, gen_len, reps):
+    """Milliseconds of gen_len steps as one graph, each time after a fresh prefill."""
+    import torch
+    graph = torch.cuda.CUDAGraph()
+    prefill()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        for t in range(gen_len):
+            step(t)
+    ms = 0.0
+    for _ in range(reps):
+        prefill()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        graph.replay()
+        e1.record()
+        torch.cuda.synchronize()
+        ms += e0.elapsed_time(e1)
+    return ms / reps
+
+
+def run_evicting(name, over, wl, data, args):
+    import torch
+    from paper_2510_11292_amd.engine import BranchConfig, BranchEngine
+    dtype = torch.bfloat16 if wl.dtype == "bf16" else torch.float32
+    # every (sequence, layer) has a prompt of its own: one branch of as many layers
+    cfg = BranchConfig(n_branches=1, n_layers=wl.n_groups, n_kv_heads=wl.n_kv_heads, n_q_heads=wl.n_q_heads,
+                       prompt_len=wl.prompt_len, budget=wl.window, prefix_budget=wl.budget, n_first=4,
+                       n_recent=wl.window // 2)
+    eng = BranchEngine(cfg, dtype, "cuda")
+    S = min(args.eval_slices, cfg.n_slices) // cfg.n_kv_heads * cfg.n_kv_heads
+    H, g, d, P = cfg.n_kv_heads, cfg.n_q_heads // cfg.n_kv_heads, cfg.head_dim, wl.prompt_len
+    first = data.queries[0].unsqueeze(2).contiguous()
+
+    def prefill():
+        eng.prefill(data.prompt_keys, data.prompt_values, first)
+
+    def step(t):
+        eng.step(data.queries[t], data.gen_keys[t], data.gen_values[t])
+    prefill()
+    recalls, overlaps = [], []
+    for t in range(wl.gen_len):
+        step(t)
+        if t % args.metric_every and t != wl.gen_len - 1:
+            continue
+        keys = torch.cat((data.prompt_keys[:S].float(), data.gen_keys[:t + 1, :S].float().transpose(0, 1)), dim=1)
+        q = data.queries[t, :S // H].float().reshape(S, g, d)
+        p = torch.softmax(torch.bmm(keys, q.transpose(1, 2).contiguous()) / d ** 0.5, dim=1)      # [S][rows][g]
+        held = torch.zeros(keys.shape[:2], dtype=torch.bool, device=keys.device)
+        rows = int(eng.n_rows[0])
+        prefix = eng.pos_prefix[:S].long() if eng.pos_prefix is not None else torch.arange(P, device=keys.device).expand(S, P)
+        held.scatter_(1, prefix, True)
+        held.scatter_(1, P + eng.pos[:S, :rows].long(), True)
+        recalls.append((p * held.unsqueeze(-1)).sum(1).reshape(-1))
+        k = min(wl.budget, P)
+        top = torch.topk(p.mean(2), k, dim=1).indices
+        overlaps.append(torch.gather(held, 1, top).sum(1).float() / k)
+    rec, ovl = torch.cat(recalls), torch.cat(overlaps)
+    ms = timed_loop(prefill, step, wl.gen_len, args.reps)
+    out = {"variant": name, "config": over, "fire_rate": 0.0, "mass_recall_mean": float(rec.mean()),
+           "mass_recall_p10": float(torch.quantile(rec, 0.1)), "topb_overlap": float(ovl.mean()),
+           "decode_steps_per_s": wl.gen_len / (ms / 1e3)}
+    del eng
+    torch.cuda.empty_cache()
+    log(f"{name:24s} recall {out['mass_recall_mean']:.4f} (p10 {out['mass_recall_p10']:.4f})  top-B overlap "
+        f"{out['topb_overlap']:.3f}  {out['decode_steps_per_s']:.0f} steps/s")
+    return out
+
+
 def run_variant(name, over, wl, data, args):
+    if over.get("evict"):
+        return run_evicting(name, over, wl, data, args)
     import torch
     from paper_2510_11292_amd.engine import LouisKVEngine, config_from_workload
     from paper_2510_11292_amd import louiskv as L
@@ -125,25 +199,8 @@ def run_variant(name, over, wl, data, args):
     rec = torch.cat(recalls)
     ovl = torch.cat(overlaps)
     # speed pass: the whole decode loop as one graph after a fresh prefill
-    def decode_all():
-        for t in range(wl.gen_len):
-            eng.step(data.queries[t], data.gen_keys[t], data.gen_values[t])
-    graph = torch.cuda.CUDAGraph()
-    eng.prefill(data.prompt_keys, data.prompt_values, data.init_idx)
-    torch.cuda.synchronize()
-    eng.t = 0
-    with torch.cuda.graph(graph):
-        decode_all()
-    ms = 0.0
-    for _ in range(args.reps):
-        eng.prefill(data.prompt_keys, data.prompt_values, data.init_idx)
-        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-        e0.record()
-        graph.replay()
-        e1.record()
-        torch.cuda.synchronize()
-        ms += e0.elapsed_time(e1)
-    ms /= args.reps
+    ms = timed_loop(lambda: eng.prefill(data.prompt_keys, data.prompt_values, data.init_idx),
+                    lambda t: eng.step(data.queries[t], data.gen_keys[t], data.gen_values[t]), wl.gen_len, args.reps)
     out = {
         "variant": name, "config": {k: v for k, v in over.items()},
         "fire_rate": fires / (wl.gen_len * cfg.n_groups),
@@ -151,7 +208,7 @@ def run_variant(name, over, wl, data, args):
         "topb_overlap": float(ovl.mean()),
         "decode_steps_per_s": wl.gen_len / (ms / 1e3),
     }
-    del graph, eng
+    del eng
     torch.cuda.empty_cache()
     log(f"{name:24s} fire {out['fire_rate']:.3f}  recall {out['mass_recall_mean']:.4f} "
         f"(p10 {out['mass_recall_p10']:.4f})  top-B overlap {out['topb_overlap']:.3f}  "
