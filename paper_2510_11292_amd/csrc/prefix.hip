@@ -561,17 +561,25 @@ __device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char*
     typename Wave<T>::Keys kf;
     typename Wave<T>::Values vf;
     typename Wave<T>::Weights pb;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      if (WK == 2 && half != wk) continue;
-      const int k0 = p0 + half * kTile;
-      if (k0 >= w_most) continue;
-      const uint32_t off = place * 2 * kHalf + half * kTile * kRow;
-      f.load_keys(off, kf);
+    auto half = [&](int x, bool more) {
+      const int k0 = p0 + x * kTile;
+      const uint32_t off = place * 2 * kHalf + x * kTile * kRow;
       f32x16 sc = f.scores(off, kf);
       f.load_values(off, vf);
+      if (more) f.load_keys(off + kTile * kRow, kf);   // the next tile's, before the exponentials
+      __builtin_amdgcn_sched_barrier(0);
       f.template soften<false>(sc, k0, k0 + kTile > w_least, false, pb);
       f.add_values(off, vf, pb);
+    };
+    if constexpr (WK == 1) {
+      if (p0 >= w_most) return;
+      f.load_keys(place * 2 * kHalf, kf);
+      half(0, true);
+      if (p0 + kTile < w_most) half(1, false);
+    } else {
+      if (p0 + wk * kTile >= w_most) return;
+      f.load_keys(place * 2 * kHalf + wk * kTile * kRow, kf);
+      half(wk, false);
     }
   };
   for (int st = st0; st < st1; st += 2) {
