@@ -653,13 +653,39 @@ struct Cut {
   int64_t blocks_p, blocks_o;
   int n_parts() const { return splits_p + splits_o; }
 };
+
+// Parts that the keys of `units` slices' query blocks are cut into, for `slots` blocks at a time:
+// the fewest of those that make the rounds of blocks times their tiles least.  A block's start
+// and end count as tiles, more where it leaves more partials; waves that take turns (w = 1)
+// take four tiles at once.
+int splits_of(int64_t units, int64_t tiles, int w, int64_t slots) {
+  if (units < 1 || tiles < 1) return 0;
+  const int64_t ends = 4 * w + 2;
+  auto length = [&](int64_t s) {
+    const int64_t t = (tiles + s - 1) / s;
+    return (w == 1 ? (t + 3) / 4 * 4 : t) + ends;
+  };
+  const int64_t most = std::max<int64_t>(1, tiles / (4 * w));
+  int64_t best = 1, cost = (units + slots - 1) / slots * length(1);
+  for (int64_t rounds = (units + slots - 1) / slots, i = 0; i < 8; ++i, ++rounds) {
+    int64_t s = std::min(most, rounds * slots / units);
+    if (s < 1) continue;
+    const int64_t len = length(s);
+    const int64_t per = w == 1 ? len - ends : (tiles + s - 1) / s;    // the fewest parts of that length
+    s = std::max<int64_t>(1, std::min(s, (tiles + per - 1) / per));
+    if (rounds * len < cost) cost = rounds * len, best = s;
+  }
+  return (int)best;
+}
+
+// float32 leaves no registers for stages that waves share: always 32 queries a block.
 Cut cut_of(int64_t n_slices, int64_t n_prefix_slices, int group_size, int n_q, int64_t prefix_rows, int64_t own_rows,
            int dtype) {
   Cut c{};
   const bool bf16 = dtype == LOUISKV_BF16;
   const int64_t resident = bf16 ? 512 : 256;      // blocks that the chip holds, two or one a CU
   const int64_t mine = (int64_t)group_size * n_q, all = prefix_rows ? mine * (n_slices / n_prefix_slices) : 0;
-  auto waves = [&](int64_t rows) { return rows <= (bf16 ? 32 : 128) ? 1 : bf16 && rows <= 64 ? 2 : 4; };
+  auto waves = [&](int64_t rows) { return !bf16 || rows <= 32 ? 1 : rows <= 64 ? 2 : 4; };
   auto groups = [](int64_t rows, int w) { return (int)((rows + 32 * w - 1) / (32 * w)); };
   c.waves_o = waves(mine);
   c.waves_p = std::max(waves(all), c.waves_o);
@@ -667,17 +693,14 @@ Cut cut_of(int64_t n_slices, int64_t n_prefix_slices, int group_size, int n_q, i
   c.groups_p = groups(all, c.waves_p);
   const int64_t tiles_p = (prefix_rows + kTile - 1) / kTile, tiles_o = (own_rows + kTile - 1) / kTile;
   const int64_t unit_p = prefix_rows ? n_prefix_slices * c.groups_p : 0, unit_o = own_rows ? n_slices * c.groups_o : 0;
-  // as many tiles a block as make no more blocks than are resident, where they can be so few
-  int64_t per = (unit_p * tiles_p + unit_o * tiles_o + resident - 1) / resident;
-  for (;; ++per) {
-    auto splits = [&](int64_t tiles, int w) {
-      const int64_t each = std::max<int64_t>(per, 4 * w);
-      return (int)std::max<int64_t>(1, (tiles + each - 1) / each);
-    };
-    c.splits_p = prefix_rows ? splits(tiles_p, c.waves_p) : 0;
-    c.splits_o = own_rows ? splits(tiles_o, c.waves_o) : 0;
-    if (unit_p + unit_o > resident / 2 || unit_p * c.splits_p + unit_o * c.splits_o <= resident) break;
-  }
+  // the two run side by side, each in its share of the chip; a few blocks of own rows get a place
+  // each, so that none waits for a prefix block to end
+  const double work_p = (double)unit_p * tiles_p, work_o = (double)unit_o * tiles_o;
+  int64_t slots = !unit_o ? resident : (int64_t)(resident * (work_p / (work_p + work_o)) + 0.5);
+  if (unit_o <= resident / 8) slots = std::min(slots, resident - unit_o);
+  slots = std::max<int64_t>(1, std::min(slots, resident - (unit_o > 0)));
+  c.splits_p = splits_of(unit_p, tiles_p, c.waves_p, slots);
+  c.splits_o = splits_of(unit_o, tiles_o, c.waves_o, unit_p ? resident - slots : resident);
   c.blocks_p = unit_p * c.splits_p;
   c.blocks_o = unit_o * c.splits_o;
   return c;
@@ -691,19 +714,18 @@ constexpr int64_t kCacheBytes = 32 << 20;
 template <class T>
 void launch_attn(const AttnArgs& a, const Cut& c, hipStream_t hs) {
   const unsigned grid = (unsigned)(c.blocks_p + c.blocks_o);
-  switch (c.waves_p * 8 + c.waves_o) {
-    case 8 + 1: attn_kernel<T, 1, 1><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
-    case 32 + 1: attn_kernel<T, 4, 1><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
-    case 16 + 1:
-      if constexpr (sizeof(T) == 2) attn_kernel<T, 2, 1><<<grid, kBlockWaves * 64, 0, hs>>>(a);
-      break;
-    case 16 + 2:
-      if constexpr (sizeof(T) == 2) attn_kernel<T, 2, 2><<<grid, kBlockWaves * 64, 0, hs>>>(a);
-      break;
-    case 32 + 2:
-      if constexpr (sizeof(T) == 2) attn_kernel<T, 4, 2><<<grid, kBlockWaves * 64, 0, hs>>>(a);
-      break;
-    default: attn_kernel<T, 4, 4><<<grid, kBlockWaves * 64, 0, hs>>>(a); break;
+  constexpr int kThreads = kBlockWaves * 64;
+  if constexpr (sizeof(T) == 4) {
+    attn_kernel<T, 1, 1><<<grid, kThreads, 0, hs>>>(a);
+  } else {
+    switch (c.waves_p * 8 + c.waves_o) {
+      case 8 + 1: attn_kernel<T, 1, 1><<<grid, kThreads, 0, hs>>>(a); break;
+      case 16 + 1: attn_kernel<T, 2, 1><<<grid, kThreads, 0, hs>>>(a); break;
+      case 16 + 2: attn_kernel<T, 2, 2><<<grid, kThreads, 0, hs>>>(a); break;
+      case 32 + 1: attn_kernel<T, 4, 1><<<grid, kThreads, 0, hs>>>(a); break;
+      case 32 + 2: attn_kernel<T, 4, 2><<<grid, kThreads, 0, hs>>>(a); break;
+      default: attn_kernel<T, 4, 4><<<grid, kThreads, 0, hs>>>(a); break;
+    }
   }
 }
 
