@@ -732,7 +732,8 @@ void launch_attn(const AttnArgs& a, const Cut& c, hipStream_t hs) {
 struct WeightArgs {
   const void* q;
   int group_size, n_q;
-  float scale;
+  float scale;       // times log2(e), rounded
+  double per_lse;    // what turns an lse into base 2 by that same rounded factor
   const void* keys;
   int key_rows;
   const int32_t* n_keys;
@@ -914,7 +915,7 @@ void weights_kernel(const WeightArgs a) {
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(lse_next), "+v"(limit_next)::"memory");
     if (w == 0) {
       const bool none = lse_next == -__builtin_inff() || limit_next <= 0;
-      s_lse[place][lane] = none ? -__builtin_inff() : -lse_next * kLog2E;
+      s_lse[place][lane] = none ? -__builtin_inff() : (float)(-lse_next * a.per_lse);
       s_limit[place][lane] = none ? 0 : limit_next;
       const bool any = __builtin_amdgcn_ballot_w64(none) != 0;
       if (lane == 0) s_dead[place] = any;
@@ -930,7 +931,7 @@ void weights_kernel(const WeightArgs a) {
       const int most = n - f0 / g, least = n - f1 / g;
       if (wk0 >= most) continue;
       keys.weigh(q_at, place * kPlace + half * 32 * kRow, &s_lse[place][half * 32], &s_limit[place][half * 32], least, dead,
-                 a.scale * kLog2E);
+                 a.scale);
     }
   };
   for (int st = st0; st < st1; st += 2) {
@@ -986,7 +987,7 @@ void weights_few_kernel(const WeightArgs a) {
     const float lse = a.lse[(s * g + head) * a.n_q + token];
     const int limit = r < total ? n - a.n_q + token + 1 : 0;
     const bool none = lse == -__builtin_inff() || limit <= 0;
-    s_lse[r] = none ? -__builtin_inff() : -lse * kLog2E;
+    s_lse[r] = none ? -__builtin_inff() : (float)(-lse * a.per_lse);
     s_limit[r] = none ? 0 : limit;
     if (none) s_dead = 1;
   }
@@ -1003,7 +1004,7 @@ void weights_few_kernel(const WeightArgs a) {
     for (int t = 0; t < tiles; ++t) {
       const int most = n - 32 * t / g, least = n - min(32 * t + 31, total - 1) / g;
       if (keys.first < most)
-        keys.weigh(q_at, t * 32 * kRow, s_lse + 32 * t, s_limit + 32 * t, least, dead, a.scale * kLog2E);
+        keys.weigh(q_at, t * 32 * kRow, s_lse + 32 * t, s_limit + 32 * t, least, dead, a.scale);
     }
     keys.each_sum(n, [&](int, float y) { *weight = before + y; });
     at += kFewWaves;
@@ -1056,7 +1057,11 @@ size_t weight_bytes(int64_t n_slices, int group_size, int n_q, int64_t key_rows)
   return most > 1 ? align_up((size_t)most * n_slices * key_rows * sizeof(float), 256) : 0;
 }
 
-int launch_weights(WeightArgs a, int dtype, void* workspace, hipStream_t hs) {
+// Logits and lse are brought to base 2 by one factor, scale * log2(e) rounded once, so that its
+// rounding is relative to their difference, which decides, and not to their size.
+int launch_weights(WeightArgs a, float scale, int dtype, void* workspace, hipStream_t hs) {
+  a.scale = scale * kLog2E;
+  a.per_lse = a.scale != 0.f ? (double)a.scale / (double)scale : 1.4426950408889634;
   const WeightCut c = weight_cut(a.n_slices, a.group_size, a.n_q, a.key_rows, dtype);
   a.splits = c.splits;
   a.part = static_cast<float*>(workspace);
@@ -1303,9 +1308,9 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
   if (with_logits) return LOUISKV_OK;
   if (!weights || own_rows == 0) return LOUISKV_OK;
   WeightArgs wa{};
-  wa.q = q; wa.group_size = group_size; wa.n_q = n_q; wa.scale = scale; wa.keys = k_own; wa.key_rows = (int)own_rows;
+  wa.q = q; wa.group_size = group_size; wa.n_q = n_q; wa.keys = k_own; wa.key_rows = (int)own_rows;
   wa.n_keys = n_own; wa.lse = a.lse_out; wa.weights = weights; wa.n_slices = n_slices;
-  return launch_weights(wa, dtype, rest, hs);
+  return launch_weights(wa, scale, dtype, rest, hs);
 }
 
 extern "C" size_t louiskv_attn_weights_workspace_size(int64_t n_slices, int32_t group_size, int32_t n_q, int32_t d,
@@ -1326,7 +1331,7 @@ extern "C" int louiskv_attn_weights(const void* q, int32_t dtype, int64_t n_slic
   const size_t need = louiskv_attn_weights_workspace_size(n_slices, group_size, n_q, d, key_rows);
   if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
   WeightArgs a{};
-  a.q = q; a.group_size = group_size; a.n_q = n_q; a.scale = scale; a.keys = keys; a.key_rows = (int)key_rows;
+  a.q = q; a.group_size = group_size; a.n_q = n_q; a.keys = keys; a.key_rows = (int)key_rows;
   a.n_keys = n_keys; a.lse = lse; a.weights = weights; a.n_slices = n_slices;
-  return launch_weights(a, dtype, workspace, as_stream(stream));
+  return launch_weights(a, scale, dtype, workspace, as_stream(stream));
 }
