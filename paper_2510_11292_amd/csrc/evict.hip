@@ -629,6 +629,14 @@ extern "C" int louiskv_store_evict(const void* k_new, const void* v_new, int32_t
   if (!aligned16(k_new, v_new, k, v)) return fail(LOUISKV_ERR_UNSUPPORTED, "k_new, v_new, k and v must be 16-byte aligned");
   const size_t need = louiskv_store_evict_workspace_size(n_slices, rows, n_new, budget);
   if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
+  // what changes overlaps nothing else
+  const size_t ns = (size_t)n_slices, row_bytes = kHeadDim * (dtype == LOUISKV_BF16 ? 2 : 4);
+  const struct { const void* p; size_t bytes; } bufs[] = {
+      {k, ns * rows * row_bytes}, {v, ns * rows * row_bytes}, {weights, ns * rows * 4}, {pos, ns * rows * 4},
+      {n_rows, ns * 4}, {n_seen, ns * 4}, {k_new, ns * n_new * row_bytes}, {v_new, ns * n_new * row_bytes}};
+  for (int i = 0; i < 6; ++i)
+    for (int j = i + 1; j < 8; ++j)
+      if (overlap(bufs[i].p, bufs[i].bytes, bufs[j].p, bufs[j].bytes)) return fail(LOUISKV_ERR_SHAPE, "buffers overlap");
   PlanArgs p;
   p.weights = weights; p.pos = pos; p.n_rows = n_rows; p.n_seen = n_seen; p.rows = (int)rows;
   p.n_keep = (int)(budget - n_new); p.n_first = n_first; p.n_recent = n_recent;

@@ -1057,6 +1057,14 @@ size_t weight_bytes(int64_t n_slices, int group_size, int n_q, int64_t key_rows)
   return most > 1 ? align_up((size_t)most * n_slices * key_rows * sizeof(float), 256) : 0;
 }
 
+// Whether the launches of launch_weights fit (of 256 threads a block, twice kMaxGrid do).
+int check_weight_grid(int64_t n_slices, int group_size, int n_q, int64_t key_rows, int dtype) {
+  const WeightCut c = weight_cut(n_slices, group_size, n_q, key_rows, dtype);
+  if (n_slices * c.key_blocks * c.splits > kMaxGrid || (!c.few && n_slices * ((key_rows + 255) / 256) > kMaxGrid))
+    return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
+  return LOUISKV_OK;
+}
+
 // Logits and lse are brought to base 2 by one factor, scale * log2(e) rounded once, so that its
 // rounding is relative to their difference, which decides, and not to their size.
 int launch_weights(WeightArgs a, float scale, int dtype, void* workspace, hipStream_t hs) {
@@ -1066,7 +1074,6 @@ int launch_weights(WeightArgs a, float scale, int dtype, void* workspace, hipStr
   a.splits = c.splits;
   a.part = static_cast<float*>(workspace);
   const int64_t grid = a.n_slices * c.key_blocks * c.splits;
-  if (grid > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   if (c.few) {
     if (dtype == LOUISKV_BF16) weights_few_kernel<uint16_t><<<(unsigned)grid, kFewWaves * 64, 0, hs>>>(a);
     else weights_few_kernel<float><<<(unsigned)grid, kFewWaves * 64, 0, hs>>>(a);
@@ -1079,7 +1086,6 @@ int launch_weights(WeightArgs a, float scale, int dtype, void* workspace, hipStr
   LKV_CHECK_LAUNCH();
   if (a.splits == 1) return LOUISKV_OK;
   const int per = (a.key_rows + 255) / 256;
-  if (a.n_slices * per > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   add_weights_kernel<<<(unsigned)(a.n_slices * per), 256, 0, hs>>>(a, per);
   LKV_CHECK_LAUNCH();
   return LOUISKV_OK;
@@ -1266,8 +1272,13 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
                                                                 prefix_rows, own_rows, weights != nullptr);
   if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
   const Cut c = cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows, dtype);
-  if (c.blocks_p + c.blocks_o > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
-  const int64_t n_rows = n_slices * group_size * n_q;
+  const int64_t n_rows = n_slices * group_size * n_q, chunks = (own_rows + kFinishKeys - 1) / kFinishKeys;
+  const bool with_logits = weights && own_rows > 0 && keeps_logits(group_size, n_q);
+  if (c.blocks_p + c.blocks_o > kMaxGrid || (with_logits && (n_rows + 3) / 4 + n_slices * chunks > 2 * kMaxGrid))
+    return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
+  if (weights && own_rows > 0 && !with_logits &&
+      (st = check_weight_grid(n_slices, group_size, n_q, own_rows, dtype)))
+    return st;
   const size_t parts = part_bytes(n_rows, c.n_parts());
   AttnArgs a{};
   a.q = q; a.group_size = group_size; a.n_q = n_q; a.scale = scale;
@@ -1282,7 +1293,6 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
   hipStream_t hs = as_stream(stream);
   if (a.n_parts == 0) return no_rows(a, n_rows, hs);
   char* rest = static_cast<char*>(workspace) + parts + align_up((size_t)n_rows * sizeof(float), 256);
-  const bool with_logits = weights && own_rows > 0 && keeps_logits(group_size, n_q);
   if (with_logits) {
     a.logits = reinterpret_cast<float*>(rest);
     a.logit_stride = logit_stride(own_rows);
@@ -1298,7 +1308,7 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
     f.merge_blocks = f.wide ? n_rows : (n_rows + 3) / 4;
     if (with_logits) {
       f.logits = a.logits; f.logit_stride = a.logit_stride; f.per_slice = group_size * n_q; f.n_own = n_own;
-      f.own_rows = (int)own_rows; f.chunks = (int)((own_rows + kFinishKeys - 1) / kFinishKeys); f.weights = weights;
+      f.own_rows = (int)own_rows; f.chunks = (int)chunks; f.weights = weights;
     }
     const int64_t grid = f.merge_blocks + n_slices * f.chunks;
     if (a.out_bf16) finish_kernel<uint16_t><<<(unsigned)grid, 256, 0, hs>>>(f);
@@ -1328,6 +1338,7 @@ extern "C" int louiskv_attn_weights(const void* q, int32_t dtype, int64_t n_slic
   if (st || (st = check_sizes(n_slices, n_kv_heads, group_size, n_q, d, key_rows))) return st;
   if (key_rows < 1) return fail(LOUISKV_ERR_SHAPE, "key_rows=%lld must be positive", (long long)key_rows);
   if (!aligned16(q, keys)) return fail(LOUISKV_ERR_UNSUPPORTED, "q and keys must be 16-byte aligned");
+  if ((st = check_weight_grid(n_slices, group_size, n_q, key_rows, dtype))) return st;
   const size_t need = louiskv_attn_weights_workspace_size(n_slices, group_size, n_q, d, key_rows);
   if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
   WeightArgs a{};

@@ -125,6 +125,20 @@ def test_store_refuses(lib):
         ({4: 0}, SHAPE), ({4: 513}, SHAPE), ({13: 601}, SHAPE), ({13: 2}, SHAPE), ({12: (1 << 30) + 1}, SHAPE),
         ({14: 446}, SHAPE), ({15: 506}, SHAPE), ({14: -1}, SHAPE), ({15: -1}, SHAPE), ({0: ODD}, UNSUPPORTED),
         ({7: ODD}, UNSUPPORTED)] + ([({16: None}, WORKSPACE), ({17: ws - 1}, WORKSPACE)] if ws else []))
+    a = [P(1 << 30 | i << 26) for i in range(1, 9)]         # buffers far from each other, but for one
+    base = [a[0], a[1], 1, 8, 3, 128, *a[2:8], 600, 512, 4, 64, D16, max(ws, 1), None]
+    refused(lib.louiskv_store_evict, base, [
+        ({0: P(a[2].value + 256)}, SHAPE), ({1: a[3]}, SHAPE), ({7: P(a[2].value + 4096)}, SHAPE), ({9: a[4]}, SHAPE),
+        ({11: a[6]}, SHAPE), ({10: a[5]}, SHAPE), ({8: a[1]}, SHAPE)])
+
+
+def test_calls_too_large_for_a_launch_are_refused_before_any(lib):
+    # 2^20 slices of 4096 own rows: as many blocks fit, the weights' do not
+    many = [D16, 1, 1 << 20, 8, 4, 16, 128, 0.1, None, None, 0, 0, None, D16, D16, 4096, None, None, D16, 1, None, D16,
+            1 << 62, None]
+    refused(lib.louiskv_shared_prefix_attn, many, [({5: 8, 15: 1 << 20, 17: D16}, SHAPE), ({17: D16, 5: 8, 2: 1 << 23}, SHAPE)])
+    refused(lib.louiskv_attn_weights, [D16, 1, 1 << 20, 8, 4, 8, 128, 0.1, D16, 1 << 20, None, D16, D16, D16, 1 << 62, None],
+            [({5: 8, 2: 1 << 23}, SHAPE), ({2: 1 << 16, 5: 128, 9: 1 << 30}, SHAPE)])
 
 
 def test_python_calls_refuse_sizes_types_and_host_memory():

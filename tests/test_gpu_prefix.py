@@ -130,6 +130,7 @@ def test_attention(dtype, case):
 MANY = [  # enough queries for every way to cut a call; the first and last slices are checked
     (64, 1, 8, 4, 1, 3000, 500), (8, 1, 8, 4, 77, 1200, 300), (4, 32, 8, 4, 1, 300, 200), (33, 1, 2, 8, 3, 5000, 100),
     (1, 1, 8, 4, 700, 0, 900), (130, 2, 8, 1, 1, 64, 33), (16, 1, 2, 4, 1, 9000, 40), (2, 1, 1, 8, 500, 800, 501),
+    (4, 32, 8, 4, 1, 0, 300), (64, 16, 1, 3, 2, 0, 1500), (130, 8, 1, 8, 6, 0, 90),
 ]
 
 
@@ -161,6 +162,23 @@ def test_nothing_to_see(dtype):
             p.n_p.zero_()
         out, lse, w = p.run()
         assert (out == 0).all() and torch.isneginf(lse).all() and (w is None or torch.equal(w, p.w))
+
+
+@pytest.mark.parametrize("case", [(4, 1, 2, 4, 1, 300, 60), (20, 1, 1, 4, 1, 300, 60), (70, 1, 1, 2, 3, 200, 40)])
+def test_a_padded_sequence_changes_no_other(case):
+    """Queries and own rows of a sequence that holds nothing may be NaN: the others' results stay, bit for bit."""
+    for dtype in DT:
+        p = Problem(*case, dtype, ragged=False)
+        p.n_o = torch.full((p.s,), case[6], dtype=torch.int32, device=DEV)
+        ref = p.run()
+        per = p.s // case[0]
+        p.q[1], p.ko[per:2 * per], p.vo[per:2 * per] = float("nan"), float("nan"), float("inf")
+        p.n_o[per:2 * per] = 0
+        got = p.run()
+        others = torch.arange(case[0], device=DEV) != 1
+        assert torch.equal(got[0][others], ref[0][others]) and torch.equal(got[1][others], ref[1][others])
+        keep = torch.arange(p.s, device=DEV) // per != 1
+        assert torch.equal(got[2][keep], ref[2][keep]) and torch.equal(got[2][~keep], p.w[~keep])
 
 
 def test_lengths_are_clamped():
