@@ -102,8 +102,8 @@ struct Scratch {
   int digit, need, equal;
 };
 
-// Sum of x over the waves before this one; every lane gives its wave's x.  Ends with a barrier
-// of its own use of `part` at the next call's first.
+// Sum of x over the waves before this one; every lane gives its wave's x.  (The next call begins
+// with a barrier, behind which `part` is free.)
 template <int kThreads>
 __device__ __forceinline__ int waves_before(int x, int* part) {
   const int wave = threadIdx.x >> 6;
@@ -193,6 +193,10 @@ __device__ __forceinline__ void each_fate(const Rows<kThreads, kValues>& rows, u
 }
 
 // Block: a slice.  Writes the row that each of the m rows is taken from.
+//
+// 64 slices of 32768 rows, 2048 kept: 21.4 us, a block each, so that its own steps bound it:
+// some 3 us until the weights are there, 6.5 for the first digit (32768 atomic additions in LDS),
+// 2.4 for each other one, mostly barriers, and 4 for the words.
 template <int kThreads, int kValues>
 __global__ __launch_bounds__(kThreads)
 void plan_kernel(const PlanArgs a) {
@@ -383,7 +387,8 @@ void append_kernel(const StoreArgs a, int rows) {
 // A store that at most 64 rows leave for, in one launch.  Block: a slice.  What a row
 // that moves, and a new one, holds is read beside the weights; the rows that leave are
 // found (one: the least key; more: by digits), and the staying rows among the last go
-// to their places in order.
+// to their places in order.  8 slices of 2048 rows 4.5 us (three launches 36), 1024 slices
+// and five new rows each 11.4 us (317): dependent trips to memory and barriers.
 constexpr int kMostGone = 64;
 template <int kRowBytes, int kThreads, int kValues>
 __global__ __launch_bounds__(kThreads)

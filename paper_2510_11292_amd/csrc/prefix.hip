@@ -225,8 +225,8 @@ struct Wave {
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) o[dt] *= f;
   }
-  // Scores of keys p0.. as base-2 logits (-inf where the query does not see the key) if
-  // kMask, and their weights.  low: the lane's weights are what the rounding to bfloat16
+  // Scores of keys p0.. become base-2 logits (masked: -inf where the query does not see the
+  // key), and their weights pb.  low: the lane's weights are what the rounding to bfloat16
   // leaves over.
   template <bool kLow>
   __device__ __forceinline__ void soften(f32x16& sc, int p0, bool masked, bool low, Weights& pb) {
@@ -378,9 +378,17 @@ __device__ __forceinline__ void add_weights(const float* logits, int stride, int
   if (i + 3 < n) weights[i + 3] += y.w;
 }
 
-// Up to 32 queries: every wave takes every fourth 32 keys, through its own place in LDS.
-// Up to 16 (bfloat16): lanes n and n + 16 hold the same query, and the second's weights
-// are what rounding the first's leaves over.
+// Up to 32 queries: every wave takes every fourth 32 keys, through its own place in LDS, so
+// that no wave waits for another.  Up to 16 (bfloat16): lanes n and n + 16 hold the same query,
+// and the second's weights are what rounding the first's leaves over, in columns of the
+// products that would be idle.
+//
+// Memory bounds it: without any arithmetic the same copies took as long (a prefix of 32768 rows
+// of 8 slices, 38.3 us for 40.5 then).  Four sequences over that prefix: 28.0 us and 4.1 for the
+// joining launch; from the first to the last copy of a block 6.6 TB/s, where plain streaming
+// reads reach 6.8 to 7.0, the rest is some 1.5 us before the first copy and 2 after the last.
+// Caches of 1024 slices (930 MB, weights added): 172 us, 5.8 TB/s with the logits.  float32: the
+// products, two channels or keys at a time, take 3.4 us a tile, more than its bytes.
 template <class T>
 __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t id, char* s_ring, float* s_m, float* s_l) {
   constexpr int kTileBytes = kTile * kRowBytes<T>;
@@ -520,6 +528,13 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
 
 // Up to 32 WR queries, 32 a wave; the waves share stages of 64 keys (two places in LDS, one
 // in flight), WR = 2 in halves.
+//
+// Eight chunks of 77 tokens over 20011 rows (2464 queries a slice): 234 to 239 us, 0.85
+// PFLOP/s of the 1.35 to 1.37 of a large product.  A tile of a wave has 16 products (512 cycles),
+// 16 exponentials (256) and 80 other vector operations; two waves of a SIMD overlap them in
+// part (matrix cores busy 42%, no LDS bank conflicts), at clocks of 1.9 to 2.1 GHz under this
+// load.  The next tile's keys read before the exponentials: 247 us for 258 on one part, both
+// scores first 244; a raised wave priority around the products 234 for 232.
 template <class T, int WR, bool own>
 __device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char* s_ring, int* s_bad) {
   constexpr int kRow = kRowBytes<T>, kHalf = kStage * kRow, WK = kBlockWaves / WR;
@@ -857,6 +872,12 @@ struct QueryOrder {
 // (two places, one in flight), the last tokens first, a token's heads together: blocks
 // of a slice begin with the same queries and meet them in the L2.  Q K^T leaves a lane 16
 // queries of one key, which it adds up.
+//
+// A tile has 8 products (256 cycles), and a multiply-add, an exponential and an add of 16 scores
+// (384), which bound it: a 32K prompt of 8 slices 4.6 to 4.7 ms, 0.95 PFLOP/s, some 520 cycles a
+// tile at the 1.93 GHz that the clock falls to; without the exponentials 4.1, with an eighth
+// of the products 2.9.  Three waves a SIMD 4.7 ms for two's 4.9; products of two tiles in turn
+// 4.9, a raised wave priority around them 4.8.
 constexpr int kQueries = 64;                            // of a stage
 constexpr int block_keys(int key_tiles) { return kBlockWaves * key_tiles * kTile; }
 
