@@ -532,7 +532,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
 // Eight chunks of 77 tokens over 20011 rows (2464 queries a slice): 234 to 239 us, 0.85
 // PFLOP/s of the 1.35 to 1.37 of a large product.  A tile of a wave has 16 products (512 cycles),
 // 16 exponentials (256) and 80 other vector operations; two waves of a SIMD overlap them in
-// part (matrix cores busy 42%, no LDS bank conflicts), at clocks of 1.9 to 2.1 GHz under this
+// part (matrix cores busy 50%, no LDS bank conflicts), at clocks of 1.9 to 2.1 GHz under this
 // load.  The next tile's keys read before the exponentials: 247 us for 258 on one part, both
 // scores first 244; a raised wave priority around the products 234 for 232.
 template <class T, int WR, bool own>
