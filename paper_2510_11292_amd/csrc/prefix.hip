@@ -54,6 +54,7 @@ constexpr int kBlockWaves = 4;
 constexpr int kStage = 64;           // keys of a stage that the block's waves share
 constexpr float kGrow = 8.0f;        // base-2 logits may pass the base by this much before the sums are rescaled
 template <class T> constexpr int kRowBytes = kHeadDim * sizeof(T);
+constexpr int kNearLogits = 3584;    // logits that LDS holds: two blocks of 80 KB a CU
 // keys and values of a tile for each wave, or of two stages
 template <class T> constexpr int kRingBytes = kBlockWaves * kTile * 2 * kRowBytes<T>;
 
@@ -387,10 +388,10 @@ __device__ __forceinline__ void add_weights(const float* logits, int stride, int
 // of 8 slices, 38.3 us for 40.5 then).  Four sequences over that prefix: 28.0 us and 4.1 for the
 // joining launch; from the first to the last copy of a block 6.6 TB/s, where plain streaming
 // reads reach 6.8 to 7.0, the rest is some 1.5 us before the first copy and 2 after the last.
-// Caches of 1024 slices (930 MB, weights added): 172 us, 5.8 TB/s with the logits.  float32: the
+// Caches of 1024 slices (930 MB, weights added): 157 us, without weights 141.  float32: the
 // products, two channels or keys at a time, take 3.4 us a tile, more than its bytes.
 template <class T>
-__device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t id, char* s_ring, float* s_m, float* s_l) {
+__device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t id, char* s_ring, float* s_m, float* s_l, float* s_logits) {
   constexpr int kTileBytes = kTile * kRowBytes<T>;
   const Side& x = own ? a.own : a.prefix;
   const Place p = place_of(a, x, own, id);
@@ -410,6 +411,9 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
   Wave<T> f;
   f.init(a, query_row(a, p, own, r), limit_of(a, p, own, r));
   f.addresses(slot, slot + kTileBytes);
+  // A block that sees all of a slice keeps the logits of its first rows in LDS: 1024 slices of 1781
+  // rows took 141 us without logits, 175 with all of them through memory.
+  const int near = a.n_parts == 1 ? kNearLogits / n_rows / kTile * kTile : 0;
   // bfloat16: a tile's operands all fit the registers, so that the next one is under way during
   // its arithmetic.  float32: the next keys follow the scores, the next values the sums.
   constexpr bool kBf16 = Wave<T>::kBf16;
@@ -459,7 +463,8 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
       clear();
     }
     if (own && a.logits && f.n < n_rows) {
-      float* to = a.logits + (p.s * p.n_rows + r) * a.logit_stride + p0 + 4 * f.h;
+      float* to = p0 < near ? s_logits + f.n * near + p0 : a.logits + (p.s * p.n_rows + r) * a.logit_stride + p0;
+      to += 4 * f.h;
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
         *reinterpret_cast<float4*>(to + 2 * i) = make_float4(sc[i], sc[i + 1], sc[i + 2], sc[i + 3]);
@@ -521,9 +526,9 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
   // the block has seen all there is: its rows' weights from the logits that its waves left
   if (w == 0 && f.h == 0) s_m[f.n] = l == 0.f ? __builtin_inff() : max_base(mm) + log2f(l);
   __syncthreads();
-  const float* logits = a.logits + p.s * p.n_rows * a.logit_stride;
+  const float* far = a.logits + p.s * p.n_rows * a.logit_stride;
   for (int i = threadIdx.x * 4; i < p.n; i += kBlockWaves * 64 * 4)
-    add_weights(logits, a.logit_stride, p.n_rows, s_m, p.n, i, a.weights + p.s * x.rows);
+    add_weights(i < near ? s_logits : far, i < near ? near : a.logit_stride, p.n_rows, s_m, p.n, i, a.weights + p.s * x.rows);
 }
 
 // Up to 32 WR queries, 32 a wave; the waves share stages of 64 keys (two places in LDS, one
@@ -645,16 +650,17 @@ __global__ __launch_bounds__(kBlockWaves * 64, sizeof(T) == 2 ? 2 : 1)
 void attn_kernel(const AttnArgs a) {
   __shared__ __align__(256) char s_ring[kRingBytes<T>];
   __shared__ float s_m[kBlockWaves * 32], s_l[kBlockWaves * 32];
+  __shared__ __align__(16) float s_logits[WO == 1 ? kNearLogits : 4];
   __shared__ int s_bad;
   const bool own = blockIdx.x >= a.prefix_blocks;
   const int64_t id = own ? blockIdx.x - a.prefix_blocks : blockIdx.x;
   if constexpr (WP == 1) {
     // one code for both: such blocks run a few iterations, and what they run has to be fetched first
-    attend_few<T>(a, own, id, s_ring, s_m, s_l);
+    attend_few<T>(a, own, id, s_ring, s_m, s_l, s_logits);
   } else if (!own) {
     attend_many<T, WP, false>(a, id, s_ring, &s_bad);
   } else if constexpr (WO == 1) {
-    attend_few<T>(a, true, id, s_ring, s_m, s_l);
+    attend_few<T>(a, true, id, s_ring, s_m, s_l, s_logits);
   } else {
     attend_many<T, WO, true>(a, id, s_ring, &s_bad);
   }
