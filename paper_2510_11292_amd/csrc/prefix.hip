@@ -524,11 +524,13 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
     store_sums(a, query_row(a, p, own, r), (own && a.prefix_blocks ? a.prefix.splits : 0) + p.split, w, f.h, o, mm, l);
   if (!own || !a.logits || a.n_parts > 1) return;
   // the block has seen all there is: its rows' weights from the logits that its waves left
-  if (w == 0 && f.h == 0) s_m[f.n] = l == 0.f ? __builtin_inff() : max_base(mm) + log2f(l);
+  // (behind the maxima, which other waves may still be reading)
+  float* s_lse = s_m + kBlockWaves * 32;
+  if (w == 0 && f.h == 0) s_lse[f.n] = l == 0.f ? __builtin_inff() : max_base(mm) + log2f(l);
   __syncthreads();
   const float* far = a.logits + p.s * p.n_rows * a.logit_stride;
   for (int i = threadIdx.x * 4; i < p.n; i += kBlockWaves * 64 * 4)
-    add_weights(i < near ? s_logits : far, i < near ? near : a.logit_stride, p.n_rows, s_m, p.n, i, a.weights + p.s * x.rows);
+    add_weights(i < near ? s_logits : far, i < near ? near : a.logit_stride, p.n_rows, s_lse, p.n, i, a.weights + p.s * x.rows);
 }
 
 // Up to 32 WR queries, 32 a wave; the waves share stages of 64 keys (two places in LDS, one
@@ -649,7 +651,7 @@ template <class T, int WP, int WO>
 __global__ __launch_bounds__(kBlockWaves * 64, sizeof(T) == 2 ? 2 : 1)
 void attn_kernel(const AttnArgs a) {
   __shared__ __align__(256) char s_ring[kRingBytes<T>];
-  __shared__ float s_m[kBlockWaves * 32], s_l[kBlockWaves * 32];
+  __shared__ float s_m[(kBlockWaves + 1) * 32], s_l[kBlockWaves * 32];
   __shared__ __align__(16) float s_logits[WO == 1 ? kNearLogits : 4];
   __shared__ int s_bad;
   const bool own = blockIdx.x >= a.prefix_blocks;

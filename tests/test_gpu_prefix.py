@@ -408,3 +408,14 @@ def test_attention_then_weights_equal_the_attention_with_weights():
         L().attn_weights(p.q, p.kv, p.ko, p.n_o, lse, w2)
         # the same formula with the same lse: float32 products, exponentials and sums of the two
         assert (w - w2).abs().max() <= 1e-4 * w.max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weights_of_many_slices_a_block_each(dtype):
+    """Two blocks a CU, whose waves join their sums at their own times: the same weights every time."""
+    p = Problem(64, 2, 4, 4, 2, 0, 230, dtype)
+    runs = [p.run() for _ in range(4)]
+    for x in runs[1:]:
+        for a, b in zip(x, runs[0]):
+            assert torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
+    p.check(*runs[0], slices=range(0, p.s, 13))
