@@ -680,8 +680,9 @@ class BranchEngine:
 
     def __init__(self, cfg: BranchConfig, dtype: torch.dtype, device="cuda", out_dtype: Optional[torch.dtype] = None):
         c = self.cfg = cfg
-        if min(c.n_branches, c.n_layers, c.n_kv_heads, c.prompt_len, c.n_new) < 1 or c.n_q_heads % c.n_kv_heads:
-            raise ValueError(f"{c}: sizes must be positive, query heads a multiple of the KV heads")
+        if (min(c.n_branches, c.n_layers, c.n_kv_heads, c.n_q_heads, c.prompt_len, c.n_new) < 1 or
+                c.n_q_heads % c.n_kv_heads or c.n_q_heads // c.n_kv_heads > 8):
+            raise ValueError(f"{c}: sizes must be positive, query heads one to eight times the KV heads")
         if c.n_first < 0 or c.n_recent < 0 or c.n_first + c.n_recent + c.n_new > c.budget:
             raise ValueError(f"n_first={c.n_first} + n_recent={c.n_recent} + n_new={c.n_new} rows do not fit "
                              f"budget={c.budget}")
@@ -746,6 +747,14 @@ class BranchEngine:
         n = 1 if k.dim() == 2 else k.shape[1]
         if n > c.n_new:
             raise ValueError(f"{n} tokens at once, n_new={c.n_new}")
+        # before the store, so that a refused step leaves the caches as they were
+        tokens = q.shape[2] if q.dim() == 4 else 1
+        want = (c.n_groups, c.n_q_heads, n, c.head_dim) if q.dim() == 4 else (c.n_groups, c.n_q_heads, c.head_dim)
+        if tuple(q.shape) != want or tokens != n or q.dtype != self.dtype or not q.is_contiguous():
+            raise ValueError(f"q {tuple(q.shape)} {q.dtype} strides {q.stride()}: contiguous {self.dtype} {want} with {n} "
+                             "new rows a slice")
+        if out is not None and (out.shape != q.shape or not out.is_contiguous()):
+            raise ValueError(f"out {tuple(out.shape)} strides {out.stride()}: contiguous {tuple(q.shape)}")
         ws, ws_store = self.ws.get(n, (None, None))
         if out is None:
             out = self.out if q.dim() == 3 else torch.empty(q.shape, dtype=self.out.dtype, device=q.device)

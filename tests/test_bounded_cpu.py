@@ -188,3 +188,36 @@ def test_python_calls_refuse_sizes_types_and_host_memory():
     with pytest.raises(TypeError, match="dtype"):
         h = torch.float16
         L.shared_prefix_attn(q.to(h), 2, kp.to(h), kp.to(h), None, None, None, None, out, stream=0)
+
+
+def test_a_step_that_is_refused_stores_nothing(monkeypatch):
+    """Queries that do not fit the new rows are refused before those enter the caches."""
+    from paper_2510_11292_amd import engine
+    from paper_2510_11292_amd.engine import BranchConfig, BranchEngine
+    e = BranchEngine(BranchConfig(n_branches=2, n_layers=1, n_kv_heads=2, n_q_heads=4, prompt_len=5, budget=16, n_first=1,
+                                  n_recent=2, n_new=3), torch.float32, "cpu")
+    k = torch.zeros(4, 128)
+    with pytest.raises(RuntimeError, match="prefill"):
+        e.step(torch.zeros(2, 4, 128), k, k)
+    e.prefill(torch.zeros(2, 5, 128), torch.zeros(2, 5, 128))
+    q = torch.zeros(2, 4, 128)
+    stores = []
+
+    class Recorder:
+        def store_evict(self, *a, **kw):
+            stores.append(a)
+    monkeypatch.setattr(engine, "L", Recorder())
+    k3 = torch.zeros(4, 3, 128)
+    for bad, rows in ((torch.zeros(2, 4, 2, 128), k), (torch.zeros(2, 4, 2, 128), k3), (q, k3), (q[:1], k), (q[:, :2], k),
+                      (q[..., :64], k), (q.bfloat16(), k), (torch.zeros(2, 128, 4).transpose(1, 2), k), (q[0], k),
+                      (torch.zeros(2, 4, 4, 128), torch.zeros(4, 4, 128))):
+        with pytest.raises(ValueError):
+            e.step(bad, rows, rows)
+    for out in (torch.zeros(2, 4, 1, 128), torch.zeros(2, 128, 4).transpose(1, 2)):
+        with pytest.raises(ValueError, match="out"):
+            e.step(q, k, k, out)
+    assert not stores and e.n_seen.eq(0).all()
+    for heads in (18, 0):
+        with pytest.raises(ValueError, match="positive"):
+            BranchEngine(BranchConfig(n_branches=1, n_layers=1, n_kv_heads=2, n_q_heads=heads, prompt_len=5, budget=200),
+                         torch.float32, "cpu")
