@@ -515,7 +515,12 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       f32x4 y = from[lane * 16 + ((4 * w + i) ^ (lane & 15))];
-      if (twice) y += from[(lane ^ 16) * 16 + ((4 * w + i) ^ (lane & 15))];
+      if (twice) {
+        // what rounding left of a weight can be 0 or negative: an infinity that it met is left out
+        const f32x4 rest = from[(lane ^ 16) * 16 + ((4 * w + i) ^ (lane & 15))];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = __builtin_isfinite(y[c]) ? y[c] + rest[c] : y[c];
+      }
 #pragma unroll
       for (int c = 0; c < 4; ++c) o[4 * i + c] += y[c] * e;
     }

@@ -239,6 +239,33 @@ def test_values_that_are_not_finite(dtype, bad, prefix, rows):
     assert torch.equal(out[..., others], ref[..., others]) and torch.isfinite(lse).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("seqs,g,n_q,prefix,rows", [
+    (2, 4, 1, 64, 0), (1, 4, 1, 0, 64), (1, 1, 1, 0, 96), (2, 4, 1, 1536, 700), (16, 1, 1, 320, 32), (4, 2, 2, 200, 130),
+    (5, 4, 1, 320, 64), (1, 8, 3, 0, 256), (1, 8, 9, 0, 320), (40, 4, 1, 640, 64), (3, 4, 20, 256, 96)])
+def test_infinite_values_wherever_they_stand(dtype, seqs, g, n_q, prefix, rows):
+    """An infinity of any row that a query sees is its result, of both signs NaN, in that channel alone."""
+    p = Problem(seqs, 1, 1, g, n_q, prefix, rows, dtype, ragged=False)
+    ref, ref_lse, ref_w = p.run(torch.float32)
+    inf = float("inf")
+    for values, n, hidden in ((p.vp, prefix, 0), (p.vo, rows, n_q - 1)):      # all queries see the rows before the hidden ones
+        last = n - hidden - 1
+        for at in sorted({0, 5, 31, 32, 63, n // 2, last - 1, last} & set(range(last + 1))):
+            keep = values[0, at].clone()
+            other = values[0, last - at].clone()
+            values[0, at, 3], values[0, at, 77] = inf, -inf
+            values[0, at, 100], values[0, last - at, 100] = inf, -inf          # twice the same row: -inf
+            out, lse, w = p.run(torch.float32)
+            values[0, last - at], values[0, at] = other, keep
+            seen = out if values is p.vp else out[:1]
+            assert (seen[..., 3] == inf).all() and (seen[..., 77] == -inf).all(), at
+            assert (torch.isneginf if 2 * at == last else torch.isnan)(seen[..., 100]).all(), at
+            same = torch.ones_like(out, dtype=torch.bool)
+            same[:len(seen)][..., [3, 77, 100]] = False
+            assert torch.equal(out[same], ref[same]) and torch.equal(lse, ref_lse), at
+            assert w is None or torch.equal(w, ref_w)
+
+
 def test_scores_of_minus_infinity_weigh_nothing():
     p = Problem(1, 1, 1, 2, 1, 30, 40, "bf16", ragged=False)
     p.q.fill_(1.0)
