@@ -675,8 +675,9 @@ class BranchConfig:
 class BranchEngine:
     """Sequences that continue one prompt, each with a cache of its own that keeps at most cfg.budget rows.
 
-    Groups are ordered branch by branch (group = branch * n_layers + layer), slices as in the library.  step() leaves
-    the counts on the device: a captured step is the next one at every replay."""
+    Groups are ordered branch by branch (group = branch * n_layers + layer), slices as in the library.  The engine owns
+    what step() reads, the prompt's rows k_prefix and v_prefix [n_layers * n_kv_heads][rows][d] among them, and leaves
+    the counts on the device: a captured step is the next one at every replay, of the prompt of the last prefill()."""
 
     def __init__(self, cfg: BranchConfig, dtype: torch.dtype, device="cuda", out_dtype: Optional[torch.dtype] = None):
         c = self.cfg = cfg
@@ -693,17 +694,18 @@ class BranchEngine:
         dev = self.device = torch.device(device)
         s, sp, d = c.n_slices, c.n_prefix_slices, c.head_dim
         i32 = dict(dtype=torch.int32, device=dev)
-        self.k_prefix = self.v_prefix = self.n_prefix = self.pos_prefix = None
+        g, rows = c.n_q_heads // c.n_kv_heads, c.prefix_budget if c.cuts_prefix else c.prompt_len
+        self.k_prefix, self.v_prefix = (torch.zeros(sp, rows, d, dtype=dtype, device=dev) for _ in range(2))
+        self.n_prefix = self.pos_prefix = None
         if c.cuts_prefix:
-            self.k_prefix, self.v_prefix = (torch.zeros(sp, c.prefix_budget, d, dtype=dtype, device=dev) for _ in range(2))
-            self.n_prefix, self.pos_prefix = torch.zeros(sp, **i32), torch.zeros(sp, c.prefix_budget, **i32)
+            self.n_prefix, self.pos_prefix = torch.zeros(sp, **i32), torch.zeros(sp, rows, **i32)
+        self.has_prompt = False
         self.k_own, self.v_own = (torch.zeros(s, c.budget, d, dtype=dtype, device=dev) for _ in range(2))
         self.weights = torch.zeros(s, c.budget, dtype=torch.float32, device=dev)
         self.pos = torch.zeros(s, c.budget, **i32)
         self.n_rows, self.n_seen = torch.zeros(s, **i32), torch.zeros(s, **i32)
         self.out = torch.zeros(c.n_groups, c.n_q_heads, d, dtype=out_dtype or dtype, device=dev)
         self.lse = torch.zeros(c.n_groups, c.n_q_heads, dtype=torch.float32, device=dev)
-        g, rows = c.n_q_heads // c.n_kv_heads, c.prefix_budget if c.cuts_prefix else c.prompt_len
         # of single tokens and full chunks; steps between them take memory of their own
         self.ws = {t: (torch.empty(L.shared_prefix_attn_workspace_size(s, sp, g, t, rows, c.budget, True),
                                    dtype=torch.uint8, device=dev),
@@ -713,10 +715,10 @@ class BranchEngine:
     def prefill(self, keys: torch.Tensor, values: torch.Tensor, q: Optional[torch.Tensor] = None,
                 lse: Optional[torch.Tensor] = None) -> None:
         """The prompt's keys and values [n_layers * n_kv_heads][prompt_len][d]; the branches' caches are emptied.
-        Without a prefix_budget they are the prefix themselves (kept, not copied).  With one the rows of most weight
-        are copied, by the softmax weights of the prompt's last queries q [n_layers][Hq][n][d]: all of them, or a
-        window (64 is usual).  lse [n_layers][Hq][n]: of the attention that the caller has computed for q already;
-        without it this computes the queries' dense attention."""
+        Without a prefix_budget all are copied, or none if they are k_prefix and v_prefix themselves, filled by the
+        caller.  With one the rows of most weight are copied, by the softmax weights of the prompt's last queries
+        q [n_layers][Hq][n][d]: all of them, or a window (64 is usual).  lse [n_layers][Hq][n]: of the attention that
+        the caller has computed for q already; without it this computes the queries' dense attention."""
         c = self.cfg
         if c.cuts_prefix:
             if q is None:
@@ -731,18 +733,22 @@ class BranchEngine:
                          self.v_prefix, None, self.pos_prefix, self.n_prefix)
         else:
             want = (c.n_prefix_slices, c.prompt_len, c.head_dim)
-            if tuple(keys.shape) != want or tuple(values.shape) != want:
-                raise ValueError(f"keys {tuple(keys.shape)} and values {tuple(values.shape)}, expected {want}")
-            self.k_prefix, self.v_prefix = keys, values
+            if tuple(keys.shape) != want or tuple(values.shape) != want or not keys.dtype == values.dtype == self.dtype:
+                raise ValueError(f"keys {tuple(keys.shape)} {keys.dtype} and values {tuple(values.shape)} {values.dtype}, "
+                                 f"expected {want} {self.dtype}")
+            for to, x in ((self.k_prefix, keys), (self.v_prefix, values)):
+                if x.data_ptr() != to.data_ptr() or x.stride() != to.stride():
+                    to.copy_(x)
         self.n_rows.zero_()
         self.n_seen.zero_()
+        self.has_prompt = True
 
     def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """One token of every branch, q [G][Hq][d], k and v [S][d], or up to cfg.n_new at once, q [G][Hq][n][d], k and v
         [S][n][d]: they enter the caches, from which the lightest rows leave, and attend to the prompt's rows and the
         caches, whose weights they add to.  Returns self.out (one token), or out (allocated if not given)."""
         c = self.cfg
-        if self.k_prefix is None:
+        if not self.has_prompt:
             raise RuntimeError("step() comes after prefill()")
         n = 1 if k.dim() == 2 else k.shape[1]
         if n > c.n_new:

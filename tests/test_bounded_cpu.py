@@ -221,3 +221,32 @@ def test_a_step_that_is_refused_stores_nothing(monkeypatch):
         with pytest.raises(ValueError, match="positive"):
             BranchEngine(BranchConfig(n_branches=1, n_layers=1, n_kv_heads=2, n_q_heads=heads, prompt_len=5, budget=200),
                          torch.float32, "cpu")
+
+
+def test_a_prompt_is_copied_to_the_engine_s_rows():
+    """A captured step reads the addresses of its capture: they stay, and hold the last prompt."""
+    from paper_2510_11292_amd.engine import BranchConfig, BranchEngine
+    e = BranchEngine(BranchConfig(n_branches=2, n_layers=3, n_kv_heads=2, n_q_heads=4, prompt_len=5, budget=16, n_first=1,
+                                  n_recent=2), torch.float32, "cpu")
+    places = set()
+    for i in range(2):
+        keys, values = torch.randn(6, 5, 128), torch.randn(5, 6, 128).transpose(0, 1)
+        e.n_rows.fill_(7)
+        e.prefill(keys, values)
+        places.add((e.k_prefix.data_ptr(), e.v_prefix.data_ptr()))
+        assert torch.equal(e.k_prefix, keys) and torch.equal(e.v_prefix, values) and e.v_prefix.is_contiguous()
+        assert (e.n_rows == 0).all() and e.k_prefix.data_ptr() != keys.data_ptr()
+    assert len(places) == 1
+    e.k_prefix.normal_()                        # the caller may fill them in place
+    keys = e.k_prefix.clone()
+    e.prefill(e.k_prefix, e.v_prefix)
+    assert torch.equal(e.k_prefix, keys) and torch.equal(e.v_prefix, values)
+    for k, v in ((keys.bfloat16(), values), (keys, values.double()), (keys[:, :4], values), (keys, values[:5])):
+        with pytest.raises(ValueError, match="expected"):
+            e.prefill(k, v)
+    assert torch.equal(e.k_prefix, keys)
+    cut = BranchEngine(BranchConfig(n_branches=2, n_layers=3, n_kv_heads=2, n_q_heads=4, prompt_len=50, budget=16, n_first=1,
+                                    n_recent=2, prefix_budget=9), torch.float32, "cpu")
+    x = torch.zeros(12, 128)
+    with pytest.raises(RuntimeError, match="prefill"):
+        cut.step(torch.zeros(6, 4, 128), x, x)

@@ -118,6 +118,37 @@ def test_captured_steps_and_a_second_prefill():
             assert (a.n_seen == t + 1).all()
 
 
+@pytest.mark.parametrize("cut", [None, 100])
+def test_captured_steps_of_one_prompt_after_another(cut):
+    """A step that was captured with the first prompt is one of the second after its prefill, whose tensors are gone."""
+    a, b = engine("bf16", prefix_budget=cut), engine("bf16", prefix_budget=cut)
+    c, gen = a.cfg, torch.Generator(device=DEV).manual_seed(5)
+    new = [torch.zeros(c.n_groups, c.n_q_heads, 128, device=DEV).bfloat16(), *(torch.zeros(c.n_slices, 128, device=DEV).bfloat16() for _ in range(2))]
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    a.prefill(*prompt(a, gen, 64))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            a.step(*new)
+    for _ in range(3):
+        tensors = prompt(a, gen, 64)
+        a.prefill(*tensors)
+        b.prefill(*tensors)
+        for x in tensors:
+            x.fill_(float("nan"))
+        for e in (a, b):
+            e.weights.zero_()
+        for t in range(50):
+            for x in new:
+                x.copy_(torch.randn(x.shape, generator=gen, device=DEV))
+            torch.cuda.synchronize()
+            graph.replay()
+            want = b.step(*new)
+            torch.cuda.synchronize()
+            assert torch.equal(a.out, want) and torch.equal(a.pos, b.pos) and torch.equal(a.lse, b.lse), t
+            assert torch.isfinite(want).all()
+
+
 def test_refusals():
     with pytest.raises(ValueError, match="budget"):
         engine("bf16", budget=10)
