@@ -690,6 +690,8 @@ class BranchEngine:
         if c.cuts_prefix and c.n_first + c.n_recent > c.prefix_budget:
             raise ValueError(f"n_first={c.n_first} + n_recent={c.n_recent} rows do not fit "
                              f"prefix_budget={c.prefix_budget}")
+        if not {dtype, out_dtype or dtype} <= {torch.float32, torch.bfloat16}:
+            raise ValueError(f"dtype {dtype}, out_dtype {out_dtype}: float32 or bfloat16")
         self.dtype = dtype
         dev = self.device = torch.device(device)
         s, sp, d = c.n_slices, c.n_prefix_slices, c.head_dim
@@ -756,11 +758,15 @@ class BranchEngine:
         # before the store, so that a refused step leaves the caches as they were
         tokens = q.shape[2] if q.dim() == 4 else 1
         want = (c.n_groups, c.n_q_heads, n, c.head_dim) if q.dim() == 4 else (c.n_groups, c.n_q_heads, c.head_dim)
-        if tuple(q.shape) != want or tokens != n or q.dtype != self.dtype or not q.is_contiguous():
-            raise ValueError(f"q {tuple(q.shape)} {q.dtype} strides {q.stride()}: contiguous {self.dtype} {want} with {n} "
-                             "new rows a slice")
-        if out is not None and (out.shape != q.shape or not out.is_contiguous()):
-            raise ValueError(f"out {tuple(out.shape)} strides {out.stride()}: contiguous {tuple(q.shape)}")
+        dev = self.k_own.device
+        if (tuple(q.shape) != want or tokens != n or q.dtype != self.dtype or not q.is_contiguous() or q.device != dev or
+                q.data_ptr() % 16):
+            raise ValueError(f"q {tuple(q.shape)} {q.dtype} strides {q.stride()} on {q.device}: contiguous, 16-byte aligned "
+                             f"{self.dtype} {want} on {dev} with {n} new rows a slice")
+        if out is not None and (out.shape != q.shape or out.dtype not in (torch.float32, torch.bfloat16) or
+                                not out.is_contiguous() or out.device != dev or out.data_ptr() % 16):
+            raise ValueError(f"out {tuple(out.shape)} {out.dtype} strides {out.stride()} on {out.device}: contiguous, 16-byte "
+                             f"aligned float32 or bfloat16 {tuple(q.shape)} on {dev}")
         ws, ws_store = self.ws.get(n, (None, None))
         if out is None:
             out = self.out if q.dim() == 3 else torch.empty(q.shape, dtype=self.out.dtype, device=q.device)

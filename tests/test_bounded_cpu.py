@@ -250,3 +250,42 @@ def test_a_prompt_is_copied_to_the_engine_s_rows():
     x = torch.zeros(12, 128)
     with pytest.raises(RuntimeError, match="prefill"):
         cut.step(torch.zeros(6, 4, 128), x, x)
+
+
+def test_a_step_stores_nothing_that_its_attention_would_refuse(monkeypatch):
+    """Queries and results of another type, place or alignment are refused before the new rows enter the caches."""
+    from paper_2510_11292_amd import engine
+    from paper_2510_11292_amd.engine import BranchConfig, BranchEngine
+    cfg = BranchConfig(n_branches=2, n_layers=1, n_kv_heads=2, n_q_heads=4, prompt_len=5, budget=16, n_first=1, n_recent=2)
+    e = BranchEngine(cfg, torch.float32, "cpu")
+    e.prefill(torch.zeros(2, 5, 128), torch.zeros(2, 5, 128))
+    q, k = torch.zeros(2, 4, 128), torch.zeros(4, 128)
+    calls = []
+
+    class Recorder:
+        def store_evict(self, *a, **kw):
+            calls.append("store")
+
+        def shared_prefix_attn(self, *a, **kw):
+            calls.append("attn")
+    monkeypatch.setattr(engine, "L", Recorder())
+
+    def odd(x):                                 # the same, 4 bytes off a 16-byte boundary
+        y = torch.zeros(x.numel() + 8)
+        at = next(i for i in range(8) if (y.data_ptr() + 4 * i) % 16 == 4)
+        return y[at:at + x.numel()].view(x.shape)
+    for bad in (odd(q), q.to("meta")):
+        with pytest.raises(ValueError, match="q "):
+            e.step(bad, k, k)
+    for out in (q.half(), q.double(), q.int(), odd(q), q.to("meta")):
+        with pytest.raises(ValueError, match="out "):
+            e.step(q, k, k, out)
+    assert not calls
+    for out in (None, torch.zeros_like(q), q.bfloat16()):
+        got = e.step(q, k, k, out)
+        assert got is (e.out if out is None else out) and calls == ["store", "attn"]
+        calls.clear()
+    monkeypatch.undo()
+    for types in ((torch.float16, None), (torch.float32, torch.float16), (torch.float64, torch.float32)):
+        with pytest.raises(ValueError, match="float32 or bfloat16"):
+            BranchEngine(cfg, types[0], "cpu", out_dtype=types[1])
