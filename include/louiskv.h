@@ -1111,8 +1111,9 @@ int louiskv_sparse_prefill_attn(const void* q, int32_t dtype, int64_t n_slices,
  *
  * Alignment   of these calls' element buffers (queries, keys, values, outputs) and
  *             workspaces: 16 bytes (LOUISKV_ERR_UNSUPPORTED, LOUISKV_ERR_WORKSPACE).
- * Limits      group_size 1 to 8; at most 2^30 rows in a slice, and 2^25 queries
- *             (n_slices * group_size * n_q) in a call.
+ * Limits      group_size 1 to 8; at most 2^30 rows in a slice, and in a call 2^22 - 1
+ *             slices, 2^25 queries (n_slices * group_size * n_q) and, where rows move,
+ *             2^24 - 2 times 32 of them (LOUISKV_ERR_SHAPE).
  */
 
 size_t louiskv_shared_prefix_attn_workspace_size(int64_t n_slices, int64_t n_prefix_slices,

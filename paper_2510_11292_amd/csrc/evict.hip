@@ -519,8 +519,18 @@ void carve(PlanArgs& p, void* workspace, int64_t n_slices) {
   p.movers = p.rows > kPlanRows ? c.take<int32_t>((size_t)n_slices * p.n_keep) : nullptr;
 }
 
+// Blocks that the moves of a slice's n_keep rows take.
+int64_t move_blocks(int64_t n_keep) { return std::max<int64_t>(1, (n_keep + 4 * kMoveRows - 1) / (4 * kMoveRows)); }
+
+// Whether the launches fit: a block a slice that plans or stores (of 1024 threads where it has more
+// than 2048 rows, half as many as kMaxGrid then), and where rows move in a launch of their own its
+// blocks of 256 threads, of which twice kMaxGrid fit.
+bool fits_launch(int64_t n_slices, int64_t rows, int64_t n_keep, bool moves) {
+  return n_slices <= (rows > 2048 ? kMaxGrid / 2 : kMaxGrid) && (!moves || n_slices * move_blocks(n_keep) <= 2 * kMaxGrid);
+}
+
 int check_sizes(int dtype, int64_t n_slices, int32_t d, int64_t rows, int64_t n_keep, int32_t n_first,
-                int32_t n_recent) {
+                int32_t n_recent, bool moves) {
   if (dtype != LOUISKV_F32 && dtype != LOUISKV_BF16) return fail(LOUISKV_ERR_DTYPE, "unknown dtype %d", dtype);
   if (d != kHeadDim) return fail(LOUISKV_ERR_UNSUPPORTED, "head dim %d not supported (only 128)", d);
   if (n_slices < 1 || n_slices > kMaxGrid || rows < 1 || rows > kMaxRows)
@@ -529,7 +539,7 @@ int check_sizes(int dtype, int64_t n_slices, int32_t d, int64_t rows, int64_t n_
   if (n_first < 0 || n_recent < 0 || (int64_t)n_first + n_recent > n_keep || n_keep > rows)
     return fail(LOUISKV_ERR_SHAPE, "n_first=%d and n_recent=%d must fit the %lld rows kept of %lld", n_first, n_recent,
                 (long long)n_keep, (long long)rows);
-  if (n_slices * ((n_keep + 3) / 4) > kMaxGrid) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
+  if (!fits_launch(n_slices, rows, n_keep, moves)) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
   return LOUISKV_OK;
 }
 
@@ -540,7 +550,7 @@ int check_workspace(const void* workspace, size_t bytes, size_t need) {
 }
 
 int launch_move(const MoveArgs& a, int64_t n_slices, int dtype, hipStream_t hs) {
-  const int per = std::max(1, (a.n_keep + 4 * kMoveRows - 1) / (4 * kMoveRows));
+  const int per = (int)move_blocks(a.n_keep);
   const unsigned grid = (unsigned)(n_slices * per);
   const bool bf16 = dtype == LOUISKV_BF16, stream = n_slices * a.n_keep * 2 * kHeadDim * (bf16 ? 2 : 4) > kCacheBytes;
   if (bf16 && stream) move_kernel<256, true><<<grid, 256, 0, hs>>>(a, per);
@@ -562,7 +572,9 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 using namespace louiskv;
 
 extern "C" size_t louiskv_evict_rows_workspace_size(int64_t n_slices, int64_t rows, int64_t n_keep) {
-  if (n_slices < 1 || n_slices > kMaxGrid || rows < 1 || rows > kMaxRows || n_keep < 1) return 0;
+  if (n_slices < 1 || n_slices > kMaxGrid || rows < 1 || rows > kMaxRows || n_keep < 1 ||
+      !fits_launch(n_slices, rows, std::min(rows, n_keep), true))
+    return 0;
   return plan_bytes(n_slices, rows, std::min(rows, n_keep));
 }
 
@@ -575,7 +587,7 @@ extern "C" int louiskv_evict_rows(const float* weights, const int32_t* pos, cons
     return fail(LOUISKV_ERR_NULL, "weights, k, v, k_to, v_to and n_rows_to are required");
   if (!pos != !n_seen) return fail(LOUISKV_ERR_NULL, "pos and n_seen go together");
   const int64_t keep = std::min(n_keep, rows);   // more rows than there are: all stay
-  int st = check_sizes(dtype, n_slices, d, rows, keep, 0, 0);
+  int st = check_sizes(dtype, n_slices, d, rows, keep, 0, 0, true);
   if (st) return st;
   if (n_keep < 1 || n_keep > rows_to || rows_to > kMaxRows || n_first < 0 || n_recent < 0 ||
       (int64_t)n_first + n_recent > n_keep)
@@ -617,7 +629,8 @@ extern "C" int louiskv_evict_rows(const float* weights, const int32_t* pos, cons
 extern "C" size_t louiskv_store_evict_workspace_size(int64_t n_slices, int64_t rows, int32_t n_new, int64_t budget) {
   if (n_slices < 1 || n_slices > kMaxGrid || rows < 1 || rows > kMaxRows || n_new < 1 || budget < n_new || budget > rows)
     return 0;
-  return stores_at_once(rows, budget, n_new) ? 0 : plan_bytes(n_slices, rows, budget - n_new);
+  return stores_at_once(rows, budget, n_new) || !fits_launch(n_slices, rows, budget - n_new, true)
+             ? 0 : plan_bytes(n_slices, rows, budget - n_new);
 }
 
 extern "C" int louiskv_store_evict(const void* k_new, const void* v_new, int32_t dtype, int64_t n_slices, int32_t n_new,
@@ -629,7 +642,7 @@ extern "C" int louiskv_store_evict(const void* k_new, const void* v_new, int32_t
   if (n_new < 1 || budget < n_new || budget > rows)
     return fail(LOUISKV_ERR_SHAPE, "n_new=%d, budget=%lld and rows=%lld must be 1 <= n_new <= budget <= rows", n_new,
                 (long long)budget, (long long)rows);
-  int st = check_sizes(dtype, n_slices, d, rows, budget - n_new, n_first, n_recent);
+  int st = check_sizes(dtype, n_slices, d, rows, budget - n_new, n_first, n_recent, !stores_at_once(rows, budget, n_new));
   if (st) return st;
   if (!aligned16(k_new, v_new, k, v)) return fail(LOUISKV_ERR_UNSUPPORTED, "k_new, v_new, k and v must be 16-byte aligned");
   const size_t need = louiskv_store_evict_workspace_size(n_slices, rows, n_new, budget);

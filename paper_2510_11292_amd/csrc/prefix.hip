@@ -1091,12 +1091,11 @@ size_t weight_bytes(int64_t n_slices, int group_size, int n_q, int64_t key_rows)
   return most > 1 ? align_up((size_t)most * n_slices * key_rows * sizeof(float), 256) : 0;
 }
 
-// Whether the launches of launch_weights fit (of 256 threads a block, twice kMaxGrid do).
-int check_weight_grid(int64_t n_slices, int group_size, int n_q, int64_t key_rows, int dtype) {
+// Whether the launches of launch_weights fit (of 256 threads a block, twice kMaxGrid do; the blocks of
+// 512 are a slice's, and a few more).
+bool weights_fit(int64_t n_slices, int group_size, int n_q, int64_t key_rows, int dtype) {
   const WeightCut c = weight_cut(n_slices, group_size, n_q, key_rows, dtype);
-  if (n_slices * c.key_blocks * c.splits > kMaxGrid || (!c.few && n_slices * ((key_rows + 255) / 256) > kMaxGrid))
-    return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
-  return LOUISKV_OK;
+  return n_slices * c.key_blocks * c.splits <= 2 * kMaxGrid && (c.few || n_slices * ((key_rows + 255) / 256) <= 2 * kMaxGrid);
 }
 
 // Logits and lse are brought to base 2 by one factor, scale * log2(e) rounded once, so that its
@@ -1250,6 +1249,21 @@ size_t weight_space(int64_t n_slices, int group_size, int n_q, int64_t own_rows)
          (keeps_logits(group_size, n_q) ? align_up(rows * logit_stride(own_rows) * sizeof(float), 256) : weight_bytes(n_slices, group_size, n_q, own_rows));
 }
 
+size_t attn_bytes(int64_t n_slices, int64_t n_prefix_slices, int group_size, int n_q, int64_t prefix_rows, int64_t own_rows,
+                  bool with_weights) {
+  auto parts = [&](int dtype) { return cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows, dtype).n_parts(); };
+  return part_bytes(n_slices * group_size * n_q, std::max(parts(LOUISKV_BF16), parts(LOUISKV_F32))) +
+         (with_weights ? weight_space(n_slices, group_size, n_q, own_rows) : 0);
+}
+
+// Whether the attention's launches fit (blocks of 256 threads).
+bool attn_fits(const Cut& c, int64_t n_slices, int group_size, int n_q, int64_t own_rows, bool with_weights, int dtype) {
+  if (c.blocks_p + c.blocks_o > 2 * kMaxGrid) return false;
+  if (!with_weights || own_rows == 0) return true;
+  if (!keeps_logits(group_size, n_q)) return weights_fit(n_slices, group_size, n_q, own_rows, dtype);
+  return (n_slices * group_size * n_q + 3) / 4 + n_slices * ((own_rows + kFinishKeys - 1) / kFinishKeys) <= 2 * kMaxGrid;
+}
+
 // Neither a prefix nor own rows: every query sees nothing.
 __global__ void no_rows_kernel(void* out, int out_bf16, float* lse_out, int64_t n_rows) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;   // four channels
@@ -1278,10 +1292,12 @@ extern "C" size_t louiskv_shared_prefix_attn_workspace_size(int64_t n_slices, in
   if (!served(n_slices, group_size, n_q, own_rows) || prefix_rows < 0 || prefix_rows > kMaxRows ||
       (prefix_rows > 0 && (n_prefix_slices < 1 || n_slices % n_prefix_slices != 0)))
     return 0;
-  const int64_t rows = n_slices * group_size * n_q;
-  auto parts = [&](int dtype) { return cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows, dtype).n_parts(); };
-  return part_bytes(rows, std::max(parts(LOUISKV_BF16), parts(LOUISKV_F32))) +
-         (with_weights ? weight_space(n_slices, group_size, n_q, own_rows) : 0);
+  auto fits = [&](int dtype) {
+    return attn_fits(cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows, dtype), n_slices, group_size, n_q,
+                     own_rows, with_weights, dtype);
+  };
+  if (!fits(LOUISKV_BF16) && !fits(LOUISKV_F32)) return 0;
+  return attn_bytes(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows, with_weights);
 }
 
 extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads,
@@ -1302,17 +1318,13 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
                 (long long)n_prefix_slices, n_kv_heads, (long long)n_slices);
   if (!aligned16(q, out, k_prefix, v_prefix, k_own, v_own))
     return fail(LOUISKV_ERR_UNSUPPORTED, "q, out, keys and values must be 16-byte aligned");
-  const size_t need = louiskv_shared_prefix_attn_workspace_size(n_slices, n_prefix_slices, group_size, n_q, d,
-                                                                prefix_rows, own_rows, weights != nullptr);
+  const size_t need = attn_bytes(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows, weights != nullptr);
   if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
   const Cut c = cut_of(n_slices, n_prefix_slices, group_size, n_q, prefix_rows, own_rows, dtype);
   const int64_t n_rows = n_slices * group_size * n_q, chunks = (own_rows + kFinishKeys - 1) / kFinishKeys;
   const bool with_logits = weights && own_rows > 0 && keeps_logits(group_size, n_q);
-  if (c.blocks_p + c.blocks_o > kMaxGrid || (with_logits && (n_rows + 3) / 4 + n_slices * chunks > 2 * kMaxGrid))
+  if (!attn_fits(c, n_slices, group_size, n_q, own_rows, weights != nullptr, dtype))
     return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
-  if (weights && own_rows > 0 && !with_logits &&
-      (st = check_weight_grid(n_slices, group_size, n_q, own_rows, dtype)))
-    return st;
   const size_t parts = part_bytes(n_rows, c.n_parts());
   AttnArgs a{};
   a.q = q; a.group_size = group_size; a.n_q = n_q; a.scale = scale;
@@ -1360,7 +1372,9 @@ extern "C" int louiskv_shared_prefix_attn(const void* q, int32_t dtype, int64_t 
 extern "C" size_t louiskv_attn_weights_workspace_size(int64_t n_slices, int32_t group_size, int32_t n_q, int32_t d,
                                                       int64_t key_rows) {
   (void)d;
-  return served(n_slices, group_size, n_q, key_rows) ? weight_bytes(n_slices, group_size, n_q, key_rows) : 0;
+  auto fits = [&](int dtype) { return weights_fit(n_slices, group_size, n_q, key_rows, dtype); };
+  return served(n_slices, group_size, n_q, key_rows) && (fits(LOUISKV_BF16) || fits(LOUISKV_F32))
+             ? weight_bytes(n_slices, group_size, n_q, key_rows) : 0;
 }
 
 extern "C" int louiskv_attn_weights(const void* q, int32_t dtype, int64_t n_slices, int32_t n_kv_heads,
@@ -1372,8 +1386,8 @@ extern "C" int louiskv_attn_weights(const void* q, int32_t dtype, int64_t n_slic
   if (st || (st = check_sizes(n_slices, n_kv_heads, group_size, n_q, d, key_rows))) return st;
   if (key_rows < 1) return fail(LOUISKV_ERR_SHAPE, "key_rows=%lld must be positive", (long long)key_rows);
   if (!aligned16(q, keys)) return fail(LOUISKV_ERR_UNSUPPORTED, "q and keys must be 16-byte aligned");
-  if ((st = check_weight_grid(n_slices, group_size, n_q, key_rows, dtype))) return st;
-  const size_t need = louiskv_attn_weights_workspace_size(n_slices, group_size, n_q, d, key_rows);
+  if (!weights_fit(n_slices, group_size, n_q, key_rows, dtype)) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
+  const size_t need = weight_bytes(n_slices, group_size, n_q, key_rows);
   if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
   WeightArgs a{};
   a.q = q; a.group_size = group_size; a.n_q = n_q; a.keys = keys; a.key_rows = (int)key_rows;

@@ -697,6 +697,11 @@ class BranchEngine:
         s, sp, d = c.n_slices, c.n_prefix_slices, c.head_dim
         i32 = dict(dtype=torch.int32, device=dev)
         g, rows = c.n_q_heads // c.n_kv_heads, c.prefix_budget if c.cuts_prefix else c.prompt_len
+        # of single tokens and full chunks; steps between them take memory of their own
+        sizes = {t: (L.shared_prefix_attn_workspace_size(s, sp, g, t, rows, c.budget, True),
+                     L.store_evict_workspace_size(s, c.budget, t, c.budget)) for t in (1, c.n_new)}
+        if not all(attn for attn, _ in sizes.values()):
+            raise ValueError(f"{s} slices of {g} query heads and n_new={c.n_new} tokens are too many for one call")
         self.k_prefix, self.v_prefix = (torch.zeros(sp, rows, d, dtype=dtype, device=dev) for _ in range(2))
         self.n_prefix = self.pos_prefix = None
         if c.cuts_prefix:
@@ -708,11 +713,7 @@ class BranchEngine:
         self.n_rows, self.n_seen = torch.zeros(s, **i32), torch.zeros(s, **i32)
         self.out = torch.zeros(c.n_groups, c.n_q_heads, d, dtype=out_dtype or dtype, device=dev)
         self.lse = torch.zeros(c.n_groups, c.n_q_heads, dtype=torch.float32, device=dev)
-        # of single tokens and full chunks; steps between them take memory of their own
-        self.ws = {t: (torch.empty(L.shared_prefix_attn_workspace_size(s, sp, g, t, rows, c.budget, True),
-                                   dtype=torch.uint8, device=dev),
-                       torch.empty(L.store_evict_workspace_size(s, c.budget, t, c.budget), dtype=torch.uint8, device=dev))
-                   for t in (1, c.n_new)}
+        self.ws = {t: tuple(torch.empty(x, dtype=torch.uint8, device=dev) for x in both) for t, both in sizes.items()}
 
     def prefill(self, keys: torch.Tensor, values: torch.Tensor, q: Optional[torch.Tensor] = None,
                 lse: Optional[torch.Tensor] = None) -> None:

@@ -289,3 +289,50 @@ def test_a_step_stores_nothing_that_its_attention_would_refuse(monkeypatch):
     for types in ((torch.float16, None), (torch.float32, torch.float16), (torch.float64, torch.float32)):
         with pytest.raises(ValueError, match="float32 or bfloat16"):
             BranchEngine(cfg, types[0], "cpu", out_dtype=types[1])
+
+
+def test_sizes_that_fit_the_card_are_not_refused(lib):
+    """64 branches of 256 (layer, KV head) slices with caches of 2048 rows, 1024 slices of 32768 rows kept, and the most
+    slices: what is refused is a buffer's alignment or the missing workspace, which are looked at behind the sizes."""
+    a = [P(1 << 30 | i << 26) for i in range(1, 12)]
+
+    def store(s, new, rows, k):
+        return lib.louiskv_store_evict(a[0], a[1], 1, s, new, 128, k, a[3], a[4], a[5], a[6], a[7], rows, rows, 4, 64, None, 0,
+                                       None)
+
+    def evict(s, rows, keep):
+        far = [P(i << 50) for i in range(1, 12)]
+        return lib.louiskv_evict_rows(far[0], far[1], far[2], far[3], 1, s, 128, rows, keep, 4, 64, far[4], far[5], far[6],
+                                      far[7], far[8], far[9], keep, far[10], None, 0, None)
+    for s, new, rows in ((16384, 1, 2048), (16384, 64, 2048), (1024, 1, 32768), (1 << 20, 1, 300), ((1 << 22) - 1, 1, 70)):
+        assert store(s, new, rows, ODD) == UNSUPPORTED, (s, new, rows)
+        assert lib.louiskv_store_evict_workspace_size(s, rows, new, rows) == 0          # one launch
+    for s, new, rows in ((16384, 100, 2048), (1024, 1, 40000), (8192, 1, 40000)):
+        size = lib.louiskv_store_evict_workspace_size(s, rows, new, rows)
+        assert size >= s * (rows - new) * 4 and store(s, new, rows, ODD) == UNSUPPORTED, (s, new, rows)
+    for s, rows, keep in ((16384, 32768, 2048), (1024, 40000, 32768), (16383, 32768, 32767), ((1 << 22) - 1, 70, 70)):
+        size = lib.louiskv_evict_rows_workspace_size(s, rows, keep)
+        assert size >= s * keep * 4 and evict(s, rows, keep) == WORKSPACE, (s, rows, keep)
+    # more blocks than a launch holds: refused, and no workspace
+    for s, rows, keep in ((16384, 32768, 32767), (1 << 22, 4096, 100), (1 << 20, 4096, 513), (1 << 14, 1 << 20, 1 << 20)):
+        assert lib.louiskv_evict_rows_workspace_size(s, rows, keep) == 0 and evict(s, rows, keep) == SHAPE, (s, rows, keep)
+    assert lib.louiskv_store_evict_workspace_size(1 << 20, 1 << 20, 100, 1 << 20) == 0
+    assert store(1 << 22, 1, 4096, ODD) == store(16384, 1, 32769, ODD) == SHAPE and store(1 << 20, 100, 1 << 20, ODD) == SHAPE
+    # the attention of as many slices, whose workspace is 0 where the call is refused
+    size = lib.louiskv_shared_prefix_attn_workspace_size
+    attn = [D16, 1, (1 << 22) - 1, 1, 4, 1, 128, 0.1, D16, D16, (1 << 22) - 1, 9, None, D16, D16, 70, None, D16, D16, 1, None,
+            None, 0, None]
+    assert size(attn[2], attn[2], 4, 1, 128, 9, 70, 1) > 0
+    refused(lib.louiskv_shared_prefix_attn, attn, [({}, WORKSPACE)])
+    assert size(1 << 20, 1, 4, 8, 128, 0, 1 << 20, 1) == size(1 << 20, 1, 4, 16, 128, 0, 1 << 20, 1) == 0
+    assert lib.louiskv_attn_weights_workspace_size(1 << 16, 4, 128, 128, 1 << 30) == 0
+
+
+def test_an_engine_that_no_step_fits_is_refused():
+    from paper_2510_11292_amd.engine import BranchConfig, BranchEngine
+    base = dict(n_branches=64, n_layers=32, n_kv_heads=8, n_q_heads=64, prompt_len=1 << 17, budget=2048)
+    BranchEngine(BranchConfig(n_new=256, **base), torch.bfloat16, "meta")
+    with pytest.raises(ValueError, match="too many"):
+        BranchEngine(BranchConfig(n_new=257, **base), torch.bfloat16, "meta")
+    with pytest.raises(ValueError, match="too many"):
+        BranchEngine(BranchConfig(**{**base, "n_branches": 1 << 16}), torch.bfloat16, "meta")

@@ -274,3 +274,56 @@ def test_branches_with_bounded_caches_together(dtype):
                 acc[i][p_] = acc[i].get(p_, 0.0) + float(p[:, keep + j].sum())
             got = torch.tensor([acc[i][p_] for p_ in held], device=DEV)
             assert (wo[i, :len(held)] - got).abs().max() < 1e-4, (t, i)
+
+
+def lightest(w, pos, seen, first, recent, k):
+    """The k rows of least weight of each slice of unprotected rows, in ascending order (weights all different)."""
+    safe = (pos < first) | (pos >= seen[:, None] - recent)
+    return torch.topk(w.masked_fill(safe, float("inf")), k, dim=1, largest=False).indices.sort(1).values
+
+
+def test_a_store_to_all_layers_of_many_branches():
+    """16384 slices (64 branches of 32 layers and 8 KV heads) of 2048 rows: their caches are full, one row of each leaves."""
+    s, rows = 16384, 2048
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    k = torch.zeros(s, rows, 128, dtype=torch.bfloat16, device=DEV)
+    v = torch.zeros_like(k)
+    k[:, :, 0] = torch.arange(rows, device=DEV) % 256
+    k[:, :, 1] = torch.arange(rows, device=DEV) // 256
+    v[:, :, 5] = k[:, :, 0] + 1
+    w = torch.rand(s, rows, generator=gen, device=DEV)
+    pos = torch.arange(rows, **I32).expand(s, -1).contiguous()
+    n, seen = torch.full((s,), rows, **I32), torch.full((s,), rows, **I32)
+    gone = lightest(w, pos, seen, 4, 128, 1)[:, 0]
+    kn, vn = torch.full((s, 128), 3.0, device=DEV).bfloat16(), torch.full((s, 128), 4.0, device=DEV).bfloat16()
+    L().store_evict(kn, vn, k, v, w, pos, n, seen, rows, 4, 128)
+    assert (n == rows).all() and (seen == rows + 1).all()
+    # the last row takes the place of the one that leaves, the new one comes behind
+    want = torch.arange(rows, device=DEV).expand(s, -1).clone()
+    want[torch.arange(s, device=DEV), gone] = rows - 1
+    want[:, rows - 1] = rows
+    assert torch.equal(pos.long(), want) and (w[:, -1] == 0).all()
+    held = want[:, :-1]
+    assert torch.equal(k[:, :-1, 0].long(), held % 256) and torch.equal(k[:, :-1, 1].long(), held // 256)
+    assert torch.equal(v[:, :-1, 5].long(), held % 256 + 1)
+    assert (k[:, -1] == 3).all() and (v[:, -1] == 4).all()
+
+
+def test_eviction_of_a_few_rows_of_many_long_slices():
+    """1024 slices of 32768 rows, of which all but 5 stay: some million blocks move rows."""
+    s, rows, keep = 1024, 32768, 32763
+    gen = torch.Generator(device=DEV).manual_seed(12)
+    k = torch.zeros(s, rows, 128, dtype=torch.bfloat16, device=DEV)
+    v = torch.zeros_like(k)
+    k[:, :, 0] = torch.arange(rows, device=DEV) % 256
+    v[:, :, 7] = torch.arange(rows, device=DEV) // 256
+    w = torch.stack([torch.randperm(rows, generator=gen, device=DEV) for _ in range(s)]).float()
+    pos = torch.arange(rows, **I32).expand(s, -1).contiguous()
+    n = torch.full((s,), rows, **I32)
+    gone = lightest(w, pos, n, 4, 128, 5)                  # none of the last 128 rows leaves
+    L().evict_rows(w, pos, n, n.clone(), keep, 4, 128, k, v, k, v, w, pos, n)
+    assert (n == keep).all()
+    want = torch.arange(keep, device=DEV).expand(s, -1).clone()
+    want.scatter_(1, gone, torch.arange(keep, rows, device=DEV).expand(s, -1).contiguous())
+    assert torch.equal(pos[:, :keep].long(), want)
+    assert torch.equal(k[:, :keep, 0].long(), want % 256) and torch.equal(v[:, :keep, 7].long(), want // 256)
