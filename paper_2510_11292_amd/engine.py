@@ -687,7 +687,7 @@ class BranchEngine:
         if c.n_first < 0 or c.n_recent < 0 or c.n_first + c.n_recent + c.n_new > c.budget:
             raise ValueError(f"n_first={c.n_first} + n_recent={c.n_recent} + n_new={c.n_new} rows do not fit "
                              f"budget={c.budget}")
-        if c.cuts_prefix and c.n_first + c.n_recent > c.prefix_budget:
+        if c.cuts_prefix and max(1, c.n_first + c.n_recent) > c.prefix_budget:
             raise ValueError(f"n_first={c.n_first} + n_recent={c.n_recent} rows do not fit "
                              f"prefix_budget={c.prefix_budget}")
         if not {dtype, out_dtype or dtype} <= {torch.float32, torch.bfloat16}:

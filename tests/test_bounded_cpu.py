@@ -336,3 +336,11 @@ def test_an_engine_that_no_step_fits_is_refused():
         BranchEngine(BranchConfig(n_new=257, **base), torch.bfloat16, "meta")
     with pytest.raises(ValueError, match="too many"):
         BranchEngine(BranchConfig(**{**base, "n_branches": 1 << 16}), torch.bfloat16, "meta")
+
+
+def test_a_prefix_of_no_rows_is_refused():
+    from paper_2510_11292_amd.engine import BranchConfig, BranchEngine
+    for budget in (0, -1):
+        with pytest.raises(ValueError, match="prefix_budget"):
+            BranchEngine(BranchConfig(n_branches=2, n_layers=1, n_kv_heads=2, n_q_heads=4, prompt_len=5, budget=16, n_first=0,
+                                      n_recent=0, prefix_budget=budget), torch.float32, "cpu")
