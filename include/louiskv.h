@@ -1144,9 +1144,10 @@ size_t louiskv_shared_prefix_attn_workspace_size(int64_t n_slices, int64_t n_pre
  *             louiskv_sparse_decode_attn; -inf and o = 0 where a query sees no row.
  * Rows that a query does not see do not reach its result, whatever they hold.
  * Scores, softmax, sums and weights are float32; for LOUISKV_BF16 the softmax
- * weights meet the values rounded to bfloat16, for the matrix cores, 2^-8 of each at
- * most, or as the sum of two bfloat16 where 16 queries or fewer read the same rows
- * (their sums, lse_out and `weights` use the unrounded ones).
+ * weights meet the values as the sum of two bfloat16, for the matrix cores, 2^-16 of
+ * each off at most, or where more than 32 queries read the same rows as one, 2^-8
+ * (their sums, lse_out and `weights` use the unrounded ones).  A value that is not
+ * finite reaches the queries that see it, in its channel.
  * out, lse_out and weights overlap no other buffer.
  * workspace   louiskv_shared_prefix_attn_workspace_size() bytes, may be 0;
  *             with_weights != 0 where weights are given.

@@ -227,10 +227,9 @@ struct Wave {
     for (int dt = 0; dt < 4; ++dt) o[dt] *= f;
   }
   // Scores of keys p0.. become base-2 logits (masked: -inf where the query does not see the
-  // key), and their weights pb.  low: the lane's weights are what the rounding to bfloat16
-  // leaves over.
-  template <bool kLow>
-  __device__ __forceinline__ void soften(f32x16& sc, int p0, bool masked, bool low, Weights& pb) {
+  // key), and their weights pb.  bfloat16: rest is what the rounding leaves over, and
+  // pb that too where `low` is set.
+  __device__ __forceinline__ void soften(f32x16& sc, int p0, bool masked, bool low, Weights& pb, Weights& rest) {
     float m = mult;
     if (masked) {
 #pragma unroll
@@ -249,9 +248,9 @@ struct Wave {
       const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], m, -base));
       sum += p;
       if constexpr (kBf16) {
-        __bf16 b = (__bf16)p;
-        if constexpr (kLow) b = low ? (__bf16)(p - (float)b) : b;
-        pb[i >> 3][i & 7] = b;
+        const __bf16 b = (__bf16)p, r = (__bf16)(p - (float)b);
+        pb[i >> 3][i & 7] = low ? r : b;
+        rest[i >> 3][i & 7] = r;
       } else {
         pb[i] = p;
       }
@@ -278,6 +277,23 @@ struct Wave {
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, pb[i], o[dt], 0, 0, 0);
         }
     }
+  }
+  // Whether the values, not the scores, make the lane's sums infinite or NaN.
+  __device__ __forceinline__ bool met_not_finite() const {
+    float zero = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) zero = fmaf(o[dt][i], 0.f, zero);
+    return zero != 0.f && __builtin_isfinite(sum);
+  }
+  __device__ __forceinline__ void restart() {
+    base = sum = 0.f;
+    grow_at = -__builtin_inff();
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   }
   // A value that is not finite, of row `key`, to the queries that see it.
   __device__ __forceinline__ void add_not_finite(const void* v, int64_t row, int key, bool skip) {
@@ -380,9 +396,11 @@ __device__ __forceinline__ void add_weights(const float* logits, int stride, int
 }
 
 // Up to 32 queries: every wave takes every fourth 32 keys, through its own place in LDS, so
-// that no wave waits for another.  Up to 16 (bfloat16): lanes n and n + 16 hold the same query,
-// and the second's weights are what rounding the first's leaves over, in columns of the
-// products that would be idle.
+// that no wave waits for another.  bfloat16: what the rounding of a weight leaves over meets the
+// values too, in products of its own, or with up to 16 queries, which lanes n and n + 16 both
+// hold then, as the second's weights, in columns that would be idle.  Such a rest is 0 or negative
+// as often as not, and an infinite value that it met NaN: a wave whose sums the values leave not
+// finite takes its tiles once more, with such values set to 0 and added apart.
 //
 // Memory bounds it: without any arithmetic the same copies took as long (a prefix of 32768 rows
 // of 8 slices, 38.3 us for 40.5 then).  Four sequences over that prefix: 28.0 us and 4.1 for the
@@ -425,17 +443,18 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
   }
 #pragma unroll
   for (int c = 0; c < Wave<T>::kQ; ++c) asm volatile("" : "+v"(f.q[c]));   // waits for the queries here, not in the loop
-  bool bad = false;
+  bool bad = false, careful = false;
+again:
   for (int tile = t0 + w; tile < t1; tile += kBlockWaves) {
     const int p0 = tile * kTile;
     const bool masked = p0 + kTile > least, more = tile + kBlockWaves < t1;
     // values that a query may not see must not reach it: 0 * inf is NaN
     auto clear = [&]() {
-      if (masked) bad |= __builtin_amdgcn_ballot_w64(clear_not_finite<T, kTileBytes>(s_ring + (w * 2 + 1) * kTileBytes)) != 0;
+      if (masked || careful) bad |= __builtin_amdgcn_ballot_w64(clear_not_finite<T, kTileBytes>(s_ring + (w * 2 + 1) * kTileBytes)) != 0;
     };
     typename Wave<T>::Keys kf;
     typename Wave<T>::Values vf;
-    typename Wave<T>::Weights pb;
+    typename Wave<T>::Weights pb, rest;
     if constexpr (kBf16) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       clear();
@@ -456,7 +475,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more) copy_k(tile + kBlockWaves);
     }
-    f.template soften<kBf16>(sc, p0, masked, low, pb);
+    f.soften(sc, p0, masked, low, pb, rest);
     if constexpr (!kBf16) {
       if (more) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");     // all but the next keys
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -470,15 +489,25 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
         *reinterpret_cast<float4*>(to + 2 * i) = make_float4(sc[i], sc[i + 1], sc[i + 2], sc[i + 3]);
     }
     f.add_values(0, vf, pb);
+    if constexpr (kBf16) {
+      if (!twice) f.add_values(0, vf, rest);
+    }
     if constexpr (!kBf16) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more) copy_v(tile + kBlockWaves);
     }
   }
+  if (kBf16 && !careful && __builtin_amdgcn_ballot_w64(f.met_not_finite())) {
+    careful = true;
+    f.restart();
+    copy_k(t0 + w);
+    copy_v(t0 + w);
+    goto again;
+  }
   if (bad) {                                    // rare
 #pragma unroll 1
     for (int tile = t0 + w; tile < t1; tile += kBlockWaves) {
-      if (tile * kTile + kTile <= least) continue;
+      if (!careful && tile * kTile + kTile <= least) continue;
 #pragma unroll 1
       for (int key = tile * kTile; key < min(tile * kTile + kTile, most); ++key)
         f.add_not_finite(x.v, p.kv_row + key, key, low);
@@ -515,12 +544,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       f32x4 y = from[lane * 16 + ((4 * w + i) ^ (lane & 15))];
-      if (twice) {
-        // what rounding left of a weight can be 0 or negative: an infinity that it met is left out
-        const f32x4 rest = from[(lane ^ 16) * 16 + ((4 * w + i) ^ (lane & 15))];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) y[c] = __builtin_isfinite(y[c]) ? y[c] + rest[c] : y[c];
-      }
+      if (twice) y += from[(lane ^ 16) * 16 + ((4 * w + i) ^ (lane & 15))];
 #pragma unroll
       for (int c = 0; c < 4; ++c) o[4 * i + c] += y[c] * e;
     }
@@ -547,6 +571,9 @@ __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t 
 // part (matrix cores busy 50%, no LDS bank conflicts), at clocks of 1.9 to 2.1 GHz under this
 // load.  The next tile's keys read before the exponentials: 247 us for 258 on one part, both
 // scores first 244; a raised wave priority around the products 234 for 232.
+// The weights are rounded to bfloat16 (2^-8 of each), as the products of what that leaves over
+// would take 304 us for 227, and 64 sequences over 32768 rows 83.5 for 72.5, all these on one part:
+// outputs are 2.1e-3 of their size off instead of 1.7e-3, a bfloat16 result's own rounding.
 template <class T, int WR, bool own>
 __device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char* s_ring, int* s_bad) {
   constexpr int kRow = kRowBytes<T>, kHalf = kStage * kRow, WK = kBlockWaves / WR;
@@ -587,7 +614,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char*
     if (st + 1 < st1) copy(st + 1, place ^ 1);
     typename Wave<T>::Keys kf;
     typename Wave<T>::Values vf;
-    typename Wave<T>::Weights pb;
+    typename Wave<T>::Weights pb, rest;
     auto half = [&](int x, bool more) {
       const int k0 = p0 + x * kTile;
       const uint32_t off = place * 2 * kHalf + x * kTile * kRow;
@@ -595,7 +622,7 @@ __device__ __forceinline__ void attend_many(const AttnArgs& a, int64_t id, char*
       f.load_values(off, vf);
       if (more) f.load_keys(off + kTile * kRow, kf);   // the next tile's, before the exponentials
       __builtin_amdgcn_sched_barrier(0);
-      f.template soften<false>(sc, k0, k0 + kTile > w_least, false, pb);
+      f.soften(sc, k0, k0 + kTile > w_least, false, pb, rest);
       f.add_values(off, vf, pb);
     };
     if constexpr (WK == 1) {

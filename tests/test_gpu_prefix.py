@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 import torch
 
-from attn_bounds import U, check_attention
+from attn_bounds import U, attention_bounds, check_attention
 from oracle import blocks as ob
 from oracle import prefix as op
 
@@ -264,6 +264,32 @@ def test_infinite_values_wherever_they_stand(dtype, seqs, g, n_q, prefix, rows):
             same[:len(seen)][..., [3, 77, 100]] = False
             assert torch.equal(out[same], ref[same]) and torch.equal(lse, ref_lse), at
             assert w is None or torch.equal(w, ref_w)
+
+
+@pytest.mark.parametrize("seqs,kv,g,n_q,prefix,rows", [
+    (1, 2, 4, 1, 0, 300), (4, 2, 4, 1, 3000, 500), (1, 1, 1, 1, 64, 0), (8, 1, 4, 1, 2000, 100), (5, 2, 4, 1, 700, 33),
+    (3, 1, 8, 1, 900, 40), (2, 1, 8, 2, 333, 64), (1, 2, 8, 4, 0, 1500), (1, 1, 6, 5, 0, 70), (17, 1, 1, 1, 128, 1)])
+def test_bf16_attention_keeps_its_weights_beyond_bf16(seqs, kv, g, n_q, prefix, rows):
+    """Up to 32 queries of the same rows: weights meet the values as two bfloat16.  What the second rounding leaves is
+    2^-8 of at most 2^-8 of a weight, so a float32 result is off by 2^-16 of the weighted mean of |v| beside the float32
+    roundings."""
+    p = Problem(seqs, 1, kv, g, n_q, prefix, rows, "bf16")
+    out, lse, _ = p.run(torch.float32)
+    on, ln, q = n64(out).reshape(p.s, g, n_q, 128), n64(lse).reshape(p.s, g, n_q), n64(p.q).reshape(p.s, g, n_q, 128)
+    worst = 0.0
+    for i in range(p.s):
+        k, v, see, n = p.rows_of(i)
+        see[:, :n] = True
+        for j in range(g):
+            o, e, mass, size = ob.masked_attention(q[i, j], k, v, see, SCALE)
+            tol, tol_lse = attention_bounds(o, mass, e, size, len(k), False, False)
+            tol = tol + 2.0 ** -16 * mass
+            err = np.abs(on[i, j] - o)
+            assert (err <= tol).all(), f"slice {i}: {(err / tol).max():.3g} of the bound"
+            worst = max(worst, (err / tol).max())
+            live = np.isfinite(e)
+            assert (np.abs(ln[i, j][live] - e[live]) <= tol_lse[live]).all() and np.array_equal(np.isneginf(ln[i, j]), ~live)
+    print(f"  largest error {worst:.3f} of the bound", flush=True)
 
 
 def test_scores_of_minus_infinity_weigh_nothing():
