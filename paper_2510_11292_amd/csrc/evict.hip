@@ -6,9 +6,6 @@
 namespace louiskv {
 namespace {
 
-constexpr int64_t kMaxRows = 1 << 30;      // of a slice
-constexpr int64_t kCacheBytes = 32 << 20;  // the L2s: what a call reads beyond them goes past them
-
 struct PlanArgs {
   const float* weights;
   const int32_t* pos;        // NULL: row numbers
@@ -540,12 +537,6 @@ int check_sizes(int dtype, int64_t n_slices, int32_t d, int64_t rows, int64_t n_
     return fail(LOUISKV_ERR_SHAPE, "n_first=%d and n_recent=%d must fit the %lld rows kept of %lld", n_first, n_recent,
                 (long long)n_keep, (long long)rows);
   if (!fits_launch(n_slices, rows, n_keep, moves)) return fail(LOUISKV_ERR_SHAPE, "problem too large for one launch");
-  return LOUISKV_OK;
-}
-
-int check_workspace(const void* workspace, size_t bytes, size_t need) {
-  if (need > 0 && (!workspace || bytes < need || !aligned16(workspace)))
-    return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, 16-byte aligned, got %zu", need, bytes);
   return LOUISKV_OK;
 }
 

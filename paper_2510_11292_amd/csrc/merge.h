@@ -11,9 +11,18 @@ constexpr float kLog2E = 1.4426950408889634f;
 // Blocks of up to 512 threads that one launch can hold: 2^32 - 1 threads.
 constexpr int64_t kMaxGrid = (1 << 23) - 1;
 
+constexpr int64_t kMaxRows = 1 << 30;      // of a slice of a shared prefix or a cache of bounded size
+constexpr int64_t kCacheBytes = 32 << 20;  // the L2s: what such a call reads beyond them goes past them
+
 // Whether kernels may read (or write) these in 16-byte pieces.
 template <class... P>
 bool aligned16(const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 15) == 0; }
+
+inline int check_workspace(const void* workspace, size_t bytes, size_t need) {
+  if (need > 0 && (!workspace || bytes < need || !aligned16(workspace)))
+    return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, 16-byte aligned, got %zu", need, bytes);
+  return LOUISKV_OK;
+}
 
 // A partial: the maximum of its base-2 logits (-inf: no key), the sum of
 // 2^(logit - max) and the weighted sum of the value rows.  Partials of row r are

@@ -9,7 +9,6 @@
 namespace louiskv {
 namespace {
 
-constexpr int64_t kMaxRows = 1 << 30;      // of a slice
 constexpr int64_t kMaxQueries = 1 << 25;   // of a call, times heads
 
 // The rows of a prefix, or of the slices' own caches.
@@ -764,8 +763,6 @@ Cut cut_of(int64_t n_slices, int64_t n_prefix_slices, int group_size, int n_q, i
 // Rows of calls that read more than the L2s hold bypass the caches where one block reads
 // them: all layers of four sequences, 930 MB, 178 us (201 through the caches), a prefix of
 // 134 MB 34.6 us (38.4); 8 MB stay (12.0 us; 13.5 past the caches).
-constexpr int64_t kCacheBytes = 32 << 20;
-
 template <class T>
 void launch_attn(const AttnArgs& a, const Cut& c, hipStream_t hs) {
   const unsigned grid = (unsigned)(c.blocks_p + c.blocks_o);
@@ -1257,12 +1254,6 @@ int check_sizes(int64_t n_slices, int32_t n_kv_heads, int32_t group_size, int32_
 bool served(int64_t n_slices, int32_t group_size, int32_t n_q, int64_t rows) {
   return n_slices >= 1 && n_slices <= kMaxGrid && group_size >= 1 && group_size <= 8 && n_q >= 1 && rows >= 0 &&
          rows <= kMaxRows && n_slices * group_size <= kMaxQueries / n_q;
-}
-
-int check_workspace(const void* workspace, size_t bytes, size_t need) {
-  if (need > 0 && (!workspace || bytes < need || !aligned16(workspace)))
-    return fail(LOUISKV_ERR_WORKSPACE, "workspace needs %zu bytes, 16-byte aligned, got %zu", need, bytes);
-  return LOUISKV_OK;
 }
 
 // Own rows' weights take the logits that the attention leaves where a slice has up to 32
