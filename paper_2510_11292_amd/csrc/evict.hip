@@ -385,7 +385,7 @@ void append_kernel(const StoreArgs a, int rows) {
 // that moves, and a new one, holds is read beside the weights; the rows that leave are
 // found (one: the least key; more: by digits), and the staying rows among the last go
 // to their places in order.  8 slices of 2048 rows 4.5 us (three launches 36), 1024 slices
-// and five new rows each 11.4 us (317): dependent trips to memory and barriers.
+// and five new rows each 11 to 14 us (317): dependent trips to memory and barriers.
 constexpr int kMostGone = 64;
 template <int kRowBytes, int kThreads, int kValues>
 __global__ __launch_bounds__(kThreads)

@@ -405,7 +405,7 @@ __device__ __forceinline__ void add_weights(const float* logits, int stride, int
 // of 8 slices, 38.3 us for 40.5 then).  Four sequences over that prefix: 28.0 us and 4.1 for the
 // joining launch; from the first to the last copy of a block 6.6 TB/s, where plain streaming
 // reads reach 6.8 to 7.0, the rest is some 1.5 us before the first copy and 2 after the last.
-// Caches of 1024 slices (930 MB, weights added): 157 us, without weights 141.  float32: the
+// Caches of 1024 slices (930 MB, weights added): 163 us, without weights 140.  float32: the
 // products, two channels or keys at a time, take 3.4 us a tile, more than its bytes.
 template <class T>
 __device__ __forceinline__ void attend_few(const AttnArgs& a, bool own, int64_t id, char* s_ring, float* s_m, float* s_l, float* s_logits) {
@@ -564,7 +564,7 @@ again:
 // Up to 32 WR queries, 32 a wave; the waves share stages of 64 keys (two places in LDS, one
 // in flight), WR = 2 in halves.
 //
-// Eight chunks of 77 tokens over 20011 rows (2464 queries a slice): 234 to 239 us, 0.85
+// Eight chunks of 77 tokens over 20011 rows (2464 queries a slice): 228 to 237 us, 0.86
 // PFLOP/s of the 1.35 to 1.37 of a large product.  A tile of a wave has 16 products (512 cycles),
 // 16 exponentials (256) and 80 other vector operations; two waves of a SIMD overlap them in
 // part (matrix cores busy 50%, no LDS bank conflicts), at clocks of 1.9 to 2.1 GHz under this
@@ -761,8 +761,9 @@ Cut cut_of(int64_t n_slices, int64_t n_prefix_slices, int group_size, int n_q, i
 }
 
 // Rows of calls that read more than the L2s hold bypass the caches where one block reads
-// them: all layers of four sequences, 930 MB, 178 us (201 through the caches), a prefix of
-// 134 MB 34.6 us (38.4); 8 MB stay (12.0 us; 13.5 past the caches).
+// them: caches of 930 MB took 178 us (201 through the caches) when all logits went through memory,
+// a prefix of 134 MB 34.6 us (38.4) before its waves joined in 16-byte pieces; 8 MB stay (12.0 us;
+// 13.5 past the caches).
 template <class T>
 void launch_attn(const AttnArgs& a, const Cut& c, hipStream_t hs) {
   const unsigned grid = (unsigned)(c.blocks_p + c.blocks_o);
