@@ -740,8 +740,8 @@ class BranchEngine:
                 raise ValueError(f"keys {tuple(keys.shape)} {keys.dtype} and values {tuple(values.shape)} {values.dtype}, "
                                  f"expected {want} {self.dtype}")
             for to, x in ((self.k_prefix, keys), (self.v_prefix, values)):
-                if x.data_ptr() != to.data_ptr() or x.stride() != to.stride():
-                    to.copy_(x)
+                if x.data_ptr() != to.data_ptr() or not x.is_contiguous():
+                    to.copy_(x.detach())
         self.n_rows.zero_()
         self.n_seen.zero_()
         self.has_prompt = True

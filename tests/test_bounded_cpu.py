@@ -241,6 +241,8 @@ def test_a_prompt_is_copied_to_the_engine_s_rows():
     keys = e.k_prefix.clone()
     e.prefill(e.k_prefix, e.v_prefix)
     assert torch.equal(e.k_prefix, keys) and torch.equal(e.v_prefix, values)
+    e.prefill(keys.clone().requires_grad_(), values)      # a model's keys: the engine holds none of their graph
+    assert torch.equal(e.k_prefix, keys) and not e.k_prefix.requires_grad
     for k, v in ((keys.bfloat16(), values), (keys, values.double()), (keys[:, :4], values), (keys, values[:5])):
         with pytest.raises(ValueError, match="expected"):
             e.prefill(k, v)
