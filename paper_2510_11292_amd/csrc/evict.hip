@@ -94,7 +94,7 @@ struct Rows {
 constexpr int kDigit = 11, kBins = 1 << kDigit;
 template <int kThreads>
 struct Scratch {
-  int hist[kBins];
+  alignas(8) int hist[kBins];   // also a wave's least key each, 8 bytes
   int part[kThreads / 64], part2[kThreads / 64];
   int digit, need, equal;
 };
